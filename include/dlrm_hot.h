@@ -379,6 +379,158 @@ int32_t dlrm_emb_bag_bwd_adagrad_timed(const dlrm_sparse_batch* batch, void* con
                                        void* workspace, size_t workspace_bytes, int32_t algo,
                                        const dlrm_bwd_timing* timing, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A history in order.  The calls above pool a bag; the calls below read it as a sequence: rows of
+ * several heads (queries, keys, values) for each item, in the order of the batch, the sequences
+ * delineated by offsets as the bags of Sec. 4.1 are.  They sit between the row lookup
+ * (dlrm_emb_bag_fwd with one index per bag) and the interaction.  Storage types are those of the
+ * tables (DLRM_F32, DLRM_F16, DLRM_BF16); sums, softmax statistics and norms are fp32.
+ * ------------------------------------------------------------------------------------------------ */
+#define DLRM_MAX_HEAD_DIM 128        /* d of a head: a multiple of 8, <= 128 */
+#define DLRM_MAX_HEADS 1024          /* query heads; key heads divide them */
+#define DLRM_MAX_ITEMS 2147483647LL  /* items of a call < 2^31 */
+
+/* Rows of heads: element (item t, head h, column c) at data[t * stride_t + h * stride_h + c].  Strides in
+ * elements; rows 16-byte aligned (data, and both strides in bytes); heads may lie side by side in one
+ * projection's output or each on its own.  Rows a call writes must not overlap each other. */
+typedef struct dlrm_heads {
+  void* data;
+  int64_t stride_t; /* >= d */
+  int64_t stride_h; /* >= d where there is more than one head */
+} dlrm_heads;
+
+/* order of the rotated pairs */
+#define DLRM_ROPE_HALF 0        /* columns i and i + rot/2 */
+#define DLRM_ROPE_INTERLEAVED 1 /* columns 2i and 2i + 1 */
+
+/*
+ * Norm and rotary position of query and key heads (host struct, device arrays).  For every row x of d columns:
+ *   n = x * w / sqrt(mean(x^2) + eps)                              (w = wq or wk; n = x where it is NULL)
+ *   pair i < rot/2, angle a = positions[t] * inv_freq[i]:
+ *   (y_a, y_b) = mscale * (n_a cos a - n_b sin a,  n_b cos a + n_a sin a);  columns >= rot: y = n
+ * The angle is reduced in fp64, so it is exact at positions up to 2^31.  Every scaling of positions for
+ * histories longer than those trained on is a choice of inv_freq and mscale by the caller.
+ */
+typedef struct dlrm_qk_rope {
+  int64_t T;                /* items, 0 <= T <= DLRM_MAX_ITEMS */
+  int32_t Hq, Hk;           /* heads, Hq >= 1, Hk >= 0 (0: no keys, their arguments are ignored) */
+  int32_t d;                /* columns of a head, multiple of 8, <= DLRM_MAX_HEAD_DIM */
+  int32_t dtype;            /* DLRM_F32 | DLRM_F16 | DLRM_BF16, of every dlrm_heads of the call */
+  int32_t rot;              /* rotated columns, even, 0 <= rot <= d */
+  int32_t layout;           /* DLRM_ROPE_HALF | DLRM_ROPE_INTERLEAVED */
+  const int32_t* positions; /* [T]; may be NULL for rot == 0 */
+  const float* inv_freq;    /* [rot/2]; may be NULL for rot == 0 */
+  const float* wq;          /* [d] norm weights of the queries, 16-byte aligned, or NULL: queries are not normed */
+  const float* wk;          /* the same of the keys */
+  float eps;                /* > 0 where there is a norm */
+  float mscale;             /* factor on the rotated columns (1 for none) */
+} dlrm_qk_rope;
+
+/* q, k -> q_out, k_out.  An output may be its input (same data and strides). */
+int32_t dlrm_qk_rope_fwd(const dlrm_qk_rope* rope, const dlrm_heads* q, const dlrm_heads* k,
+                         const dlrm_heads* q_out, const dlrm_heads* k_out, void* stream);
+
+/* Bytes of workspace dlrm_qk_rope_bwd needs; 0 for an unsupported shape. */
+size_t dlrm_qk_rope_bwd_workspace_bytes(const dlrm_qk_rope* rope);
+
+/*
+ * Chain rule on the above.  q, k: the forward's inputs; dq_out, dk_out: gradients of its outputs;
+ * dq, dk: gradients of its inputs (may be dq_out, dk_out); dwq, dwk: fp32 [d], gradients of the norm weights summed over
+ * all rows (written; ignored where the weights are NULL).  The sums' order depends on the shape alone:
+ * bitwise reproducible.  workspace: 256-byte aligned device memory; contents are scratch.
+ */
+int32_t dlrm_qk_rope_bwd(const dlrm_qk_rope* rope, const dlrm_heads* q, const dlrm_heads* k,
+                         const dlrm_heads* dq_out, const dlrm_heads* dk_out, const dlrm_heads* dq,
+                         const dlrm_heads* dk, float* dwq, float* dwk, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * A paged cache of keys and values (host struct, device arrays).  Page p holds `page` consecutive items of one
+ * sequence: element (head h, item i of the page, column c) at [((p * Hk + h) * page + i) * d + c].
+ * Item n of sequence s is item n % page of page table[s * table_cols + n / page].  Page numbers outside
+ * [0, n_pages) stand for pages that are not there: nothing is stored to them or read from them.
+ */
+typedef struct dlrm_kv_cache {
+  void* k;              /* [n_pages, Hk, page, d], 16-byte aligned */
+  void* v;              /* the same */
+  const int32_t* table; /* [B, table_cols] */
+  int32_t B;            /* sequences, >= 1 */
+  int32_t table_cols;   /* >= 1 */
+  int32_t n_pages;      /* >= 1 */
+  int32_t page;         /* items of a page, a power of two <= 1024 */
+  int32_t Hk, d, dtype;
+} dlrm_kv_cache;
+
+/*
+ * dlrm_qk_rope_fwd for new items of cached sequences: queries go to q_out; the normed and rotated keys, and the values as
+ * they are, go to the cache, item t as item positions[t] of sequence seqs[t].  An item whose seqs[t] is
+ * outside [0, B), or whose position is outside the table's pages, is not stored.  Two items of a call must not have the same place.
+ * positions is required; rope->Hk, d and dtype are the cache's.  A prompt's items and one new item for each of many
+ * sequences are the same call.
+ */
+int32_t dlrm_qk_rope_append(const dlrm_qk_rope* rope, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
+                            const dlrm_heads* q_out, const dlrm_kv_cache* cache, const int32_t* seqs, void* stream);
+
+/*
+ * Sequences that attend (host struct, device arrays): sequence s has the query items [q_off[s], q_off[s+1]) and
+ * the key items [k_off[s], k_off[s+1]); items of different sequences never see each other.  With nq, nk items,
+ * query i stands at place p = i + nk - nq among the keys.  Key j is visible to it if
+ *   causal == 0, or j <= p, or j < prefix[s].
+ * Its score is  x = scale * <q, k>;  x = cap * tanh(x / cap) if cap > 0;  x - slopes[h] * |p - j| with slopes;
+ * weights are the softmax of the scores over the visible keys.  A query that sees no key gets zeros.
+ * Keys and values at places that no query of the sequence's tile of 32 sees, and rows outside the sequence, are not part of any result,
+ * whatever they hold; within a tile, values (and in the backward queries and upstream gradients) that are
+ * not finite reach other rows of the tile too.
+ */
+typedef struct dlrm_seq_batch {
+  int32_t B;             /* sequences, >= 1 */
+  int32_t causal;        /* 0 or 1 */
+  int64_t Tq, Tk;        /* host copies of q_off[B], k_off[B] */
+  int32_t max_q, max_k;  /* host upper bounds on a sequence's query / key items, >= 0 */
+  const int64_t* q_off;  /* [B+1], q_off[0] = 0, ascending */
+  const int64_t* k_off;  /* [B+1]; the same array as q_off where every item attends over its own sequence */
+  const int32_t* prefix; /* [B] or NULL; only with causal */
+  const float* slopes;   /* [Hq] or NULL */
+  float scale;
+  float cap;             /* >= 0; 0 = none */
+} dlrm_seq_batch;
+
+/*
+ * Attention forward: q [Tq, Hq, d], k and v [Tk, Hk, d] -> out [Tq, Hq, d]; query head h reads key head
+ * h / (Hq / Hk).  lse: fp32 [Hq, Tq], the logarithm of the softmax's denominator (-inf for a query that sees no key),
+ * which the backward reads; NULL if it is not wanted.
+ */
+int32_t dlrm_seq_attn_fwd(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype,
+                          const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v, const dlrm_heads* out,
+                          float* lse, void* stream);
+
+/* Bytes of workspace dlrm_seq_attn_bwd needs; 0 for an unsupported shape. */
+size_t dlrm_seq_attn_bwd_workspace_bytes(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype);
+
+/*
+ * Attention backward by the chain rule: out and lse as the forward wrote them, dout the gradient of out.  The
+ * gradients of a key head are the sums over its query heads.  Without atomics: bitwise reproducible.
+ * workspace: 256-byte aligned device memory; contents are scratch.
+ */
+int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype,
+                          const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v, const dlrm_heads* out,
+                          const float* lse, const dlrm_heads* dout, const dlrm_heads* dq, const dlrm_heads* dk,
+                          const dlrm_heads* dv, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace dlrm_cache_attn needs for up to max_len cached items a sequence; 0 for an unsupported shape. */
+size_t dlrm_cache_attn_workspace_bytes(const dlrm_kv_cache* cache, int32_t Hq, int32_t max_len);
+
+/*
+ * Attention of the newest item of every sequence over its cache: q, out [B, Hq, d]; sequence s has lens[s] items in the cache
+ * (its newest at lens[s] - 1, where the query stands).  Scores as for dlrm_seq_batch.  lens[s] <= 0 gives zeros; a length above
+ * max_len or above the table's pages counts as that.  max_len: host upper bound on lens, >= 1.
+ * The length is split over workgroups and their parts are joined by a second launch where one workgroup per sequence and key
+ * head would leave the device empty.  slopes: [Hq] or NULL.  workspace: 256-byte aligned device memory; contents are scratch.
+ */
+int32_t dlrm_cache_attn(const dlrm_kv_cache* cache, const int32_t* lens, int32_t max_len, int32_t Hq,
+                        const dlrm_heads* q, const dlrm_heads* out, const float* slopes, float scale, float cap,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,7 @@ F32, F16, BF16 = 0, 1, 2
 I64, I32 = 0, 1
 BWD_AUTO, BWD_SORT, BWD_ATOMIC, BWD_SORT_PREPARED, BWD_SORT_PREPARED_FLAT = 0, 1, 2, 3, 4
 FWD_AUTO, FWD_FUSED, FWD_SPLIT = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 _TORCH_DTYPE = {F32: torch.float32, F16: torch.float16, BF16: torch.bfloat16}
 _ELEM = {F32: 4, F16: 2, BF16: 2}
 
@@ -37,6 +38,33 @@ class _SparseBatchC(C.Structure):
         ("tables", C.c_void_p), ("rows", C.c_void_p), ("indices", C.c_void_p),
         ("offsets", C.c_void_p), ("tbl_off", C.c_void_p), ("weights", C.c_void_p),
         ("index_dtype", C.c_int32),
+    ]
+
+
+class _HeadsC(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
+class _QkRopeC(C.Structure):
+    _fields_ = [
+        ("T", C.c_int64), ("Hq", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32),
+        ("rot", C.c_int32), ("layout", C.c_int32), ("positions", C.c_void_p), ("inv_freq", C.c_void_p),
+        ("wq", C.c_void_p), ("wk", C.c_void_p), ("eps", C.c_float), ("mscale", C.c_float),
+    ]
+
+
+class _KvCacheC(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("table", C.c_void_p), ("B", C.c_int32), ("table_cols", C.c_int32),
+        ("n_pages", C.c_int32), ("page", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32), ("dtype", C.c_int32),
+    ]
+
+
+class _SeqBatchC(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("causal", C.c_int32), ("Tq", C.c_int64), ("Tk", C.c_int64), ("max_q", C.c_int32),
+        ("max_k", C.c_int32), ("q_off", C.c_void_p), ("k_off", C.c_void_p), ("prefix", C.c_void_p),
+        ("slopes", C.c_void_p), ("scale", C.c_float), ("cap", C.c_float),
     ]
 
 
@@ -98,6 +126,25 @@ def lib() -> C.CDLL:
         L.dlrm_emb_bag_bwd_sgd_timed.argtypes = [sb, vp, i64, i64, f32, vp, sz, i32, tm, vp]
         L.dlrm_emb_bag_bwd_adagrad_timed.restype = i32
         L.dlrm_emb_bag_bwd_adagrad_timed.argtypes = [sb, vp, vp, i64, i64, f32, f32, vp, sz, i32, tm, vp]
+        hd, rp, kc, sq = C.POINTER(_HeadsC), C.POINTER(_QkRopeC), C.POINTER(_KvCacheC), C.POINTER(_SeqBatchC)
+        L.dlrm_qk_rope_fwd.restype = i32
+        L.dlrm_qk_rope_fwd.argtypes = [rp, hd, hd, hd, hd, vp]
+        L.dlrm_qk_rope_bwd_workspace_bytes.restype = sz
+        L.dlrm_qk_rope_bwd_workspace_bytes.argtypes = [rp]
+        L.dlrm_qk_rope_bwd.restype = i32
+        L.dlrm_qk_rope_bwd.argtypes = [rp, hd, hd, hd, hd, hd, hd, vp, vp, vp, sz, vp]
+        L.dlrm_qk_rope_append.restype = i32
+        L.dlrm_qk_rope_append.argtypes = [rp, hd, hd, hd, hd, kc, vp, vp]
+        L.dlrm_seq_attn_fwd.restype = i32
+        L.dlrm_seq_attn_fwd.argtypes = [sq, i32, i32, i32, i32, hd, hd, hd, hd, vp, vp]
+        L.dlrm_seq_attn_bwd_workspace_bytes.restype = sz
+        L.dlrm_seq_attn_bwd_workspace_bytes.argtypes = [sq, i32, i32, i32, i32]
+        L.dlrm_seq_attn_bwd.restype = i32
+        L.dlrm_seq_attn_bwd.argtypes = [sq, i32, i32, i32, i32, hd, hd, hd, hd, vp, hd, hd, hd, hd, vp, sz, vp]
+        L.dlrm_cache_attn_workspace_bytes.restype = sz
+        L.dlrm_cache_attn_workspace_bytes.argtypes = [kc, i32, i32]
+        L.dlrm_cache_attn.restype = i32
+        L.dlrm_cache_attn.argtypes = [kc, vp, i32, i32, hd, hd, vp, f32, f32, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -352,3 +399,228 @@ def alloc_workspace(batch: SparseBatch) -> torch.Tensor:
         raise DlrmError("dlrm_emb_bag_bwd_workspace_bytes", -2)
     # torch's caching allocator returns 512-byte aligned blocks
     return torch.empty(n, dtype=torch.uint8, device=batch.offsets.device)
+
+
+# ------------------------------------------------------------------ a history in order
+_DTYPE_OF = {t: c for c, t in _TORCH_DTYPE.items()}
+
+
+class Heads:
+    """A tensor [items, heads, d] (any item and head stride, columns next to each other) as the calls below take it.  They take the
+    tensor too; a program that keeps its buffers saves the host a microsecond per tensor and call with views made once."""
+
+    def __init__(self, x: torch.Tensor):
+        if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+            raise ValueError("rows of heads are [items, heads, d] with the columns next to each other: got %s with strides %s"
+                             % (tuple(x.shape), x.stride()))
+        if x.dtype not in _DTYPE_OF:
+            raise DlrmError("Heads", -3)
+        self.x = x
+        self.shape, self.dtype = tuple(x.shape), _DTYPE_OF[x.dtype]
+        st, sh = x.stride(0), x.stride(1)
+        # (a stride along an axis of one element means nothing, and torch may give any)
+        self.c = _HeadsC(x.data_ptr(), st if x.shape[0] > 1 else 0, sh if x.shape[1] > 1 else 0)
+
+
+def _heads(fn: str, x, n: int, H: int, d: int, dtype: int):
+    v = x if type(x) is Heads else Heads(x)
+    if v.shape != (n, H, d):
+        raise ValueError("%s: a tensor of shape %s where %s is wanted" % (fn, v.shape, (n, H, d)))
+    if v.dtype != dtype:
+        raise DlrmError(fn, -3)
+    return C.byref(v.c)
+
+
+def _first(x):
+    """(view, shape, storage type) of the tensor that the others of a call go by."""
+    v = x if type(x) is Heads else Heads(x)
+    return v, v.shape, v.dtype
+
+
+def _vector(fn: str, x: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[int]:
+    if x is None:
+        return None
+    if x.dtype != dtype or x.numel() != n or not x.is_contiguous():
+        raise ValueError("%s: a contiguous %s array of %d elements is wanted, got %s %s" % (fn, dtype, n, x.dtype, tuple(x.shape)))
+    return x.data_ptr()
+
+
+def _workspace(x: Optional[torch.Tensor]):
+    return (None, 0) if x is None else (x.data_ptr(), x.numel() * x.element_size())
+
+
+class QkRope:
+    """Norm and rotary position of Hq query and Hk key heads of d columns for the items at `positions` (dlrm_qk_rope).
+    wq, wk: norm weights or None; inv_freq: radians per position of every rotated pair (see rope_frequencies)."""
+
+    def __init__(self, positions: Optional[torch.Tensor], Hq: int, Hk: int, d: int, inv_freq: Optional[torch.Tensor] = None,
+                 rot: Optional[int] = None, layout: int = ROPE_HALF, wq: Optional[torch.Tensor] = None,
+                 wk: Optional[torch.Tensor] = None, eps: float = 1e-6, mscale: float = 1.0, T: Optional[int] = None):
+        if rot is None:
+            rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        if T is None:
+            if positions is None:
+                raise ValueError("QkRope: positions or the number of items T is needed")
+            T = positions.numel()
+        self.T, self.Hq, self.Hk, self.d = int(T), Hq, Hk, d
+        self.positions, self.inv_freq, self.wq, self.wk = positions, inv_freq, wq, wk
+        self.c = _QkRopeC(self.T, Hq, Hk, d, F32, rot, layout, _vector("QkRope", positions, self.T, torch.int32),
+                          _vector("QkRope", inv_freq, rot // 2, torch.float32), _vector("QkRope", wq, d, torch.float32),
+                          _vector("QkRope", wk, d, torch.float32), eps, mscale)
+
+    def ref(self, dtype: int):
+        self.c.dtype = dtype
+        return C.byref(self.c)
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, stretch: float = 1.0, keep_turns: Optional[float] = None,
+                     drop_turns: float = 1.0, trained_length: int = 0, device=None) -> torch.Tensor:
+    """inv_freq of QkRope: base ** (-2 i / rot), positions divided by `stretch` for histories that long times the trained ones.  With
+    keep_turns the division is by parts: a pair that turns at least keep_turns times over trained_length keeps its frequency, one
+    that turns at most drop_turns times is divided, those between are blended linearly in their number of turns."""
+    f = base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    if keep_turns is None:
+        f = f / stretch
+    else:
+        if not (trained_length > 0 and keep_turns > drop_turns):
+            raise ValueError("rope_frequencies: keep_turns > drop_turns and the trained length are needed for scaling by parts")
+        turns = trained_length * f / 6.283185307179586
+        keep = ((turns - drop_turns) / (keep_turns - drop_turns)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / stretch)
+    return f.to(torch.float32).to(device)
+
+
+def dlrm_qk_rope_fwd(rope: QkRope, q, k, q_out, k_out):
+    """q, q_out: [T, Hq, d]; k, k_out: [T, Hk, d] (None for Hk = 0).  An output may be its input."""
+    fn = "dlrm_qk_rope_fwd"
+    v, _, dt = _first(q)
+    n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
+    _check(fn, lib().dlrm_qk_rope_fwd(rope.ref(dt), _heads(fn, v, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt) if Hk else None,
+                                      _heads(fn, q_out, n, Hq, d, dt), _heads(fn, k_out, n, Hk, d, dt) if Hk else None, _stream()))
+
+
+def dlrm_qk_rope_bwd(rope: QkRope, q, k, dq_out, dk_out, dq, dk, dwq: Optional[torch.Tensor], dwk: Optional[torch.Tensor],
+                     workspace: Optional[torch.Tensor]):
+    """Gradients dq, dk of the forward's inputs (may be dq_out, dk_out) and dwq, dwk (fp32 [d], written) of the norm weights."""
+    fn = "dlrm_qk_rope_bwd"
+    v, _, dt = _first(q)
+    n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
+    queries = [_heads(fn, x, n, Hq, d, dt) for x in (v, dq_out, dq)]
+    keys = [_heads(fn, x, n, Hk, d, dt) for x in (k, dk_out, dk)] if Hk else [None] * 3
+    ws, ws_bytes = _workspace(workspace)
+    _check(fn, lib().dlrm_qk_rope_bwd(rope.ref(dt), queries[0], keys[0], queries[1], keys[1], queries[2], keys[2],
+                                      _vector(fn, dwq, d, torch.float32), _vector(fn, dwk, d, torch.float32), ws, ws_bytes, _stream()))
+
+
+def alloc_qk_rope_workspace(rope: QkRope) -> torch.Tensor:
+    n = int(lib().dlrm_qk_rope_bwd_workspace_bytes(rope.ref(rope.c.dtype)))
+    # (sized for any storage type: the widest rows take the most groups)
+    n = max([n] + [int(lib().dlrm_qk_rope_bwd_workspace_bytes(rope.ref(t))) for t in (F32, F16, BF16)])
+    if n == 0:
+        raise DlrmError("dlrm_qk_rope_bwd_workspace_bytes", -2)
+    device = next((x.device for x in (rope.positions, rope.wq, rope.wk) if x is not None), None)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+class KvCache:
+    """Pages of keys and values, k and v: [n_pages, Hk, page, d]; table: int32 [B, pages of a sequence] (dlrm_kv_cache)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_contiguous() and v.is_contiguous()):
+            raise ValueError("KvCache: k and v are contiguous [pages, heads, items of a page, d] of one type")
+        if table.dim() != 2 or table.dtype != torch.int32 or not table.is_contiguous():
+            raise ValueError("KvCache: the table is a contiguous int32 [sequences, pages of a sequence]")
+        if k.dtype not in _DTYPE_OF:
+            raise DlrmError("KvCache", -3)
+        self.k, self.v, self.table = k, v, table
+        self.B = int(table.shape[0])
+        self.n_pages, self.Hk, self.page, self.d = (int(x) for x in k.shape)
+        self.dtype = _DTYPE_OF[k.dtype]
+        self.c = _KvCacheC(k.data_ptr(), v.data_ptr(), table.data_ptr(), self.B, int(table.shape[1]), self.n_pages, self.page, self.Hk,
+                           self.d, self.dtype)
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def dlrm_qk_rope_append(rope: QkRope, q, k, v, q_out, cache: KvCache, seqs: torch.Tensor):
+    """Queries to q_out, keys (normed and rotated) and values to the cache, item t as item positions[t] of sequence seqs[t]."""
+    fn = "dlrm_qk_rope_append"
+    qv, _, dt = _first(q)
+    n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
+    if not Hk:
+        raise DlrmError(fn, -2)
+    _check(fn, lib().dlrm_qk_rope_append(rope.ref(dt), _heads(fn, qv, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt),
+                                         _heads(fn, v, n, Hk, d, dt), _heads(fn, q_out, n, Hq, d, dt), cache.ref(),
+                                         _vector(fn, seqs, n, torch.int32), _stream()))
+
+
+class SeqBatch:
+    """Sequences that attend (dlrm_seq_batch).  q_off, k_off: int64 [B + 1]; Tq, Tk: their last elements; max_q, max_k: bounds on a
+    sequence's items; scale: of the products, 1 / sqrt(d) unless given."""
+
+    def __init__(self, q_off: torch.Tensor, k_off: torch.Tensor, Tq: int, Tk: int, max_q: int, max_k: int, causal: bool = True,
+                 prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                 cap: float = 0.0):
+        self.B = int(q_off.numel()) - 1
+        self.q_off, self.k_off, self.prefix, self.slopes, self.scale = q_off, k_off, prefix, slopes, scale
+        if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
+            raise ValueError("SeqBatch: slopes are contiguous float32, one for each query head")
+        self.Tq, self.Tk = int(Tq), int(Tk)
+        self.c = _SeqBatchC(self.B, int(causal), self.Tq, self.Tk, max_q, max_k, _vector("SeqBatch", q_off, self.B + 1, torch.int64),
+                            _vector("SeqBatch", k_off, self.B + 1, torch.int64), _vector("SeqBatch", prefix, self.B, torch.int32),
+                            _ptr(slopes), 0.0, cap)
+
+    def ref(self, Hq: int, d: int):
+        if self.slopes is not None and self.slopes.numel() != Hq:
+            raise ValueError("SeqBatch: %d slopes for %d query heads" % (self.slopes.numel(), Hq))
+        self.c.scale = d ** -0.5 if self.scale is None else self.scale
+        return C.byref(self.c)
+
+
+def dlrm_seq_attn_fwd(seq: SeqBatch, q, k, v, out, lse: Optional[torch.Tensor] = None):
+    """q, out: [Tq, Hq, d]; k, v: [Tk, Hk, d]; lse: fp32 [Hq, Tq] for the backward, or None."""
+    fn = "dlrm_seq_attn_fwd"
+    qv, (_, Hq, d), dt = _first(q)
+    kv, (_, Hk, _), _ = _first(k)
+    _check(fn, lib().dlrm_seq_attn_fwd(seq.ref(Hq, d), Hq, Hk, d, dt, _heads(fn, qv, seq.Tq, Hq, d, dt), _heads(fn, kv, seq.Tk, Hk, d, dt),
+                                       _heads(fn, v, seq.Tk, Hk, d, dt), _heads(fn, out, seq.Tq, Hq, d, dt),
+                                       _vector(fn, lse, Hq * seq.Tq, torch.float32), _stream()))
+
+
+def dlrm_seq_attn_bwd(seq: SeqBatch, q, k, v, out, lse: torch.Tensor, dout, dq, dk, dv, workspace: torch.Tensor):
+    fn = "dlrm_seq_attn_bwd"
+    qv, (_, Hq, d), dt = _first(q)
+    kv, (_, Hk, _), _ = _first(k)
+    queries = [_heads(fn, x, seq.Tq, Hq, d, dt) for x in (qv, out, dout, dq)]
+    keys = [_heads(fn, x, seq.Tk, Hk, d, dt) for x in (kv, v, dk, dv)]
+    ws, ws_bytes = _workspace(workspace)
+    _check(fn, lib().dlrm_seq_attn_bwd(seq.ref(Hq, d), Hq, Hk, d, dt, queries[0], keys[0], keys[1], queries[1],
+                                       _vector(fn, lse, Hq * seq.Tq, torch.float32), queries[2], queries[3], keys[2], keys[3], ws, ws_bytes,
+                                       _stream()))
+
+
+def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: int = F32) -> torch.Tensor:
+    n = int(lib().dlrm_seq_attn_bwd_workspace_bytes(seq.ref(Hq, d), Hq, Hk, d, dtype))
+    if n == 0:
+        raise DlrmError("dlrm_seq_attn_bwd_workspace_bytes", -2)
+    return torch.empty(n, dtype=torch.uint8, device=seq.q_off.device)
+
+
+def dlrm_cache_attn(cache: KvCache, lens: torch.Tensor, max_len: int, q, out, workspace: Optional[torch.Tensor],
+                    slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None, cap: float = 0.0):
+    """q, out: [B, Hq, d]; lens: int32 [B], items of every sequence in the cache, its newest among them."""
+    fn = "dlrm_cache_attn"
+    qv, (_, Hq, d), dt = _first(q)
+    ws, ws_bytes = _workspace(workspace)
+    _check(fn, lib().dlrm_cache_attn(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, Hq,
+                                     _heads(fn, qv, cache.B, Hq, cache.d, cache.dtype), _heads(fn, out, cache.B, Hq, cache.d, cache.dtype),
+                                     _vector(fn, slopes, Hq, torch.float32), d ** -0.5 if scale is None else scale, cap, ws, ws_bytes,
+                                     _stream()))
+
+
+def alloc_cache_attn_workspace(cache: KvCache, Hq: int, max_len: int) -> torch.Tensor:
+    n = int(lib().dlrm_cache_attn_workspace_bytes(cache.ref(), Hq, max_len))
+    if n == 0:
+        raise DlrmError("dlrm_cache_attn_workspace_bytes", -2)
+    return torch.empty(n, dtype=torch.uint8, device=cache.table.device)

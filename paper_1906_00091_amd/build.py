@@ -14,7 +14,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdlrm_hot.so")
 SOURCES = ["bwd_reduce_sgd.hip", "bwd_reduce_adagrad.hip", "bwd_reduce_sgd_weighted.hip",
            "bwd_reduce_adagrad_weighted.hip", "bwd_tail.hip", "bwd_partition.hip", "bwd_export.hip",
-           "emb_bwd.hip", "emb_fwd.hip", "interact.hip", "pooled_interact.hip", "util.hip"]
+           "emb_bwd.hip", "emb_fwd.hip", "interact.hip", "pooled_interact.hip", "util.hip",
+           "qk_rope.hip", "seq_attn_f32.hip", "seq_attn_f16.hip", "seq_attn_bf16.hip", "seq_attn.hip", "cache_attn.hip"]
 CEIL_LIB = os.path.join(PKG, "libdlrm_ceilings.so")
 CEIL_SOURCES = ["ceilings.hip"]
 

@@ -1,0 +1,447 @@
+// Attention of one new item per sequence over a paged cache of keys and values.
+//
+// Bound by memory: the cache is read once.  All query heads of a key head (16 at a time) are the columns of one matrix tile, so a key row
+// is loaded once for all of them, straight from its page into the registers that the product takes it in: a lane's 16 bytes are
+// 8 consecutive columns of one key.  S^T = K Q^T leaves a lane four keys of one head, and those registers are, with the contracted
+// index permuted, what O^T = V^T P^T takes; values pass through a piece of LDS that belongs to the wavefront alone, to be read by
+// columns.  So the wavefronts of a workgroup run without a barrier, each with its own running maximum and sum, over
+// every fourth tile of 32 keys, and are joined once at the end.
+//
+// The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in
+// the order of the chunks.
+#include <math.h>
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "heads.h"
+
+namespace dlrm {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kInf = __builtin_inff();
+constexpr int kCacheThreads = 256, kCacheWaves = 4, kKeys = 32, kHeads = 16;
+constexpr int kTablePages = 1024;  // pages of a chunk, at most
+
+struct CacheArgs {
+  Rows q, out;
+  const char* k;
+  const char* v;
+  const int32_t* table;
+  const int32_t* lens;
+  const float* slopes;
+  int B, Hq, Hk, d, cols, n_pages, page_shift, max_len;
+  int chunk, splits, blocks;  // keys of a chunk; chunks of a sequence; groups of 16 heads of a key head
+  float scale, cap;
+  float* po;  // [B][Hq][splits][d] unnormalised sums
+  float* pm;  // [B][Hq][splits][2] maximum (powers of two), sum of weights
+};
+
+// operand of mfma 16x16: 8 values a lane; lane group g = lane / 16 holds values 8g..8g+7 of 32
+template <int DT>
+struct Op16;
+template <>
+struct Op16<DLRM_BF16> {
+  u32x4 v;
+  __device__ static inline f32x4 mma(const Op16& a, const Op16& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
+  }
+};
+template <>
+struct Op16<DLRM_F16> {
+  u32x4 v;
+  __device__ static inline f32x4 mma(const Op16& a, const Op16& b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.v), __builtin_bit_cast(f16x8, b.v), c, 0, 0, 0);
+  }
+};
+template <>
+struct Op16<DLRM_F32> {
+  float f[8];
+  __device__ static inline f32x4 mma(const Op16& a, const Op16& b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[j], b.f[j], c, 0, 0, 0);
+    return c;
+  }
+};
+template <int DT>
+__device__ inline Op16<DT> op16_load(const char* p, bool there) {
+  Op16<DT> o;
+  if constexpr (DT == DLRM_F32) {
+    f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    if (there) {
+      a = *reinterpret_cast<const f32x4*>(p);
+      b = *reinterpret_cast<const f32x4*>(p + 16);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      o.f[j] = a[j];
+      o.f[4 + j] = b[j];
+    }
+  } else {
+    o.v = u32x4{0, 0, 0, 0};
+    if (there) o.v = load16(p);
+  }
+  return o;
+}
+template <int DT>
+__device__ inline Op16<DT> op16_set(const float* f) {
+  Op16<DT> o;
+  if constexpr (DT == DLRM_F32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o.f[j] = f[j];
+  } else {
+    o.v = narrow<DT>(f);
+  }
+  return o;
+}
+
+template <int DT>
+__device__ inline float bent16(float z) {
+  if constexpr (DT == DLRM_F32) {
+    return tanhf(z);
+  } else {
+    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
+  }
+}
+
+template <int DT, int DP>
+__global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) {
+  constexpr int EB = Tab<DT>::EB, E = Tab<DT>::ELEMS, STEPS = DP / 32, NB = DP / 16;
+  constexpr int CH = DP * EB / 16, NV = kKeys * CH / DLRM_WAVE;  // chunks of a row; of a tile, per lane
+  constexpr int STRIDE = DP * EB + 16;
+  constexpr int OS = DP + 4;  // row of the joined sums
+  constexpr int VBYTES = kCacheWaves * kKeys * STRIDE, OBYTES = kCacheWaves * kHeads * OS * 4;
+  __shared__ __attribute__((aligned(16))) char lds[VBYTES > OBYTES ? VBYTES : OBYTES];
+  __shared__ int pages[kTablePages];
+  __shared__ float stat[kCacheWaves][2][kHeads];
+  const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
+  const int blk = rest % a.blocks, hk = rest / a.blocks % a.Hk, s = rest / a.blocks / a.Hk;
+  const int G = a.Hq / a.Hk;
+  const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
+  const int start = split * a.chunk, end = min(len, start + a.chunk);
+  if (start >= end && split > 0) return;  // the first chunk of an empty sequence gives zeros
+  const int lane = lane_id(), g = lane >> 4, n = lane & 15, wave = wave_id();
+  const int head = hk * G + blk * kHeads + n;  // of this lane's column
+  const bool head_there = blk * kHeads + n < G;
+
+  const int page0 = start >> a.page_shift, n_pages = start < end ? ((end - 1) >> a.page_shift) - page0 + 1 : 0;
+  for (int p = threadIdx.x; p < n_pages; p += kCacheThreads) pages[p] = a.table[(int64_t)s * a.cols + page0 + p];
+  Op16<DT> qf[STEPS];
+  const char* qrow = row_of(a.q, s, head_there ? head : hk * G);
+#pragma unroll
+  for (int st = 0; st < STEPS; ++st) qf[st] = op16_load<DT>(qrow + (32 * st + 8 * g) * EB, head_there && 32 * st + 8 * g < a.d);
+  const float c = a.scale * kLog2e, slope = a.slopes && head_there ? a.slopes[head] * kLog2e : 0.0f;
+  const bool bend = a.cap > 0.0f;
+  const float zs = bend ? a.scale / a.cap : 0.0f, cl = a.cap * kLog2e;
+  __syncthreads();
+
+  const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;
+  const int64_t head_bytes = (int64_t)row_bytes << a.page_shift, page_bytes = head_bytes * a.Hk;
+  // byte offset of key j's row in the cache, or -1: past the end, or on a page that is not there
+  auto row_at = [&](int j) -> int64_t {
+    if (j >= end) return -1;
+    const int p = pages[(j >> a.page_shift) - page0];
+    if (p < 0 || p >= a.n_pages) return -1;
+    return p * page_bytes + hk * head_bytes + (int64_t)((j & mask) * row_bytes);
+  };
+  char* vs = lds + wave * kKeys * STRIDE;
+  Op16<DT> kf[2][STEPS];
+  u32x4 vf[NV];
+  bool seen[2];
+  auto fetch = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t at = row_at(j0 + 16 * u + n);
+      seen[u] = at >= 0;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) kf[u][st] = op16_load<DT>(a.k + at + (32 * st + 8 * g) * EB, at >= 0 && 32 * st + 8 * g < a.d);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int id = lane + i * DLRM_WAVE, r = id / CH, cc = id % CH;
+      const int64_t at = row_at(j0 + r);
+      vf[i] = u32x4{0, 0, 0, 0};
+      if (at >= 0 && cc * E < a.d) vf[i] = load16(a.v + at + cc * 16);
+    }
+  };
+
+  f32x4 o[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) o[b] = f32x4{0, 0, 0, 0};
+  float m = -kInf, l = 0.0f;
+  int j0 = start + wave * kKeys;
+  if (j0 < end) fetch(j0);
+  for (; j0 < end; j0 += kCacheWaves * kKeys) {
+    f32x4 sc[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      sc[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) sc[u] = Op16<DT>::mma(kf[u][st], qf[st], sc[u]);
+    }
+    // which of the four keys of each register set are there: their lanes know
+    const uint64_t have0 = __ballot(seen[0]), have1 = __ballot(seen[1]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int id = lane + i * DLRM_WAVE;
+      *reinterpret_cast<u32x4*>(vs + (id / CH) * STRIDE + (id % CH) * 16) = vf[i];
+    }
+    const int jn = j0 + kCacheWaves * kKeys;
+    if (jn < end) fetch(jn);
+    float x[8];
+    float top = -kInf;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = 4 * g + r;
+        float y = sc[u][r];
+        y = bend ? bent16<DT>(y * zs) * cl : y * c;
+        y -= slope * (float)(len - 1 - (j0 + 16 * u + key));
+        x[4 * u + r] = ((u ? have1 : have0) >> key) & 1 ? y : -kInf;
+        top = fmaxf(top, x[4 * u + r]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16, DLRM_WAVE));
+    top = fmaxf(top, __shfl_xor(top, 32, DLRM_WAVE));
+    const float m1 = fmaxf(m, top), ms = m1 == -kInf ? 0.0f : m1;
+    const float f = __builtin_amdgcn_exp2f(m - ms);
+    m = m1;
+    l *= f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) o[b] *= f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(x[r] - ms);
+      l += x[r];
+    }
+    const Op16<DT> p = op16_set<DT>(x);
+    // the values' columns: rows 4g..4g+3 and 16+4g..16+4g+3 of the tile for lane group g
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      Op16<DT> vt;
+      if constexpr (EB == 2) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const char* q = vs + (4 * g + (n >> 2)) * STRIDE + (16 * b + 4 * (n & 3)) * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 16 * STRIDE));
+        const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+        vt.v = u32x4{l2.x, l2.y, h2.x, h2.y};
+      } else {
+        const char* q = vs + 4 * g * STRIDE + (16 * b + n) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          vt.f[j] = *reinterpret_cast<const float*>(q + j * STRIDE);
+          vt.f[4 + j] = *reinterpret_cast<const float*>(q + (16 + j) * STRIDE);
+        }
+      }
+      o[b] = Op16<DT>::mma(vt, p, o[b]);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  l += __shfl_xor(l, 16, DLRM_WAVE);
+  l += __shfl_xor(l, 32, DLRM_WAVE);
+  __syncthreads();  // every wavefront is done with its values
+  if (g == 0) {
+    stat[wave][0][n] = m;
+    stat[wave][1][n] = l;
+  }
+  float* os = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+    *reinterpret_cast<f32x4*>(os + (wave * kHeads + n) * OS + 16 * b + 4 * g) = o[b];
+  __syncthreads();
+  // join the wavefronts: a thread takes 4 columns of a head
+  const int per_head = a.d / 4, rows = min(kHeads, G - blk * kHeads);
+  for (int id = threadIdx.x; id < rows * per_head; id += kCacheThreads) {
+    const int hn = id / per_head, col = id % per_head * 4, hd = hk * G + blk * kHeads + hn;
+    float top = -kInf;
+#pragma unroll
+    for (int w = 0; w < kCacheWaves; ++w) top = fmaxf(top, stat[w][0][hn]);
+    const float ms = top == -kInf ? 0.0f : top;
+    f32x4 sum = {0, 0, 0, 0};
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kCacheWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(stat[w][0][hn] - ms);
+      total += f * stat[w][1][hn];
+      sum += f * *reinterpret_cast<const f32x4*>(os + (w * kHeads + hn) * OS + col);
+    }
+    if (a.splits == 1) {
+      const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+      char* dst = row_of(a.out, s, hd) + col * EB;
+      sum *= inv;
+      if constexpr (DT == DLRM_F32) {
+        *reinterpret_cast<f32x4*>(dst) = sum;
+      } else {
+        const float y[8] = {sum[0], sum[1], sum[2], sum[3], 0, 0, 0, 0};
+        const u32x4 r = narrow<DT>(y);
+        *reinterpret_cast<u32x2*>(dst) = u32x2{r.x, r.y};
+      }
+    } else {
+      const int64_t at = ((int64_t)s * a.Hq + hd) * a.splits + split;
+      *reinterpret_cast<f32x4*>(a.po + at * a.d + col) = sum;
+      if (col == 0) {
+        a.pm[at * 2] = top;
+        a.pm[at * 2 + 1] = total;
+      }
+    }
+  }
+}
+
+// Joins the chunks of one sequence and head: 8 wavefronts, each half of a wavefront takes every 16th chunk, 4 columns a lane.
+constexpr int kJoinThreads = 512;
+template <int DT>
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
+  constexpr int ROWS = kJoinThreads / 32;
+  __shared__ float red[ROWS];
+  __shared__ f32x4 part[ROWS][32];
+  __shared__ float tot[ROWS];
+  const int64_t row = blockIdx.x;
+  const int s = (int)(row / a.Hq), head = (int)(row - (int64_t)s * a.Hq);
+  const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
+  const int n = max(1, (len + a.chunk - 1) / a.chunk);
+  const float* pm = a.pm + row * a.splits * 2;
+  const float* po = a.po + row * a.splits * a.d;
+  const int y = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4;
+  float top = -kInf;
+  for (int i = threadIdx.x; i < n; i += kJoinThreads) top = fmaxf(top, pm[2 * i]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, DLRM_WAVE));
+  if ((threadIdx.x & 31) == 0) red[y] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) top = fmaxf(top, red[i]);
+  const float ms = top == -kInf ? 0.0f : top;
+  f32x4 sum = {0, 0, 0, 0};
+  float total = 0.0f;
+  for (int i = y; i < n; i += ROWS) {
+    const float f = __builtin_amdgcn_exp2f(pm[2 * i] - ms);
+    total += f * pm[2 * i + 1];
+    if (col < a.d) sum += f * loadf4(po + (int64_t)i * a.d + col);
+  }
+  part[y][threadIdx.x & 31] = sum;
+  if ((threadIdx.x & 31) == 0) tot[y] = total;
+  __syncthreads();
+  if (y != 0 || col >= a.d) return;
+  sum = f32x4{0, 0, 0, 0};
+  total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    sum += part[i][threadIdx.x];
+    total += tot[i];
+  }
+  sum *= total > 0.0f ? 1.0f / total : 0.0f;
+  char* dst = row_of(a.out, s, head) + col * Tab<DT>::EB;
+  if constexpr (DT == DLRM_F32) {
+    *reinterpret_cast<f32x4*>(dst) = sum;
+  } else {
+    const float v[8] = {sum[0], sum[1], sum[2], sum[3], 0, 0, 0, 0};
+    const u32x4 r = narrow<DT>(v);
+    *reinterpret_cast<u32x2*>(dst) = u32x2{r.x, r.y};
+  }
+}
+
+// Keys of a chunk: as many workgroups as fill the device several times over, at least two tiles a wavefront.
+static int chunk_of(const dlrm_kv_cache* c, int Hq, int max_len) {
+  const int64_t rows = (int64_t)c->B * c->Hk * ((Hq / c->Hk + kHeads - 1) / kHeads);
+  const int64_t wanted = 4096;
+  int64_t n = (rows * max_len + wanted - 1) / wanted;
+  if (n < 256) n = 256;
+  const int64_t most = (int64_t)kTablePages * c->page;  // a chunk starts on a page where it is a multiple of the page
+  n = (n + 127) / 128 * 128;
+  if (n > most - c->page) n = most - c->page;
+  if (n < 1) n = 1;
+  return (int)(n > max_len ? max_len : n);
+}
+
+static int check_cache_attn(const dlrm_kv_cache* c, int Hq, int max_len) {
+  if (int st = check_cache(c)) return st;
+  if (int st = check_head_shape(Hq, c->Hk, c->d, c->dtype)) return st;
+  if (max_len < 1) return DLRM_ERR_BAD_SHAPE;
+  return DLRM_OK;
+}
+
+static int splits_of(const dlrm_kv_cache* c, int Hq, int max_len) {
+  const int64_t held = (int64_t)c->table_cols * c->page;
+  if (max_len > held) max_len = (int)held;
+  const int n = chunk_of(c, Hq, max_len);
+  return (max_len + n - 1) / n;
+}
+
+}  // namespace dlrm
+
+using namespace dlrm;
+
+extern "C" size_t dlrm_cache_attn_workspace_bytes(const dlrm_kv_cache* c, int32_t Hq, int32_t max_len) {
+  if (check_cache_attn(c, Hq, max_len) != DLRM_OK) return 0;
+  const size_t n = (size_t)c->B * Hq * splits_of(c, Hq, max_len) * (c->d + 2) * sizeof(float);
+  return (n + 255) / 256 * 256;
+}
+
+extern "C" int32_t dlrm_cache_attn(const dlrm_kv_cache* c, const int32_t* lens, int32_t max_len, int32_t Hq, const dlrm_heads* q,
+                                   const dlrm_heads* out, const float* slopes, float scale, float cap, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  if (int st = check_cache_attn(c, Hq, max_len)) return st;
+  if (!lens) return DLRM_ERR_NULL;
+  if (!(scale > 0.0f) || !isfinite(scale) || !(cap >= 0.0f) || !isfinite(cap)) return DLRM_ERR_BAD_SHAPE;
+  const int eb = elem_bytes(c->dtype);
+  for (const dlrm_heads* x : {q, out})
+    if (int st = check_heads(x, c->B, Hq, c->d, eb)) return st;
+  CacheArgs a = {};
+  a.q = rows_of(q, eb);
+  a.out = rows_of(out, eb);
+  a.k = static_cast<const char*>(c->k);
+  a.v = static_cast<const char*>(c->v);
+  a.table = c->table;
+  a.lens = lens;
+  a.slopes = slopes;
+  a.B = c->B;
+  a.Hq = Hq;
+  a.Hk = c->Hk;
+  a.d = c->d;
+  a.cols = c->table_cols;
+  a.n_pages = c->n_pages;
+  a.page_shift = ilog2_ceil(c->page);
+  const int64_t held = (int64_t)c->table_cols * c->page;
+  a.max_len = max_len > held ? (int)held : max_len;
+  a.chunk = chunk_of(c, Hq, a.max_len);
+  a.splits = (a.max_len + a.chunk - 1) / a.chunk;
+  a.blocks = (Hq / c->Hk + kHeads - 1) / kHeads;
+  a.scale = scale;
+  a.cap = cap;
+  const int64_t grid = (int64_t)a.splits * a.blocks * a.Hk * a.B;
+  if (grid > 0x7fffffff || (int64_t)a.B * Hq > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;
+  if (a.splits > 1) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < dlrm_cache_attn_workspace_bytes(c, Hq, max_len))
+      return DLRM_ERR_WORKSPACE;
+    a.po = static_cast<float*>(workspace);
+    a.pm = a.po + (int64_t)a.B * Hq * a.splits * a.d;
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto by_type = [&](auto dt) {
+    auto go = [&](auto dp) {
+      hipLaunchKernelGGL((cache_attn_kernel<dt(), dp()>), dim3((unsigned)grid), dim3(kCacheThreads), 0, st, a);
+      DLRM_CHECK_LAUNCH();
+      if (a.splits > 1) {
+        hipLaunchKernelGGL(cache_join_kernel<dt()>, dim3((unsigned)(a.B * Hq)), dim3(kJoinThreads), 0, st, a);
+        DLRM_CHECK_LAUNCH();
+      }
+      return (int)DLRM_OK;
+    };
+    if (a.d <= 32) return go(std::integral_constant<int, 32>{});
+    if (a.d <= 64) return go(std::integral_constant<int, 64>{});
+    if (a.d <= 96) return go(std::integral_constant<int, 96>{});
+    return go(std::integral_constant<int, 128>{});
+  };
+  switch (c->dtype) {
+    case DLRM_F32: return by_type(std::integral_constant<int, DLRM_F32>{});
+    case DLRM_F16: return by_type(std::integral_constant<int, DLRM_F16>{});
+    default: return by_type(std::integral_constant<int, DLRM_BF16>{});
+  }
+}

@@ -1,0 +1,56 @@
+// Rows of heads: what the kernels that read a history in order share (views, storage types, argument checks).
+#pragma once
+
+#include "common.h"
+
+namespace dlrm {
+
+// one dlrm_heads on its way to a kernel, strides in bytes
+struct Rows {
+  char* p;
+  int64_t st, sh;
+};
+
+__device__ inline char* row_of(const Rows& r, int64_t t, int h) { return r.p + t * r.st + h * r.sh; }
+
+__host__ inline Rows rows_of(const dlrm_heads* x, int eb) {
+  return Rows{static_cast<char*>(x->data), x->stride_t * eb, x->stride_h * eb};
+}
+
+// Checks a view of H heads of d columns, n items.
+__host__ inline int check_heads(const dlrm_heads* x, int64_t n, int H, int d, int eb) {
+  if (!x || (!x->data && n > 0)) return DLRM_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(x->data) & 15) return DLRM_ERR_BAD_SHAPE;
+  if ((n > 1 && x->stride_t < d) || (H > 1 && x->stride_h < d)) return DLRM_ERR_BAD_SHAPE;
+  // a tile's rows are reached with 32-bit byte offsets
+  if (x->stride_t < 0 || x->stride_h < 0 || x->stride_t > (1 << 23) || x->stride_h >= (int64_t)1 << 40) return DLRM_ERR_BAD_SHAPE;
+  if (((x->stride_t * eb) & 15) != 0 || ((x->stride_h * eb) & 15) != 0) return DLRM_ERR_BAD_SHAPE;
+  return DLRM_OK;
+}
+
+__host__ inline int check_head_shape(int Hq, int Hk, int d, int dtype) {
+  if (!dtype_ok(dtype)) return DLRM_ERR_BAD_DTYPE;
+  if (Hq < 1 || Hq > DLRM_MAX_HEADS || Hk < 1 || Hq % Hk != 0) return DLRM_ERR_BAD_SHAPE;
+  if (d < 8 || d > DLRM_MAX_HEAD_DIM || (d & 7)) return DLRM_ERR_BAD_SHAPE;
+  return DLRM_OK;
+}
+
+// 16-byte chunk <- fp32 values, rounded to nearest-even once where the storage type has 16 bits
+template <int DT>
+__device__ inline u32x4 narrow(const float* f) {
+  if constexpr (DT == DLRM_F32) {
+    return u32x4{f2u(f[0]), f2u(f[1]), f2u(f[2]), f2u(f[3])};
+  } else if constexpr (DT == DLRM_F16) {
+    return u32x4{float2_to_half2(f[0], f[1]), float2_to_half2(f[2], f[3]), float2_to_half2(f[4], f[5]), float2_to_half2(f[6], f[7])};
+  } else {
+    typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
+    b16x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (__bf16)f[j];
+    return __builtin_bit_cast(u32x4, v);
+  }
+}
+
+int check_cache(const dlrm_kv_cache* c);  // qk_rope.hip
+
+}  // namespace dlrm

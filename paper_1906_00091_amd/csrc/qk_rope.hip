@@ -1,0 +1,515 @@
+// Norm and rotary position of query and key heads, forward, backward and on the way into a paged cache.
+//
+// A row of d columns is held by a group of G lanes (a power of two), 16 bytes a lane; the sum of squares and the
+// backward's <g w, n> are joined by lane exchanges inside the group.  A group stays with one item and walks its heads, so that the
+// item's angles are reduced and their sines and cosines taken once, in registers, for all of its heads: the angle in turns is
+// position * frequency / 2 pi in fp64 (24 + 31 bits of product, exact; fp32 would be off by 1e-3 radians at position 2^14),
+// its fraction goes to sincospi in fp32.  In the half layout a column's partner lies rot/2 columns away: in another lane at the same
+// place of the chunk where rot/2 is a multiple of a chunk's columns (one exchange of the raw chunk), else anywhere (through LDS).
+//
+// Bound by memory: every row is read and written once.
+#include <initializer_list>
+#include <type_traits>
+
+#include "heads.h"
+
+namespace dlrm {
+
+struct RopeArgs {
+  Rows q, k, v, qo, ko;   // forward
+  Rows dqo, dko, dq, dk;  // backward
+  int64_t T;
+  int Hq, Hk, d, rot, splits;
+  const int32_t* pos;
+  const float* inv_freq;
+  const float* wq;
+  const float* wk;
+  float eps, mscale;
+  float* part;  // [workgroups][2][d] (backward)
+  // cache
+  char* ck;
+  char* cv;
+  const int32_t* table;
+  const int32_t* seqs;
+  int cB, cols, n_pages, page_shift;
+};
+
+constexpr int kRopeThreads = 256;
+enum { kPairs = 0, kHalfChunks = 1, kHalfAny = 2 };  // where a column's partner is
+
+template <int DT>
+struct RopeLane {
+  static constexpr int E = Tab<DT>::ELEMS;
+  float c[E], s[E];  // of the pair that column j of this lane's chunk is in; (1, 0) where it is not rotated; s signed
+};
+
+// sign: +1 forward, -1 backward (the transpose of the rotation)
+template <int DT, int MODE>
+__device__ inline void lane_angles(const RopeArgs& a, int64_t t, int col0, float sign, RopeLane<DT>& L) {
+  constexpr int E = RopeLane<DT>::E;
+  const int n = a.rot >> 1;
+  const double turn = a.rot > 0 ? (double)a.pos[t] * 0.15915494309189533577 : 0.0;
+  constexpr int STEP = MODE == kPairs ? 2 : 1;
+#pragma unroll
+  for (int j = 0; j < E; j += STEP) {
+    const int c = col0 + j;
+    float cs = 1.0f, sn = 0.0f;
+    if (c < a.rot) {
+      const int i = MODE == kPairs ? c >> 1 : c < n ? c : c - n;
+      const double x = turn * (double)a.inv_freq[i];
+      sincospif((float)(2.0 * (x - rint(x))), &sn, &cs);
+      cs *= a.mscale;
+      sn *= a.mscale * sign;
+    }
+    if constexpr (MODE == kPairs) {
+      L.c[j] = L.c[j + 1] = cs;
+      L.s[j] = -sn;
+      L.s[j + 1] = sn;
+    } else {
+      L.c[j] = cs;
+      L.s[j] = c < n ? -sn : sn;
+    }
+  }
+}
+
+// y = c x + s partner(x) for the E columns of this lane; xs: this wavefront's row buffer in LDS (kHalfAny)
+template <int DT, int MODE>
+__device__ inline void turn_row(const RopeLane<DT>& L, const float* x, float* y, int lane, int col0, int rot, float* xs) {
+  constexpr int E = RopeLane<DT>::E;
+  if constexpr (MODE == kPairs) {
+#pragma unroll
+    for (int j = 0; j < E; j += 2) {
+      y[j] = L.c[j] * x[j] + L.s[j] * x[j + 1];
+      y[j + 1] = L.c[j + 1] * x[j + 1] + L.s[j + 1] * x[j];
+    }
+  } else {
+    const int n = rot >> 1;
+    float p[E];
+    if constexpr (MODE == kHalfChunks) {
+      const int step = n / E;  // lanes to the partner; a lane past the rotated columns takes its own
+      const int from = col0 < n ? lane + step : col0 < rot ? lane - step : lane;
+#pragma unroll
+      for (int j = 0; j < E; ++j) p[j] = __shfl(x[j], from, DLRM_WAVE);
+    } else {
+      float* row = xs + (lane * E - col0);  // of this lane's group
+#pragma unroll
+      for (int j = 0; j < E; ++j) xs[lane * E + j] = x[j];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        const int c = col0 + j;
+        p[j] = row[c < n ? c + n : c < rot ? c - n : c];
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) y[j] = L.c[j] * x[j] + L.s[j] * p[j];
+  }
+}
+
+template <int G>
+__device__ inline float group_sum(float v) {
+#pragma unroll
+  for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, DLRM_WAVE);
+  return v;
+}
+
+// Forward.  Groups of G lanes; group g of the grid takes item g / splits and the heads g % splits, + splits, ...
+template <int DT, int MODE, int G, bool CACHE>
+__global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
+  constexpr int E = Tab<DT>::ELEMS;
+  __shared__ float xs_all[MODE == kHalfAny ? kRopeThreads * E : 1];
+  float* xs = xs_all + (MODE == kHalfAny ? wave_id() * DLRM_WAVE * E : 0);
+  const int lane = lane_id(), col0 = (lane & (G - 1)) * E;
+  const int64_t group = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
+  const int64_t t = group / a.splits;
+  const int first = (int)(group - t * a.splits);
+  // lanes of the last group past the row, and groups past the last item, go along with nothing (exchanges need every lane)
+  const bool in = t < a.T && col0 < a.d;
+  const int64_t tt = t < a.T ? t : a.T - 1;
+  RopeLane<DT> L;
+  lane_angles<DT, MODE>(a, tt, col0, 1.0f, L);
+  float wq[E], wk[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) wq[j] = wk[j] = 1.0f;
+  if (col0 < a.d) {
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      if (a.wq) load_cols<4>(a.wq + col0 + j, true, wq + j);
+      if (a.wk) load_cols<4>(a.wk + col0 + j, true, wk + j);
+    }
+  }
+  const float inv_d = 1.0f / (float)a.d;
+  char* slot_k = nullptr;
+  char* slot_v = nullptr;
+  int64_t head_bytes = 0;
+  if constexpr (CACHE) {
+    const int64_t row = (int64_t)a.d * Tab<DT>::EB;
+    const int s = a.seqs[tt], p = a.pos[tt], c = p >> a.page_shift;
+    head_bytes = row << a.page_shift;
+    if (s >= 0 && s < a.cB && p >= 0 && c < a.cols) {
+      const int page = a.table[(int64_t)s * a.cols + c];
+      if (page >= 0 && page < a.n_pages) {
+        const int64_t at = (int64_t)page * a.Hk * head_bytes + (p & ((1 << a.page_shift) - 1)) * row;
+        slot_k = a.ck + at;
+        slot_v = a.cv + at;
+      }
+    }
+  }
+  const int H = a.Hq + a.Hk + (CACHE ? a.Hk : 0);
+  const int cb = col0 * Tab<DT>::EB;
+  auto src = [&](int h) {
+    const char* p = h < a.Hq ? row_of(a.q, tt, h) : h < a.Hq + a.Hk ? row_of(a.k, tt, h - a.Hq) : row_of(a.v, tt, h - a.Hq - a.Hk);
+    return p + cb;
+  };
+  u32x4 next = {0, 0, 0, 0};
+  if (in && first < H) next = load16(src(first));
+  for (int h = first; h < H; h += a.splits) {
+    const u32x4 raw = next;
+    if (in && h + a.splits < H) next = load16(src(h + a.splits));
+    const bool is_q = h < a.Hq;
+    if (CACHE && h >= a.Hq + a.Hk) {
+      if (in && slot_v) store16(slot_v + (h - a.Hq - a.Hk) * head_bytes + cb, raw);
+      continue;
+    }
+    float x[E], y[E];
+    Tab<DT>::widen(raw, x);
+    if ((is_q ? a.wq : a.wk) != nullptr) {
+      float ss = 0.0f;
+#pragma unroll
+      for (int j = 0; j < E; ++j) ss += x[j] * x[j];
+      const float r = 1.0f / sqrtf(group_sum<G>(ss) * inv_d + a.eps);
+#pragma unroll
+      for (int j = 0; j < E; ++j) x[j] = x[j] * r * (is_q ? wq[j] : wk[j]);
+    }
+    turn_row<DT, MODE>(L, x, y, lane, col0, a.rot, xs);
+    if (!in) continue;
+    const u32x4 out = narrow<DT>(y);
+    if (is_q)
+      store16(row_of(a.qo, tt, h) + cb, out);
+    else if (CACHE) {
+      if (slot_k) store16(slot_k + (h - a.Hq) * head_bytes + cb, out);
+    } else {
+      store16(row_of(a.ko, tt, h - a.Hq) + cb, out);
+    }
+  }
+}
+
+// Backward.  A group walks the items group, group + groups of the grid, ...; the weights' gradients of all its rows stay in
+// registers, are added over the workgroup's groups once at the end, and one row of sums per workgroup goes to the workspace.
+template <int DT, int MODE, int G>
+__global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
+  constexpr int E = Tab<DT>::ELEMS;
+  constexpr int NW = kRopeThreads / DLRM_WAVE;
+  __shared__ float xs_all[MODE == kHalfAny ? kRopeThreads * E : 1];
+  __shared__ float red[NW][2][DLRM_MAX_HEAD_DIM];
+  float* xs = xs_all + (MODE == kHalfAny ? wave_id() * DLRM_WAVE * E : 0);
+  const int lane = lane_id(), col0 = (lane & (G - 1)) * E;
+  const int64_t groups = (int64_t)gridDim.x * (kRopeThreads / G);
+  const int64_t g0 = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
+  const float inv_d = 1.0f / (float)a.d;
+  float wq[E], wk[E], sq[E], sk[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    wq[j] = wk[j] = 1.0f;
+    sq[j] = sk[j] = 0.0f;
+  }
+  if (col0 < a.d) {
+#pragma unroll
+    for (int j = 0; j < E; j += 4) {
+      if (a.wq) load_cols<4>(a.wq + col0 + j, true, wq + j);
+      if (a.wk) load_cols<4>(a.wk + col0 + j, true, wk + j);
+    }
+  }
+  const int H = a.Hq + a.Hk, cb = col0 * Tab<DT>::EB;
+  const int64_t rounds = (a.T + groups - 1) / groups;  // the same for every lane of the workgroup
+  for (int64_t i = 0; i < rounds; ++i) {
+    const int64_t t = g0 + i * groups;
+    const bool in = t < a.T && col0 < a.d;
+    const int64_t tt = t < a.T ? t : a.T - 1;
+    RopeLane<DT> L;
+    lane_angles<DT, MODE>(a, tt, col0, -1.0f, L);
+    auto src = [&](int h) { return (h < a.Hq ? row_of(a.q, tt, h) : row_of(a.k, tt, h - a.Hq)) + cb; };
+    auto dsrc = [&](int h) { return (h < a.Hq ? row_of(a.dqo, tt, h) : row_of(a.dko, tt, h - a.Hq)) + cb; };
+    u32x4 nx = {0, 0, 0, 0}, nd = {0, 0, 0, 0};
+    if (in) {
+      nx = load16(src(0));
+      nd = load16(dsrc(0));
+    }
+    for (int h = 0; h < H; ++h) {
+      const u32x4 rx = nx, rd = nd;
+      if (in && h + 1 < H) {
+        nx = load16(src(h + 1));
+        nd = load16(dsrc(h + 1));
+      }
+      const bool is_q = h < a.Hq;
+      float x[E], dy[E], g[E];
+      Tab<DT>::widen(rx, x);
+      Tab<DT>::widen(rd, dy);
+      turn_row<DT, MODE>(L, dy, g, lane, col0, a.rot, xs);
+      if ((is_q ? a.wq : a.wk) != nullptr) {
+        float ss = 0.0f, sg = 0.0f;
+        float gw[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          gw[j] = g[j] * (is_q ? wq[j] : wk[j]);
+          ss += x[j] * x[j];
+          sg += gw[j] * x[j];
+        }
+#pragma unroll
+        for (int o = G >> 1; o > 0; o >>= 1) {
+          ss += __shfl_xor(ss, o, DLRM_WAVE);
+          sg += __shfl_xor(sg, o, DLRM_WAVE);
+        }
+        const float r = 1.0f / sqrtf(ss * inv_d + a.eps);
+        const float m = sg * r * r * inv_d;  // mean(g w n) r
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const float dw = in ? g[j] * (x[j] * r) : 0.0f;
+          if (is_q)
+            sq[j] += dw;
+          else
+            sk[j] += dw;
+          g[j] = r * (gw[j] - x[j] * m);
+        }
+      }
+      if (in) store16((is_q ? row_of(a.dq, tt, h) : row_of(a.dk, tt, h - a.Hq)) + cb, narrow<DT>(g));
+    }
+  }
+  if (a.part == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+#pragma unroll
+    for (int o = G; o < DLRM_WAVE; o <<= 1) {
+      sq[j] += __shfl_xor(sq[j], o, DLRM_WAVE);
+      sk[j] += __shfl_xor(sk[j], o, DLRM_WAVE);
+    }
+    if (lane < G && col0 < a.d) {
+      red[wave_id()][0][col0 + j] = sq[j];
+      red[wave_id()][1][col0 + j] = sk[j];
+    }
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 2 * a.d; c += kRopeThreads) {
+    const int w = c >= a.d, col = c - w * a.d;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) sum += red[i][w][col];
+    a.part[(int64_t)blockIdx.x * 2 * a.d + c] = sum;
+  }
+}
+
+// dw[c] = sum of the workgroups' rows; 16 columns a workgroup, 16 threads a column
+__global__ __launch_bounds__(256) void qk_rope_dw_kernel(const float* part, int rows, int d, float* dwq, float* dwk) {
+  __shared__ float red[16][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), y = threadIdx.x >> 4;
+  float sum = 0.0f;
+  if (c < 2 * d)
+    for (int i = y; i < rows; i += 16) sum += part[(int64_t)i * 2 * d + c];
+  red[y][threadIdx.x & 15] = sum;
+  __syncthreads();
+  if (y == 0 && c < 2 * d) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += red[i][threadIdx.x];
+    float* dst = c < d ? dwq : dwk;
+    if (dst) dst[c < d ? c : c - d] = s;
+  }
+}
+
+static int check_rope(const dlrm_qk_rope* r) {
+  if (!r) return DLRM_ERR_NULL;
+  if (int st = check_head_shape(r->Hq, 1, r->d, r->dtype)) return st;
+  if (r->Hk < 0 || r->Hk > DLRM_MAX_HEADS) return DLRM_ERR_BAD_SHAPE;
+  if (r->T < 0 || r->T > DLRM_MAX_ITEMS) return DLRM_ERR_BAD_SHAPE;
+  if (r->rot < 0 || r->rot > r->d || (r->rot & 1)) return DLRM_ERR_BAD_SHAPE;
+  if (r->layout != DLRM_ROPE_HALF && r->layout != DLRM_ROPE_INTERLEAVED) return DLRM_ERR_BAD_SHAPE;
+  if (r->rot > 0 && (!r->inv_freq || (r->T > 0 && !r->positions))) return DLRM_ERR_NULL;
+  if ((r->wq || r->wk) && !(r->eps > 0.0f)) return DLRM_ERR_BAD_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(r->wq) & 15) || (reinterpret_cast<uintptr_t>(r->wk) & 15)) return DLRM_ERR_BAD_SHAPE;
+  return DLRM_OK;
+}
+
+int check_cache(const dlrm_kv_cache* c) {
+  if (!c) return DLRM_ERR_NULL;
+  if (!c->k || !c->v || !c->table) return DLRM_ERR_NULL;
+  if (int st = check_head_shape(c->Hk, 1, c->d, c->dtype)) return st;
+  if (c->B < 1 || c->table_cols < 1 || c->n_pages < 1) return DLRM_ERR_BAD_SHAPE;
+  if (c->page < 1 || c->page > 1024 || (c->page & (c->page - 1))) return DLRM_ERR_BAD_SHAPE;
+  if ((int64_t)c->table_cols * c->page > DLRM_MAX_ITEMS) return DLRM_ERR_BAD_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(c->k) & 15) || (reinterpret_cast<uintptr_t>(c->v) & 15)) return DLRM_ERR_BAD_SHAPE;
+  return DLRM_OK;
+}
+
+static int group_lanes(const dlrm_qk_rope* r) { return pow2_ceil(r->d * elem_bytes(r->dtype) / 16); }
+
+static int partner_mode(const dlrm_qk_rope* r) {
+  if (r->layout == DLRM_ROPE_INTERLEAVED) return kPairs;
+  return (r->rot / 2) % (16 / elem_bytes(r->dtype)) == 0 ? kHalfChunks : kHalfAny;
+}
+
+static RopeArgs rope_args(const dlrm_qk_rope* r) {
+  RopeArgs a = {};
+  a.T = r->T;
+  a.Hq = r->Hq;
+  a.Hk = r->Hk;
+  a.d = r->d;
+  a.rot = r->rot;
+  a.splits = 1;
+  a.pos = r->positions;
+  a.inv_freq = r->inv_freq;
+  a.wq = r->wq;
+  a.wk = r->Hk > 0 ? r->wk : nullptr;
+  a.eps = r->eps;
+  a.mscale = r->mscale;
+  return a;
+}
+
+// Calls f with the storage type, the partner's place and the lanes of a group as compile-time constants.
+template <typename F>
+static int for_row_kind(int dtype, int mode, int lanes, F f) {
+  auto by_lanes = [&](auto dt, auto md) {
+    switch (lanes) {
+      case 1: return f(dt, md, std::integral_constant<int, 1>{});
+      case 2: return f(dt, md, std::integral_constant<int, 2>{});
+      case 4: return f(dt, md, std::integral_constant<int, 4>{});
+      case 8: return f(dt, md, std::integral_constant<int, 8>{});
+      case 16: return f(dt, md, std::integral_constant<int, 16>{});
+      default: return f(dt, md, std::integral_constant<int, 32>{});
+    }
+  };
+  auto by_mode = [&](auto dt) {
+    switch (mode) {
+      case kPairs: return by_lanes(dt, std::integral_constant<int, kPairs>{});
+      case kHalfChunks: return by_lanes(dt, std::integral_constant<int, kHalfChunks>{});
+      default: return by_lanes(dt, std::integral_constant<int, kHalfAny>{});
+    }
+  };
+  switch (dtype) {
+    case DLRM_F32: return by_mode(std::integral_constant<int, DLRM_F32>{});
+    case DLRM_F16: return by_mode(std::integral_constant<int, DLRM_F16>{});
+    default: return by_mode(std::integral_constant<int, DLRM_BF16>{});
+  }
+}
+
+// Heads of an item are shared out over several groups where the items alone would not fill the device.
+static int head_splits(const dlrm_qk_rope* r, int heads) {
+  const int64_t wanted = 65536 / group_lanes(r);  // 1024 wavefronts
+  int64_t s = r->T > 0 ? wanted / r->T : 1;
+  return (int)(s < 1 ? 1 : s > heads ? heads : s);
+}
+
+template <bool CACHE>
+static int launch_fwd(const dlrm_qk_rope* r, RopeArgs a, hipStream_t st) {
+  if (r->T == 0) return DLRM_OK;
+  a.splits = head_splits(r, r->Hq + r->Hk * (CACHE ? 2 : 1));
+  const int64_t blocks = (r->T * a.splits * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
+  if (blocks > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;
+  return for_row_kind(r->dtype, partner_mode(r), group_lanes(r), [&](auto dt, auto md, auto g) {
+    hipLaunchKernelGGL((qk_rope_fwd_kernel<dt(), md(), g(), CACHE>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+    DLRM_CHECK_LAUNCH();
+    return (int)DLRM_OK;
+  });
+}
+
+static int bwd_blocks(const dlrm_qk_rope* r) {
+  const int64_t b = (r->T * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
+  return (int)(b > 2048 ? 2048 : b);
+}
+
+}  // namespace dlrm
+
+using namespace dlrm;
+
+extern "C" int32_t dlrm_qk_rope_fwd(const dlrm_qk_rope* r, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* q_out,
+                                    const dlrm_heads* k_out, void* stream) {
+  if (int st = check_rope(r)) return st;
+  const int eb = elem_bytes(r->dtype);
+  for (const dlrm_heads* x : {q, q_out})
+    if (int st = check_heads(x, r->T, r->Hq, r->d, eb)) return st;
+  RopeArgs a = rope_args(r);
+  a.q = rows_of(q, eb);
+  a.qo = rows_of(q_out, eb);
+  if (r->Hk > 0) {
+    for (const dlrm_heads* x : {k, k_out})
+      if (int st = check_heads(x, r->T, r->Hk, r->d, eb)) return st;
+    a.k = rows_of(k, eb);
+    a.ko = rows_of(k_out, eb);
+  }
+  return launch_fwd<false>(r, a, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int32_t dlrm_qk_rope_append(const dlrm_qk_rope* r, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
+                                       const dlrm_heads* q_out, const dlrm_kv_cache* c, const int32_t* seqs, void* stream) {
+  if (int st = check_rope(r)) return st;
+  if (int st = check_cache(c)) return st;
+  if (r->Hk != c->Hk || r->d != c->d) return DLRM_ERR_BAD_SHAPE;
+  if (r->dtype != c->dtype) return DLRM_ERR_BAD_DTYPE;
+  if (r->T > 0 && (!seqs || !r->positions)) return DLRM_ERR_NULL;
+  const int eb = elem_bytes(r->dtype);
+  for (const dlrm_heads* x : {q, q_out})
+    if (int st = check_heads(x, r->T, r->Hq, r->d, eb)) return st;
+  for (const dlrm_heads* x : {k, v})
+    if (int st = check_heads(x, r->T, r->Hk, r->d, eb)) return st;
+  RopeArgs a = rope_args(r);
+  a.q = rows_of(q, eb);
+  a.qo = rows_of(q_out, eb);
+  a.k = rows_of(k, eb);
+  a.v = rows_of(v, eb);
+  a.ck = static_cast<char*>(c->k);
+  a.cv = static_cast<char*>(c->v);
+  a.table = c->table;
+  a.seqs = seqs;
+  a.cB = c->B;
+  a.cols = c->table_cols;
+  a.n_pages = c->n_pages;
+  a.page_shift = ilog2_ceil(c->page);
+  return launch_fwd<true>(r, a, static_cast<hipStream_t>(stream));
+}
+
+extern "C" size_t dlrm_qk_rope_bwd_workspace_bytes(const dlrm_qk_rope* r) {
+  if (check_rope(r) != DLRM_OK) return 0;
+  const size_t n = (size_t)bwd_blocks(r) * 2 * r->d * sizeof(float);
+  return n < 256 ? 256 : (n + 255) / 256 * 256;
+}
+
+extern "C" int32_t dlrm_qk_rope_bwd(const dlrm_qk_rope* r, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* dq_out,
+                                    const dlrm_heads* dk_out, const dlrm_heads* dq, const dlrm_heads* dk, float* dwq, float* dwk,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  if (int st = check_rope(r)) return st;
+  const int eb = elem_bytes(r->dtype);
+  for (const dlrm_heads* x : {q, dq_out, dq})
+    if (int st = check_heads(x, r->T, r->Hq, r->d, eb)) return st;
+  RopeArgs a = rope_args(r);
+  a.q = rows_of(q, eb);
+  a.dqo = rows_of(dq_out, eb);
+  a.dq = rows_of(dq, eb);
+  if (r->Hk > 0) {
+    for (const dlrm_heads* x : {k, dk_out, dk})
+      if (int st = check_heads(x, r->T, r->Hk, r->d, eb)) return st;
+    a.k = rows_of(k, eb);
+    a.dko = rows_of(dk_out, eb);
+    a.dk = rows_of(dk, eb);
+  }
+  const bool norm = a.wq || a.wk;
+  if ((a.wq && !dwq) || (a.wk && !dwk)) return DLRM_ERR_NULL;
+  if (norm && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < dlrm_qk_rope_bwd_workspace_bytes(r)))
+    return DLRM_ERR_WORKSPACE;
+  a.part = norm ? static_cast<float*>(workspace) : nullptr;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int blocks = bwd_blocks(r);
+  if (blocks > 0) {
+    const int rc = for_row_kind(r->dtype, partner_mode(r), group_lanes(r), [&](auto dt, auto md, auto g) {
+      hipLaunchKernelGGL((qk_rope_bwd_kernel<dt(), md(), g()>), dim3(blocks), dim3(kRopeThreads), 0, st, a);
+      DLRM_CHECK_LAUNCH();
+      return (int)DLRM_OK;
+    });
+    if (rc != DLRM_OK) return rc;
+  }
+  if (!norm) return DLRM_OK;
+  hipLaunchKernelGGL(qk_rope_dw_kernel, dim3((2 * r->d + 15) / 16), dim3(256), 0, st, a.part, blocks, r->d, a.wq ? dwq : nullptr,
+                     a.wk ? dwk : nullptr);
+  DLRM_CHECK_LAUNCH();
+  return DLRM_OK;
+}

@@ -1,0 +1,97 @@
+// Attention over sequences: entry points and argument checks (the kernels: seq_attn.h).
+#include "seq_attn.h"
+
+#include <math.h>
+
+#include <initializer_list>
+
+using namespace dlrm;
+
+static int check_seq(const dlrm_seq_batch* s, int Hq, int Hk, int d, int dtype) {
+  if (!s) return DLRM_ERR_NULL;
+  if (int st = check_head_shape(Hq, Hk, d, dtype)) return st;
+  if (s->B < 1 || s->B == 0x7fffffff || s->Tq < 0 || s->Tk < 0 || s->Tq > DLRM_MAX_ITEMS || s->Tk > DLRM_MAX_ITEMS) return DLRM_ERR_BAD_SHAPE;
+  if (s->max_q < 0 || s->max_k < 0 || (s->Tq > 0 && s->max_q == 0) || (s->Tk > 0 && s->max_k == 0)) return DLRM_ERR_BAD_SHAPE;
+  if (!s->q_off || !s->k_off) return DLRM_ERR_NULL;
+  if ((s->causal != 0 && s->causal != 1) || (s->prefix && !s->causal)) return DLRM_ERR_BAD_SHAPE;
+  if (!(s->scale > 0.0f) || !isfinite(s->scale) || !(s->cap >= 0.0f) || !isfinite(s->cap)) return DLRM_ERR_BAD_SHAPE;
+  return DLRM_OK;
+}
+
+static SeqArgs seq_args(const dlrm_seq_batch* s, int Hq, int Hk, int d) {
+  SeqArgs a = {};
+  a.q_off = s->q_off;
+  a.k_off = s->k_off;
+  a.prefix = s->prefix;
+  a.slopes = s->slopes;
+  a.Tq = s->Tq;
+  a.B = s->B;
+  a.Hq = Hq;
+  a.Hk = Hk;
+  a.d = d;
+  a.causal = s->causal;
+  a.scale = s->scale;
+  a.cap = s->cap;
+  return a;
+}
+
+extern "C" int32_t dlrm_seq_attn_fwd(const dlrm_seq_batch* s, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype, const dlrm_heads* q,
+                                     const dlrm_heads* k, const dlrm_heads* v, const dlrm_heads* out, float* lse, void* stream) {
+  if (int st = check_seq(s, Hq, Hk, d, dtype)) return st;
+  const int eb = elem_bytes(dtype);
+  for (const dlrm_heads* x : {q, out})
+    if (int st = check_heads(x, s->Tq, Hq, d, eb)) return st;
+  for (const dlrm_heads* x : {k, v})
+    if (int st = check_heads(x, s->Tk, Hk, d, eb)) return st;
+  SeqArgs a = seq_args(s, Hq, Hk, d);
+  a.q = rows_of(q, eb);
+  a.k = rows_of(k, eb);
+  a.v = rows_of(v, eb);
+  a.out = rows_of(out, eb);
+  a.lse = lse;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case DLRM_F32: return launch_seq_fwd<DLRM_F32>(s, a, hs);
+    case DLRM_F16: return launch_seq_fwd<DLRM_F16>(s, a, hs);
+    default: return launch_seq_fwd<DLRM_BF16>(s, a, hs);
+  }
+}
+
+extern "C" size_t dlrm_seq_attn_bwd_workspace_bytes(const dlrm_seq_batch* s, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype) {
+  if (check_seq(s, Hq, Hk, d, dtype) != DLRM_OK) return 0;
+  const size_t n = (size_t)Hq * s->Tq * sizeof(float);
+  return n < 256 ? 256 : (n + 255) / 256 * 256;
+}
+
+extern "C" int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* s, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype, const dlrm_heads* q,
+                                     const dlrm_heads* k, const dlrm_heads* v, const dlrm_heads* out, const float* lse,
+                                     const dlrm_heads* dout, const dlrm_heads* dq, const dlrm_heads* dk, const dlrm_heads* dv,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (int st = check_seq(s, Hq, Hk, d, dtype)) return st;
+  const int eb = elem_bytes(dtype);
+  for (const dlrm_heads* x : {q, out, dout, dq})
+    if (int st = check_heads(x, s->Tq, Hq, d, eb)) return st;
+  for (const dlrm_heads* x : {k, v, dk, dv})
+    if (int st = check_heads(x, s->Tk, Hk, d, eb)) return st;
+  if (!lse && s->Tq > 0) return DLRM_ERR_NULL;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
+      workspace_bytes < dlrm_seq_attn_bwd_workspace_bytes(s, Hq, Hk, d, dtype))
+    return DLRM_ERR_WORKSPACE;
+  SeqArgs a = seq_args(s, Hq, Hk, d);
+  a.q = rows_of(q, eb);
+  a.k = rows_of(k, eb);
+  a.v = rows_of(v, eb);
+  a.out = rows_of(out, eb);
+  a.dout = rows_of(dout, eb);
+  a.dq = rows_of(dq, eb);
+  a.dk = rows_of(dk, eb);
+  a.dv = rows_of(dv, eb);
+  a.lse = const_cast<float*>(lse);
+  a.delta = static_cast<float*>(workspace);
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  switch (dtype) {
+    case DLRM_F32: return launch_seq_bwd<DLRM_F32>(s, a, hs);
+    case DLRM_F16: return launch_seq_bwd<DLRM_F16>(s, a, hs);
+    default: return launch_seq_bwd<DLRM_BF16>(s, a, hs);
+  }
+}
