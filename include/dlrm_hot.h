@@ -395,8 +395,8 @@ int32_t dlrm_emb_bag_bwd_adagrad_timed(const dlrm_sparse_batch* batch, void* con
  * projection's output or each on its own.  Rows a call writes must not overlap each other. */
 typedef struct dlrm_heads {
   void* data;
-  int64_t stride_t; /* >= d */
-  int64_t stride_h; /* >= d where there is more than one head */
+  int64_t stride_t; /* d .. 2^23 where there is more than one item */
+  int64_t stride_h; /* d .. 2^40 where there is more than one head */
 } dlrm_heads;
 
 /* order of the rotated pairs */

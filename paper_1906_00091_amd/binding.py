@@ -417,24 +417,31 @@ class Heads:
             raise DlrmError("Heads", -3)
         self.x = x
         self.shape, self.dtype = tuple(x.shape), _DTYPE_OF[x.dtype]
-        st, sh = x.stride(0), x.stride(1)
-        # (a stride along an axis of one element means nothing, and torch may give any)
-        self.c = _HeadsC(x.data_ptr(), st if x.shape[0] > 1 else 0, sh if x.shape[1] > 1 else 0)
+        self.c = _HeadsC(x.data_ptr(), x.stride(0), x.stride(1))
 
 
 def _heads(fn: str, x, n: int, H: int, d: int, dtype: int):
-    v = x if type(x) is Heads else Heads(x)
-    if v.shape != (n, H, d):
-        raise ValueError("%s: a tensor of shape %s where %s is wanted" % (fn, v.shape, (n, H, d)))
-    if v.dtype != dtype:
+    if type(x) is Heads:
+        shape, dt, c = x.shape, x.dtype, x.c
+    else:  # (what Heads does, without the object: 1 us less of the host's time per tensor)
+        shape, stride, dt = x.shape, x.stride(), _DTYPE_OF.get(x.dtype)
+        if len(shape) != 3 or stride[2] != 1 != d:
+            Heads(x)
+        c = _HeadsC(x.data_ptr(), stride[0], stride[1])
+    if shape != (n, H, d):
+        raise ValueError("%s: a tensor of shape %s where %s is wanted" % (fn, tuple(shape), (n, H, d)))
+    if dt != dtype:
         raise DlrmError(fn, -3)
-    return C.byref(v.c)
+    return C.byref(c)
 
 
 def _first(x):
-    """(view, shape, storage type) of the tensor that the others of a call go by."""
-    v = x if type(x) is Heads else Heads(x)
-    return v, v.shape, v.dtype
+    """(shape, storage type) of the tensor that the others of a call go by."""
+    if type(x) is Heads:
+        return x.shape, x.dtype
+    if x.dim() != 3 or x.dtype not in _DTYPE_OF:
+        Heads(x)
+    return x.shape, _DTYPE_OF[x.dtype]
 
 
 def _vector(fn: str, x: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[int]:
@@ -493,9 +500,9 @@ def rope_frequencies(rot: int, base: float = 10000.0, stretch: float = 1.0, keep
 def dlrm_qk_rope_fwd(rope: QkRope, q, k, q_out, k_out):
     """q, q_out: [T, Hq, d]; k, k_out: [T, Hk, d] (None for Hk = 0).  An output may be its input."""
     fn = "dlrm_qk_rope_fwd"
-    v, _, dt = _first(q)
+    dt = _first(q)[1]
     n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
-    _check(fn, lib().dlrm_qk_rope_fwd(rope.ref(dt), _heads(fn, v, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt) if Hk else None,
+    _check(fn, lib().dlrm_qk_rope_fwd(rope.ref(dt), _heads(fn, q, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt) if Hk else None,
                                       _heads(fn, q_out, n, Hq, d, dt), _heads(fn, k_out, n, Hk, d, dt) if Hk else None, _stream()))
 
 
@@ -503,9 +510,9 @@ def dlrm_qk_rope_bwd(rope: QkRope, q, k, dq_out, dk_out, dq, dk, dwq: Optional[t
                      workspace: Optional[torch.Tensor]):
     """Gradients dq, dk of the forward's inputs (may be dq_out, dk_out) and dwq, dwk (fp32 [d], written) of the norm weights."""
     fn = "dlrm_qk_rope_bwd"
-    v, _, dt = _first(q)
+    dt = _first(q)[1]
     n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
-    queries = [_heads(fn, x, n, Hq, d, dt) for x in (v, dq_out, dq)]
+    queries = [_heads(fn, x, n, Hq, d, dt) for x in (q, dq_out, dq)]
     keys = [_heads(fn, x, n, Hk, d, dt) for x in (k, dk_out, dk)] if Hk else [None] * 3
     ws, ws_bytes = _workspace(workspace)
     _check(fn, lib().dlrm_qk_rope_bwd(rope.ref(dt), queries[0], keys[0], queries[1], keys[1], queries[2], keys[2],
@@ -546,11 +553,11 @@ class KvCache:
 def dlrm_qk_rope_append(rope: QkRope, q, k, v, q_out, cache: KvCache, seqs: torch.Tensor):
     """Queries to q_out, keys (normed and rotated) and values to the cache, item t as item positions[t] of sequence seqs[t]."""
     fn = "dlrm_qk_rope_append"
-    qv, _, dt = _first(q)
+    dt = _first(q)[1]
     n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
     if not Hk:
         raise DlrmError(fn, -2)
-    _check(fn, lib().dlrm_qk_rope_append(rope.ref(dt), _heads(fn, qv, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt),
+    _check(fn, lib().dlrm_qk_rope_append(rope.ref(dt), _heads(fn, q, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt),
                                          _heads(fn, v, n, Hk, d, dt), _heads(fn, q_out, n, Hq, d, dt), cache.ref(),
                                          _vector(fn, seqs, n, torch.int32), _stream()))
 
@@ -581,19 +588,19 @@ class SeqBatch:
 def dlrm_seq_attn_fwd(seq: SeqBatch, q, k, v, out, lse: Optional[torch.Tensor] = None):
     """q, out: [Tq, Hq, d]; k, v: [Tk, Hk, d]; lse: fp32 [Hq, Tq] for the backward, or None."""
     fn = "dlrm_seq_attn_fwd"
-    qv, (_, Hq, d), dt = _first(q)
-    kv, (_, Hk, _), _ = _first(k)
-    _check(fn, lib().dlrm_seq_attn_fwd(seq.ref(Hq, d), Hq, Hk, d, dt, _heads(fn, qv, seq.Tq, Hq, d, dt), _heads(fn, kv, seq.Tk, Hk, d, dt),
+    (_, Hq, d), dt = _first(q)
+    Hk = _first(k)[0][1]
+    _check(fn, lib().dlrm_seq_attn_fwd(seq.ref(Hq, d), Hq, Hk, d, dt, _heads(fn, q, seq.Tq, Hq, d, dt), _heads(fn, k, seq.Tk, Hk, d, dt),
                                        _heads(fn, v, seq.Tk, Hk, d, dt), _heads(fn, out, seq.Tq, Hq, d, dt),
                                        _vector(fn, lse, Hq * seq.Tq, torch.float32), _stream()))
 
 
 def dlrm_seq_attn_bwd(seq: SeqBatch, q, k, v, out, lse: torch.Tensor, dout, dq, dk, dv, workspace: torch.Tensor):
     fn = "dlrm_seq_attn_bwd"
-    qv, (_, Hq, d), dt = _first(q)
-    kv, (_, Hk, _), _ = _first(k)
-    queries = [_heads(fn, x, seq.Tq, Hq, d, dt) for x in (qv, out, dout, dq)]
-    keys = [_heads(fn, x, seq.Tk, Hk, d, dt) for x in (kv, v, dk, dv)]
+    (_, Hq, d), dt = _first(q)
+    Hk = _first(k)[0][1]
+    queries = [_heads(fn, x, seq.Tq, Hq, d, dt) for x in (q, out, dout, dq)]
+    keys = [_heads(fn, x, seq.Tk, Hk, d, dt) for x in (k, v, dk, dv)]
     ws, ws_bytes = _workspace(workspace)
     _check(fn, lib().dlrm_seq_attn_bwd(seq.ref(Hq, d), Hq, Hk, d, dt, queries[0], keys[0], keys[1], queries[1],
                                        _vector(fn, lse, Hq * seq.Tq, torch.float32), queries[2], queries[3], keys[2], keys[3], ws, ws_bytes,
@@ -611,10 +618,10 @@ def dlrm_cache_attn(cache: KvCache, lens: torch.Tensor, max_len: int, q, out, wo
                     slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None, cap: float = 0.0):
     """q, out: [B, Hq, d]; lens: int32 [B], items of every sequence in the cache, its newest among them."""
     fn = "dlrm_cache_attn"
-    qv, (_, Hq, d), dt = _first(q)
+    (_, Hq, d), dt = _first(q)
     ws, ws_bytes = _workspace(workspace)
     _check(fn, lib().dlrm_cache_attn(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, Hq,
-                                     _heads(fn, qv, cache.B, Hq, cache.d, cache.dtype), _heads(fn, out, cache.B, Hq, cache.d, cache.dtype),
+                                     _heads(fn, q, cache.B, Hq, cache.d, cache.dtype), _heads(fn, out, cache.B, Hq, cache.d, cache.dtype),
                                      _vector(fn, slopes, Hq, torch.float32), d ** -0.5 if scale is None else scale, cap, ws, ws_bytes,
                                      _stream()))
 

@@ -68,22 +68,28 @@ struct Op16<DLRM_F32> {
   }
 };
 template <int DT>
-__device__ inline Op16<DT> op16_load(const char* p, bool there) {
+__device__ inline Op16<DT> op16_load(const char* p) {
   Op16<DT> o;
   if constexpr (DT == DLRM_F32) {
-    f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-    if (there) {
-      a = *reinterpret_cast<const f32x4*>(p);
-      b = *reinterpret_cast<const f32x4*>(p + 16);
-    }
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 16);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       o.f[j] = a[j];
       o.f[4 + j] = b[j];
     }
   } else {
+    o.v = load16(p);
+  }
+  return o;
+}
+template <int DT>
+__device__ inline Op16<DT> op16_zero() {
+  Op16<DT> o;
+  if constexpr (DT == DLRM_F32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o.f[j] = 0.0f;
+  } else {
     o.v = u32x4{0, 0, 0, 0};
-    if (there) o.v = load16(p);
   }
   return o;
 }
@@ -121,51 +127,61 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
   const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
   const int blk = rest % a.blocks, hk = rest / a.blocks % a.Hk, s = rest / a.blocks / a.Hk;
   const int G = a.Hq / a.Hk;
-  const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
-  const int start = split * a.chunk, end = min(len, start + a.chunk);
-  if (start >= end && split > 0) return;  // the first chunk of an empty sequence gives zeros
   const int lane = lane_id(), g = lane >> 4, n = lane & 15, wave = wave_id();
   const int head = hk * G + blk * kHeads + n;  // of this lane's column
   const bool head_there = blk * kHeads + n < G;
-
-  const int page0 = start >> a.page_shift, n_pages = start < end ? ((end - 1) >> a.page_shift) - page0 + 1 : 0;
-  for (int p = threadIdx.x; p < n_pages; p += kCacheThreads) pages[p] = a.table[(int64_t)s * a.cols + page0 + p];
+  // the chunk's page numbers and the queries are loaded beside the length, not after it
+  const int start = split * a.chunk, page0 = start >> a.page_shift;
+  const int most_pages = min(((start + a.chunk - 1) >> a.page_shift) + 1, a.cols) - page0;
+  for (int p = threadIdx.x; p < most_pages; p += kCacheThreads) pages[p] = a.table[(int64_t)s * a.cols + page0 + p];
   Op16<DT> qf[STEPS];
   const char* qrow = row_of(a.q, s, head_there ? head : hk * G);
 #pragma unroll
-  for (int st = 0; st < STEPS; ++st) qf[st] = op16_load<DT>(qrow + (32 * st + 8 * g) * EB, head_there && 32 * st + 8 * g < a.d);
+  for (int st = 0; st < STEPS; ++st) {
+    qf[st] = op16_zero<DT>();
+    if (head_there && 32 * st + 8 * g < a.d) qf[st] = op16_load<DT>(qrow + (32 * st + 8 * g) * EB);
+  }
   const float c = a.scale * kLog2e, slope = a.slopes && head_there ? a.slopes[head] * kLog2e : 0.0f;
   const bool bend = a.cap > 0.0f;
   const float zs = bend ? a.scale / a.cap : 0.0f, cl = a.cap * kLog2e;
+  const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
+  const int end = min(len, start + a.chunk), last_page = max(page0, (end - 1) >> a.page_shift);
+  if (start >= end && split > 0) return;  // the first chunk of an empty sequence gives zeros
   __syncthreads();
 
   const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;
   const int64_t head_bytes = (int64_t)row_bytes << a.page_shift, page_bytes = head_bytes * a.Hk;
-  // byte offset of key j's row in the cache, or -1: past the end, or on a page that is not there
-  auto row_at = [&](int j) -> int64_t {
-    if (j >= end) return -1;
-    const int p = pages[(j >> a.page_shift) - page0];
-    if (p < 0 || p >= a.n_pages) return -1;
-    return p * page_bytes + hk * head_bytes + (int64_t)((j & mask) * row_bytes);
+  // Byte offset of key j's row in the cache; a key past the end, or on a page that is not there, gives the first row of the cache and false.
+  // No load stands in a branch (the wait for it would come with the branch's end): what came for no reason is masked where it is used.
+  auto row_at = [&](int j, bool& there) -> int64_t {
+    const int p = pages[min(j >> a.page_shift, last_page) - page0];
+    there = j < end && p >= 0 && p < a.n_pages;
+    return there ? p * page_bytes + hk * head_bytes + (int64_t)((j & mask) * row_bytes) : 0;
   };
   char* vs = lds + wave * kKeys * STRIDE;
   Op16<DT> kf[2][STEPS];
   u32x4 vf[NV];
   bool seen[2];
+  uint32_t v_there = 0;  // bit i: chunk i of the values
+  // columns past d: another chunk of the same row; the query's zeros there cancel the key's, and the values' are never written out
+  int kcol[STEPS];
+#pragma unroll
+  for (int st = 0; st < STEPS; ++st) kcol[st] = min(32 * st + 8 * g, a.d - 8) * EB;
   auto fetch = [&](int j0) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int64_t at = row_at(j0 + 16 * u + n);
-      seen[u] = at >= 0;
+      const int64_t at = row_at(j0 + 16 * u + n, seen[u]);
 #pragma unroll
-      for (int st = 0; st < STEPS; ++st) kf[u][st] = op16_load<DT>(a.k + at + (32 * st + 8 * g) * EB, at >= 0 && 32 * st + 8 * g < a.d);
+      for (int st = 0; st < STEPS; ++st) kf[u][st] = op16_load<DT>(a.k + at + kcol[st]);
     }
+    v_there = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int id = lane + i * DLRM_WAVE, r = id / CH, cc = id % CH;
-      const int64_t at = row_at(j0 + r);
-      vf[i] = u32x4{0, 0, 0, 0};
-      if (at >= 0 && cc * E < a.d) vf[i] = load16(a.v + at + cc * 16);
+      const int id = lane + i * DLRM_WAVE, r = id / CH, cc = min(id % CH, a.d / E - 1);
+      bool there;
+      const int64_t at = row_at(j0 + r, there);
+      v_there |= there ? 1u << i : 0u;
+      vf[i] = load16(a.v + at + cc * 16);
     }
   };
 
@@ -188,7 +204,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int id = lane + i * DLRM_WAVE;
-      *reinterpret_cast<u32x4*>(vs + (id / CH) * STRIDE + (id % CH) * 16) = vf[i];
+      *reinterpret_cast<u32x4*>(vs + (id / CH) * STRIDE + (id % CH) * 16) = v_there >> i & 1 ? vf[i] : u32x4{0, 0, 0, 0};
     }
     const int jn = j0 + kCacheWaves * kKeys;
     if (jn < end) fetch(jn);
@@ -294,48 +310,67 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
   }
 }
 
-// Joins the chunks of one sequence and head: 8 wavefronts, each half of a wavefront takes every 16th chunk, 4 columns a lane.
+// Joins the chunks of one sequence and head: the chunks' factors are made 512 at a time, then half a wavefront takes every 16th chunk,
+// 4 columns a lane, four chunks in flight.
 constexpr int kJoinThreads = 512;
 template <int DT>
 __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
-  constexpr int ROWS = kJoinThreads / 32;
-  __shared__ float red[ROWS];
+  constexpr int ROWS = kJoinThreads / 32, AHEAD = 4;
+  __shared__ float red[kJoinThreads / DLRM_WAVE];
   __shared__ f32x4 part[ROWS][32];
-  __shared__ float tot[ROWS];
+  __shared__ float factor[kJoinThreads];
   const int64_t row = blockIdx.x;
   const int s = (int)(row / a.Hq), head = (int)(row - (int64_t)s * a.Hq);
   const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
   const int n = max(1, (len + a.chunk - 1) / a.chunk);
   const float* pm = a.pm + row * a.splits * 2;
   const float* po = a.po + row * a.splits * a.d;
-  const int y = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4;
+  const int y = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4, wave = wave_id();
+  auto over_block = [&](float v, auto f) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, DLRM_WAVE));
+    if (lane_id() == 0) red[wave] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int i = 1; i < kJoinThreads / DLRM_WAVE; ++i) v = f(v, red[i]);
+    __syncthreads();
+    return v;
+  };
   float top = -kInf;
   for (int i = threadIdx.x; i < n; i += kJoinThreads) top = fmaxf(top, pm[2 * i]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, DLRM_WAVE));
-  if ((threadIdx.x & 31) == 0) red[y] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) top = fmaxf(top, red[i]);
+  top = over_block(top, [](float u, float v) { return fmaxf(u, v); });
   const float ms = top == -kInf ? 0.0f : top;
   f32x4 sum = {0, 0, 0, 0};
   float total = 0.0f;
-  for (int i = y; i < n; i += ROWS) {
-    const float f = __builtin_amdgcn_exp2f(pm[2 * i] - ms);
-    total += f * pm[2 * i + 1];
-    if (col < a.d) sum += f * loadf4(po + (int64_t)i * a.d + col);
+  for (int i0 = 0; i0 < n; i0 += kJoinThreads) {
+    const int i = i0 + threadIdx.x;
+    float f = 0.0f;
+    if (i < n) {
+      f = __builtin_amdgcn_exp2f(pm[2 * i] - ms);
+      total += f * pm[2 * i + 1];
+    }
+    factor[threadIdx.x] = f;
+    __syncthreads();
+    const int m = min(n - i0, kJoinThreads);
+    if (col < a.d) {
+      for (int r = y; r < m; r += AHEAD * ROWS) {
+        f32x4 v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) v[j] = loadf4(po + (int64_t)(i0 + (r + j * ROWS < m ? r + j * ROWS : r)) * a.d + col);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) sum += (r + j * ROWS < m ? factor[r + j * ROWS] : 0.0f) * v[j];
+      }
+    }
+    __syncthreads();
   }
+  total = over_block(total, [](float u, float v) { return u + v; });
   part[y][threadIdx.x & 31] = sum;
-  if ((threadIdx.x & 31) == 0) tot[y] = total;
   __syncthreads();
   if (y != 0 || col >= a.d) return;
   sum = f32x4{0, 0, 0, 0};
-  total = 0.0f;
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    sum += part[i][threadIdx.x];
-    total += tot[i];
-  }
+  for (int i = 0; i < ROWS; ++i) sum += part[i][threadIdx.x];
   sum *= total > 0.0f ? 1.0f / total : 0.0f;
   char* dst = row_of(a.out, s, head) + col * Tab<DT>::EB;
   if constexpr (DT == DLRM_F32) {
@@ -350,7 +385,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
 // Keys of a chunk: as many workgroups as fill the device several times over, at least two tiles a wavefront.
 static int chunk_of(const dlrm_kv_cache* c, int Hq, int max_len) {
   const int64_t rows = (int64_t)c->B * c->Hk * ((Hq / c->Hk + kHeads - 1) / kHeads);
-  const int64_t wanted = 4096;
+  const int64_t wanted = 1024;
   int64_t n = (rows * max_len + wanted - 1) / wanted;
   if (n < 256) n = 256;
   const int64_t most = (int64_t)kTablePages * c->page;  // a chunk starts on a page where it is a multiple of the page

@@ -21,10 +21,10 @@ __host__ inline Rows rows_of(const dlrm_heads* x, int eb) {
 __host__ inline int check_heads(const dlrm_heads* x, int64_t n, int H, int d, int eb) {
   if (!x || (!x->data && n > 0)) return DLRM_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(x->data) & 15) return DLRM_ERR_BAD_SHAPE;
-  if ((n > 1 && x->stride_t < d) || (H > 1 && x->stride_h < d)) return DLRM_ERR_BAD_SHAPE;
-  // a tile's rows are reached with 32-bit byte offsets
-  if (x->stride_t < 0 || x->stride_h < 0 || x->stride_t > (1 << 23) || x->stride_h >= (int64_t)1 << 40) return DLRM_ERR_BAD_SHAPE;
-  if (((x->stride_t * eb) & 15) != 0 || ((x->stride_h * eb) & 15) != 0) return DLRM_ERR_BAD_SHAPE;
+  // (a stride along an axis of one element means nothing; a tile's rows are reached with 32-bit byte offsets)
+  const int64_t st = n > 1 ? x->stride_t : d, sh = H > 1 ? x->stride_h : d;
+  if (st < d || sh < d || st > (1 << 23) || sh >= (int64_t)1 << 40) return DLRM_ERR_BAD_SHAPE;
+  if (((st * eb) & 15) != 0 || ((sh * eb) & 15) != 0) return DLRM_ERR_BAD_SHAPE;
   return DLRM_OK;
 }
 

@@ -158,16 +158,19 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
     }
   }
   const int H = a.Hq + a.Hk + (CACHE ? a.Hk : 0);
-  const int cb = col0 * Tab<DT>::EB;
+  const int cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
+  // (loads stand in no branch, so that the next row's is in flight while this one is worked on: a lane past the row or a head past the last
+  // loads what is there, and it is not used)
   auto src = [&](int h) {
+    h = min(h, H - 1);
     const char* p = h < a.Hq ? row_of(a.q, tt, h) : h < a.Hq + a.Hk ? row_of(a.k, tt, h - a.Hq) : row_of(a.v, tt, h - a.Hq - a.Hk);
-    return p + cb;
+    return load16(p + lb);
   };
-  u32x4 next = {0, 0, 0, 0};
-  if (in && first < H) next = load16(src(first));
+  u32x4 next = src(first);
   for (int h = first; h < H; h += a.splits) {
-    const u32x4 raw = next;
-    if (in && h + a.splits < H) next = load16(src(h + a.splits));
+    u32x4 raw = next;
+    next = src(h + a.splits);
+    if (col0 >= a.d) raw = u32x4{0, 0, 0, 0};
     const bool is_q = h < a.Hq;
     if (CACHE && h >= a.Hq + a.Hk) {
       if (in && slot_v) store16(slot_v + (h - a.Hq - a.Hk) * head_bytes + cb, raw);
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
       if (a.wk) load_cols<4>(a.wk + col0 + j, true, wk + j);
     }
   }
-  const int H = a.Hq + a.Hk, cb = col0 * Tab<DT>::EB;
+  const int H = a.Hq + a.Hk, cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
   const int64_t rounds = (a.T + groups - 1) / groups;  // the same for every lane of the workgroup
   for (int64_t i = 0; i < rounds; ++i) {
     const int64_t t = g0 + i * groups;
@@ -230,19 +233,14 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
     const int64_t tt = t < a.T ? t : a.T - 1;
     RopeLane<DT> L;
     lane_angles<DT, MODE>(a, tt, col0, -1.0f, L);
-    auto src = [&](int h) { return (h < a.Hq ? row_of(a.q, tt, h) : row_of(a.k, tt, h - a.Hq)) + cb; };
-    auto dsrc = [&](int h) { return (h < a.Hq ? row_of(a.dqo, tt, h) : row_of(a.dko, tt, h - a.Hq)) + cb; };
-    u32x4 nx = {0, 0, 0, 0}, nd = {0, 0, 0, 0};
-    if (in) {
-      nx = load16(src(0));
-      nd = load16(dsrc(0));
-    }
+    auto src = [&](int h) { return load16((h < a.Hq ? row_of(a.q, tt, h) : row_of(a.k, tt, h - a.Hq)) + lb); };
+    auto dsrc = [&](int h) { return load16((h < a.Hq ? row_of(a.dqo, tt, h) : row_of(a.dko, tt, h - a.Hq)) + lb); };
+    u32x4 nx = src(0), nd = dsrc(0);
     for (int h = 0; h < H; ++h) {
-      const u32x4 rx = nx, rd = nd;
-      if (in && h + 1 < H) {
-        nx = load16(src(h + 1));
-        nd = load16(dsrc(h + 1));
-      }
+      u32x4 rx = nx, rd = nd;
+      nx = src(min(h + 1, H - 1));
+      nd = dsrc(min(h + 1, H - 1));
+      if (col0 >= a.d) rx = rd = u32x4{0, 0, 0, 0};
       const bool is_q = h < a.Hq;
       float x[E], dy[E], g[E];
       Tab<DT>::widen(rx, x);
@@ -300,21 +298,32 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
   }
 }
 
-// dw[c] = sum of the workgroups' rows; 16 columns a workgroup, 16 threads a column
-__global__ __launch_bounds__(256) void qk_rope_dw_kernel(const float* part, int rows, int d, float* dwq, float* dwk) {
-  __shared__ float red[16][17];
-  const int c = blockIdx.x * 16 + (threadIdx.x & 15), y = threadIdx.x >> 4;
-  float sum = 0.0f;
-  if (c < 2 * d)
-    for (int i = y; i < rows; i += 16) sum += part[(int64_t)i * 2 * d + c];
-  red[y][threadIdx.x & 15] = sum;
-  __syncthreads();
-  if (y == 0 && c < 2 * d) {
-    float s = 0.0f;
+// dw[c] = sum of the workgroups' rows; 16 columns a workgroup, 64 threads a column, four rows in flight each.  (16 threads a column
+// and one row in flight: 50 us for 2048 rows of 256 columns.)
+constexpr int kDwThreads = 1024, kDwCols = 16, kDwRows = kDwThreads / kDwCols;
+__global__ __launch_bounds__(kDwThreads) void qk_rope_dw_kernel(const float* part, int rows, int d, float* dwq, float* dwk) {
+  __shared__ float red[kDwRows][kDwCols + 1];
+  const int x = threadIdx.x % kDwCols, y = threadIdx.x / kDwCols, c = blockIdx.x * kDwCols + x;
+  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < 2 * d) {
+    for (int i = y; i < rows; i += 4 * kDwRows) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += red[i][threadIdx.x];
+      for (int j = 0; j < 4; ++j) {
+        const int r = i + j * kDwRows;
+        const float v = part[(int64_t)(r < rows ? r : y) * 2 * d + c];
+        sum[j] += r < rows ? v : 0.0f;
+      }
+    }
+  }
+  red[y][x] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  __syncthreads();
+  for (int o = kDwRows / 2; o > 0; o >>= 1) {
+    if (y < o) red[y][x] += red[y + o][x];
+    __syncthreads();
+  }
+  if (y == 0 && c < 2 * d) {
     float* dst = c < d ? dwq : dwk;
-    if (dst) dst[c < d ? c : c - d] = s;
+    if (dst) dst[c < d ? c : c - d] = red[0][x];
   }
 }
 
@@ -508,7 +517,7 @@ extern "C" int32_t dlrm_qk_rope_bwd(const dlrm_qk_rope* r, const dlrm_heads* q, 
     if (rc != DLRM_OK) return rc;
   }
   if (!norm) return DLRM_OK;
-  hipLaunchKernelGGL(qk_rope_dw_kernel, dim3((2 * r->d + 15) / 16), dim3(256), 0, st, a.part, blocks, r->d, a.wq ? dwq : nullptr,
+  hipLaunchKernelGGL(qk_rope_dw_kernel, dim3((2 * r->d + kDwCols - 1) / kDwCols), dim3(kDwThreads), 0, st, a.part, blocks, r->d, a.wq ? dwq : nullptr,
                      a.wk ? dwk : nullptr);
   DLRM_CHECK_LAUNCH();
   return DLRM_OK;

@@ -118,28 +118,39 @@ struct Tile {
   }
 };
 
-constexpr int kSeqThreads = 256, kSeqWaves = 4;
+// Buffer descriptor of `bytes` from base on: loads past them give zeros.  base and bytes are the same for the whole wavefront.
+__device__ inline __amdgpu_buffer_rsrc_t span_of_bytes(const char* base, uint32_t bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  const uint64_t u = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p);
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(u), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
+}
 
-// A tile on its way from global memory to LDS, in the registers of the workgroup's threads.
-template <int DT, int DP, int ROWS>
+// A tile on its way from global memory to LDS, in the registers of the workgroup's threads.  Rows past the sequence and columns past d
+// are zeros, by the bounds of the buffer descriptor: the loads stand in no branch, so nothing waits for them before the store.
+template <int DT, int DP, int ROWS, int THREADS>
 struct Staged {
   static constexpr int CH = DP * Tab<DT>::EB / 16;  // chunks of 16 bytes in a row
-  static constexpr int N = (ROWS * CH + kSeqThreads - 1) / kSeqThreads;
+  static constexpr int N = (ROWS * CH + THREADS - 1) / THREADS;
   u32x4 v[N];
-  // rows row0.. of which `n` are there, columns < d; the rest are zeros
-  __device__ inline void load(const char* base, int64_t stride, int n, int d) {
+  uint32_t at[N];  // byte offset of each chunk in the tile
+  __device__ inline Staged(int64_t stride, int d) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + i * kSeqThreads, r = id / CH, c = id % CH;
-      v[i] = u32x4{0, 0, 0, 0};
-      if (r < n && r < ROWS && c * Tab<DT>::ELEMS < d) v[i] = load16(base + ((uint32_t)r * (uint32_t)stride + c * 16u));
+      const int id = threadIdx.x + i * THREADS, r = id / CH, c = id % CH;
+      at[i] = r < ROWS && c * Tab<DT>::ELEMS < d ? (uint32_t)r * (uint32_t)stride + c * 16u : 0xfffffff0u;
     }
+  }
+  // the n >= 1 rows from base on
+  __device__ inline void load(const char* base, int64_t stride, int n, int d) {
+    const auto rs = span_of_bytes(base, (uint32_t)(min(n, ROWS) - 1) * (uint32_t)stride + d * Tab<DT>::EB);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, at[i], 0, 0);
   }
   __device__ inline void store(char* s) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + i * kSeqThreads, r = id / CH, c = id % CH;
-      if (ROWS * CH % kSeqThreads == 0 || r < ROWS) *reinterpret_cast<u32x4*>(s + r * Tile<DT, DP>::STRIDE + c * 16) = v[i];
+      const int id = threadIdx.x + i * THREADS, r = id / CH, c = id % CH;
+      if (ROWS * CH % THREADS == 0 || r < ROWS) *reinterpret_cast<u32x4*>(s + r * Tile<DT, DP>::STRIDE + c * 16) = v[i];
     }
   }
 };
@@ -154,43 +165,71 @@ struct SeqArgs {
   float* delta;  // [Hq, Tq]
   int64_t Tq;
   int B, Hq, Hk, d, causal;
-  int slots;       // of 128 rows
+  int slots;
   int per_seq;     // slots of a sequence where all have the same number, else 0
   float scale, cap;
 };
 
-// Slot -> sequence and first row.  A sequence with n rows needs ceil(n / 128) slots, and how many rows it has stands in device memory.
-// Where all sequences fit into few slots each gets as many as the longest may need.  Else sequence s starts at slot off[s] / 128 + s, which leaves it
-// enough; slots past its rows end at once.  The sequence is found by all 64 lanes at once: each step asks 64 places.
-constexpr int kSlotRows = 128;
-__device__ inline bool find_slot(const int64_t* off, int B, int per_seq, int slot, int& seq, int& row0) {
+// Slot -> sequence and first row, slots of ROWS rows.  A sequence with n rows needs ceil(n / ROWS) of them, and how many rows it has
+// stands in device memory.  Where all sequences fit into few slots each gets as many as the longest may need, and the slots go block by
+// block through all sequences: with causal sequences the blocks of most work of every one of them start first.  Else sequence s
+// starts at slot off[s] / ROWS + s, which leaves it enough; slots past its rows end at once.  The sequence is found by all 64 lanes
+// at once: each step asks 64 places.
+template <int ROWS>
+__device__ inline void find_slot(const int64_t* off, int B, int per_seq, int slot, int& seq, int& row0) {
   if (per_seq > 0) {
-    seq = slot / per_seq;
-    row0 = (slot - seq * per_seq) * kSlotRows;
-    return true;
+    const int block = slot / B;
+    seq = (slot - block * B + block) % B;  // turned from block to block: workgroups go to the 8 dies in turn, and no die gets the same sequences' all
+    row0 = block * ROWS;
+    return;
   }
   int lo = 0, hi = B;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) >> 6, s = lo + lane_id() * step;
-    const bool before = s < hi && off[s] / kSlotRows + s <= slot;
+    const bool before = s < hi && off[s] / ROWS + s <= slot;
     const int n = __popcll(__ballot(before));  // >= 1: the first place always is
     hi = min(lo + n * step, hi);
     lo = lo + (n - 1) * step;
   }
   seq = __builtin_amdgcn_readfirstlane(lo);
-  row0 = (slot - (int)(off[seq] / kSlotRows) - seq) * kSlotRows;
-  return true;
+  row0 = (slot - (int)(off[seq] / ROWS) - seq) * ROWS;
 }
 
-// tanh from one exponential; fp32 operands take the library's, whose error near 0 is relative
-template <int DT>
-__device__ inline float bent(float z) {
-  if constexpr (DT == DLRM_F32) {
-    return tanhf(z);
-  } else {
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * (2.0f * kLog2e)) + 1.0f);
+// What a score is made of, fixed at compile time: without a cap and slopes an element costs a multiply-add and an exponential.
+enum { kPlain = 0, kSlopes = 1, kBend = 2 };  // bits
+
+// The score of a product s is, in powers of two, c * y(s) + base - slope * |distance|:
+//   without a cap  y = s, c = scale log2 e, base = 0;
+//   with a cap     tanh(z) = 1 - 2 r, r = 1 / (exp(2 z) + 1): an exponential and a reciprocal; y = -r, c = 2 cap log2 e,
+//                  base = cap log2 e, and the derivative 1 - tanh^2 is 4 r (1 - r) = -4 (y + y^2);
+//   fp32 with cap  y = tanh(z) of the library, whose error near 0 is relative; c = cap log2 e, base = 0, derivative 1 - y^2.
+// The derivative's constant factor goes into `grad`, which the gradients are multiplied by at the end, as scale does.
+template <int DT, int KIND>
+struct Score {
+  static constexpr bool BEND = (KIND & kBend) != 0, FAST = DT != DLRM_F32;
+  float zs, c, base, slope, grad;
+  __device__ inline Score(const SeqArgs& a, int head) {
+    zs = BEND ? a.scale / a.cap * (FAST ? 2.0f * kLog2e : 1.0f) : 0.0f;
+    c = BEND ? a.cap * (FAST ? 2.0f * kLog2e : kLog2e) : a.scale * kLog2e;
+    base = BEND && FAST ? a.cap * kLog2e : 0.0f;
+    slope = (KIND & kSlopes) ? a.slopes[head] * kLog2e : 0.0f;
+    grad = BEND && FAST ? -4.0f * a.scale : a.scale;
   }
-}
+  __device__ inline float y(float s) const {
+    if constexpr (!BEND) return s;
+    if constexpr (FAST) return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * zs));
+    return tanhf(s * zs);
+  }
+  // exponent of 2 of a weight: the score less `rest`
+  __device__ inline float exponent(float y, float away, float rest) const {
+    if constexpr ((KIND & kSlopes) != 0) return fmaf(y, c, fmaf(-slope, fabsf(away), -rest));
+    return fmaf(y, c, -rest);
+  }
+  __device__ inline float derivative(float y) const {
+    if constexpr (!BEND) return 1.0f;
+    return FAST ? fmaf(y, y, y) : fmaf(-y, y, 1.0f);
+  }
+};
 
 // the other lane half's value
 __device__ inline float other_half(float v) { return __shfl_xor(v, 32, DLRM_WAVE); }
@@ -251,33 +290,18 @@ __device__ inline Span span_of(const SeqArgs& a, int s, int64_t& q0, int64_t& k0
 // Key j of accumulator register r of subtile u, lane half h
 __device__ inline int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
-template <int DT>
-struct Score {  // of one head
-  float c, zs, cl, slope;
-  bool bend;
-  __device__ inline Score(const SeqArgs& a, int head) {
-    bend = a.cap > 0.0f;
-    c = a.scale * kLog2e;
-    zs = bend ? a.scale / a.cap : 0.0f;
-    cl = a.cap * kLog2e;
-    slope = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-  }
-  // product -> score in powers of two, without the factor `c` where there is neither cap nor slope
-  __device__ inline bool simple(const SeqArgs& a) const { return !bend && a.slopes == nullptr; }
-};
-
 // ---------------------------------------------------------------------------------------------------------------
 // Forward: a workgroup takes 128 queries of one head (32 a wavefront), tiles of 64 keys and values go by, two of them in LDS.
-template <int DT, int DP>
-__global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_fwd_kernel(SeqArgs a) {
-  constexpr int BK = 64, STEPS = DP / 16, NB = DP / 32;
+template <int DT, int DP, int KIND, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_fwd_kernel(SeqArgs a) {
+  constexpr int BK = 64, STEPS = DP / 16, NB = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char sk[2][BK * T::STRIDE];
   __shared__ __attribute__((aligned(16))) char sv[2][BK * T::STRIDE];
   const int hh = blockIdx.x % a.Hq, slot = a.slots - 1 - blockIdx.x / a.Hq;  // late rows see most keys: first
   const int G = a.Hq / a.Hk, hk = hh % a.Hk, head = hk * G + hh / a.Hk;
   int seq, row0;
-  find_slot(a.q_off, a.B, a.per_seq, slot, seq, row0);
+  find_slot<ROWS>(a.q_off, a.B, a.per_seq, slot, seq, row0);
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
   if (row0 >= sp.nq) return;
@@ -287,9 +311,8 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
   own_rows<DT, STEPS>(qf, row_of(a.q, q0 + i, head), there, a.d, h);
   const int vis = there ? sp.vis(i) : 0;
   const int wave_vis = w0 < sp.nq ? sp.vis(min(w0 + 31, sp.nq - 1)) : 0, wave_full = w0 < sp.nq ? sp.vis(w0) : 0;
-  const int end = sp.vis(min(row0 + kSlotRows - 1, sp.nq - 1));
-  const Score<DT> sc(a, head);
-  const bool simple = sc.simple(a);
+  const int end = sp.vis(min(row0 + ROWS - 1, sp.nq - 1));
+  const Score<DT, KIND> sc(a, head);
   const float place = (float)(i + sp.shift);
 
   f32x16 o[NB];
@@ -300,7 +323,7 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
   const char* kb = row_of(a.k, k0, hk);
   const char* vb = row_of(a.v, k0, hk);
   const int tiles = (end + BK - 1) / BK;
-  Staged<DT, DP, BK> tk, tv;
+  Staged<DT, DP, BK, THREADS> tk(a.k.st, a.d), tv(a.v.st, a.d);
   if (tiles > 0) {
     tk.load(kb, a.k.st, sp.nk, a.d);
     tv.load(vb, a.v.st, sp.nk, a.d);
@@ -324,15 +347,16 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) s[u] = Op<DT>::mma(T::by_row(ks, 32 * u + (lane & 31), st, h), qf[st], s[u]);
       }
-      float c = sc.c;
-      if (!simple) {
-        c = 1.0f;
+      // with slopes the whole score, else what the factor c still goes to, in the multiply-add before the exponential
+      const float c = KIND & kSlopes ? 1.0f : sc.c;
+      if constexpr (KIND != kPlain) {
+        const float away = place - (float)(j0 + 4 * h);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            float x = sc.bend ? bent<DT>(s[u][r] * sc.zs) * sc.cl : s[u][r] * sc.c;
-            s[u][r] = x - sc.slope * fabsf(place - (float)(j0 + 32 * u + acc_row(r, h)));
+            s[u][r] = sc.y(s[u][r]);
+            if constexpr ((KIND & kSlopes) != 0) s[u][r] = sc.exponent(s[u][r], away - (float)(32 * u + acc_row(r, 0)), 0.0f);
           }
       }
       if (j0 + BK > wave_full) {
@@ -348,15 +372,17 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
       top = fmaxf(top, other_half(top));
-      const float m1 = fmaxf(m, top * c);
-      const float ms = m1 == -kInf ? 0.0f : m1;  // nothing seen yet: every weight below is exp2(-inf)
-      if (__ballot(m1 > m)) {
-        const float f = __builtin_amdgcn_exp2f(m - ms);
+      // The sums are rescaled only where a maximum grew by more than 2^8: until then weights of up to 2^8 are as good as weights of
+      // up to 1 (fp32 sums; 16-bit weights keep their relative precision).  Exact either way: m is whatever the sums were made with.
+      if (__ballot(top * c > m + 8.0f)) {
+        const float m1 = fmaxf(m, top * c);
+        const float f = __builtin_amdgcn_exp2f(m - (m1 == -kInf ? 0.0f : m1));
         l *= f;
 #pragma unroll
         for (int b = 0; b < NB; ++b) o[b] *= f;
         m = m1;
       }
+      const float ms = m == -kInf ? 0.0f : m;  // nothing seen yet: every weight below is exp2(-inf)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -381,44 +407,25 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
   l += other_half(l);
   if (!there) return;
   store_rows<DT, NB>(o, l > 0.0f ? 1.0f / l : 0.0f, row_of(a.out, q0 + i, head), a.d, h);
-  if (a.lse && h == 0) a.lse[(int64_t)head * a.Tq + q0 + i] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
-}
-
-// Weight and score gradient of one product: s -> p = exp2(score - lse), ds = p (dp - delta) d score / d product / scale
-template <int DT>
-__device__ inline void weight_and_grad(const Score<DT>& sc, float s, float away, float lse2, float dp, float delta, float& p, float& ds) {
-  float x, f = 1.0f;
-  if (sc.bend) {
-    const float t = bent<DT>(s * sc.zs);
-    x = t * sc.cl;
-    f = 1.0f - t * t;
-  } else {
-    x = s * sc.c;
-  }
-  p = __builtin_amdgcn_exp2f(x - sc.slope * away - lse2);
-  ds = p * (dp - delta) * f;
+  if (a.lse && h == 0) a.lse[(int64_t)head * a.Tq + q0 + i] = l > 0.0f ? (m + sc.base + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
 }
 
 // a row's lse in powers of two, +inf (all weights 0) for a row that sees nothing or is not there
-__device__ inline float lse2_of(const float* lse, int64_t at, bool there) {
-  if (!there) return kInf;
-  const float x = lse[at];
-  return x == -kInf ? kInf : x * kLog2e;
-}
+__device__ inline float lse2_of(float lse, bool there) { return !there || lse == -kInf ? kInf : lse * kLog2e; }
 
 // ---------------------------------------------------------------------------------------------------------------
 // Queries' gradient, and delta = <dout, out> of every row for the kernel after it.  As the forward, with
 // dP^T = V dO^T beside S^T and dQ^T = K^T dS^T.
-template <int DT, int DP>
-__global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_dq_kernel(SeqArgs a) {
-  constexpr int BK = 32, STEPS = DP / 16, NB = DP / 32;
+template <int DT, int DP, int KIND, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_dq_kernel(SeqArgs a) {
+  constexpr int BK = 32, STEPS = DP / 16, NB = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char sk[2][BK * T::STRIDE];
   __shared__ __attribute__((aligned(16))) char sv[2][BK * T::STRIDE];
   const int hh = blockIdx.x % a.Hq, slot = a.slots - 1 - blockIdx.x / a.Hq;
   const int G = a.Hq / a.Hk, hk = hh % a.Hk, head = hk * G + hh / a.Hk;
   int seq, row0;
-  find_slot(a.q_off, a.B, a.per_seq, slot, seq, row0);
+  find_slot<ROWS>(a.q_off, a.B, a.per_seq, slot, seq, row0);
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
   if (row0 >= sp.nq) return;
@@ -439,12 +446,12 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
   }
   const int64_t at = (int64_t)head * a.Tq + q0 + i;
   if (there && h == 0) a.delta[at] = delta;
-  const float lse2 = lse2_of(a.lse, at, there);
+  const float lse = there ? a.lse[at] : 0.0f;
   const int vis = there ? sp.vis(i) : 0;
   const int wave_vis = w0 < sp.nq ? sp.vis(min(w0 + 31, sp.nq - 1)) : 0, wave_full = w0 < sp.nq ? sp.vis(w0) : 0;
-  const int end = sp.vis(min(row0 + kSlotRows - 1, sp.nq - 1));
-  const Score<DT> sc(a, head);
-  const float place = (float)(i + sp.shift);
+  const int end = sp.vis(min(row0 + ROWS - 1, sp.nq - 1));
+  const Score<DT, KIND> sc(a, head);
+  const float place = (float)(i + sp.shift), rest = lse2_of(lse, there) - sc.base;
 
   f32x16 g[NB];
 #pragma unroll
@@ -452,7 +459,7 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
   const char* kb = row_of(a.k, k0, hk);
   const char* vb = row_of(a.v, k0, hk);
   const int tiles = (end + BK - 1) / BK;
-  Staged<DT, DP, BK> tk, tv;
+  Staged<DT, DP, BK, THREADS> tk(a.k.st, a.d), tv(a.v.st, a.d);
   if (tiles > 0) {
     tk.load(kb, a.k.st, sp.nk, a.d);
     tv.load(vb, a.v.st, sp.nk, a.d);
@@ -475,18 +482,23 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
         s = Op<DT>::mma(T::by_row(ks, lane & 31, st, h), qf[st], s);
         dp = Op<DT>::mma(T::by_row(vs, lane & 31, st, h), df[st], dp);
       }
-      const bool masked = j0 + BK > wave_full;
+      const float away = place - (float)(j0 + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float y = sc.y(s[r]);
+        s[r] = __builtin_amdgcn_exp2f(sc.exponent(y, away - (float)acc_row(r, 0), rest)) * (dp[r] - delta);
+        if constexpr ((KIND & kBend) != 0) s[r] *= sc.derivative(y);
+      }
+      if (j0 + BK > wave_full) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (j0 + acc_row(r, h) >= vis) s[r] = 0.0f;
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         Op<DT> ds;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const int j = j0 + acc_row(8 * c + r, h);
-          float p, x;
-          weight_and_grad<DT>(sc, s[8 * c + r], fabsf(place - (float)j), lse2, dp[8 * c + r], delta, p, x);
-          if (masked && j >= vis) x = 0.0f;
-          ds.set(r, x);
-        }
+        for (int r = 0; r < 8; ++r) ds.set(r, s[8 * c + r]);
 #pragma unroll
         for (int b = 0; b < NB; ++b) g[b] = Op<DT>::mma(T::by_column(ks, 16 * c, b, lane), ds, g[b]);
       }
@@ -497,32 +509,54 @@ __global__ __launch_bounds__(kSeqThreads, DT == DLRM_F32 ? 1 : 2) void seq_attn_
     }
     __syncthreads();
   }
-  if (there) store_rows<DT, NB>(g, a.scale, row_of(a.dq, q0 + i, head), a.d, h);
+  if (there) store_rows<DT, NB>(g, sc.grad, row_of(a.dq, q0 + i, head), a.d, h);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Keys' and values' gradients: a workgroup takes 128 keys of one key head (32 a wavefront); the queries and upstream gradients of
+// Keys' and values' gradients: a workgroup takes KEYS keys of one key head (32 a wavefront); the queries and upstream gradients of
 // all query heads that share it go by in tiles, so the sum over the heads stays in registers.
 // S = Q K^T and dP = dO V^T have the keys as columns; dV^T = dO^T P and dK^T = Q^T dS.
-template <int DT, int DP>
-__global__ __launch_bounds__(kSeqThreads, 1) void seq_attn_dkv_kernel(SeqArgs a) {
-  constexpr int BQ = 32, STEPS = DP / 16, NB = DP / 32;
+// Two wavefronts share 32 keys, one for each half of a tile's 64 queries, and add their sums at the end: the keys that all
+// queries of a long sequence see are the longest work of all, and go by in half the steps.
+template <int DT, int DP, int GROUPS_, int PARTS_>
+struct Dkv {
+  static constexpr int GROUPS = GROUPS_, PARTS = PARTS_, KEYS = 32 * GROUPS, THREADS = 64 * GROUPS * PARTS, BQ = 32 * PARTS;
+  static constexpr int STEPS = DP / 16, NB = DP / 32;
+  // Wide 16-bit rows: the values' operands are read from LDS again for every tile, or the accumulators and both operands would
+  // not fit the registers of two wavefronts per SIMD.
+  static constexpr bool V_LDS = DT != DLRM_F32 && DP > 64;
   typedef Tile<DT, DP> T;
-  __shared__ __attribute__((aligned(16))) char sq[2][BQ * T::STRIDE];
-  __shared__ __attribute__((aligned(16))) char sd[2][BQ * T::STRIDE];
-  __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];  // lse2, delta
+  static constexpr int TILE = BQ * T::STRIDE, V_AT = 4 * TILE, STAT_AT = V_AT + (V_LDS ? KEYS * T::STRIDE : 0);
+  static constexpr int BYTES = STAT_AT + 2 * 2 * BQ * 4;
+  static constexpr int JOIN = GROUPS * NB * 16 * DLRM_WAVE * 4;  // one of the two sums of half the wavefronts
+  static constexpr int LDS = PARTS == 1 || BYTES > JOIN ? BYTES : JOIN;
+};
+
+template <int DT, int DP, int KIND, int GROUPS, int PARTS>
+__global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void seq_attn_dkv_kernel(SeqArgs a) {
+  typedef Dkv<DT, DP, GROUPS, PARTS> W;
+  typedef typename W::T T;
+  constexpr int BQ = W::BQ, STEPS = W::STEPS, NB = W::NB;
+  __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;  // early keys are seen by most queries: first
   const int G = a.Hq / a.Hk;
   int seq, row0;
-  find_slot(a.k_off, a.B, a.per_seq, slot, seq, row0);
+  find_slot<W::KEYS>(a.k_off, a.B, a.per_seq, slot, seq, row0);
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
   if (row0 >= sp.nk) return;
-  const int lane = lane_id(), h = lane >> 5, w0 = row0 + wave_id() * 32, j = w0 + (lane & 31);
+  const int lane = lane_id(), h = lane >> 5, group = wave_id() % W::GROUPS, part = wave_id() / W::GROUPS;
+  const int w0 = row0 + group * 32, j = w0 + (lane & 31);
   const bool there = j < sp.nk;
-  Op<DT> kf[STEPS], vf[STEPS];
+  Op<DT> kf[STEPS], vf[W::V_LDS ? 1 : STEPS];
   own_rows<DT, STEPS>(kf, row_of(a.k, k0 + j, hk), there, a.d, h);
-  own_rows<DT, STEPS>(vf, row_of(a.v, k0 + j, hk), there, a.d, h);
+  if constexpr (W::V_LDS) {
+    Staged<DT, DP, W::KEYS, W::THREADS> t(a.v.st, a.d);
+    t.load(row_of(a.v, k0 + row0, hk), a.v.st, sp.nk - row0, a.d);
+    t.store(lds + W::V_AT);
+  } else {
+    own_rows<DT, STEPS>(vf, row_of(a.v, k0 + j, hk), there, a.d, h);
+  }
   const int from = there ? sp.first_query(j) : 0x7fffffff;
   const int wave_from = w0 < sp.nk ? sp.first_query(w0) : 0x7fffffff;
   const int wave_full = w0 < sp.nk ? sp.first_query(min(w0 + 31, sp.nk - 1)) : 0x7fffffff;
@@ -531,64 +565,86 @@ __global__ __launch_bounds__(kSeqThreads, 1) void seq_attn_dkv_kernel(SeqArgs a)
   f32x16 gk[NB], gv[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) gk[b] = gv[b] = f32x16{};
-  Staged<DT, DP, BQ> tq, td;
-  float st0 = 0.0f;
-  auto fetch = [&](int n) {  // tile n of all heads' tiles
-    const int head = hk * G + n / tiles, i0 = (t0 + n % tiles) * BQ;
+  Staged<DT, DP, BQ, W::THREADS> tq(a.q.st, a.d), td(a.dout.st, a.d);
+  // lse and delta of the tile's rows: loaded by every thread, row clamped and not yet looked at, so that no branch and no wait comes before
+  // the tile is put away
+  const int srow = threadIdx.x % BQ;
+  const float* const sfrom = (threadIdx.x / BQ & 1 ? a.delta : a.lse) + q0;
+  float sraw = 0.0f;
+  int head = hk * G, t = t0;  // of the tile that is on its way
+  const float base = Score<DT, KIND>(a, head).base;
+  auto fetch = [&]() {
+    const int i0 = t * BQ;
     tq.load(row_of(a.q, q0 + i0, head), a.q.st, sp.nq - i0, a.d);
     td.load(row_of(a.dout, q0 + i0, head), a.dout.st, sp.nq - i0, a.d);
-    if (threadIdx.x < 2 * BQ) {
-      const int i = threadIdx.x % BQ;
-      const int64_t at = (int64_t)head * a.Tq + q0 + i0 + i;
-      const bool row = i0 + i < sp.nq;
-      st0 = threadIdx.x < BQ ? lse2_of(a.lse, at, row) : row ? a.delta[at] : 0.0f;
-    }
+    sraw = sfrom[(int64_t)head * a.Tq + min(i0 + srow, sp.nq - 1)];
   };
   auto put = [&](int n) {
-    tq.store(sq[n & 1]);
-    td.store(sd[n & 1]);
-    if (threadIdx.x < 2 * BQ) stat[n & 1][threadIdx.x / BQ][threadIdx.x % BQ] = st0;
+    tq.store(lds + (n & 1) * 2 * W::TILE);
+    td.store(lds + ((n & 1) * 2 + 1) * W::TILE);
+    if (threadIdx.x < 2 * BQ) {
+      const bool row = t * BQ + srow < sp.nq;
+      float* stat = reinterpret_cast<float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ;
+      stat[threadIdx.x] = threadIdx.x < BQ ? lse2_of(sraw, row) - base : row ? sraw : 0.0f;
+    }
   };
   const int all = tiles * G;
   if (all > 0) {
-    fetch(0);
+    fetch();
     put(0);
   }
   __syncthreads();
   for (int n = 0; n < all; ++n) {
-    if (n + 1 < all) fetch(n + 1);
-    const int i0 = (t0 + n % tiles) * BQ;
-    if (i0 + BQ > wave_from) {
-      const Score<DT> sc(a, hk * G + n / tiles);
-      const char* qs = sq[n & 1];
-      const char* ds_ = sd[n & 1];
+    const int at = head, i0 = t * BQ + 32 * part;
+    if (n + 1 < all) {
+      if (++t == t0 + tiles) {
+        t = t0;
+        ++head;
+      }
+      fetch();
+    }
+    if (i0 + 32 > wave_from && i0 < sp.nq) {
+      const Score<DT, KIND> sc(a, at);
+      const char* qs = lds + (n & 1) * 2 * W::TILE + 32 * part * T::STRIDE;
+      const char* os = qs + W::TILE;
+      const float* stat = reinterpret_cast<const float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ + 32 * part + 4 * h;
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
         s = Op<DT>::mma(T::by_row(qs, lane & 31, st, h), kf[st], s);
-        dp = Op<DT>::mma(T::by_row(ds_, lane & 31, st, h), vf[st], dp);
+        dp = Op<DT>::mma(T::by_row(os, lane & 31, st, h), W::V_LDS ? T::by_row(lds + W::V_AT, group * 32 + (lane & 31), st, h) : vf[W::V_LDS ? 0 : st], dp);
       }
-      const bool masked = i0 < wave_full;
+      const float away = (float)(i0 + sp.shift + 4 * h) - (float)j;
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);
+        const f32x4 del = *reinterpret_cast<const f32x4*>(stat + BQ + 8 * r4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * r4 + i;
+          const float y = sc.y(s[r]);
+          const float p = __builtin_amdgcn_exp2f(sc.exponent(y, away + (float)acc_row(r, 0), rest[i]));
+          dp[r] = p * (dp[r] - del[i]);
+          if constexpr ((KIND & kBend) != 0) dp[r] *= sc.derivative(y);
+          s[r] = p;
+        }
+      }
+      if (i0 < wave_full) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (i0 + acc_row(r, h) < from) s[r] = dp[r] = 0.0f;
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         Op<DT> p, ds;
 #pragma unroll
-        for (int r4 = 0; r4 < 2; ++r4) {
-          const f32x4 lse2 = *reinterpret_cast<const f32x4*>(&stat[n & 1][0][acc_row(8 * c + 4 * r4, h)]);
-          const f32x4 del = *reinterpret_cast<const f32x4*>(&stat[n & 1][1][acc_row(8 * c + 4 * r4, h)]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = i0 + acc_row(8 * c + 4 * r4 + r, h);
-            float w, x;
-            weight_and_grad<DT>(sc, s[8 * c + 4 * r4 + r], fabsf((float)(i + sp.shift) - (float)j), lse2[r], dp[8 * c + 4 * r4 + r], del[r], w, x);
-            if (masked && i < from) w = x = 0.0f;
-            p.set(4 * r4 + r, w);
-            ds.set(4 * r4 + r, x);
-          }
+        for (int r = 0; r < 8; ++r) {
+          p.set(r, s[8 * c + r]);
+          ds.set(r, dp[8 * c + r]);
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          gv[b] = Op<DT>::mma(T::by_column(ds_, 16 * c, b, lane), p, gv[b]);
+          gv[b] = Op<DT>::mma(T::by_column(os, 16 * c, b, lane), p, gv[b]);
           gk[b] = Op<DT>::mma(T::by_column(qs, 16 * c, b, lane), ds, gk[b]);
         }
       }
@@ -596,56 +652,109 @@ __global__ __launch_bounds__(kSeqThreads, 1) void seq_attn_dkv_kernel(SeqArgs a)
     if (n + 1 < all) put(n + 1);
     __syncthreads();
   }
-  if (!there) return;
-  store_rows<DT, NB>(gk, a.scale, row_of(a.dk, k0 + j, hk), a.d, h);
+  // the second half's sums join the first's, one of the two gradients after the other
+  f32x4* join = reinterpret_cast<f32x4*>(lds) + group * NB * 4 * DLRM_WAVE + lane;
+#pragma unroll
+  for (int g = 0; g < (PARTS == 2 ? 2 : 0); ++g) {
+    f32x16* x = g ? gv : gk;
+    if (g) __syncthreads();
+    if (part == 1) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) join[(b * 4 + q) * DLRM_WAVE] = f32x4{x[b][4 * q], x[b][4 * q + 1], x[b][4 * q + 2], x[b][4 * q + 3]};
+    }
+    __syncthreads();
+    if (part == 0) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 y = join[(b * 4 + q) * DLRM_WAVE];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[b][4 * q + e] += y[e];
+        }
+    }
+  }
+  if (part == 1 || !there) return;
+  store_rows<DT, NB>(gk, Score<DT, KIND>(a, hk * G).grad, row_of(a.dk, k0 + j, hk), a.d, h);
   store_rows<DT, NB>(gv, 1.0f, row_of(a.dv, k0 + j, hk), a.d, h);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// slots of 128 rows for n rows in B sequences of at most `longest`
-__host__ inline bool slots_of(SeqArgs& a, int64_t n, int longest, int heads) {
-  const int64_t each = ((int64_t)longest + kSlotRows - 1) / kSlotRows;
-  const int64_t even = each * a.B, searched = n / kSlotRows + a.B;
-  a.per_seq = even <= searched ? (int)each : 0;
-  const int64_t s = even <= searched ? even : searched;
+// slots of `rows` rows for n rows in B sequences of at most `longest`
+__host__ inline bool slots_of(SeqArgs& a, int64_t n, int longest, int heads, int rows) {
+  const int64_t each = ((int64_t)longest + rows - 1) / rows;
+  const int64_t even = each * a.B, searched = n / rows + a.B;
+  // Block by block while at most two in three slots are empty: an empty workgroup ends in under a microsecond, while histories one after
+  // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
+  const bool block_by_block = even <= 3 * searched;
+  a.per_seq = block_by_block ? (int)each : 0;
+  const int64_t s = block_by_block ? even : searched;
   a.slots = (int)s;
   return s * heads <= 0x7fffffff;
 }
 
-template <int DT, typename F>
-__host__ inline int for_width(int d, F f) {
-  if (d <= 32) return f(std::integral_constant<int, 32>{});
-  if (d <= 64) return f(std::integral_constant<int, 64>{});
-  if (d <= 96) return f(std::integral_constant<int, 96>{});
-  return f(std::integral_constant<int, 128>{});
+// Calls f with the padded width and the kind of score as compile-time constants.
+template <typename F>
+__host__ inline int for_kind(const SeqArgs& a, F f) {
+  auto by_kind = [&](auto dp) {
+    switch ((a.slopes ? kSlopes : 0) | (a.cap > 0.0f ? kBend : 0)) {
+      case kPlain: return f(dp, std::integral_constant<int, kPlain>{});
+      case kSlopes: return f(dp, std::integral_constant<int, kSlopes>{});
+      case kBend: return f(dp, std::integral_constant<int, kBend>{});
+      default: return f(dp, std::integral_constant<int, kSlopes | kBend>{});
+    }
+  };
+  if (a.d <= 32) return by_kind(std::integral_constant<int, 32>{});
+  if (a.d <= 64) return by_kind(std::integral_constant<int, 64>{});
+  if (a.d <= 96) return by_kind(std::integral_constant<int, 96>{});
+  return by_kind(std::integral_constant<int, 128>{});
 }
 
-template <int DT>
-int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  if (!slots_of(a, s->Tq, s->max_q, a.Hq)) return DLRM_ERR_BAD_SHAPE;
+template <int DT, int WAVES>
+int launch_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
+  if (!slots_of(a, s->Tq, s->max_q, a.Hq, 32 * WAVES)) return DLRM_ERR_BAD_SHAPE;
   if (a.slots == 0) return DLRM_OK;
-  return for_width<DT>(a.d, [&](auto dp) {
-    hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp()>), dim3((unsigned)(a.slots * a.Hq)), dim3(kSeqThreads), 0, st, a);
+  return for_kind(a, [&](auto dp, auto kind) {
+    hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), WAVES>), dim3((unsigned)(a.slots * a.Hq)), dim3(64 * WAVES), 0, st, a);
+    DLRM_CHECK_LAUNCH();
+    return (int)DLRM_OK;
+  });
+}
+
+template <int DT, int WAVES>
+int launch_dq(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
+  if (!slots_of(a, s->Tq, s->max_q, a.Hq, 32 * WAVES)) return DLRM_ERR_BAD_SHAPE;
+  if (a.slots == 0) return DLRM_OK;
+  return for_kind(a, [&](auto dp, auto kind) {
+    hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), WAVES>), dim3((unsigned)(a.slots * a.Hq)), dim3(64 * WAVES), 0, st, a);
+    DLRM_CHECK_LAUNCH();
+    return (int)DLRM_OK;
+  });
+}
+
+template <int DT, int GROUPS, int PARTS>
+int launch_dkv(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
+  if (!slots_of(a, s->Tk, s->max_k, a.Hk, 32 * GROUPS)) return DLRM_ERR_BAD_SHAPE;
+  if (a.slots == 0) return DLRM_OK;
+  return for_kind(a, [&](auto dp, auto kind) {
+    hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), GROUPS, PARTS>), dim3((unsigned)(a.slots * a.Hk)), dim3(64 * GROUPS * PARTS), 0, st, a);
     DLRM_CHECK_LAUNCH();
     return (int)DLRM_OK;
   });
 }
 
 template <int DT>
+int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
+  return launch_fwd<DT, 4>(s, a, st);
+}
+
+template <int DT>
 int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  SeqArgs b = a;
-  if (!slots_of(a, s->Tq, s->max_q, a.Hq) || !slots_of(b, s->Tk, s->max_k, a.Hk)) return DLRM_ERR_BAD_SHAPE;
-  return for_width<DT>(a.d, [&](auto dp) {
-    if (a.slots > 0) {
-      hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp()>), dim3((unsigned)(a.slots * a.Hq)), dim3(kSeqThreads), 0, st, a);
-      DLRM_CHECK_LAUNCH();
-    }
-    if (b.slots > 0) {
-      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp()>), dim3((unsigned)(b.slots * b.Hk)), dim3(kSeqThreads), 0, st, b);
-      DLRM_CHECK_LAUNCH();
-    }
-    return (int)DLRM_OK;
-  });
+  if (const int rc = launch_dq<DT, 4>(s, a, st)) return rc;
+  if (s->max_q <= 256) return launch_dkv<DT, 2, 1>(s, a, st);
+  return launch_dkv<DT, DT == DLRM_F32 ? 2 : 4, 2>(s, a, st);
 }
 
 extern template int launch_seq_fwd<DLRM_F32>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
