@@ -170,13 +170,13 @@ struct SeqArgs {
   float scale, cap;
 };
 
-// Slot -> sequence and first row, slots of ROWS rows.  A sequence with n rows needs ceil(n / ROWS) of them, and how many rows it has
-// stands in device memory.  Where all sequences fit into few slots each gets as many as the longest may need, and the slots go block by
-// block through all sequences: with causal sequences the blocks of most work of every one of them start first.  Else sequence s
-// starts at slot off[s] / ROWS + s, which leaves it enough; slots past its rows end at once.  The sequence is found by all 64 lanes
-// at once: each step asks 64 places.
+// Slot -> sequence and first row, slots of ROWS rows, `per` rows for each item of `off`.  A sequence with n rows needs
+// ceil(n / ROWS) of them, and how many rows it has stands in device memory.  Where all sequences fit into few slots each gets as many as the
+// longest may need, and the slots go block by block through all sequences: with causal sequences the blocks of most work of every one
+// of them start first.  Else sequence s starts at slot off[s] * per / ROWS + s, which leaves it enough; slots past its rows end at
+// once.  The sequence is found by all 64 lanes at once: each step asks 64 places.
 template <int ROWS>
-__device__ inline void find_slot(const int64_t* off, int B, int per_seq, int slot, int& seq, int& row0) {
+__device__ inline void find_slot(const int64_t* off, int per, int B, int per_seq, int slot, int& seq, int& row0) {
   if (per_seq > 0) {
     const int block = slot / B;
     seq = (slot - block * B + block) % B;  // turned from block to block: workgroups go to the 8 dies in turn, and no die gets the same sequences' all
@@ -186,13 +186,13 @@ __device__ inline void find_slot(const int64_t* off, int B, int per_seq, int slo
   int lo = 0, hi = B;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) >> 6, s = lo + lane_id() * step;
-    const bool before = s < hi && off[s] / ROWS + s <= slot;
+    const bool before = s < hi && off[s] * per / ROWS + s <= slot;
     const int n = __popcll(__ballot(before));  // >= 1: the first place always is
     hi = min(lo + n * step, hi);
     lo = lo + (n - 1) * step;
   }
   seq = __builtin_amdgcn_readfirstlane(lo);
-  row0 = (slot - (int)(off[seq] / ROWS) - seq) * ROWS;
+  row0 = (slot - (int)(off[seq] * per / ROWS) - seq) * ROWS;
 }
 
 // What a score is made of, fixed at compile time: without a cap and slopes an element costs a multiply-add and an exponential.
@@ -291,58 +291,115 @@ __device__ inline Span span_of(const SeqArgs& a, int s, int64_t& q0, int64_t& k0
 __device__ inline int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Forward: a workgroup takes 128 queries of one head (32 a wavefront), tiles of 64 keys and values go by, two of them in LDS.
-template <int DT, int DP, int KIND, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_fwd_kernel(SeqArgs a) {
-  constexpr int BK = 64, STEPS = DP / 16, NB = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
-  typedef Tile<DT, DP> T;
-  __shared__ __attribute__((aligned(16))) char sk[2][BK * T::STRIDE];
-  __shared__ __attribute__((aligned(16))) char sv[2][BK * T::STRIDE];
-  const int hh = blockIdx.x % a.Hq, slot = a.slots - 1 - blockIdx.x / a.Hq;  // late rows see most keys: first
-  const int G = a.Hq / a.Hk, hk = hh % a.Hk, head = hk * G + hh / a.Hk;
-  int seq, row0;
-  find_slot<ROWS>(a.q_off, a.B, a.per_seq, slot, seq, row0);
+// Rows of the forward and of the queries' gradient: the queries of all query heads that share a key head, item by item, are the rows of one
+// walk over its keys: row r is item r / G, head r % G of the G.  Short histories and few candidates fill a wavefront's rows this way,
+// the keys pass through LDS once for all G, and a causal block ends G times nearer to its diagonal.
+// GROUPS x 32 rows a workgroup; PARTS wavefronts share 32 rows, each with its part of a tile's keys, and join at the end: where the rows
+// are few, or a product is slow (fp32), the longest rows' walk is what the call waits for.
+struct MyRow {
+  int64_t t;  // item of q, out, ...
+  int i, head;
+  bool there;
+};
+template <int GROUPS, int PARTS>
+struct RowWork {
+  int seq, row0, group, part, hk, G;
   int64_t q0, k0;
-  const Span sp = span_of(a, seq, q0, k0);
-  if (row0 >= sp.nq) return;
-  const int lane = lane_id(), h = lane >> 5, w0 = row0 + wave_id() * 32, i = w0 + (lane & 31);
-  const bool there = i < sp.nq;
+  Span sp;
+  MyRow me;
+  int vis, wave_vis, wave_full, end;  // keys that my row, the wavefront's last, its first, and the workgroup's last row see
+  __device__ inline bool find(const SeqArgs& a) {
+    constexpr int ROWS = 32 * GROUPS;
+    G = a.Hq / a.Hk;
+    hk = blockIdx.x % a.Hk;
+    find_slot<ROWS>(a.q_off, G, a.B, a.per_seq, a.slots - 1 - blockIdx.x / a.Hk, seq, row0);  // late rows see most keys: first
+    sp = span_of(a, seq, q0, k0);
+    const int rows = sp.nq * G;
+    if (row0 >= rows) return false;
+    group = wave_id() % GROUPS;
+    part = wave_id() / GROUPS;
+    const int w0 = row0 + group * 32, r = w0 + (lane_id() & 31);
+    me.there = r < rows;
+    me.i = me.there ? r / G : 0;
+    me.head = hk * G + (me.there ? r - me.i * G : 0);
+    me.t = q0 + me.i;
+    vis = me.there ? sp.vis(me.i) : 0;
+    wave_vis = w0 < rows ? sp.vis(min(w0 + 31, rows - 1) / G) : 0;
+    wave_full = w0 < rows ? sp.vis(w0 / G) : 0;
+    end = sp.vis(min(row0 + ROWS - 1, rows - 1) / G);
+    return true;
+  }
+};
+
+// Adds (f = nullptr) or rescales and adds the sums of the wavefronts of part 1 to those of part 0, through LDS.
+template <int NB, int GROUPS>
+__device__ inline void join_parts(f32x16* x, char* lds, int group, int part, float mine, float other) {
+  f32x4* at = reinterpret_cast<f32x4*>(lds) + group * NB * 4 * DLRM_WAVE + lane_id();
+  if (part == 1) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) at[(b * 4 + q) * DLRM_WAVE] = f32x4{x[b][4 * q], x[b][4 * q + 1], x[b][4 * q + 2], x[b][4 * q + 3]};
+  }
+  __syncthreads();
+  if (part == 0) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 y = at[(b * 4 + q) * DLRM_WAVE];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[b][4 * q + e] = x[b][4 * q + e] * mine + y[e] * other;
+      }
+  }
+}
+
+// Forward: tiles of 64 keys and values go by, two of them in LDS.
+template <int DT, int DP, int KIND, int GROUPS, int PARTS>
+__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_attn_fwd_kernel(SeqArgs a) {
+  constexpr int SUB = 2 / PARTS, BK = 32 * SUB * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
+  typedef Tile<DT, DP> T;
+  constexpr int TILE = BK * T::STRIDE, JOIN = PARTS == 2 ? GROUPS * NB * 16 * DLRM_WAVE * 4 : 0;
+  __shared__ __attribute__((aligned(16))) char lds[4 * TILE > JOIN ? 4 * TILE : JOIN];
+  __shared__ float stat[PARTS == 2 ? GROUPS * 2 * 32 : 1];
+  RowWork<GROUPS, PARTS> w;
+  if (!w.find(a)) return;
+  const Span& sp = w.sp;
+  const int lane = lane_id(), h = lane >> 5;
   Op<DT> qf[STEPS];
-  own_rows<DT, STEPS>(qf, row_of(a.q, q0 + i, head), there, a.d, h);
-  const int vis = there ? sp.vis(i) : 0;
-  const int wave_vis = w0 < sp.nq ? sp.vis(min(w0 + 31, sp.nq - 1)) : 0, wave_full = w0 < sp.nq ? sp.vis(w0) : 0;
-  const int end = sp.vis(min(row0 + ROWS - 1, sp.nq - 1));
-  const Score<DT, KIND> sc(a, head);
-  const float place = (float)(i + sp.shift);
+  own_rows<DT, STEPS>(qf, row_of(a.q, w.me.t, w.me.head), w.me.there, a.d, h);
+  const Score<DT, KIND> sc(a, w.me.head);
+  const float place = (float)(w.me.i + sp.shift);
 
   f32x16 o[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) o[b] = f32x16{};
   float m = -kInf, l = 0.0f;
 
-  const char* kb = row_of(a.k, k0, hk);
-  const char* vb = row_of(a.v, k0, hk);
-  const int tiles = (end + BK - 1) / BK;
+  const char* kb = row_of(a.k, w.k0, w.hk);
+  const char* vb = row_of(a.v, w.k0, w.hk);
+  const int tiles = (w.end + BK - 1) / BK;
   Staged<DT, DP, BK, THREADS> tk(a.k.st, a.d), tv(a.v.st, a.d);
   if (tiles > 0) {
     tk.load(kb, a.k.st, sp.nk, a.d);
     tv.load(vb, a.v.st, sp.nk, a.d);
-    tk.store(sk[0]);
-    tv.store(sv[0]);
+    tk.store(lds);
+    tv.store(lds + TILE);
   }
   __syncthreads();
   for (int t = 0; t < tiles; ++t) {
-    const int j0 = t * BK;
+    const int jt = t * BK;
     if (t + 1 < tiles) {
-      tk.load(kb + (int64_t)(j0 + BK) * a.k.st, a.k.st, sp.nk - j0 - BK, a.d);
-      tv.load(vb + (int64_t)(j0 + BK) * a.v.st, a.v.st, sp.nk - j0 - BK, a.d);
+      tk.load(kb + (int64_t)(jt + BK) * a.k.st, a.k.st, sp.nk - jt - BK, a.d);
+      tv.load(vb + (int64_t)(jt + BK) * a.v.st, a.v.st, sp.nk - jt - BK, a.d);
     }
-    if (j0 < wave_vis) {
-      const char* ks = sk[t & 1];
-      const char* vs = sv[t & 1];
-      f32x16 s[2];
+    const int j0 = jt + 32 * SUB * w.part;
+    if (j0 < w.wave_vis) {
+      const char* ks = lds + (t & 1) * 2 * TILE + 32 * SUB * w.part * T::STRIDE;
+      const char* vs = ks + TILE;
+      f32x16 s[SUB];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < SUB; ++u) {
         s[u] = f32x16{};
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) s[u] = Op<DT>::mma(T::by_row(ks, 32 * u + (lane & 31), st, h), qf[st], s[u]);
@@ -352,23 +409,23 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_f
       if constexpr (KIND != kPlain) {
         const float away = place - (float)(j0 + 4 * h);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             s[u][r] = sc.y(s[u][r]);
             if constexpr ((KIND & kSlopes) != 0) s[u][r] = sc.exponent(s[u][r], away - (float)(32 * u + acc_row(r, 0)), 0.0f);
           }
       }
-      if (j0 + BK > wave_full) {
+      if (j0 + 32 * SUB > w.wave_full) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (j0 + 32 * u + acc_row(r, h) >= vis) s[u][r] = -kInf;
+            if (j0 + 32 * u + acc_row(r, h) >= w.vis) s[u][r] = -kInf;
       }
       float top = s[0][0];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < SUB; ++u)
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[u][r]);
       top = fmaxf(top, other_half(top));
@@ -384,7 +441,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_f
       }
       const float ms = m == -kInf ? 0.0f : m;  // nothing seen yet: every weight below is exp2(-inf)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < SUB; ++u)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           Op<DT> p;
@@ -399,15 +456,30 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_f
         }
     }
     if (t + 1 < tiles) {
-      tk.store(sk[(t + 1) & 1]);
-      tv.store(sv[(t + 1) & 1]);
+      tk.store(lds + ((t + 1) & 1) * 2 * TILE);
+      tv.store(lds + ((t + 1) & 1) * 2 * TILE + TILE);
     }
     __syncthreads();
   }
   l += other_half(l);
-  if (!there) return;
-  store_rows<DT, NB>(o, l > 0.0f ? 1.0f / l : 0.0f, row_of(a.out, q0 + i, head), a.d, h);
-  if (a.lse && h == 0) a.lse[(int64_t)head * a.Tq + q0 + i] = l > 0.0f ? (m + sc.base + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
+  if constexpr (PARTS == 2) {
+    float* st = stat + w.group * 64 + (lane & 31);
+    if (w.part == 1 && h == 0) {
+      st[0] = m;
+      st[32] = l;
+    }
+    __syncthreads();
+    const float m2 = st[0], top = fmaxf(m, m2), ts = top == -kInf ? 0.0f : top;
+    const float f1 = __builtin_amdgcn_exp2f(m - ts), f2 = __builtin_amdgcn_exp2f(m2 - ts);
+    join_parts<NB, GROUPS>(o, lds, w.group, w.part, f1, f2);
+    l = l * f1 + st[32] * f2;
+    m = top;
+    if (w.part == 1) return;
+  }
+  if (!w.me.there) return;
+  store_rows<DT, NB>(o, l > 0.0f ? 1.0f / l : 0.0f, row_of(a.out, w.me.t, w.me.head), a.d, h);
+  if (a.lse && h == 0)
+    a.lse[(int64_t)w.me.head * a.Tq + w.me.t] = l > 0.0f ? (m + sc.base + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
 }
 
 // a row's lse in powers of two, +inf (all weights 0) for a row that sees nothing or is not there
@@ -416,66 +488,60 @@ __device__ inline float lse2_of(float lse, bool there) { return !there || lse ==
 // ---------------------------------------------------------------------------------------------------------------
 // Queries' gradient, and delta = <dout, out> of every row for the kernel after it.  As the forward, with
 // dP^T = V dO^T beside S^T and dQ^T = K^T dS^T.
-template <int DT, int DP, int KIND, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_dq_kernel(SeqArgs a) {
-  constexpr int BK = 32, STEPS = DP / 16, NB = DP / 32, ROWS = 32 * WAVES, THREADS = 64 * WAVES;
+// The stored output is rounded where rows have 16 bits, and with few keys that rounding is what ds = p (dp - delta) is left with (a row
+// with one key has dp = delta).  A row whose keys all lie in the first 32 has them at hand, and takes delta = sum p dp instead.
+template <int DT, int DP, int KIND, int GROUPS, int PARTS>
+__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
+  constexpr int BK = 32 * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   typedef Tile<DT, DP> T;
-  __shared__ __attribute__((aligned(16))) char sk[2][BK * T::STRIDE];
-  __shared__ __attribute__((aligned(16))) char sv[2][BK * T::STRIDE];
-  const int hh = blockIdx.x % a.Hq, slot = a.slots - 1 - blockIdx.x / a.Hq;
-  const int G = a.Hq / a.Hk, hk = hh % a.Hk, head = hk * G + hh / a.Hk;
-  int seq, row0;
-  find_slot<ROWS>(a.q_off, a.B, a.per_seq, slot, seq, row0);
-  int64_t q0, k0;
-  const Span sp = span_of(a, seq, q0, k0);
-  if (row0 >= sp.nq) return;
-  const int lane = lane_id(), h = lane >> 5, w0 = row0 + wave_id() * 32, i = w0 + (lane & 31);
-  const bool there = i < sp.nq;
+  constexpr int TILE = BK * T::STRIDE, JOIN = PARTS == 2 ? GROUPS * NB * 16 * DLRM_WAVE * 4 : 0;
+  __shared__ __attribute__((aligned(16))) char lds[4 * TILE > JOIN ? 4 * TILE : JOIN];
+  RowWork<GROUPS, PARTS> w;
+  if (!w.find(a)) return;
+  const Span& sp = w.sp;
+  const int lane = lane_id(), h = lane >> 5;
   Op<DT> qf[STEPS], df[STEPS];
-  own_rows<DT, STEPS>(qf, row_of(a.q, q0 + i, head), there, a.d, h);
-  own_rows<DT, STEPS>(df, row_of(a.dout, q0 + i, head), there, a.d, h);
+  own_rows<DT, STEPS>(qf, row_of(a.q, w.me.t, w.me.head), w.me.there, a.d, h);
+  own_rows<DT, STEPS>(df, row_of(a.dout, w.me.t, w.me.head), w.me.there, a.d, h);
   float delta = 0.0f;
   {
     Op<DT> of[STEPS];
-    own_rows<DT, STEPS>(of, row_of(a.out, q0 + i, head), there, a.d, h);
+    own_rows<DT, STEPS>(of, row_of(a.out, w.me.t, w.me.head), w.me.there, a.d, h);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
       for (int j = 0; j < 8; ++j) delta += of[s].get(j) * df[s].get(j);
     delta += other_half(delta);
   }
-  const int64_t at = (int64_t)head * a.Tq + q0 + i;
-  if (there && h == 0) a.delta[at] = delta;
-  const float lse = there ? a.lse[at] : 0.0f;
-  const int vis = there ? sp.vis(i) : 0;
-  const int wave_vis = w0 < sp.nq ? sp.vis(min(w0 + 31, sp.nq - 1)) : 0, wave_full = w0 < sp.nq ? sp.vis(w0) : 0;
-  const int end = sp.vis(min(row0 + ROWS - 1, sp.nq - 1));
-  const Score<DT, KIND> sc(a, head);
-  const float place = (float)(i + sp.shift), rest = lse2_of(lse, there) - sc.base;
+  const int64_t at = (int64_t)w.me.head * a.Tq + w.me.t;
+  const float lse = w.me.there ? a.lse[at] : 0.0f;
+  const Score<DT, KIND> sc(a, w.me.head);
+  const float place = (float)(w.me.i + sp.shift), rest = lse2_of(lse, w.me.there) - sc.base;
 
   f32x16 g[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) g[b] = f32x16{};
-  const char* kb = row_of(a.k, k0, hk);
-  const char* vb = row_of(a.v, k0, hk);
-  const int tiles = (end + BK - 1) / BK;
+  const char* kb = row_of(a.k, w.k0, w.hk);
+  const char* vb = row_of(a.v, w.k0, w.hk);
+  const int tiles = (w.end + BK - 1) / BK;
   Staged<DT, DP, BK, THREADS> tk(a.k.st, a.d), tv(a.v.st, a.d);
   if (tiles > 0) {
     tk.load(kb, a.k.st, sp.nk, a.d);
     tv.load(vb, a.v.st, sp.nk, a.d);
-    tk.store(sk[0]);
-    tv.store(sv[0]);
+    tk.store(lds);
+    tv.store(lds + TILE);
   }
   __syncthreads();
   for (int t = 0; t < tiles; ++t) {
-    const int j0 = t * BK;
+    const int jt = t * BK;
     if (t + 1 < tiles) {
-      tk.load(kb + (int64_t)(j0 + BK) * a.k.st, a.k.st, sp.nk - j0 - BK, a.d);
-      tv.load(vb + (int64_t)(j0 + BK) * a.v.st, a.v.st, sp.nk - j0 - BK, a.d);
+      tk.load(kb + (int64_t)(jt + BK) * a.k.st, a.k.st, sp.nk - jt - BK, a.d);
+      tv.load(vb + (int64_t)(jt + BK) * a.v.st, a.v.st, sp.nk - jt - BK, a.d);
     }
-    if (j0 < wave_vis) {
-      const char* ks = sk[t & 1];
-      const char* vs = sv[t & 1];
+    const int j0 = jt + 32 * w.part;
+    if (j0 < w.wave_vis) {
+      const char* ks = lds + (t & 1) * 2 * TILE + 32 * w.part * T::STRIDE;
+      const char* vs = ks + TILE;
       f32x16 s = {}, dp = {};
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
@@ -483,16 +549,26 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_d
         dp = Op<DT>::mma(T::by_row(vs, lane & 31, st, h), df[st], dp);
       }
       const float away = place - (float)(j0 + 4 * h);
+      if (j0 == 0 && w.wave_full <= 32) {  // once a wavefront, and only the first of a sequence
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = __builtin_amdgcn_exp2f(sc.exponent(sc.y(s[r]), away - (float)acc_row(r, 0), rest));
+          sum += acc_row(r, h) < w.vis ? p * dp[r] : 0.0f;
+        }
+        sum += other_half(sum);
+        if (w.vis <= 32) delta = sum;
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float y = sc.y(s[r]);
         s[r] = __builtin_amdgcn_exp2f(sc.exponent(y, away - (float)acc_row(r, 0), rest)) * (dp[r] - delta);
         if constexpr ((KIND & kBend) != 0) s[r] *= sc.derivative(y);
       }
-      if (j0 + BK > wave_full) {
+      if (j0 + 32 > w.wave_full) {
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (j0 + acc_row(r, h) >= vis) s[r] = 0.0f;
+          if (j0 + acc_row(r, h) >= w.vis) s[r] = 0.0f;
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -504,12 +580,18 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void seq_attn_d
       }
     }
     if (t + 1 < tiles) {
-      tk.store(sk[(t + 1) & 1]);
-      tv.store(sv[(t + 1) & 1]);
+      tk.store(lds + ((t + 1) & 1) * 2 * TILE);
+      tv.store(lds + ((t + 1) & 1) * 2 * TILE + TILE);
     }
     __syncthreads();
   }
-  if (there) store_rows<DT, NB>(g, sc.grad, row_of(a.dq, q0 + i, head), a.d, h);
+  if constexpr (PARTS == 2) {
+    join_parts<NB, GROUPS>(g, lds, w.group, w.part, 1.0f, 1.0f);
+    if (w.part == 1) return;
+  }
+  if (!w.me.there) return;
+  if (h == 0) a.delta[at] = delta;
+  store_rows<DT, NB>(g, sc.grad, row_of(a.dq, w.me.t, w.me.head), a.d, h);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -541,7 +623,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;  // early keys are seen by most queries: first
   const int G = a.Hq / a.Hk;
   int seq, row0;
-  find_slot<W::KEYS>(a.k_off, a.B, a.per_seq, slot, seq, row0);
+  find_slot<W::KEYS>(a.k_off, 1, a.B, a.per_seq, slot, seq, row0);
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
   if (row0 >= sp.nk) return;
@@ -652,29 +734,10 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     if (n + 1 < all) put(n + 1);
     __syncthreads();
   }
-  // the second half's sums join the first's, one of the two gradients after the other
-  f32x4* join = reinterpret_cast<f32x4*>(lds) + group * NB * 4 * DLRM_WAVE + lane;
-#pragma unroll
-  for (int g = 0; g < (PARTS == 2 ? 2 : 0); ++g) {
-    f32x16* x = g ? gv : gk;
-    if (g) __syncthreads();
-    if (part == 1) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) join[(b * 4 + q) * DLRM_WAVE] = f32x4{x[b][4 * q], x[b][4 * q + 1], x[b][4 * q + 2], x[b][4 * q + 3]};
-    }
+  if constexpr (PARTS == 2) {  // one of the two gradients after the other
+    join_parts<NB, GROUPS>(gk, lds, group, part, 1.0f, 1.0f);
     __syncthreads();
-    if (part == 0) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 y = join[(b * 4 + q) * DLRM_WAVE];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[b][4 * q + e] += y[e];
-        }
-    }
+    join_parts<NB, GROUPS>(gv, lds, group, part, 1.0f, 1.0f);
   }
   if (part == 1 || !there) return;
   store_rows<DT, NB>(gk, Score<DT, KIND>(a, hk * G).grad, row_of(a.dk, k0 + j, hk), a.d, h);
@@ -682,10 +745,11 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// slots of `rows` rows for n rows in B sequences of at most `longest`
-__host__ inline bool slots_of(SeqArgs& a, int64_t n, int longest, int heads, int rows) {
-  const int64_t each = ((int64_t)longest + rows - 1) / rows;
-  const int64_t even = each * a.B, searched = n / rows + a.B;
+// slots of `rows` rows for n items in B sequences of at most `longest`, `per` rows an item
+__host__ inline bool slots_of(SeqArgs& a, int64_t n, int longest, int per, int heads, int rows) {
+  if ((int64_t)longest * per > 0x7fffffff - 1024) return false;
+  const int64_t each = ((int64_t)longest * per + rows - 1) / rows;
+  const int64_t even = each * a.B, searched = n * per / rows + a.B;
   // Block by block while at most two in three slots are empty: an empty workgroup ends in under a microsecond, while histories one after
   // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
   const bool block_by_block = even <= 3 * searched;
@@ -694,6 +758,9 @@ __host__ inline bool slots_of(SeqArgs& a, int64_t n, int longest, int heads, int
   a.slots = (int)s;
   return s * heads <= 0x7fffffff;
 }
+
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 // Calls f with the padded width and the kind of score as compile-time constants.
 template <typename F>
@@ -712,49 +779,58 @@ __host__ inline int for_kind(const SeqArgs& a, F f) {
   return by_kind(std::integral_constant<int, 128>{});
 }
 
-template <int DT, int WAVES>
-int launch_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  if (!slots_of(a, s->Tq, s->max_q, a.Hq, 32 * WAVES)) return DLRM_ERR_BAD_SHAPE;
-  if (a.slots == 0) return DLRM_OK;
-  return for_kind(a, [&](auto dp, auto kind) {
-    hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), WAVES>), dim3((unsigned)(a.slots * a.Hq)), dim3(64 * WAVES), 0, st, a);
-    DLRM_CHECK_LAUNCH();
-    return (int)DLRM_OK;
-  });
-}
-
-template <int DT, int WAVES>
-int launch_dq(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  if (!slots_of(a, s->Tq, s->max_q, a.Hq, 32 * WAVES)) return DLRM_ERR_BAD_SHAPE;
-  if (a.slots == 0) return DLRM_OK;
-  return for_kind(a, [&](auto dp, auto kind) {
-    hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), WAVES>), dim3((unsigned)(a.slots * a.Hq)), dim3(64 * WAVES), 0, st, a);
-    DLRM_CHECK_LAUNCH();
-    return (int)DLRM_OK;
-  });
-}
-
-template <int DT, int GROUPS, int PARTS>
-int launch_dkv(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  if (!slots_of(a, s->Tk, s->max_k, a.Hk, 32 * GROUPS)) return DLRM_ERR_BAD_SHAPE;
-  if (a.slots == 0) return DLRM_OK;
-  return for_kind(a, [&](auto dp, auto kind) {
-    hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), GROUPS, PARTS>), dim3((unsigned)(a.slots * a.Hk)), dim3(64 * GROUPS * PARTS), 0, st, a);
-    DLRM_CHECK_LAUNCH();
-    return (int)DLRM_OK;
-  });
-}
+// Two wavefronts to 32 rows where blocks of 128 rows would not give every CU two workgroups.
+__host__ inline bool few_rows(const dlrm_seq_batch* s, const SeqArgs& a) { return s->Tq * a.Hq < 512 * 128; }
 
 template <int DT>
 int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  return launch_fwd<DT, 4>(s, a, st);
+  return for_kind(a, [&](auto dp, auto kind) -> int {
+    auto go = [&](auto groups, auto parts) -> int {
+      if (!slots_of(a, s->Tq, s->max_q, a.Hq / a.Hk, a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      if (a.slots == 0) return DLRM_OK;
+      hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts()>), dim3((unsigned)(a.slots * a.Hk)),
+                         dim3(64 * groups() * parts()), 0, st, a);
+      DLRM_CHECK_LAUNCH();
+      return DLRM_OK;
+    };
+    if (few_rows(s, a)) return go(Int<2>{}, Int<2>{});
+    return go(Int<4>{}, Int<DT == DLRM_F32 ? 2 : 1>{});
+  });
 }
 
 template <int DT>
 int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  if (const int rc = launch_dq<DT, 4>(s, a, st)) return rc;
-  if (s->max_q <= 256) return launch_dkv<DT, 2, 1>(s, a, st);
-  return launch_dkv<DT, DT == DLRM_F32 ? 2 : 4, 2>(s, a, st);
+  return for_kind(a, [&](auto dp, auto kind) -> int {
+    constexpr bool F32 = DT == DLRM_F32;
+    auto dq = [&](auto groups, auto parts) -> int {
+      if (!slots_of(a, s->Tq, s->max_q, a.Hq / a.Hk, a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      if (a.slots == 0) return DLRM_OK;
+      hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), dim3((unsigned)(a.slots * a.Hk)),
+                         dim3(64 * groups() * parts()), 0, st, a);
+      DLRM_CHECK_LAUNCH();
+      return DLRM_OK;
+    };
+    auto dkv = [&](auto groups, auto parts) -> int {
+      if (!slots_of(a, s->Tk, s->max_k, 1, a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      if (a.slots == 0) return DLRM_OK;
+      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), dim3((unsigned)(a.slots * a.Hk)),
+                         dim3(64 * groups() * parts()), 0, st, a);
+      DLRM_CHECK_LAUNCH();
+      return DLRM_OK;
+    };
+    // fp32 rows of 128 columns need more registers than eight wavefronts of a CU have
+    constexpr bool WIDE_F32 = F32 && dp() > 96;
+    int rc;
+    if (WIDE_F32 || few_rows(s, a))
+      rc = dq(Int<2>{}, Int<2>{});
+    else if constexpr (!WIDE_F32)
+      rc = dq(Int<4>{}, Int<F32 ? 2 : 1>{});
+    if (rc != DLRM_OK) return rc;
+    // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
+    // of up to 200 items, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
+    if (s->max_q <= 256) return dkv(Int<(!F32 && dp() > 64) ? 4 : 2>{}, Int<1>{});
+    return dkv(Int<F32 ? 2 : 4>{}, Int<2>{});
+  });
 }
 
 extern template int launch_seq_fwd<DLRM_F32>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
