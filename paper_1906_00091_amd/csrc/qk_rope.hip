@@ -5,7 +5,9 @@
 // item's angles are reduced and their sines and cosines taken once, in registers, for all of its heads: the angle in turns is
 // position * frequency / 2 pi in fp64 (24 + 31 bits of product, exact; fp32 would be off by 1e-3 radians at position 2^14),
 // its fraction goes to sincospi in fp32.  In the half layout a column's partner lies rot/2 columns away: in another lane at the same
-// place of the chunk where rot/2 is a multiple of a chunk's columns (one exchange of the raw chunk), else anywhere (through LDS).
+// place of the chunk where rot/2 is a multiple of a chunk's columns (an exchange of the raw chunk), else anywhere (through LDS).
+// With p the partner of column j,  y_j = r (c_j w_j x_j + s_j w_p x_p):  the norm's weights go into the coefficients once an item, and
+// the exchange of the row as it was loaded does not wait for its norm.
 //
 // Bound by memory: every row is read and written once.
 #include <initializer_list>
@@ -72,50 +74,78 @@ __device__ inline void lane_angles(const RopeArgs& a, int64_t t, int col0, float
   }
 }
 
-// y = c x + s partner(x) for the E columns of this lane; xs: this wavefront's row buffer in LDS (kHalfAny)
+// The partners of this lane's E columns in a row as it was loaded; xs: this wavefront's buffer in LDS (kHalfAny).
 template <int DT, int MODE>
-__device__ inline void turn_row(const RopeLane<DT>& L, const float* x, float* y, int lane, int col0, int rot, float* xs) {
-  constexpr int E = RopeLane<DT>::E;
+__device__ inline void partners(u32x4 raw, const float* x, float* p, int lane, int col0, int rot, float* xs) {
+  constexpr int E = Tab<DT>::ELEMS;
+  const int n = rot >> 1;
   if constexpr (MODE == kPairs) {
 #pragma unroll
-    for (int j = 0; j < E; j += 2) {
-      y[j] = L.c[j] * x[j] + L.s[j] * x[j + 1];
-      y[j + 1] = L.c[j + 1] * x[j + 1] + L.s[j + 1] * x[j];
-    }
+    for (int j = 0; j < E; ++j) p[j] = x[j ^ 1];
+  } else if constexpr (MODE == kHalfChunks) {
+    const int step = n / E;  // lanes to the partner; a lane past the rotated columns takes its own
+    const int from = col0 < n ? lane + step : col0 < rot ? lane - step : lane;
+    u32x4 q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = (uint32_t)__shfl((int)raw[j], from, DLRM_WAVE);
+    Tab<DT>::widen(q, p);
   } else {
-    const int n = rot >> 1;
-    float p[E];
-    if constexpr (MODE == kHalfChunks) {
-      const int step = n / E;  // lanes to the partner; a lane past the rotated columns takes its own
-      const int from = col0 < n ? lane + step : col0 < rot ? lane - step : lane;
+    const float* row = xs + (lane * E - col0);  // of this lane's group
 #pragma unroll
-      for (int j = 0; j < E; ++j) p[j] = __shfl(x[j], from, DLRM_WAVE);
-    } else {
-      float* row = xs + (lane * E - col0);  // of this lane's group
+    for (int j = 0; j < E; ++j) xs[lane * E + j] = x[j];
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int j = 0; j < E; ++j) xs[lane * E + j] = x[j];
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const int c = col0 + j;
-        p[j] = row[c < n ? c + n : c < rot ? c - n : c];
-      }
-      __builtin_amdgcn_wave_barrier();
+    for (int j = 0; j < E; ++j) {
+      const int c = col0 + j;
+      p[j] = row[c < n ? c + n : c < rot ? c - n : c];
     }
-#pragma unroll
-    for (int j = 0; j < E; ++j) y[j] = L.c[j] * x[j] + L.s[j] * p[j];
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
+// The norm's weights of this lane's columns and of their partners (ones without a norm)
+template <int DT, int MODE>
+struct Weights {
+  static constexpr int E = Tab<DT>::ELEMS;
+  float own[E], other[E];
+  __device__ inline Weights(const float* w, int col0, int d, int rot) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) own[j] = other[j] = 1.0f;
+    if (w == nullptr) return;
+    const int n = rot >> 1, at = min(col0, d - E);
+#pragma unroll
+    for (int j = 0; j < E; j += 4) load_cols<4>(w + at + j, true, own + j);
+    if constexpr (MODE == kPairs) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) other[j] = own[j ^ 1];
+    } else if constexpr (MODE == kHalfChunks) {
+      const int from = at >= rot ? at : at < n ? at + n : at - n;
+#pragma unroll
+      for (int j = 0; j < E; j += 4) load_cols<4>(w + from + j, true, other + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) other[j] = w[at + j >= rot ? at + j : at + j < n ? at + j + n : at + j - n];
+    }
+  }
+};
+
+// Sum over a group of G lanes, in every lane: exchanges within 16 lanes go through the vector unit.
+template <int CTRL>
+__device__ inline float dpp(float v) {
+  return u2f((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f2u(v), CTRL, 0xf, 0xf, true));
+}
 template <int G>
 __device__ inline float group_sum(float v) {
-#pragma unroll
-  for (int o = G >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, DLRM_WAVE);
+  if constexpr (G >= 2) v += dpp<0xB1>(v);    // lanes 1 0 3 2 of four
+  if constexpr (G >= 4) v += dpp<0x4E>(v);    // lanes 2 3 0 1 of four
+  if constexpr (G >= 8) v += dpp<0x141>(v);   // 8 lanes mirrored
+  if constexpr (G >= 16) v += dpp<0x140>(v);  // 16 lanes mirrored
+  if constexpr (G >= 32) v += __shfl_xor(v, 16, DLRM_WAVE);
   return v;
 }
 
-// Forward.  Groups of G lanes; group g of the grid takes item g / splits and the heads g % splits, + splits, ...
+// Forward.  Groups of G lanes; group g of the grid takes item g / splits, and of its queries, keys and values every splits-th head.
 template <int DT, int MODE, int G, bool CACHE>
 __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
   constexpr int E = Tab<DT>::ELEMS;
@@ -123,78 +153,74 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
   float* xs = xs_all + (MODE == kHalfAny ? wave_id() * DLRM_WAVE * E : 0);
   const int lane = lane_id(), col0 = (lane & (G - 1)) * E;
   const int64_t group = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
-  const int64_t t = group / a.splits;
-  const int first = (int)(group - t * a.splits);
+  const int64_t t = a.splits == 1 ? group : group / a.splits;
+  // the group's first query, key and value: where every group has one row at most, no two of them meet
+  const int fq = (int)(group - t * a.splits), fk = a.splits - 1 - fq, fv = fk >= a.Hk ? fk - a.Hk : fk - a.Hk + a.splits;
   // lanes of the last group past the row, and groups past the last item, go along with nothing (exchanges need every lane)
   const bool in = t < a.T && col0 < a.d;
   const int64_t tt = t < a.T ? t : a.T - 1;
-  RopeLane<DT> L;
-  lane_angles<DT, MODE>(a, tt, col0, 1.0f, L);
-  float wq[E], wk[E];
-#pragma unroll
-  for (int j = 0; j < E; ++j) wq[j] = wk[j] = 1.0f;
-  if (col0 < a.d) {
-#pragma unroll
-    for (int j = 0; j < E; j += 4) {
-      if (a.wq) load_cols<4>(a.wq + col0 + j, true, wq + j);
-      if (a.wk) load_cols<4>(a.wk + col0 + j, true, wk + j);
-    }
-  }
-  const float inv_d = 1.0f / (float)a.d;
-  char* slot_k = nullptr;
-  char* slot_v = nullptr;
-  int64_t head_bytes = 0;
-  if constexpr (CACHE) {
-    const int64_t row = (int64_t)a.d * Tab<DT>::EB;
-    const int s = a.seqs[tt], p = a.pos[tt], c = p >> a.page_shift;
-    head_bytes = row << a.page_shift;
-    if (s >= 0 && s < a.cB && p >= 0 && c < a.cols) {
-      const int page = a.table[(int64_t)s * a.cols + c];
-      if (page >= 0 && page < a.n_pages) {
-        const int64_t at = (int64_t)page * a.Hk * head_bytes + (p & ((1 << a.page_shift) - 1)) * row;
-        slot_k = a.ck + at;
-        slot_v = a.cv + at;
-      }
-    }
-  }
-  const int H = a.Hq + a.Hk + (CACHE ? a.Hk : 0);
   const int cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
   // (loads stand in no branch, so that the next row's is in flight while this one is worked on: a lane past the row or a head past the last
   // loads what is there, and it is not used)
-  auto src = [&](int h) {
-    h = min(h, H - 1);
-    const char* p = h < a.Hq ? row_of(a.q, tt, h) : h < a.Hq + a.Hk ? row_of(a.k, tt, h - a.Hq) : row_of(a.v, tt, h - a.Hq - a.Hk);
-    return load16(p + lb);
+  auto load = [&](const Rows& rows, int h, int H) { return load16(row_of(rows, tt, min(h, H - 1)) + lb); };
+  u32x4 row_q = load(a.q, fq, a.Hq), row_k = {0, 0, 0, 0};
+  if (a.Hk > 0) row_k = load(a.k, fk, a.Hk);
+  // the item's page, looked up beside the rows (clamped: whether it is there is asked where it is used)
+  int seq = 0, col = 0, page = 0;
+  if constexpr (CACHE) {
+    seq = a.seqs[tt];
+    col = a.pos[tt] >> a.page_shift;
+    page = a.table[(int64_t)min(max(seq, 0), a.cB - 1) * a.cols + min(max(col, 0), a.cols - 1)];
+  }
+  RopeLane<DT> L;
+  lane_angles<DT, MODE>(a, tt, col0, 1.0f, L);
+  const float inv_d = 1.0f / (float)a.d;
+
+  auto turn = [&](const Rows& rows, int first, int H, u32x4 next, const float* weights, auto to) {
+    const Weights<DT, MODE> w(weights, col0, a.d, a.rot);
+    float c[E], s[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      c[j] = L.c[j] * w.own[j];
+      s[j] = L.s[j] * w.other[j];
+    }
+    for (int h = first; h < H; h += a.splits) {
+      u32x4 raw = next;
+      next = load(rows, h + a.splits, H);
+      if (col0 >= a.d) raw = u32x4{0, 0, 0, 0};
+      float x[E], p[E], y[E];
+      Tab<DT>::widen(raw, x);
+      partners<DT, MODE>(raw, x, p, lane, col0, a.rot, xs);
+      float r = 1.0f;
+      if (weights != nullptr) {
+        float ss = 0.0f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) ss += x[j] * x[j];
+        r = 1.0f / sqrtf(group_sum<G>(ss) * inv_d + a.eps);
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) y[j] = r * fmaf(c[j], x[j], s[j] * p[j]);
+      char* dst = to(h);
+      if (in && dst) store16(dst + cb, narrow<DT>(y));
+    }
   };
-  u32x4 next = src(first);
-  for (int h = first; h < H; h += a.splits) {
-    u32x4 raw = next;
-    next = src(h + a.splits);
-    if (col0 >= a.d) raw = u32x4{0, 0, 0, 0};
-    const bool is_q = h < a.Hq;
-    if (CACHE && h >= a.Hq + a.Hk) {
-      if (in && slot_v) store16(slot_v + (h - a.Hq - a.Hk) * head_bytes + cb, raw);
-      continue;
-    }
-    float x[E], y[E];
-    Tab<DT>::widen(raw, x);
-    if ((is_q ? a.wq : a.wk) != nullptr) {
-      float ss = 0.0f;
+  turn(a.q, fq, a.Hq, row_q, a.wq, [&](int h) { return row_of(a.qo, tt, h); });
+  if constexpr (!CACHE) {
+    turn(a.k, fk, a.Hk, row_k, a.wk, [&](int h) { return row_of(a.ko, tt, h); });
+  } else {
+    const int64_t row = (int64_t)a.d * Tab<DT>::EB, head_bytes = row << a.page_shift;
+    const bool there = seq >= 0 && seq < a.cB && col >= 0 && col < a.cols && page >= 0 && page < a.n_pages;
+    const int64_t at = there ? (int64_t)page * a.Hk * head_bytes + (a.pos[tt] & ((1 << a.page_shift) - 1)) * row : -1;
+    turn(a.k, fk, a.Hk, row_k, a.wk, [&](int h) { return at < 0 ? nullptr : a.ck + at + h * head_bytes; });
+    for (int h0 = fv; h0 < a.Hk; h0 += 4 * a.splits) {
+      u32x4 v[4];
 #pragma unroll
-      for (int j = 0; j < E; ++j) ss += x[j] * x[j];
-      const float r = 1.0f / sqrtf(group_sum<G>(ss) * inv_d + a.eps);
+      for (int i = 0; i < 4; ++i) v[i] = load(a.v, h0 + i * a.splits, a.Hk);
 #pragma unroll
-      for (int j = 0; j < E; ++j) x[j] = x[j] * r * (is_q ? wq[j] : wk[j]);
-    }
-    turn_row<DT, MODE>(L, x, y, lane, col0, a.rot, xs);
-    if (!in) continue;
-    const u32x4 out = narrow<DT>(y);
-    if (is_q)
-      store16(row_of(a.qo, tt, h) + cb, out);
-    else if (CACHE) {
-      if (slot_k) store16(slot_k + (h - a.Hq) * head_bytes + cb, out);
-    } else {
-      store16(row_of(a.ko, tt, h - a.Hq) + cb, out);
+      for (int i = 0; i < 4; ++i) {
+        const int h = h0 + i * a.splits;
+        if (in && at >= 0 && h < a.Hk) store16(a.cv + at + h * head_bytes + cb, v[i]);
+      }
     }
   }
 }
@@ -225,55 +251,55 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
       if (a.wk) load_cols<4>(a.wk + col0 + j, true, wk + j);
     }
   }
-  const int H = a.Hq + a.Hk, cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
+  const int cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
   const int64_t rounds = (a.T + groups - 1) / groups;  // the same for every lane of the workgroup
   for (int64_t i = 0; i < rounds; ++i) {
     const int64_t t = g0 + i * groups;
     const bool in = t < a.T && col0 < a.d;
     const int64_t tt = t < a.T ? t : a.T - 1;
+    auto load = [&](const Rows& rows, int h, int H) { return load16(row_of(rows, tt, min(h, H - 1)) + lb); };
+    u32x4 xq = load(a.q, 0, a.Hq), dq = load(a.dqo, 0, a.Hq), xk = {0, 0, 0, 0}, dk = {0, 0, 0, 0};
+    if (a.Hk > 0) {
+      xk = load(a.k, 0, a.Hk);
+      dk = load(a.dko, 0, a.Hk);
+    }
     RopeLane<DT> L;
     lane_angles<DT, MODE>(a, tt, col0, -1.0f, L);
-    auto src = [&](int h) { return load16((h < a.Hq ? row_of(a.q, tt, h) : row_of(a.k, tt, h - a.Hq)) + lb); };
-    auto dsrc = [&](int h) { return load16((h < a.Hq ? row_of(a.dqo, tt, h) : row_of(a.dko, tt, h - a.Hq)) + lb); };
-    u32x4 nx = src(0), nd = dsrc(0);
-    for (int h = 0; h < H; ++h) {
-      u32x4 rx = nx, rd = nd;
-      nx = src(min(h + 1, H - 1));
-      nd = dsrc(min(h + 1, H - 1));
-      if (col0 >= a.d) rx = rd = u32x4{0, 0, 0, 0};
-      const bool is_q = h < a.Hq;
-      float x[E], dy[E], g[E];
-      Tab<DT>::widen(rx, x);
-      Tab<DT>::widen(rd, dy);
-      turn_row<DT, MODE>(L, dy, g, lane, col0, a.rot, xs);
-      if ((is_q ? a.wq : a.wk) != nullptr) {
-        float ss = 0.0f, sg = 0.0f;
-        float gw[E];
+    auto turn = [&](const Rows& rows, const Rows& drows, const Rows& to, int H, u32x4 nx, u32x4 nd, const float* wp, const float* w, float* sum) {
+      for (int h = 0; h < H; ++h) {
+        u32x4 rx = nx, rd = nd;
+        nx = load(rows, h + 1, H);
+        nd = load(drows, h + 1, H);
+        if (col0 >= a.d) rx = rd = u32x4{0, 0, 0, 0};
+        float x[E], dy[E], g[E];
+        Tab<DT>::widen(rx, x);
+        Tab<DT>::widen(rd, dy);
+        partners<DT, MODE>(rd, dy, g, lane, col0, a.rot, xs);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          gw[j] = g[j] * (is_q ? wq[j] : wk[j]);
-          ss += x[j] * x[j];
-          sg += gw[j] * x[j];
-        }
+        for (int j = 0; j < E; ++j) g[j] = fmaf(L.c[j], dy[j], L.s[j] * g[j]);
+        if (wp != nullptr) {
+          float ss = 0.0f, sg = 0.0f, gw[E];
 #pragma unroll
-        for (int o = G >> 1; o > 0; o >>= 1) {
-          ss += __shfl_xor(ss, o, DLRM_WAVE);
-          sg += __shfl_xor(sg, o, DLRM_WAVE);
-        }
-        const float r = 1.0f / sqrtf(ss * inv_d + a.eps);
-        const float m = sg * r * r * inv_d;  // mean(g w n) r
+          for (int j = 0; j < E; ++j) {
+            gw[j] = g[j] * w[j];
+            ss += x[j] * x[j];
+            sg += gw[j] * x[j];
+          }
+          ss = group_sum<G>(ss);
+          sg = group_sum<G>(sg);
+          const float r = 1.0f / sqrtf(ss * inv_d + a.eps);
+          const float m = sg * r * r * inv_d;  // mean(g w n) r
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const float dw = in ? g[j] * (x[j] * r) : 0.0f;
-          if (is_q)
-            sq[j] += dw;
-          else
-            sk[j] += dw;
-          g[j] = r * (gw[j] - x[j] * m);
+          for (int j = 0; j < E; ++j) {
+            sum[j] += in ? g[j] * (x[j] * r) : 0.0f;
+            g[j] = r * (gw[j] - x[j] * m);
+          }
         }
+        if (in) store16(row_of(to, tt, h) + cb, narrow<DT>(g));
       }
-      if (in) store16((is_q ? row_of(a.dq, tt, h) : row_of(a.dk, tt, h - a.Hq)) + cb, narrow<DT>(g));
-    }
+    };
+    turn(a.q, a.dqo, a.dq, a.Hq, xq, dq, a.wq, wq, sq);
+    turn(a.k, a.dko, a.dk, a.Hk, xk, dk, a.wk, wk, sk);
   }
   if (a.part == nullptr) return;
 #pragma unroll

@@ -165,25 +165,29 @@ struct SeqArgs {
   float* delta;  // [Hq, Tq]
   int64_t Tq;
   int B, Hq, Hk, d, causal;
-  int slots;
-  int per_seq;     // slots of a sequence where all have the same number, else 0
+  int by_block;  // the grid is (key head, sequence, block), else key heads times slots
   float scale, cap;
 };
 
-// Slot -> sequence and first row, slots of ROWS rows, `per` rows for each item of `off`.  A sequence with n rows needs
-// ceil(n / ROWS) of them, and how many rows it has stands in device memory.  Where all sequences fit into few slots each gets as many as the
-// longest may need, and the slots go block by block through all sequences: with causal sequences the blocks of most work of every one
-// of them start first.  Else sequence s starts at slot off[s] * per / ROWS + s, which leaves it enough; slots past its rows end at
-// once.  The sequence is found by all 64 lanes at once: each step asks 64 places.
+// Workgroup -> key head, sequence and first row, blocks of ROWS rows, `per` rows for each item of `off`.  A sequence with n rows needs
+// ceil(n / ROWS) blocks, and how many rows it has stands in device memory.
+// Where all sequences fit into few blocks the grid is (key head, sequence, block), as many blocks as the longest may need: block by block
+// through all sequences, so with causal sequences the blocks of most work of every one of them start first.  Else it is key heads times
+// slots: sequence s starts at slot off[s] * per / ROWS + s, which leaves it enough, and is found by all 64 lanes at once, each step
+// asking 64 places.  Workgroups past a sequence's rows end at once.
 template <int ROWS>
-__device__ inline void find_slot(const int64_t* off, int per, int B, int per_seq, int slot, int& seq, int& row0) {
-  if (per_seq > 0) {
-    const int block = slot / B;
-    seq = (slot - block * B + block) % B;  // turned from block to block: workgroups go to the 8 dies in turn, and no die gets the same sequences' all
-    row0 = block * ROWS;
+__device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per, bool last_first, int& hk, int& seq, int& row0) {
+  if (a.by_block) {
+    hk = blockIdx.x;
+    // turned from block to block: workgroups go to the 8 dies in turn, and no die gets all of the same sequences
+    seq = blockIdx.y + blockIdx.z;
+    if (seq >= a.B) seq %= a.B;
+    row0 = (last_first ? gridDim.z - 1 - blockIdx.z : blockIdx.z) * ROWS;
     return;
   }
-  int lo = 0, hi = B;
+  const int at = blockIdx.x / a.Hk, slot = last_first ? gridDim.x / a.Hk - 1 - at : at;
+  hk = blockIdx.x - at * a.Hk;
+  int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) >> 6, s = lo + lane_id() * step;
     const bool before = s < hi && off[s] * per / ROWS + s <= slot;
@@ -311,8 +315,7 @@ struct RowWork {
   __device__ inline bool find(const SeqArgs& a) {
     constexpr int ROWS = 32 * GROUPS;
     G = a.Hq / a.Hk;
-    hk = blockIdx.x % a.Hk;
-    find_slot<ROWS>(a.q_off, G, a.B, a.per_seq, a.slots - 1 - blockIdx.x / a.Hk, seq, row0);  // late rows see most keys: first
+    find_block<ROWS>(a, a.q_off, G, true, hk, seq, row0);  // late rows see most keys
     sp = span_of(a, seq, q0, k0);
     const int rows = sp.nq * G;
     if (row0 >= rows) return false;
@@ -320,13 +323,14 @@ struct RowWork {
     part = wave_id() / GROUPS;
     const int w0 = row0 + group * 32, r = w0 + (lane_id() & 31);
     me.there = r < rows;
-    me.i = me.there ? r / G : 0;
+    auto item = [&](int row) { return G == 1 ? row : row / G; };
+    me.i = me.there ? item(r) : 0;
     me.head = hk * G + (me.there ? r - me.i * G : 0);
     me.t = q0 + me.i;
     vis = me.there ? sp.vis(me.i) : 0;
-    wave_vis = w0 < rows ? sp.vis(min(w0 + 31, rows - 1) / G) : 0;
-    wave_full = w0 < rows ? sp.vis(w0 / G) : 0;
-    end = sp.vis(min(row0 + ROWS - 1, rows - 1) / G);
+    wave_vis = w0 < rows ? sp.vis(item(min(w0 + 31, rows - 1))) : 0;
+    wave_full = w0 < rows ? sp.vis(item(w0)) : 0;
+    end = sp.vis(item(min(row0 + ROWS - 1, rows - 1)));
     return true;
   }
 };
@@ -354,10 +358,10 @@ __device__ inline void join_parts(f32x16* x, char* lds, int group, int part, flo
   }
 }
 
-// Forward: tiles of 64 keys and values go by, two of them in LDS.
-template <int DT, int DP, int KIND, int GROUPS, int PARTS>
-__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_attn_fwd_kernel(SeqArgs a) {
-  constexpr int SUB = 2 / PARTS, BK = 32 * SUB * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
+// Forward: tiles of keys and values go by, SUB x 32 keys for each part, two tiles in LDS.
+template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
+__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? (SUB * PARTS == 1 ? 4 : 2) : 1) void seq_attn_fwd_kernel(SeqArgs a) {
+  constexpr int BK = 32 * SUB * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   typedef Tile<DT, DP> T;
   constexpr int TILE = BK * T::STRIDE, JOIN = PARTS == 2 ? GROUPS * NB * 16 * DLRM_WAVE * 4 : 0;
   __shared__ __attribute__((aligned(16))) char lds[4 * TILE > JOIN ? 4 * TILE : JOIN];
@@ -620,10 +624,9 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   typedef typename W::T T;
   constexpr int BQ = W::BQ, STEPS = W::STEPS, NB = W::NB;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
-  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;  // early keys are seen by most queries: first
   const int G = a.Hq / a.Hk;
-  int seq, row0;
-  find_slot<W::KEYS>(a.k_off, 1, a.B, a.per_seq, slot, seq, row0);
+  int hk, seq, row0;
+  find_block<W::KEYS>(a, a.k_off, 1, false, hk, seq, row0);  // early keys are seen by most queries
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
   if (row0 >= sp.nk) return;
@@ -745,18 +748,15 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// slots of `rows` rows for n items in B sequences of at most `longest`, `per` rows an item
-__host__ inline bool slots_of(SeqArgs& a, int64_t n, int longest, int per, int heads, int rows) {
+// Grid for n items in B sequences of at most `longest`, `per` rows an item, blocks of `rows` rows (see find_block); false: too large
+__host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, int per, int rows) {
   if ((int64_t)longest * per > 0x7fffffff - 1024) return false;
-  const int64_t each = ((int64_t)longest * per + rows - 1) / rows;
-  const int64_t even = each * a.B, searched = n * per / rows + a.B;
-  // Block by block while at most two in three slots are empty: an empty workgroup ends in under a microsecond, while histories one after
+  const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B;
+  // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
   // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
-  const bool block_by_block = even <= 3 * searched;
-  a.per_seq = block_by_block ? (int)each : 0;
-  const int64_t s = block_by_block ? even : searched;
-  a.slots = (int)s;
-  return s * heads <= 0x7fffffff;
+  a.by_block = each * a.B <= 3 * slots && a.B <= 65535 && each <= 65535;
+  grid = a.by_block ? dim3(a.Hk, a.B, (unsigned)each) : dim3((unsigned)(slots * a.Hk), 1, 1);
+  return (a.by_block ? each * a.B : slots) * a.Hk < (int64_t)1 << 23;  // fewer than 2^32 threads
 }
 
 template <int N>
@@ -785,16 +785,26 @@ __host__ inline bool few_rows(const dlrm_seq_batch* s, const SeqArgs& a) { retur
 template <int DT>
 int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
   return for_kind(a, [&](auto dp, auto kind) -> int {
-    auto go = [&](auto groups, auto parts) -> int {
-      if (!slots_of(a, s->Tq, s->max_q, a.Hq / a.Hk, a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
-      if (a.slots == 0) return DLRM_OK;
-      hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts()>), dim3((unsigned)(a.slots * a.Hk)),
+    auto go = [&](auto groups, auto parts, auto sub) -> int {
+      dim3 grid;
+      if (s->Tq == 0) return DLRM_OK;
+      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid,
                          dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     };
-    if (few_rows(s, a)) return go(Int<2>{}, Int<2>{});
-    return go(Int<4>{}, Int<DT == DLRM_F32 ? 2 : 1>{});
+    if (few_rows(s, a)) return go(Int<2>{}, Int<2>{}, Int<1>{});
+    if constexpr (DT == DLRM_F32) {
+      return go(Int<4>{}, Int<2>{}, Int<1>{});
+    } else {
+      // Short histories of narrow rows: tiles of 32 keys leave registers for four workgroups a CU.  (2048 histories of up to 200 items, d 64:
+      // 131 us, 143 with 64 keys; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
+      if constexpr (dp() <= 64) {
+        if (s->max_k <= 256) return go(Int<4>{}, Int<1>{}, Int<1>{});
+      }
+      return go(Int<4>{}, Int<1>{}, Int<2>{});
+    }
   });
 }
 
@@ -803,17 +813,19 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
   return for_kind(a, [&](auto dp, auto kind) -> int {
     constexpr bool F32 = DT == DLRM_F32;
     auto dq = [&](auto groups, auto parts) -> int {
-      if (!slots_of(a, s->Tq, s->max_q, a.Hq / a.Hk, a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
-      if (a.slots == 0) return DLRM_OK;
-      hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), dim3((unsigned)(a.slots * a.Hk)),
+      dim3 grid;
+      if (s->Tq == 0) return DLRM_OK;
+      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), grid,
                          dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     };
     auto dkv = [&](auto groups, auto parts) -> int {
-      if (!slots_of(a, s->Tk, s->max_k, 1, a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
-      if (a.slots == 0) return DLRM_OK;
-      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), dim3((unsigned)(a.slots * a.Hk)),
+      dim3 grid;
+      if (s->Tk == 0) return DLRM_OK;
+      if (!blocks_of(a, grid, s->Tk, s->max_k, 1, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid,
                          dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
