@@ -21,7 +21,8 @@ struct RopeArgs {
   Rows q, k, v, qo, ko;   // forward
   Rows dqo, dko, dq, dk;  // backward
   int64_t T;
-  int Hq, Hk, d, rot, splits;
+  int Hq, Hk, d, rot;
+  int splits, shift_v;  // groups of an item; Hk modulo splits
   const int32_t* pos;
   const float* inv_freq;
   const float* wq;
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
   const int64_t group = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
   const int64_t t = a.splits == 1 ? group : group / a.splits;
   // the group's first query, key and value: where every group has one row at most, no two of them meet
-  const int fq = (int)(group - t * a.splits), fk = a.splits - 1 - fq, fv = fk >= a.Hk ? fk - a.Hk : fk - a.Hk + a.splits;
+  const int fq = (int)(group - t * a.splits), fk = a.splits - 1 - fq, fv = fk >= a.shift_v ? fk - a.shift_v : fk - a.shift_v + a.splits;
   // lanes of the last group past the row, and groups past the last item, go along with nothing (exchanges need every lane)
   const bool in = t < a.T && col0 < a.d;
   const int64_t tt = t < a.T ? t : a.T - 1;
@@ -439,6 +440,7 @@ template <bool CACHE>
 static int launch_fwd(const dlrm_qk_rope* r, RopeArgs a, hipStream_t st) {
   if (r->T == 0) return DLRM_OK;
   a.splits = head_splits(r, r->Hq + r->Hk * (CACHE ? 2 : 1));
+  a.shift_v = r->Hk % a.splits;
   const int64_t blocks = (r->T * a.splits * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
   if (blocks > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;
   return for_row_kind(r->dtype, partner_mode(r), group_lanes(r), [&](auto dt, auto md, auto g) {

@@ -27,6 +27,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kInf = __builtin_inff();
 
@@ -492,14 +495,20 @@ __device__ inline float lse2_of(float lse, bool there) { return !there || lse ==
 // ---------------------------------------------------------------------------------------------------------------
 // Queries' gradient, and delta = <dout, out> of every row for the kernel after it.  As the forward, with
 // dP^T = V dO^T beside S^T and dQ^T = K^T dS^T.
-// The stored output is rounded where rows have 16 bits, and with few keys that rounding is what ds = p (dp - delta) is left with (a row
-// with one key has dp = delta).  A row whose keys all lie in the first 32 has them at hand, and takes delta = sum p dp instead.
+// The stored output is rounded where rows have 16 bits, and where few keys carry a row's weight that rounding shows in
+// ds = p (dp - delta) (a row with one key has dp = delta).  So delta is summed again on the way as sum p dp, in fp32: the kernel after this
+// one takes that; a row whose keys all lie in the first 32 has it before its first use here; and for the other rows what the rounding
+// of the output leaves is made up for by taking ds in two 16-bit parts, with a second product, where that costs little or is most needed: narrow
+// rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  2048 histories of up to 200 items in bf16, slopes: dq
+// 2.5e-3 off in one part, 2.0e-3 in two, 1.7e-3 being the rounding of dq itself.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
   constexpr int BK = 32 * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
+  constexpr bool TWO = DT != DLRM_F32 && (DP <= 64 || (KIND & kSlopes) != 0);  // ds in two parts
   typedef Tile<DT, DP> T;
   constexpr int TILE = BK * T::STRIDE, JOIN = PARTS == 2 ? GROUPS * NB * 16 * DLRM_WAVE * 4 : 0;
   __shared__ __attribute__((aligned(16))) char lds[4 * TILE > JOIN ? 4 * TILE : JOIN];
+  __shared__ float sums[PARTS == 2 ? GROUPS * 32 : 1];
   RowWork<GROUPS, PARTS> w;
   if (!w.find(a)) return;
   const Span& sp = w.sp;
@@ -525,6 +534,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_
   f32x16 g[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) g[b] = f32x16{};
+  float sum = 0.0f;  // of p dp
   const char* kb = row_of(a.k, w.k0, w.hk);
   const char* vb = row_of(a.v, w.k0, w.hk);
   const int tiles = (w.end + BK - 1) / BK;
@@ -554,33 +564,44 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_
       }
       const float away = place - (float)(j0 + 4 * h);
       if (j0 == 0 && w.wave_full <= 32) {  // once a wavefront, and only the first of a sequence
-        float sum = 0.0f;
+        float all = 0.0f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float p = __builtin_amdgcn_exp2f(sc.exponent(sc.y(s[r]), away - (float)acc_row(r, 0), rest));
-          sum += acc_row(r, h) < w.vis ? p * dp[r] : 0.0f;
+          all += acc_row(r, h) < w.vis ? p * dp[r] : 0.0f;
         }
-        sum += other_half(sum);
-        if (w.vis <= 32) delta = sum;
+        all += other_half(all);
+        if (w.vis <= 32) delta = all;
       }
+      auto gradient = [&](auto masked) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float y = sc.y(s[r]);
-        s[r] = __builtin_amdgcn_exp2f(sc.exponent(y, away - (float)acc_row(r, 0), rest)) * (dp[r] - delta);
-        if constexpr ((KIND & kBend) != 0) s[r] *= sc.derivative(y);
-      }
-      if (j0 + 32 > w.wave_full) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (j0 + acc_row(r, h) >= w.vis) s[r] = 0.0f;
-      }
+        for (int r = 0; r < 16; ++r) {
+          const float y = sc.y(s[r]);
+          float p = __builtin_amdgcn_exp2f(sc.exponent(y, away - (float)acc_row(r, 0), rest)), x = dp[r];
+          if (masked() && j0 + acc_row(r, h) >= w.vis) p = x = 0.0f;
+          sum = fmaf(p, x, sum);
+          s[r] = p * (x - delta);
+          if constexpr ((KIND & kBend) != 0) s[r] *= sc.derivative(y);
+        }
+      };
+      if (j0 + 32 > w.wave_full)
+        gradient(Int<1>{});
+      else
+        gradient(Int<0>{});
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        Op<DT> ds;
+        Op<DT> ds, low;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) ds.set(r, s[8 * c + r]);
+        for (int r = 0; r < 8; ++r) {
+          ds.set(r, s[8 * c + r]);
+          if constexpr (TWO) low.set(r, s[8 * c + r] - ds.get(r));
+        }
 #pragma unroll
-        for (int b = 0; b < NB; ++b) g[b] = Op<DT>::mma(T::by_column(ks, 16 * c, b, lane), ds, g[b]);
+        for (int b = 0; b < NB; ++b) {
+          const Op<DT> kt = T::by_column(ks, 16 * c, b, lane);
+          g[b] = Op<DT>::mma(kt, ds, g[b]);
+          if constexpr (TWO) g[b] = Op<DT>::mma(kt, low, g[b]);
+        }
       }
     }
     if (t + 1 < tiles) {
@@ -589,12 +610,15 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_
     }
     __syncthreads();
   }
+  sum += other_half(sum);
   if constexpr (PARTS == 2) {
+    if (w.part == 1 && h == 0) sums[w.group * 32 + lane] = sum;
     join_parts<NB, GROUPS>(g, lds, w.group, w.part, 1.0f, 1.0f);
     if (w.part == 1) return;
+    sum += sums[w.group * 32 + (lane & 31)];
   }
   if (!w.me.there) return;
-  if (h == 0) a.delta[at] = delta;
+  if (h == 0) a.delta[at] = sum;
   store_rows<DT, NB>(g, sc.grad, row_of(a.dq, w.me.t, w.me.head), a.d, h);
 }
 
@@ -758,9 +782,6 @@ __host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, i
   grid = a.by_block ? dim3(a.Hk, a.B, (unsigned)each) : dim3((unsigned)(slots * a.Hk), 1, 1);
   return (a.by_block ? each * a.B : slots) * a.Hk < (int64_t)1 << 23;  // fewer than 2^32 threads
 }
-
-template <int N>
-using Int = std::integral_constant<int, N>;
 
 // Calls f with the padded width and the kind of score as compile-time constants.
 template <typename F>

@@ -171,6 +171,30 @@ def test_append_stores_what_the_forward_gives_and_nothing_else(dtype, page, Hk, 
     assert torch.equal(pool.cpu(), want)
 
 
+@pytest.mark.parametrize("T,Hq,Hk", [(1, 3, 5), (3000, 2, 7), (9000, 4, 5), (40000, 8, 8)])
+def test_append_of_any_number_of_items(T, Hq, Hk):
+    """From every head of an item on its own to all heads of an item in one walk (fp32, d 16: four lanes a row)."""
+    g, d, page = gen(T), 16, 8
+    q, k, v = (rand(g, T, H, d).to(DEV) for H in (Hq, Hk, Hk))
+    n = (T + page - 1) // page
+    table = torch.randperm(n, generator=g).view(1, n).to(torch.int32)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    plan = hot.QkRope(pos, Hq, Hk, d, inv_freq=hot.rope_frequencies(d, device=DEV))
+    qo, ko, qa = torch.empty_like(q), torch.empty_like(k), torch.empty_like(q)
+    hot.dlrm_qk_rope_fwd(plan, q, k, qo, ko)
+    how = (pos.cpu(), hot.rope_frequencies(d), d, "half", 1e-6, 1.0)
+    for a, b in ((q, qo), (k, ko)):
+        y = ref.rope(a.cpu(), None, *how)
+        ref.close(b, y, rope_bound(torch.float32, a.cpu(), None, y, 1.0, d), "rows")
+    pool = torch.full((2, n, Hk, page, d), 7.0, device=DEV)
+    hot.dlrm_qk_rope_append(plan, q, k, v, qa, hot.KvCache(pool[0], pool[1], table.to(DEV)), torch.zeros(T, dtype=torch.int32, device=DEV))
+    assert torch.equal(qa, qo)
+    at = table[0].to(DEV).long()
+    for x, y in ((ko, pool[0]), (v, pool[1])):
+        rows = y[at].transpose(1, 2).reshape(n * page, Hk, d)
+        assert torch.equal(rows[:T], x) and (rows[T:] == 7.0).all()
+
+
 def test_items_past_the_table_are_not_stored():
     pool = torch.zeros(2, 4, 1, 8, 16, device=DEV)
     x = torch.ones(2, 1, 16, device=DEV)
@@ -242,6 +266,47 @@ def test_sequence_attention_forward_and_backward(i, bound):
     hot.dlrm_seq_attn_bwd(seq, Q, K, V, out, lse, DO, *again[1:], ws)
     for a, b in zip(again, (out, dq, dk, dv)):
         assert torch.equal(a, b)
+
+
+MANY = [
+    # dtype, d, Hq, Hk, sequences, lengths up to, keys up to (None: the same items), causal, prefix, slopes, cap
+    ("bf16", 64, 4, 4, 700, 60, None, True, False, True, 0.0),
+    ("f16", 40, 8, 2, 500, 40, 700, False, False, False, 0.0),
+    ("f16", 32, 6, 2, 900, 33, None, True, True, False, 10.0),
+    ("bf16", 96, 4, 2, 800, 50, None, True, False, False, 0.0),
+    ("bf16", 128, 16, 4, 14, 600, None, True, True, False, 30.0),
+    ("bf16", 128, 16, 2, 14, 600, None, True, False, True, 0.0),
+    ("f16", 72, 12, 12, 16, 700, None, True, False, False, 0.0),
+    ("f32", 96, 8, 4, 24, 700, None, True, False, False, 0.0),
+    ("f32", 128, 16, 2, 14, 600, None, True, False, True, 0.0),
+    ("f32", 24, 4, 2, 700, 60, None, True, True, False, 20.0),
+]
+
+
+@pytest.mark.parametrize("i", range(len(MANY)))
+def test_many_rows(i):
+    """Enough rows for the kernels that big batches take, short and long sequences, some without items."""
+    print("[case]", i, MANY[i], flush=True)
+    dtype, d, Hq, Hk, B, top, ktop, causal, prefix, slopes, cap = MANY[i]
+    rng, g, dt = np.random.RandomState(i), gen(1200 + i), DT[dtype]
+    ql = rng.randint(0, top + 1, B)
+    ql[:2] = top, 0
+    kl = ql if ktop is None else rng.randint(0, ktop + 1, B)
+    qo, ko = ref.offsets(ql), ref.offsets(kl)
+    Tq, Tk = int(ql.sum()), int(kl.sum())
+    q, k, v, do = (rand(g, T, H, d, dtype=dt) for T, H in ((Tq, Hq), (Tk, Hk), (Tk, Hk), (Tq, Hq)))
+    pre = torch.tensor(kl // 4, dtype=torch.int32) if prefix else None
+    sl = torch.tensor([2.0 ** -(1 + h % 8) for h in range(Hq)]) if slopes else None
+    up = lambda t: None if t is None else t.to(DEV)
+    seq = hot.SeqBatch(up(qo), up(ko), Tq, Tk, int(ql.max()), int(kl.max()), causal=causal, prefix=up(pre), slopes=up(sl), cap=cap)
+    Q, K, V, DO = (up(x) for x in (q, k, v, do))
+    out, dq, dk, dv = (torch.full_like(x, NAN) for x in (Q, Q, K, V))
+    lse = torch.full((Hq, Tq), NAN, device=DEV)
+    hot.dlrm_seq_attn_fwd(seq, Q, K, V, out, lse)
+    hot.dlrm_seq_attn_bwd(seq, Q, K, V, out, lse, DO, dq, dk, dv, hot.alloc_seq_attn_workspace(seq, Hq, Hk, d))
+    want = ref.attention(q, k, v, qo, ko, causal, pre, sl, d ** -0.5, cap, do)
+    for n, x in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        ref.close(x, want[n], want[n + "_tol"], n)
 
 
 def test_long_sequences():
