@@ -1,6 +1,8 @@
 """Operators that read a history in order (dlrm_qk_rope_*, dlrm_seq_attn_*, dlrm_cache_attn) against plain 64-bit forms
 (history_ref), with elementwise bounds."""
 import math
+import os
+import sys
 
 import numpy as np
 import pytest
@@ -527,3 +529,12 @@ def test_calls_in_a_graph_replay_like_eager_calls():
         torch.cuda.synchronize()
         for a, b in zip(got, (out, lse, dq, dk, dv, cout)):
             assert torch.equal(a, b)
+
+
+def test_the_sequence_encoder_learns_and_its_cache_agrees():
+    """examples/history_encoder.py: lookup, projections, norm and rotation, attention, the way back, the row update, and the cache."""
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import history_encoder
+    losses, off = history_encoder.main(["--steps", "12", "--users", "64", "--items", "500"])
+    assert all(math.isfinite(x) for x in losses) and losses[-1] < 0.97 * losses[0]
+    assert off < 1e-5
