@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
 // Backward.  A group walks the items group, group + groups of the grid, ...; the weights' gradients of all its rows stay in
 // registers, are added over the workgroup's groups once at the end, and one row of sums per workgroup goes to the workspace.
 template <int DT, int MODE, int G>
-__global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
+__global__ __launch_bounds__(kRopeThreads, 4) void qk_rope_bwd_kernel(RopeArgs a) {
   constexpr int E = Tab<DT>::ELEMS;
   constexpr int NW = kRopeThreads / DLRM_WAVE;
   __shared__ float xs_all[MODE == kHalfAny ? kRopeThreads * E : 1];
@@ -239,19 +239,9 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
   const int64_t groups = (int64_t)gridDim.x * (kRopeThreads / G);
   const int64_t g0 = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
   const float inv_d = 1.0f / (float)a.d;
-  float wq[E], wk[E], sq[E], sk[E];
+  float sq[E], sk[E];
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    wq[j] = wk[j] = 1.0f;
-    sq[j] = sk[j] = 0.0f;
-  }
-  if (col0 < a.d) {
-#pragma unroll
-    for (int j = 0; j < E; j += 4) {
-      if (a.wq) load_cols<4>(a.wq + col0 + j, true, wq + j);
-      if (a.wk) load_cols<4>(a.wk + col0 + j, true, wk + j);
-    }
-  }
+  for (int j = 0; j < E; ++j) sq[j] = sk[j] = 0.0f;
   const int cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
   const int64_t rounds = (a.T + groups - 1) / groups;  // the same for every lane of the workgroup
   for (int64_t i = 0; i < rounds; ++i) {
@@ -266,7 +256,14 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
     }
     RopeLane<DT> L;
     lane_angles<DT, MODE>(a, tt, col0, -1.0f, L);
-    auto turn = [&](const Rows& rows, const Rows& drows, const Rows& to, int H, u32x4 nx, u32x4 nd, const float* wp, const float* w, float* sum) {
+    auto turn = [&](const Rows& rows, const Rows& drows, const Rows& to, int H, u32x4 nx, u32x4 nd, const float* wp, float* sum) {
+      float w[E];  // (loaded again for every item: the registers are worth more)
+#pragma unroll
+      for (int j = 0; j < E; ++j) w[j] = 1.0f;
+      if (wp != nullptr) {
+#pragma unroll
+        for (int j = 0; j < E; j += 4) load_cols<4>(wp + min(col0, a.d - E) + j, true, w + j);
+      }
       for (int h = 0; h < H; ++h) {
         u32x4 rx = nx, rd = nd;
         nx = load(rows, h + 1, H);
@@ -299,8 +296,8 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(RopeArgs a) {
         if (in) store16(row_of(to, tt, h) + cb, narrow<DT>(g));
       }
     };
-    turn(a.q, a.dqo, a.dq, a.Hq, xq, dq, a.wq, wq, sq);
-    turn(a.k, a.dko, a.dk, a.Hk, xk, dk, a.wk, wk, sk);
+    turn(a.q, a.dqo, a.dq, a.Hq, xq, dq, a.wq, sq);
+    turn(a.k, a.dko, a.dk, a.Hk, xk, dk, a.wk, sk);
   }
   if (a.part == nullptr) return;
 #pragma unroll
@@ -452,7 +449,7 @@ static int launch_fwd(const dlrm_qk_rope* r, RopeArgs a, hipStream_t st) {
 
 static int bwd_blocks(const dlrm_qk_rope* r) {
   const int64_t b = (r->T * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
-  return (int)(b > 2048 ? 2048 : b);
+  return (int)(b > 1024 ? 1024 : b);  // as many as are resident
 }
 
 }  // namespace dlrm
