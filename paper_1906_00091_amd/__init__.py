@@ -8,6 +8,6 @@ from .binding import (  # noqa: F401
     state_pointers, dlrm_emb_bag_bwd_workspace_bytes,
     dlrm_emb_bag_fwd, dlrm_emb_interact_fwd, dlrm_emb_interact_bwd, dlrm_emb_interact_fwd_stamped, dlrm_interact_dot_bwd, dlrm_interact_dot_fwd, dlrm_lengths_to_offsets,
     dlrm_place_dense, dlrm_emb_bag_bwd_sgd_timed, dlrm_emb_bag_bwd_adagrad_timed, dlrm_table_init_hash, dlrm_validate_csr, lib, status_string, version,
-    ROPE_HALF, ROPE_INTERLEAVED, Heads, KvCache, QkRope, SeqBatch, alloc_cache_attn_workspace, alloc_qk_rope_workspace, alloc_seq_attn_workspace,
+    ROPE_HALF, ROPE_INTERLEAVED, KvCache, QkRope, SeqBatch, alloc_cache_attn_workspace, alloc_qk_rope_workspace, alloc_seq_attn_workspace,
     dlrm_cache_attn, dlrm_qk_rope_append, dlrm_qk_rope_bwd, dlrm_qk_rope_fwd, dlrm_seq_attn_bwd, dlrm_seq_attn_fwd, rope_frequencies,
 )

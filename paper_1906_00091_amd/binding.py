@@ -6,6 +6,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+import threading
 from typing import List, Optional, Sequence
 
 import torch
@@ -39,10 +41,6 @@ class _SparseBatchC(C.Structure):
         ("offsets", C.c_void_p), ("tbl_off", C.c_void_p), ("weights", C.c_void_p),
         ("index_dtype", C.c_int32),
     ]
-
-
-class _HeadsC(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
 
 
 class _QkRopeC(C.Structure):
@@ -126,7 +124,8 @@ def lib() -> C.CDLL:
         L.dlrm_emb_bag_bwd_sgd_timed.argtypes = [sb, vp, i64, i64, f32, vp, sz, i32, tm, vp]
         L.dlrm_emb_bag_bwd_adagrad_timed.restype = i32
         L.dlrm_emb_bag_bwd_adagrad_timed.argtypes = [sb, vp, vp, i64, i64, f32, f32, vp, sz, i32, tm, vp]
-        hd, rp, kc, sq = C.POINTER(_HeadsC), C.POINTER(_QkRopeC), C.POINTER(_KvCacheC), C.POINTER(_SeqBatchC)
+        rp, kc, sq = C.POINTER(_QkRopeC), C.POINTER(_KvCacheC), C.POINTER(_SeqBatchC)
+        hd = vp  # dlrm_heads*
         L.dlrm_qk_rope_fwd.restype = i32
         L.dlrm_qk_rope_fwd.argtypes = [rp, hd, hd, hd, hd, vp]
         L.dlrm_qk_rope_bwd_workspace_bytes.restype = sz
@@ -405,43 +404,46 @@ def alloc_workspace(batch: SparseBatch) -> torch.Tensor:
 _DTYPE_OF = {t: c for c, t in _TORCH_DTYPE.items()}
 
 
-class Heads:
-    """A tensor [items, heads, d] (any item and head stride, columns next to each other) as the calls below take it.  They take the
-    tensor too; a program that keeps its buffers saves the host a microsecond per tensor and call with views made once."""
+class _Scratch(threading.local):
+    """The dlrm_heads of one call, 24 bytes each, which the library reads before it returns.  Written by one pack: an object
+    per tensor costs the host 0.4 us more each, and a backward pass has eight."""
 
-    def __init__(self, x: torch.Tensor):
-        if x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
-            raise ValueError("rows of heads are [items, heads, d] with the columns next to each other: got %s with strides %s"
-                             % (tuple(x.shape), x.stride()))
-        if x.dtype not in _DTYPE_OF:
-            raise DlrmError("Heads", -3)
-        self.x = x
-        self.shape, self.dtype = tuple(x.shape), _DTYPE_OF[x.dtype]
-        self.c = _HeadsC(x.data_ptr(), x.stride(0), x.stride(1))
+    def __init__(self):
+        self.buf = bytearray(8 * 24)
+        self.at = C.addressof((C.c_char * len(self.buf)).from_buffer(self.buf))
 
 
-def _heads(fn: str, x, n: int, H: int, d: int, dtype: int):
-    if type(x) is Heads:
-        shape, dt, c = x.shape, x.dtype, x.c
-    else:  # (what Heads does, without the object: 1 us less of the host's time per tensor)
-        shape, stride, dt = x.shape, x.stride(), _DTYPE_OF.get(x.dtype)
-        if len(shape) != 3 or stride[2] != 1 != d:
-            Heads(x)
-        c = _HeadsC(x.data_ptr(), stride[0], stride[1])
-    if shape != (n, H, d):
-        raise ValueError("%s: a tensor of shape %s where %s is wanted" % (fn, tuple(shape), (n, H, d)))
-    if dt != dtype:
-        raise DlrmError(fn, -3)
-    return C.byref(c)
+_scratch = _Scratch()
+_PACK = [struct.Struct("%dq" % (3 * n)).pack_into for n in range(9)]
 
 
-def _first(x):
+def _heads(fn: str, dtype: int, rows):
+    """Addresses of the dlrm_heads of `rows`, pairs of a tensor [items, heads, d] (any item and head stride, columns next to each other)
+    and the shape it has to have."""
+    want = _TORCH_DTYPE[dtype]
+    vals = []
+    for x, shape in rows:
+        if x.shape != shape:
+            raise ValueError("%s: a tensor of shape %s where %s is wanted" % (fn, tuple(x.shape), shape))
+        if x.dtype is not want:
+            raise DlrmError(fn, -3)
+        t, h, c = x.stride()
+        if c != 1 != shape[2]:
+            raise ValueError("%s: the columns of a head have to lie next to each other, got strides %s" % (fn, x.stride()))
+        vals += (x.data_ptr(), t, h)
+    s = _scratch
+    _PACK[len(rows)](s.buf, 0, *vals)
+    return range(s.at, s.at + 24 * len(rows), 24)
+
+
+def _first(fn: str, x: torch.Tensor):
     """(shape, storage type) of the tensor that the others of a call go by."""
-    if type(x) is Heads:
-        return x.shape, x.dtype
-    if x.dim() != 3 or x.dtype not in _DTYPE_OF:
-        Heads(x)
-    return x.shape, _DTYPE_OF[x.dtype]
+    if x.dim() != 3:
+        raise ValueError("%s: rows of heads are [items, heads, d], got %s" % (fn, tuple(x.shape)))
+    dt = _DTYPE_OF.get(x.dtype)
+    if dt is None:
+        raise DlrmError(fn, -3)
+    return x.shape, dt
 
 
 def _vector(fn: str, x: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[int]:
@@ -497,26 +499,33 @@ def rope_frequencies(rot: int, base: float = 10000.0, stretch: float = 1.0, keep
     return f.to(torch.float32).to(device)
 
 
-def dlrm_qk_rope_fwd(rope: QkRope, q, k, q_out, k_out):
+def dlrm_qk_rope_fwd(rope: QkRope, q: torch.Tensor, k: Optional[torch.Tensor], q_out: torch.Tensor, k_out: Optional[torch.Tensor]):
     """q, q_out: [T, Hq, d]; k, k_out: [T, Hk, d] (None for Hk = 0).  An output may be its input."""
     fn = "dlrm_qk_rope_fwd"
-    dt = _first(q)[1]
-    n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
-    _check(fn, lib().dlrm_qk_rope_fwd(rope.ref(dt), _heads(fn, q, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt) if Hk else None,
-                                      _heads(fn, q_out, n, Hq, d, dt), _heads(fn, k_out, n, Hk, d, dt) if Hk else None, _stream()))
+    dt = _first(fn, q)[1]
+    rq, rk = (rope.T, rope.Hq, rope.d), (rope.T, rope.Hk, rope.d)
+    if rope.Hk:
+        a, b, c, d = _heads(fn, dt, ((q, rq), (k, rk), (q_out, rq), (k_out, rk)))
+    else:
+        (a, c), b, d = _heads(fn, dt, ((q, rq), (q_out, rq))), None, None
+    _check(fn, lib().dlrm_qk_rope_fwd(rope.ref(dt), a, b, c, d, _stream()))
 
 
-def dlrm_qk_rope_bwd(rope: QkRope, q, k, dq_out, dk_out, dq, dk, dwq: Optional[torch.Tensor], dwk: Optional[torch.Tensor],
+def dlrm_qk_rope_bwd(rope: QkRope, q: torch.Tensor, k: Optional[torch.Tensor], dq_out: torch.Tensor, dk_out: Optional[torch.Tensor],
+                     dq: torch.Tensor, dk: Optional[torch.Tensor], dwq: Optional[torch.Tensor], dwk: Optional[torch.Tensor],
                      workspace: Optional[torch.Tensor]):
     """Gradients dq, dk of the forward's inputs (may be dq_out, dk_out) and dwq, dwk (fp32 [d], written) of the norm weights."""
     fn = "dlrm_qk_rope_bwd"
-    dt = _first(q)[1]
-    n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
-    queries = [_heads(fn, x, n, Hq, d, dt) for x in (q, dq_out, dq)]
-    keys = [_heads(fn, x, n, Hk, d, dt) for x in (k, dk_out, dk)] if Hk else [None] * 3
+    dt = _first(fn, q)[1]
+    rq, rk = (rope.T, rope.Hq, rope.d), (rope.T, rope.Hk, rope.d)
+    if rope.Hk:
+        v = _heads(fn, dt, ((q, rq), (k, rk), (dq_out, rq), (dk_out, rk), (dq, rq), (dk, rk)))
+    else:
+        a, b, c = _heads(fn, dt, ((q, rq), (dq_out, rq), (dq, rq)))
+        v = (a, None, b, None, c, None)
     ws, ws_bytes = _workspace(workspace)
-    _check(fn, lib().dlrm_qk_rope_bwd(rope.ref(dt), queries[0], keys[0], queries[1], keys[1], queries[2], keys[2],
-                                      _vector(fn, dwq, d, torch.float32), _vector(fn, dwk, d, torch.float32), ws, ws_bytes, _stream()))
+    _check(fn, lib().dlrm_qk_rope_bwd(rope.ref(dt), *v, _vector(fn, dwq, rope.d, torch.float32), _vector(fn, dwk, rope.d, torch.float32), ws,
+                                      ws_bytes, _stream()))
 
 
 def alloc_qk_rope_workspace(rope: QkRope) -> torch.Tensor:
@@ -553,13 +562,12 @@ class KvCache:
 def dlrm_qk_rope_append(rope: QkRope, q, k, v, q_out, cache: KvCache, seqs: torch.Tensor):
     """Queries to q_out, keys (normed and rotated) and values to the cache, item t as item positions[t] of sequence seqs[t]."""
     fn = "dlrm_qk_rope_append"
-    dt = _first(q)[1]
-    n, Hq, Hk, d = rope.T, rope.Hq, rope.Hk, rope.d
-    if not Hk:
+    dt = _first(fn, q)[1]
+    if not rope.Hk:
         raise DlrmError(fn, -2)
-    _check(fn, lib().dlrm_qk_rope_append(rope.ref(dt), _heads(fn, q, n, Hq, d, dt), _heads(fn, k, n, Hk, d, dt),
-                                         _heads(fn, v, n, Hk, d, dt), _heads(fn, q_out, n, Hq, d, dt), cache.ref(),
-                                         _vector(fn, seqs, n, torch.int32), _stream()))
+    rq, rk = (rope.T, rope.Hq, rope.d), (rope.T, rope.Hk, rope.d)
+    _check(fn, lib().dlrm_qk_rope_append(rope.ref(dt), *_heads(fn, dt, ((q, rq), (k, rk), (v, rk), (q_out, rq))), cache.ref(),
+                                         _vector(fn, seqs, rope.T, torch.int32), _stream()))
 
 
 class SeqBatch:
@@ -585,26 +593,27 @@ class SeqBatch:
         return C.byref(self.c)
 
 
-def dlrm_seq_attn_fwd(seq: SeqBatch, q, k, v, out, lse: Optional[torch.Tensor] = None):
+def dlrm_seq_attn_fwd(seq: SeqBatch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None):
     """q, out: [Tq, Hq, d]; k, v: [Tk, Hk, d]; lse: fp32 [Hq, Tq] for the backward, or None."""
     fn = "dlrm_seq_attn_fwd"
-    (_, Hq, d), dt = _first(q)
-    Hk = _first(k)[0][1]
-    _check(fn, lib().dlrm_seq_attn_fwd(seq.ref(Hq, d), Hq, Hk, d, dt, _heads(fn, q, seq.Tq, Hq, d, dt), _heads(fn, k, seq.Tk, Hk, d, dt),
-                                       _heads(fn, v, seq.Tk, Hk, d, dt), _heads(fn, out, seq.Tq, Hq, d, dt),
+    (_, Hq, d), dt = _first(fn, q)
+    Hk = _first(fn, k)[0][1]
+    rq, rk = (seq.Tq, Hq, d), (seq.Tk, Hk, d)
+    _check(fn, lib().dlrm_seq_attn_fwd(seq.ref(Hq, d), Hq, Hk, d, dt, *_heads(fn, dt, ((q, rq), (k, rk), (v, rk), (out, rq))),
                                        _vector(fn, lse, Hq * seq.Tq, torch.float32), _stream()))
 
 
-def dlrm_seq_attn_bwd(seq: SeqBatch, q, k, v, out, lse: torch.Tensor, dout, dq, dk, dv, workspace: torch.Tensor):
+def dlrm_seq_attn_bwd(seq: SeqBatch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, dout: torch.Tensor,
+                      dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, workspace: torch.Tensor):
+    """out, lse: the forward's; dout: gradient of out; dq, dk, dv: written."""
     fn = "dlrm_seq_attn_bwd"
-    (_, Hq, d), dt = _first(q)
-    Hk = _first(k)[0][1]
-    queries = [_heads(fn, x, seq.Tq, Hq, d, dt) for x in (q, out, dout, dq)]
-    keys = [_heads(fn, x, seq.Tk, Hk, d, dt) for x in (k, v, dk, dv)]
+    (_, Hq, d), dt = _first(fn, q)
+    Hk = _first(fn, k)[0][1]
+    rq, rk = (seq.Tq, Hq, d), (seq.Tk, Hk, d)
+    h = _heads(fn, dt, ((q, rq), (k, rk), (v, rk), (out, rq), (dout, rq), (dq, rq), (dk, rk), (dv, rk)))
     ws, ws_bytes = _workspace(workspace)
-    _check(fn, lib().dlrm_seq_attn_bwd(seq.ref(Hq, d), Hq, Hk, d, dt, queries[0], keys[0], keys[1], queries[1],
-                                       _vector(fn, lse, Hq * seq.Tq, torch.float32), queries[2], queries[3], keys[2], keys[3], ws, ws_bytes,
-                                       _stream()))
+    _check(fn, lib().dlrm_seq_attn_bwd(seq.ref(Hq, d), Hq, Hk, d, dt, h[0], h[1], h[2], h[3], _vector(fn, lse, Hq * seq.Tq, torch.float32),
+                                       h[4], h[5], h[6], h[7], ws, ws_bytes, _stream()))
 
 
 def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: int = F32) -> torch.Tensor:
@@ -614,15 +623,16 @@ def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: int
     return torch.empty(n, dtype=torch.uint8, device=seq.q_off.device)
 
 
-def dlrm_cache_attn(cache: KvCache, lens: torch.Tensor, max_len: int, q, out, workspace: Optional[torch.Tensor],
+def dlrm_cache_attn(cache: KvCache, lens: torch.Tensor, max_len: int, q: torch.Tensor, out: torch.Tensor, workspace: Optional[torch.Tensor],
                     slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None, cap: float = 0.0):
     """q, out: [B, Hq, d]; lens: int32 [B], items of every sequence in the cache, its newest among them."""
     fn = "dlrm_cache_attn"
-    (_, Hq, d), dt = _first(q)
+    Hq = _first(fn, q)[0][1]
+    rows = (cache.B, Hq, cache.d)
+    a, b = _heads(fn, cache.dtype, ((q, rows), (out, rows)))
     ws, ws_bytes = _workspace(workspace)
-    _check(fn, lib().dlrm_cache_attn(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, Hq,
-                                     _heads(fn, q, cache.B, Hq, cache.d, cache.dtype), _heads(fn, out, cache.B, Hq, cache.d, cache.dtype),
-                                     _vector(fn, slopes, Hq, torch.float32), d ** -0.5 if scale is None else scale, cap, ws, ws_bytes,
+    _check(fn, lib().dlrm_cache_attn(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, Hq, a, b,
+                                     _vector(fn, slopes, Hq, torch.float32), cache.d ** -0.5 if scale is None else scale, cap, ws, ws_bytes,
                                      _stream()))
 
 

@@ -147,16 +147,19 @@ __device__ inline float group_sum(float v) {
 }
 
 // Forward.  Groups of G lanes; group g of the grid takes item g / splits, and of its queries, keys and values every splits-th head.
-template <int DT, int MODE, int G, bool CACHE>
+// SPLIT: several groups share an item.  Where none do, a head is the same for the whole wavefront, and its address is scalar work.
+template <int DT, int MODE, int G, bool SPLIT, bool CACHE>
 __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
   constexpr int E = Tab<DT>::ELEMS;
   __shared__ float xs_all[MODE == kHalfAny ? kRopeThreads * E : 1];
   float* xs = xs_all + (MODE == kHalfAny ? wave_id() * DLRM_WAVE * E : 0);
   const int lane = lane_id(), col0 = (lane & (G - 1)) * E;
   const int64_t group = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
-  const int64_t t = a.splits == 1 ? group : group / a.splits;
+  const int step = SPLIT ? a.splits : 1;
+  const int64_t t = SPLIT ? group / step : group;
   // the group's first query, key and value: where every group has one row at most, no two of them meet
-  const int fq = (int)(group - t * a.splits), fk = a.splits - 1 - fq, fv = fk >= a.shift_v ? fk - a.shift_v : fk - a.shift_v + a.splits;
+  const int fq = SPLIT ? (int)(group - t * step) : 0, fk = SPLIT ? step - 1 - fq : 0;
+  const int fv = !SPLIT ? 0 : fk >= a.shift_v ? fk - a.shift_v : fk - a.shift_v + step;
   // lanes of the last group past the row, and groups past the last item, go along with nothing (exchanges need every lane)
   const bool in = t < a.T && col0 < a.d;
   const int64_t tt = t < a.T ? t : a.T - 1;
@@ -185,9 +188,9 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
       c[j] = L.c[j] * w.own[j];
       s[j] = L.s[j] * w.other[j];
     }
-    for (int h = first; h < H; h += a.splits) {
+    for (int h = first; h < H; h += step) {
       u32x4 raw = next;
-      next = load(rows, h + a.splits, H);
+      next = load(rows, h + step, H);
       if (col0 >= a.d) raw = u32x4{0, 0, 0, 0};
       float x[E], p[E], y[E];
       Tab<DT>::widen(raw, x);
@@ -213,22 +216,22 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
     const bool there = seq >= 0 && seq < a.cB && col >= 0 && col < a.cols && page >= 0 && page < a.n_pages;
     const int64_t at = there ? (int64_t)page * a.Hk * head_bytes + (a.pos[tt] & ((1 << a.page_shift) - 1)) * row : -1;
     turn(a.k, fk, a.Hk, row_k, a.wk, [&](int h) { return at < 0 ? nullptr : a.ck + at + h * head_bytes; });
-    for (int h0 = fv; h0 < a.Hk; h0 += 4 * a.splits) {
+    for (int h0 = fv; h0 < a.Hk; h0 += 4 * step) {
       u32x4 v[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = load(a.v, h0 + i * a.splits, a.Hk);
+      for (int i = 0; i < 4; ++i) v[i] = load(a.v, h0 + i * step, a.Hk);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int h = h0 + i * a.splits;
+        const int h = h0 + i * step;
         if (in && at >= 0 && h < a.Hk) store16(a.cv + at + h * head_bytes + cb, v[i]);
       }
     }
   }
 }
 
-// Backward.  A group walks the items group, group + groups of the grid, ...; the weights' gradients of all its rows stay in
+// Backward.  Groups share an item as in the forward, and walk from item to item; the weights' gradients of all its rows stay in
 // registers, are added over the workgroup's groups once at the end, and one row of sums per workgroup goes to the workspace.
-template <int DT, int MODE, int G>
+template <int DT, int MODE, int G, bool SPLIT>
 __global__ __launch_bounds__(kRopeThreads, 4) void qk_rope_bwd_kernel(RopeArgs a) {
   constexpr int E = Tab<DT>::ELEMS;
   constexpr int NW = kRopeThreads / DLRM_WAVE;
@@ -236,27 +239,30 @@ __global__ __launch_bounds__(kRopeThreads, 4) void qk_rope_bwd_kernel(RopeArgs a
   __shared__ float red[NW][2][DLRM_MAX_HEAD_DIM];
   float* xs = xs_all + (MODE == kHalfAny ? wave_id() * DLRM_WAVE * E : 0);
   const int lane = lane_id(), col0 = (lane & (G - 1)) * E;
-  const int64_t groups = (int64_t)gridDim.x * (kRopeThreads / G);
   const int64_t g0 = ((int64_t)blockIdx.x * kRopeThreads + threadIdx.x) / G;
+  const int step = SPLIT ? a.splits : 1;
+  const int64_t walkers = (int64_t)gridDim.x * (kRopeThreads / G) / step;  // items in a round
+  const int64_t t0 = SPLIT ? g0 / step : g0;
+  const int fq = SPLIT ? (int)(g0 - t0 * step) : 0, fk = SPLIT ? step - 1 - fq : 0;  // the group's first query and key head
   const float inv_d = 1.0f / (float)a.d;
   float sq[E], sk[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) sq[j] = sk[j] = 0.0f;
   const int cb = col0 * Tab<DT>::EB, lb = min(col0, a.d - E) * Tab<DT>::EB;
-  const int64_t rounds = (a.T + groups - 1) / groups;  // the same for every lane of the workgroup
+  const int64_t rounds = (a.T + walkers - 1) / walkers;  // the same for every lane of the workgroup
   for (int64_t i = 0; i < rounds; ++i) {
-    const int64_t t = g0 + i * groups;
-    const bool in = t < a.T && col0 < a.d;
+    const int64_t t = t0 + i * walkers;
+    const bool in = t0 < walkers && t < a.T && col0 < a.d;
     const int64_t tt = t < a.T ? t : a.T - 1;
     auto load = [&](const Rows& rows, int h, int H) { return load16(row_of(rows, tt, min(h, H - 1)) + lb); };
-    u32x4 xq = load(a.q, 0, a.Hq), dq = load(a.dqo, 0, a.Hq), xk = {0, 0, 0, 0}, dk = {0, 0, 0, 0};
+    u32x4 xq = load(a.q, fq, a.Hq), dq = load(a.dqo, fq, a.Hq), xk = {0, 0, 0, 0}, dk = {0, 0, 0, 0};
     if (a.Hk > 0) {
-      xk = load(a.k, 0, a.Hk);
-      dk = load(a.dko, 0, a.Hk);
+      xk = load(a.k, fk, a.Hk);
+      dk = load(a.dko, fk, a.Hk);
     }
     RopeLane<DT> L;
     lane_angles<DT, MODE>(a, tt, col0, -1.0f, L);
-    auto turn = [&](const Rows& rows, const Rows& drows, const Rows& to, int H, u32x4 nx, u32x4 nd, const float* wp, float* sum) {
+    auto turn = [&](const Rows& rows, const Rows& drows, const Rows& to, int first, int H, u32x4 nx, u32x4 nd, const float* wp, float* sum) {
       float w[E];  // (loaded again for every item: the registers are worth more)
 #pragma unroll
       for (int j = 0; j < E; ++j) w[j] = 1.0f;
@@ -264,10 +270,10 @@ __global__ __launch_bounds__(kRopeThreads, 4) void qk_rope_bwd_kernel(RopeArgs a
 #pragma unroll
         for (int j = 0; j < E; j += 4) load_cols<4>(wp + min(col0, a.d - E) + j, true, w + j);
       }
-      for (int h = 0; h < H; ++h) {
+      for (int h = first; h < H; h += step) {
         u32x4 rx = nx, rd = nd;
-        nx = load(rows, h + 1, H);
-        nd = load(drows, h + 1, H);
+        nx = load(rows, h + step, H);
+        nd = load(drows, h + step, H);
         if (col0 >= a.d) rx = rd = u32x4{0, 0, 0, 0};
         float x[E], dy[E], g[E];
         Tab<DT>::widen(rx, x);
@@ -296,8 +302,8 @@ __global__ __launch_bounds__(kRopeThreads, 4) void qk_rope_bwd_kernel(RopeArgs a
         if (in) store16(row_of(to, tt, h) + cb, narrow<DT>(g));
       }
     };
-    turn(a.q, a.dqo, a.dq, a.Hq, xq, dq, a.wq, sq);
-    turn(a.k, a.dko, a.dk, a.Hk, xk, dk, a.wk, sk);
+    turn(a.q, a.dqo, a.dq, fq, a.Hq, xq, dq, a.wq, sq);
+    turn(a.k, a.dko, a.dk, fk, a.Hk, xk, dk, a.wk, sk);
   }
   if (a.part == nullptr) return;
 #pragma unroll
@@ -399,30 +405,33 @@ static RopeArgs rope_args(const dlrm_qk_rope* r) {
   return a;
 }
 
-// Calls f with the storage type, the partner's place and the lanes of a group as compile-time constants.
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+// Calls f with the storage type, the partner's place, the lanes of a group and whether groups share an item as compile-time constants.
 template <typename F>
-static int for_row_kind(int dtype, int mode, int lanes, F f) {
+static int for_row_kind(const dlrm_qk_rope* r, const RopeArgs& a, F f) {
+  auto by_split = [&](auto dt, auto md, auto g) { return a.splits > 1 ? f(dt, md, g, Int<1>{}) : f(dt, md, g, Int<0>{}); };
   auto by_lanes = [&](auto dt, auto md) {
-    switch (lanes) {
-      case 1: return f(dt, md, std::integral_constant<int, 1>{});
-      case 2: return f(dt, md, std::integral_constant<int, 2>{});
-      case 4: return f(dt, md, std::integral_constant<int, 4>{});
-      case 8: return f(dt, md, std::integral_constant<int, 8>{});
-      case 16: return f(dt, md, std::integral_constant<int, 16>{});
-      default: return f(dt, md, std::integral_constant<int, 32>{});
+    switch (group_lanes(r)) {
+      case 2: return by_split(dt, md, Int<2>{});
+      case 4: return by_split(dt, md, Int<4>{});
+      case 8: return by_split(dt, md, Int<8>{});
+      case 16: return by_split(dt, md, Int<16>{});
     }
+    return by_split(dt, md, Int<dt() == DLRM_F32 ? 32 : 1>{});  // fp32 rows of more than 64 columns; 16-bit rows of 8
   };
   auto by_mode = [&](auto dt) {
-    switch (mode) {
-      case kPairs: return by_lanes(dt, std::integral_constant<int, kPairs>{});
-      case kHalfChunks: return by_lanes(dt, std::integral_constant<int, kHalfChunks>{});
-      default: return by_lanes(dt, std::integral_constant<int, kHalfAny>{});
+    switch (partner_mode(r)) {
+      case kPairs: return by_lanes(dt, Int<kPairs>{});
+      case kHalfChunks: return by_lanes(dt, Int<kHalfChunks>{});
+      default: return by_lanes(dt, Int<kHalfAny>{});
     }
   };
-  switch (dtype) {
-    case DLRM_F32: return by_mode(std::integral_constant<int, DLRM_F32>{});
-    case DLRM_F16: return by_mode(std::integral_constant<int, DLRM_F16>{});
-    default: return by_mode(std::integral_constant<int, DLRM_BF16>{});
+  switch (r->dtype) {
+    case DLRM_F32: return by_mode(Int<DLRM_F32>{});
+    case DLRM_F16: return by_mode(Int<DLRM_F16>{});
+    default: return by_mode(Int<DLRM_BF16>{});
   }
 }
 
@@ -440,15 +449,15 @@ static int launch_fwd(const dlrm_qk_rope* r, RopeArgs a, hipStream_t st) {
   a.shift_v = r->Hk % a.splits;
   const int64_t blocks = (r->T * a.splits * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
   if (blocks > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;
-  return for_row_kind(r->dtype, partner_mode(r), group_lanes(r), [&](auto dt, auto md, auto g) {
-    hipLaunchKernelGGL((qk_rope_fwd_kernel<dt(), md(), g(), CACHE>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
+  return for_row_kind(r, a, [&](auto dt, auto md, auto g, auto split) {
+    hipLaunchKernelGGL((qk_rope_fwd_kernel<dt(), md(), g(), split(), CACHE>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
     DLRM_CHECK_LAUNCH();
     return (int)DLRM_OK;
   });
 }
 
 static int bwd_blocks(const dlrm_qk_rope* r) {
-  const int64_t b = (r->T * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
+  const int64_t b = (r->T * head_splits(r, r->Hq + r->Hk) * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
   return (int)(b > 1024 ? 1024 : b);  // as many as are resident
 }
 
@@ -531,11 +540,12 @@ extern "C" int32_t dlrm_qk_rope_bwd(const dlrm_qk_rope* r, const dlrm_heads* q, 
   if (norm && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < dlrm_qk_rope_bwd_workspace_bytes(r)))
     return DLRM_ERR_WORKSPACE;
   a.part = norm ? static_cast<float*>(workspace) : nullptr;
+  a.splits = head_splits(r, r->Hq + r->Hk);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int blocks = bwd_blocks(r);
   if (blocks > 0) {
-    const int rc = for_row_kind(r->dtype, partner_mode(r), group_lanes(r), [&](auto dt, auto md, auto g) {
-      hipLaunchKernelGGL((qk_rope_bwd_kernel<dt(), md(), g()>), dim3(blocks), dim3(kRopeThreads), 0, st, a);
+    const int rc = for_row_kind(r, a, [&](auto dt, auto md, auto g, auto split) {
+      hipLaunchKernelGGL((qk_rope_bwd_kernel<dt(), md(), g(), split()>), dim3(blocks), dim3(kRopeThreads), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return (int)DLRM_OK;
     });

@@ -14,8 +14,12 @@ P = 0x10000
 NULL, SHAPE, DTYPE, WORKSPACE = -1, -2, -3, -4
 
 
+class HeadsC(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+
+
 def heads(data=P, st=1024, sh=64):
-    return C.byref(binding._HeadsC(data, st, sh))
+    return C.byref(HeadsC(data, st, sh))
 
 
 def rope(**kw):
@@ -155,13 +159,13 @@ def test_cache_attention_refuses_bad_arguments():
 
 def test_the_binding_refuses_tensors_that_do_not_fit():
     x = torch.zeros(4, 2, 16)
-    for bad in (torch.zeros(4, 16), torch.zeros(4, 16, 2).transpose(1, 2)):
-        with pytest.raises(ValueError):
-            hot.Heads(bad)
-    with pytest.raises(hot.DlrmError):
-        hot.Heads(x.double())
     off = torch.tensor([0, 4])
     s = hot.SeqBatch(off, off, 4, 4, 4, 4)
+    for bad in (torch.zeros(4, 16), torch.zeros(4, 16, 2).transpose(1, 2)):
+        with pytest.raises(ValueError):
+            hot.dlrm_seq_attn_fwd(s, bad, x, x, x.clone())
+    with pytest.raises(hot.DlrmError):
+        hot.dlrm_seq_attn_fwd(s, x.double(), x, x, x.clone())
     with pytest.raises(ValueError):
         hot.dlrm_seq_attn_fwd(s, x, x, x, torch.zeros(4, 1, 16))
     with pytest.raises(hot.DlrmError):
