@@ -616,8 +616,9 @@ def dlrm_seq_attn_bwd(seq: SeqBatch, q: torch.Tensor, k: torch.Tensor, v: torch.
                                        h[4], h[5], h[6], h[7], ws, ws_bytes, _stream()))
 
 
-def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: int = F32) -> torch.Tensor:
-    n = int(lib().dlrm_seq_attn_bwd_workspace_bytes(seq.ref(Hq, d), Hq, Hk, d, dtype))
+def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: Optional[int] = None) -> torch.Tensor:
+    """For rows of one storage type, or of any."""
+    n = max(int(lib().dlrm_seq_attn_bwd_workspace_bytes(seq.ref(Hq, d), Hq, Hk, d, t)) for t in ((F32, F16, BF16) if dtype is None else (dtype,)))
     if n == 0:
         raise DlrmError("dlrm_seq_attn_bwd_workspace_bytes", -2)
     return torch.empty(n, dtype=torch.uint8, device=seq.q_off.device)

@@ -169,30 +169,33 @@ struct SeqArgs {
   const float* slopes;
   float* lse;    // [Hq, Tq]
   float* delta;  // [Hq, Tq]
-  int64_t Tq;
+  float* part;   // [splits][dk, dv][Tk][Hk][d]: sums of the keys' gradients where several workgroups share a block's queries
+  int64_t Tq, Tk;
   int B, Hq, Hk, d, causal;
-  int by_block;  // the grid is (key head, sequence, block), else key heads times slots
+  int splits;    // workgroups that share a block of rows (keys' gradients)
+  int by_block;  // the grid is (walk, sequence, block), else walks times slots
   float scale, cap;
 };
 
-// Workgroup -> key head, sequence and first row, blocks of ROWS rows, `per` rows for each item of `off`.  A sequence with n rows needs
+// Workgroup -> walk (key head + Hk * split), sequence and first row, blocks of ROWS rows, `per` rows for each item of `off`.  A sequence with n rows needs
 // ceil(n / ROWS) blocks, and how many rows it has stands in device memory.
-// Where all sequences fit into few blocks the grid is (key head, sequence, block), as many blocks as the longest may need: block by block
-// through all sequences, so with causal sequences the blocks of most work of every one of them start first.  Else it is key heads times
+// Where all sequences fit into few blocks the grid is (walk, sequence, block), as many blocks as the longest may need: block by block
+// through all sequences, so with causal sequences the blocks of most work of every one of them start first.  Else it is walks times
 // slots: sequence s starts at slot off[s] * per / ROWS + s, which leaves it enough, and is found by all 64 lanes at once, each step
 // asking 64 places.  Workgroups past a sequence's rows end at once.
 template <int ROWS>
-__device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per, bool last_first, int& hk, int& seq, int& row0) {
+__device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per, bool last_first, int& walk, int& seq, int& row0) {
+  const int walks = a.Hk * a.splits;
   if (a.by_block) {
-    hk = blockIdx.x;
+    walk = blockIdx.x;
     // turned from block to block: workgroups go to the 8 dies in turn, and no die gets all of the same sequences
     seq = blockIdx.y + blockIdx.z;
     if (seq >= a.B) seq %= a.B;
     row0 = (last_first ? gridDim.z - 1 - blockIdx.z : blockIdx.z) * ROWS;
     return;
   }
-  const int at = blockIdx.x / a.Hk, slot = last_first ? gridDim.x / a.Hk - 1 - at : at;
-  hk = blockIdx.x - at * a.Hk;
+  const int at = blockIdx.x / walks, slot = last_first ? gridDim.x / walks - 1 - at : at;
+  walk = blockIdx.x - at * walks;
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) >> 6, s = lo + lane_id() * step;
@@ -656,8 +659,9 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   constexpr int BQ = W::BQ, STEPS = W::STEPS, NB = W::NB;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   const int G = a.Hq / a.Hk;
-  int hk, seq, row0;
-  find_block<W::KEYS>(a, a.k_off, 1, false, hk, seq, row0);  // early keys are seen by most queries
+  int walk, seq, row0;
+  find_block<W::KEYS>(a, a.k_off, 1, false, walk, seq, row0);  // early keys are seen by most queries
+  const int split = a.splits == 1 ? 0 : walk / a.Hk, hk = walk - split * a.Hk;
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
   if (row0 >= sp.nk) return;
@@ -687,8 +691,15 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   const int srow = threadIdx.x % BQ;
   const float* const sfrom = (threadIdx.x / BQ & 1 ? a.delta : a.lse) + q0;
   float sraw = 0.0f;
+  // this workgroup's share of the tiles of all heads
+  const int share = a.splits == 1 ? tiles * G : (tiles * G + a.splits - 1) / a.splits;
+  const int first = split * share, all = max(0, min(tiles * G, first + share) - first);
   int head = hk * G, t = t0;  // of the tile that is on its way
-  const float base = Score<DT, KIND>(a, head).base;
+  if (first > 0 && tiles > 0) {
+    head += first / tiles;
+    t += first % tiles;
+  }
+  const float base = Score<DT, KIND>(a, hk * G).base;
   auto fetch = [&]() {
     const int i0 = t * BQ;
     tq.load(row_of(a.q, q0 + i0, head), a.q.st, sp.nq - i0, a.d);
@@ -704,7 +715,6 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       stat[threadIdx.x] = threadIdx.x < BQ ? lse2_of(sraw, row) - base : row ? sraw : 0.0f;
     }
   };
-  const int all = tiles * G;
   if (all > 0) {
     fetch();
     put(0);
@@ -778,20 +788,51 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     join_parts<NB, GROUPS>(gv, lds, group, part, 1.0f, 1.0f);
   }
   if (part == 1 || !there) return;
-  store_rows<DT, NB>(gk, Score<DT, KIND>(a, hk * G).grad, row_of(a.dk, k0 + j, hk), a.d, h);
-  store_rows<DT, NB>(gv, 1.0f, row_of(a.dv, k0 + j, hk), a.d, h);
+  const float grad = Score<DT, KIND>(a, hk * G).grad;
+  if (a.splits == 1) {
+    store_rows<DT, NB>(gk, grad, row_of(a.dk, k0 + j, hk), a.d, h);
+    store_rows<DT, NB>(gv, 1.0f, row_of(a.dv, k0 + j, hk), a.d, h);
+  } else {
+    const int64_t rows = a.Tk * a.Hk, at = (k0 + j) * a.Hk + hk;
+    store_rows<DLRM_F32, NB>(gk, grad, reinterpret_cast<char*>(a.part + (2 * split * rows + at) * a.d), a.d, h);
+    store_rows<DLRM_F32, NB>(gv, 1.0f, reinterpret_cast<char*>(a.part + ((2 * split + 1) * rows + at) * a.d), a.d, h);
+  }
+}
+
+// Sums of the workgroups that shared the keys' blocks, in their order; 8 columns a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void seq_attn_join_kernel(SeqArgs a) {
+  const int chunks = a.d / 8;
+  const int64_t rows = a.Tk * a.Hk, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = id / chunks;
+  const int c = (int)(id - row * chunks) * 8, which = blockIdx.y;
+  if (row >= rows) return;
+  float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  const float* p = a.part + (which * rows + row) * a.d + c;
+  for (int s = 0; s < a.splits; ++s, p += 2 * rows * a.d) {
+    const f32x4 u = loadf4(p), v = loadf4(p + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] += u[j];
+      x[4 + j] += v[j];
+    }
+  }
+  const int64_t t = row / a.Hk;
+  char* dst = row_of(which ? a.dv : a.dk, t, (int)(row - t * a.Hk)) + c * Tab<DT>::EB;
+  store16(dst, narrow<DT>(x));
+  if constexpr (DT == DLRM_F32) store16(dst + 16, narrow<DT>(x + 4));
 }
 
 // ---------------------------------------------------------------------------------------------------------------
 // Grid for n items in B sequences of at most `longest`, `per` rows an item, blocks of `rows` rows (see find_block); false: too large
 __host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, int per, int rows) {
   if ((int64_t)longest * per > 0x7fffffff - 1024) return false;
-  const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B;
+  const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B, walks = (int64_t)a.Hk * a.splits;
   // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
   // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
   a.by_block = each * a.B <= 3 * slots && a.B <= 65535 && each <= 65535;
-  grid = a.by_block ? dim3(a.Hk, a.B, (unsigned)each) : dim3((unsigned)(slots * a.Hk), 1, 1);
-  return (a.by_block ? each * a.B : slots) * a.Hk < (int64_t)1 << 23;  // fewer than 2^32 threads
+  grid = a.by_block ? dim3((unsigned)walks, a.B, (unsigned)each) : dim3((unsigned)(slots * walks), 1, 1);
+  return (a.by_block ? each * a.B : slots) * walks < (int64_t)1 << 23;  // fewer than 2^32 threads
 }
 
 // Calls f with the padded width and the kind of score as compile-time constants.
@@ -809,6 +850,26 @@ __host__ inline int for_kind(const SeqArgs& a, F f) {
   if (a.d <= 64) return by_kind(std::integral_constant<int, 64>{});
   if (a.d <= 96) return by_kind(std::integral_constant<int, 96>{});
   return by_kind(std::integral_constant<int, 128>{});
+}
+
+// The keys' gradients: workgroups that share a block of keys.  A block walks through all queries of the heads that share its key
+// head, and the longest walk bounds the call: it is shared out where it is longer than what every CU has to do on average (little is known
+// here: bounds and totals), a piece no shorter than 8 tiles, and the pieces' fp32 sums are joined by a launch of their own.
+// (13 histories of up to 1999 items in fp32, two to a block: 620 -> 567 us with the join; 94 of 121 queries and up to 8 keys, eight query heads
+// to a key head, fp32, four to a block: 130 -> 67 us forward and backward.)
+__host__ inline bool short_walks(const dlrm_seq_batch* s) { return s->max_q <= 256; }
+__host__ inline int dkv_splits(const dlrm_seq_batch* s, int Hq, int Hk, int d, int dtype) {
+  const bool wide = dtype != DLRM_F32 && (d > 64 || !short_walks(s));
+  const int keys = wide ? 128 : 64, tile = short_walks(s) ? 32 : 64, G = Hq / Hk;
+  const double resident = short_walks(s) ? 1024 : 256;
+  const double walk = (double)((s->max_q + tile - 1) / tile) * G;
+  const double blocks = ((double)s->Tk / keys + 0.5 * s->B) * Hk;
+  const double mean = blocks * ((double)s->Tq / s->B / tile + 1) * G * (s->causal ? 0.5 : 1.0) / resident;
+  int n = (int)(walk / (mean > 8 ? mean : 8) + 0.5);
+  n = n < 1 ? 1 : n > 16 ? 16 : n;
+  const int64_t bytes = 2 * s->Tk * Hk * d * 4;  // of one workgroup's sums
+  while (n > 1 && n * bytes > (int64_t)256 << 20) --n;
+  return n;
 }
 
 // Two wavefronts to 32 rows where blocks of 128 rows would not give every CU two workgroups.
@@ -857,8 +918,10 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       dim3 grid;
       if (s->Tk == 0) return DLRM_OK;
       if (!blocks_of(a, grid, s->Tk, s->max_k, 1, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
-      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid,
-                         dim3(64 * groups() * parts()), 0, st, a);
+      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(64 * groups() * parts()), 0, st, a);
+      DLRM_CHECK_LAUNCH();
+      if (a.splits == 1) return DLRM_OK;
+      hipLaunchKernelGGL(seq_attn_join_kernel<DT>, dim3(div_up(a.Tk * a.Hk * (a.d / 8), 256), 2), dim3(256), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     };
@@ -870,9 +933,10 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
     else if constexpr (!WIDE_F32)
       rc = dq(Int<4>{}, Int<F32 ? 2 : 1>{});
     if (rc != DLRM_OK) return rc;
+    a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
     // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
     // of up to 200 items, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
-    if (s->max_q <= 256) return dkv(Int<(!F32 && dp() > 64) ? 4 : 2>{}, Int<1>{});
+    if (short_walks(s)) return dkv(Int<(!F32 && dp() > 64) ? 4 : 2>{}, Int<1>{});
     return dkv(Int<F32 ? 2 : 4>{}, Int<2>{});
   });
 }

@@ -25,6 +25,8 @@ static SeqArgs seq_args(const dlrm_seq_batch* s, int Hq, int Hk, int d) {
   a.prefix = s->prefix;
   a.slopes = s->slopes;
   a.Tq = s->Tq;
+  a.Tk = s->Tk;
+  a.splits = 1;
   a.B = s->B;
   a.Hq = Hq;
   a.Hk = Hk;
@@ -57,10 +59,14 @@ extern "C" int32_t dlrm_seq_attn_fwd(const dlrm_seq_batch* s, int32_t Hq, int32_
   }
 }
 
+static size_t delta_bytes(const dlrm_seq_batch* s, int Hq) { return ((size_t)Hq * s->Tq * sizeof(float) + 255) / 256 * 256; }
+
 extern "C" size_t dlrm_seq_attn_bwd_workspace_bytes(const dlrm_seq_batch* s, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype) {
   if (check_seq(s, Hq, Hk, d, dtype) != DLRM_OK) return 0;
-  const size_t n = (size_t)Hq * s->Tq * sizeof(float);
-  return n < 256 ? 256 : (n + 255) / 256 * 256;
+  const int splits = dkv_splits(s, Hq, Hk, d, dtype);
+  const size_t sums = splits > 1 ? (size_t)splits * 2 * s->Tk * Hk * d * sizeof(float) : 0;
+  const size_t n = delta_bytes(s, Hq) + (sums + 255) / 256 * 256;
+  return n < 256 ? 256 : n;
 }
 
 extern "C" int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* s, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype, const dlrm_heads* q,
@@ -88,6 +94,7 @@ extern "C" int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* s, int32_t Hq, int32_
   a.dv = rows_of(dv, eb);
   a.lse = const_cast<float*>(lse);
   a.delta = static_cast<float*>(workspace);
+  a.part = a.delta + delta_bytes(s, Hq) / sizeof(float);
   hipStream_t hs = static_cast<hipStream_t>(stream);
   switch (dtype) {
     case DLRM_F32: return launch_seq_bwd<DLRM_F32>(s, a, hs);
