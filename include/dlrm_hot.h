@@ -478,9 +478,9 @@ int32_t dlrm_qk_rope_append(const dlrm_qk_rope* rope, const dlrm_heads* q, const
  *   causal == 0, or j <= p, or j < prefix[s].
  * Its score is  x = scale * <q, k>;  x = cap * tanh(x / cap) if cap > 0;  x - slopes[h] * |p - j| with slopes;
  * weights are the softmax of the scores over the visible keys.  A query that sees no key gets zeros.
- * Keys and values at places that no query of the sequence's tile of 32 sees, and rows outside the sequence, are not part of any result,
- * whatever they hold; within a tile, values (and in the backward queries and upstream gradients) that are
- * not finite reach other rows of the tile too.
+ * Rows outside the sequences, and rows of other sequences, are not part of a result, whatever they hold.  Within a sequence a hidden
+ * key has weight 0, and 0 times a value that is not finite is NaN: a value (in the backward a key, query or
+ * upstream gradient too) that is not finite may show in rows it is hidden from that stand up to 96 places away.
  */
 typedef struct dlrm_seq_batch {
   int32_t B;             /* sequences, >= 1 */

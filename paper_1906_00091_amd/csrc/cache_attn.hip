@@ -5,7 +5,8 @@
 // 8 consecutive columns of one key.  S^T = K Q^T leaves a lane four keys of one head, and those registers are, with the contracted
 // index permuted, what O^T = V^T P^T takes; values pass through a piece of LDS that belongs to the wavefront alone, to be read by
 // columns.  So the wavefronts of a workgroup run without a barrier, each with its own running maximum and sum, over
-// every fourth tile of 32 keys, and are joined once at the end.
+// every fourth tile of 32 keys, and are joined once at the end.  256 sequences of up to 8192 items, 16 query heads on 4, bf16, d 128: 432 us for
+// 2.15 GB, 5.0 TB/s; a large copy on the same card moves 4.7.
 //
 // The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in
 // the order of the chunks.
@@ -24,7 +25,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kInf = __builtin_inff();
-constexpr int kCacheThreads = 256, kCacheWaves = 4, kKeys = 32, kHeads = 16;
+constexpr int kKeys = 32, kHeads = 16;
 constexpr int kTablePages = 1024;  // pages of a chunk, at most
 
 struct CacheArgs {
@@ -114,16 +115,16 @@ __device__ inline float bent16(float z) {
   }
 }
 
-template <int DT, int DP>
-__global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) {
+template <int DT, int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
   constexpr int EB = Tab<DT>::EB, E = Tab<DT>::ELEMS, STEPS = DP / 32, NB = DP / 16;
   constexpr int CH = DP * EB / 16, NV = kKeys * CH / DLRM_WAVE;  // chunks of a row; of a tile, per lane
   constexpr int STRIDE = DP * EB + 16;
   constexpr int OS = DP + 4;  // row of the joined sums
-  constexpr int VBYTES = kCacheWaves * kKeys * STRIDE, OBYTES = kCacheWaves * kHeads * OS * 4;
+  constexpr int VBYTES = WAVES * kKeys * STRIDE, OBYTES = WAVES * kHeads * OS * 4;
   __shared__ __attribute__((aligned(16))) char lds[VBYTES > OBYTES ? VBYTES : OBYTES];
   __shared__ int pages[kTablePages];
-  __shared__ float stat[kCacheWaves][2][kHeads];
+  __shared__ float stat[WAVES][2][kHeads];
   const int split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits;
   const int blk = rest % a.blocks, hk = rest / a.blocks % a.Hk, s = rest / a.blocks / a.Hk;
   const int G = a.Hq / a.Hk;
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
   // the chunk's page numbers and the queries are loaded beside the length, not after it
   const int start = split * a.chunk, page0 = start >> a.page_shift;
   const int most_pages = min(((start + a.chunk - 1) >> a.page_shift) + 1, a.cols) - page0;
-  for (int p = threadIdx.x; p < most_pages; p += kCacheThreads) pages[p] = a.table[(int64_t)s * a.cols + page0 + p];
+  for (int p = threadIdx.x; p < most_pages; p += 64 * WAVES) pages[p] = a.table[(int64_t)s * a.cols + page0 + p];
   Op16<DT> qf[STEPS];
   const char* qrow = row_of(a.q, s, head_there ? head : hk * G);
 #pragma unroll
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
   float m = -kInf, l = 0.0f;
   int j0 = start + wave * kKeys;
   if (j0 < end) fetch(j0);
-  for (; j0 < end; j0 += kCacheWaves * kKeys) {
+  for (; j0 < end; j0 += WAVES * kKeys) {
     f32x4 sc[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
       const int id = lane + i * DLRM_WAVE;
       *reinterpret_cast<u32x4*>(vs + (id / CH) * STRIDE + (id % CH) * 16) = v_there >> i & 1 ? vf[i] : u32x4{0, 0, 0, 0};
     }
-    const int jn = j0 + kCacheWaves * kKeys;
+    const int jn = j0 + WAVES * kKeys;
     if (jn < end) fetch(jn);
     float x[8];
     float top = -kInf;
@@ -274,16 +275,16 @@ __global__ __launch_bounds__(kCacheThreads) void cache_attn_kernel(CacheArgs a) 
   __syncthreads();
   // join the wavefronts: a thread takes 4 columns of a head
   const int per_head = a.d / 4, rows = min(kHeads, G - blk * kHeads);
-  for (int id = threadIdx.x; id < rows * per_head; id += kCacheThreads) {
+  for (int id = threadIdx.x; id < rows * per_head; id += 64 * WAVES) {
     const int hn = id / per_head, col = id % per_head * 4, hd = hk * G + blk * kHeads + hn;
     float top = -kInf;
 #pragma unroll
-    for (int w = 0; w < kCacheWaves; ++w) top = fmaxf(top, stat[w][0][hn]);
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, stat[w][0][hn]);
     const float ms = top == -kInf ? 0.0f : top;
     f32x4 sum = {0, 0, 0, 0};
     float total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kCacheWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float f = __builtin_amdgcn_exp2f(stat[w][0][hn] - ms);
       total += f * stat[w][1][hn];
       sum += f * *reinterpret_cast<const f32x4*>(os + (w * kHeads + hn) * OS + col);
@@ -382,7 +383,9 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
   }
 }
 
-// Keys of a chunk: as many workgroups as fill the device several times over, at least two tiles a wavefront.
+// Keys of a chunk: 1024 workgroups, four a CU, and at least two tiles a wavefront.  (The 256 sequences above: 436 us with chunks for 1024 workgroups,
+// 474 for 2048, 498 for 4096, 537 for 8192, whose joins read more.  One sequence of 131072 items on 4 key heads, four workgroups if it were not
+// split: 48 us with its join.)
 static int chunk_of(const dlrm_kv_cache* c, int Hq, int max_len) {
   const int64_t rows = (int64_t)c->B * c->Hk * ((Hq / c->Hk + kHeads - 1) / kHeads);
   const int64_t wanted = 1024;
@@ -458,10 +461,17 @@ extern "C" int32_t dlrm_cache_attn(const dlrm_kv_cache* c, const int32_t* lens, 
     a.po = static_cast<float*>(workspace);
     a.pm = a.po + (int64_t)a.B * Hq * a.splits * a.d;
   }
+  // Short sequences, and enough of them: a wavefront each, with nothing to join.  (1356 of 24 items, 8 key heads, fp32, d 32: 22 us, 47 with four
+  // wavefronts; 2048 of up to 200, 4 key heads, fp32, d 64: 95 us, 133.  64 of up to 64, 8 key heads, bf16, d 64: 6.6 us, 5.6 with four, and
+  // 2048 of up to 512, 4 key heads, bf16, d 64: 114 us, 110.)
+  const bool one_wave = a.max_len <= 256 && grid > 8 * (int64_t)a.max_len;
   hipStream_t st = static_cast<hipStream_t>(stream);
   auto by_type = [&](auto dt) {
     auto go = [&](auto dp) {
-      hipLaunchKernelGGL((cache_attn_kernel<dt(), dp()>), dim3((unsigned)grid), dim3(kCacheThreads), 0, st, a);
+      if (one_wave)
+        hipLaunchKernelGGL((cache_attn_kernel<dt(), dp(), 1>), dim3((unsigned)grid), dim3(64), 0, st, a);
+      else
+        hipLaunchKernelGGL((cache_attn_kernel<dt(), dp(), 4>), dim3((unsigned)grid), dim3(256), 0, st, a);
       DLRM_CHECK_LAUNCH();
       if (a.splits > 1) {
         hipLaunchKernelGGL(cache_join_kernel<dt()>, dim3((unsigned)(a.B * Hq)), dim3(kJoinThreads), 0, st, a);

@@ -344,15 +344,17 @@ struct RowWork {
   }
 };
 
-// Adds (f = nullptr) or rescales and adds the sums of the wavefronts of part 1 to those of part 0, through LDS.
-template <int NB, int GROUPS>
-__device__ inline void join_parts(f32x16* x, char* lds, int group, int part, float mine, float other) {
+// x of part 0 becomes x f[0] + (x of part 1) f[1] + ..., through LDS; LDS has to be free.
+template <int NB, int GROUPS, int PARTS>
+__device__ inline void join_parts(f32x16* x, char* lds, int group, int part, const float* f) {
+  constexpr int REGION = GROUPS * NB * 4 * DLRM_WAVE;
   f32x4* at = reinterpret_cast<f32x4*>(lds) + group * NB * 4 * DLRM_WAVE + lane_id();
-  if (part == 1) {
+  if (part > 0) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) at[(b * 4 + q) * DLRM_WAVE] = f32x4{x[b][4 * q], x[b][4 * q + 1], x[b][4 * q + 2], x[b][4 * q + 3]};
+      for (int q = 0; q < 4; ++q)
+        at[(part - 1) * REGION + (b * 4 + q) * DLRM_WAVE] = f32x4{x[b][4 * q], x[b][4 * q + 1], x[b][4 * q + 2], x[b][4 * q + 3]};
   }
   __syncthreads();
   if (part == 0) {
@@ -360,21 +362,42 @@ __device__ inline void join_parts(f32x16* x, char* lds, int group, int part, flo
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const f32x4 y = at[(b * 4 + q) * DLRM_WAVE];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[b][4 * q + e] = x[b][4 * q + e] * mine + y[e] * other;
+        for (int e = 0; e < 4; ++e) x[b][4 * q + e] *= f[0];
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p) {
+          const f32x4 y = at[(p - 1) * REGION + (b * 4 + q) * DLRM_WAVE];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[b][4 * q + e] = fmaf(y[e], f[p], x[b][4 * q + e]);
+        }
       }
   }
 }
 
+// LDS of a kernel that walks over tiles of BK keys: two tiles of keys and values, one where eight parts take so many keys at a time, or the
+// parts' sums.
+template <int DT, int DP, int GROUPS, int PARTS, int SUB>
+struct Walk {
+  static constexpr int BK = 32 * SUB * PARTS, BUFS = PARTS > 2 ? 1 : 2, TILE = BK * Tile<DT, DP>::STRIDE;
+  static constexpr int JOIN = (PARTS - 1) * GROUPS * DP / 2 * DLRM_WAVE * 4;
+  static constexpr int LDS = 2 * BUFS * TILE > JOIN ? 2 * BUFS * TILE : JOIN;
+};
+
+// Wavefronts of a SIMD that the forward's registers are to leave room for: four for short walks of narrow 16-bit rows, one where the rows are
+// too few to give a SIMD two.
+constexpr int fwd_resident(int dt, int dp, int groups, int parts, int sub) {
+  if (groups == 2) return 1;
+  return groups == 4 && parts * sub == 1 && dp <= 64 && dt != DLRM_F32 ? 4 : 2;
+}
+
 // Forward: tiles of keys and values go by, SUB x 32 keys for each part, two tiles in LDS.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
-__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? (SUB * PARTS == 1 ? 4 : 2) : 1) void seq_attn_fwd_kernel(SeqArgs a) {
-  constexpr int BK = 32 * SUB * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
+__global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
+  typedef Walk<DT, DP, GROUPS, PARTS, SUB> W;
+  constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   typedef Tile<DT, DP> T;
-  constexpr int TILE = BK * T::STRIDE, JOIN = PARTS == 2 ? GROUPS * NB * 16 * DLRM_WAVE * 4 : 0;
-  __shared__ __attribute__((aligned(16))) char lds[4 * TILE > JOIN ? 4 * TILE : JOIN];
-  __shared__ float stat[PARTS == 2 ? GROUPS * 2 * 32 : 1];
+  __shared__ __attribute__((aligned(16))) char lds[W::LDS];
+  __shared__ float stat[PARTS > 1 ? PARTS * GROUPS * 2 * 32 : 1];
   RowWork<GROUPS, PARTS> w;
   if (!w.find(a)) return;
   const Span& sp = w.sp;
@@ -408,7 +431,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? (SUB * PARTS == 
     }
     const int j0 = jt + 32 * SUB * w.part;
     if (j0 < w.wave_vis) {
-      const char* ks = lds + (t & 1) * 2 * TILE + 32 * SUB * w.part * T::STRIDE;
+      const char* ks = lds + (t & (W::BUFS - 1)) * 2 * TILE + 32 * SUB * w.part * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 s[SUB];
       __builtin_amdgcn_s_setprio(1);
@@ -470,26 +493,34 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? (SUB * PARTS == 
           for (int b = 0; b < NB; ++b) o[b] = Op<DT>::mma(T::by_column(vs, 32 * u + 16 * g, b, lane), p, o[b]);
         }
     }
+    if (W::BUFS == 1) __syncthreads();
     if (t + 1 < tiles) {
-      tk.store(lds + ((t + 1) & 1) * 2 * TILE);
-      tv.store(lds + ((t + 1) & 1) * 2 * TILE + TILE);
+      tk.store(lds + ((t + 1) & (W::BUFS - 1)) * 2 * TILE);
+      tv.store(lds + ((t + 1) & (W::BUFS - 1)) * 2 * TILE + TILE);
     }
     __syncthreads();
   }
   l += other_half(l);
-  if constexpr (PARTS == 2) {
-    float* st = stat + w.group * 64 + (lane & 31);
-    if (w.part == 1 && h == 0) {
-      st[0] = m;
-      st[32] = l;
+  if constexpr (PARTS > 1) {
+    float* st = stat + (w.group * PARTS) * 64 + (lane & 31);
+    if (h == 0) {
+      st[w.part * 64] = m;
+      st[w.part * 64 + 32] = l;
     }
     __syncthreads();
-    const float m2 = st[0], top = fmaxf(m, m2), ts = top == -kInf ? 0.0f : top;
-    const float f1 = __builtin_amdgcn_exp2f(m - ts), f2 = __builtin_amdgcn_exp2f(m2 - ts);
-    join_parts<NB, GROUPS>(o, lds, w.group, w.part, f1, f2);
-    l = l * f1 + st[32] * f2;
+    float top = -kInf, f[PARTS];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) top = fmaxf(top, st[p * 64]);
+    const float ts = top == -kInf ? 0.0f : top;
+    l = 0.0f;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      f[p] = __builtin_amdgcn_exp2f(st[p * 64] - ts);
+      l = fmaf(st[p * 64 + 32], f[p], l);
+    }
     m = top;
-    if (w.part == 1) return;
+    join_parts<NB, GROUPS, PARTS>(o, lds, w.group, w.part, f);
+    if (w.part > 0) return;
   }
   if (!w.me.there) return;
   store_rows<DT, NB>(o, l > 0.0f ? 1.0f / l : 0.0f, row_of(a.out, w.me.t, w.me.head), a.d, h);
@@ -510,13 +541,13 @@ __device__ inline float lse2_of(float lse, bool there) { return !there || lse ==
 // rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  2048 histories of up to 200 items in bf16, slopes: dq
 // 2.5e-3 off in one part, 2.0e-3 in two, 1.7e-3 being the rounding of dq itself.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
-__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
-  constexpr int BK = 32 * PARTS, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
+__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
+  typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
+  constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   constexpr bool TWO = DT != DLRM_F32 && (DP <= 64 || (KIND & kSlopes) != 0);  // ds in two parts
   typedef Tile<DT, DP> T;
-  constexpr int TILE = BK * T::STRIDE, JOIN = PARTS == 2 ? GROUPS * NB * 16 * DLRM_WAVE * 4 : 0;
-  __shared__ __attribute__((aligned(16))) char lds[4 * TILE > JOIN ? 4 * TILE : JOIN];
-  __shared__ float sums[PARTS == 2 ? GROUPS * 32 : 1];
+  __shared__ __attribute__((aligned(16))) char lds[W::LDS];
+  __shared__ float sums[PARTS > 1 ? PARTS * GROUPS * 32 : 1];
   RowWork<GROUPS, PARTS> w;
   if (!w.find(a)) return;
   const Span& sp = w.sp;
@@ -562,7 +593,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_
     }
     const int j0 = jt + 32 * w.part;
     if (j0 < w.wave_vis) {
-      const char* ks = lds + (t & 1) * 2 * TILE + 32 * w.part * T::STRIDE;
+      const char* ks = lds + (t & (W::BUFS - 1)) * 2 * TILE + 32 * w.part * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 s = {}, dp = {};
       __builtin_amdgcn_s_setprio(1);
@@ -614,18 +645,25 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 ? 2 : 1) void seq_
         }
       }
     }
+    if (W::BUFS == 1) __syncthreads();
     if (t + 1 < tiles) {
-      tk.store(lds + ((t + 1) & 1) * 2 * TILE);
-      tv.store(lds + ((t + 1) & 1) * 2 * TILE + TILE);
+      tk.store(lds + ((t + 1) & (W::BUFS - 1)) * 2 * TILE);
+      tv.store(lds + ((t + 1) & (W::BUFS - 1)) * 2 * TILE + TILE);
     }
     __syncthreads();
   }
   sum += other_half(sum);
-  if constexpr (PARTS == 2) {
-    if (w.part == 1 && h == 0) sums[w.group * 32 + lane] = sum;
-    join_parts<NB, GROUPS>(g, lds, w.group, w.part, 1.0f, 1.0f);
-    if (w.part == 1) return;
-    sum += sums[w.group * 32 + (lane & 31)];
+  if constexpr (PARTS > 1) {
+    float* st = sums + w.group * 32 + (lane & 31);
+    if (h == 0) st[w.part * GROUPS * 32] = sum;
+    float ones[PARTS];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) ones[p] = 1.0f;
+    join_parts<NB, GROUPS, PARTS>(g, lds, w.group, w.part, ones);
+    if (w.part > 0) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) sum += st[p * GROUPS * 32];
   }
   if (!w.me.there) return;
   if (h == 0) a.delta[at] = sum;
@@ -783,9 +821,10 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     __syncthreads();
   }
   if constexpr (PARTS == 2) {  // one of the two gradients after the other
-    join_parts<NB, GROUPS>(gk, lds, group, part, 1.0f, 1.0f);
+    const float ones[2] = {1.0f, 1.0f};
+    join_parts<NB, GROUPS, PARTS>(gk, lds, group, part, ones);
     __syncthreads();
-    join_parts<NB, GROUPS>(gv, lds, group, part, 1.0f, 1.0f);
+    join_parts<NB, GROUPS, PARTS>(gv, lds, group, part, ones);
   }
   if (part == 1 || !there) return;
   const float grad = Score<DT, KIND>(a, hk * G).grad;
@@ -872,8 +911,18 @@ __host__ inline int dkv_splits(const dlrm_seq_batch* s, int Hq, int Hk, int d, i
   return n;
 }
 
-// Two wavefronts to 32 rows where blocks of 128 rows would not give every CU two workgroups.
-__host__ inline bool few_rows(const dlrm_seq_batch* s, const SeqArgs& a) { return s->Tq * a.Hq < 512 * 128; }
+// How the rows' kernels are cut, by what there is of rows and keys (GROUPS x PARTS wavefronts; `sub` tiles of 32 keys to a part and step).
+// Short keys: no walk to share.  Few rows: two wavefronts to 32 rows where blocks of 128 rows would not give every CU two workgroups, and eight
+// where 32 rows to a workgroup would not give every CU one, if the walk is long and a step's keys fit into LDS.
+// Forward and backward together: 16 histories of 2694 items under one or two queries, f16, d 80: two wavefronts 116 us, eight 68; 2 of up to 1762
+// items, fp32, d 16: 141 and 89.  Forward and queries' gradient, 259 histories of one item or none, fp32, d 88: two parts 53 us, one 32.
+enum { kMany, kManyShort, kFew, kFewShort, kFewest };
+__host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool fits8) {
+  const int64_t rows = s->Tq * a.Hq, blocks = rows / 32 + (int64_t)s->B * a.Hk / 2;
+  if (s->max_k <= 64) return rows < 512 * 128 ? kFewShort : kManyShort;
+  if (fits8 && blocks <= 256 && s->max_k >= 512) return kFewest;
+  return rows < 512 * 128 ? kFew : kMany;
+}
 
 template <int DT>
 int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
@@ -882,20 +931,24 @@ int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       dim3 grid;
       if (s->Tq == 0) return DLRM_OK;
       if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
-      hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid,
-                         dim3(64 * groups() * parts()), 0, st, a);
+      hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid, dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     };
-    if (few_rows(s, a)) return go(Int<2>{}, Int<2>{}, Int<1>{});
-    if constexpr (DT == DLRM_F32) {
+    constexpr bool F32 = DT == DLRM_F32, FITS8 = !F32 || dp() <= 64;
+    const int cut = cut_of(s, a, FITS8);
+    if (cut == kFewShort) return go(Int<2>{}, Int<1>{}, Int<1>{});
+    if (cut == kManyShort) return go(Int<4>{}, Int<1>{}, Int<1>{});
+    if (cut == kFew) return go(Int<2>{}, Int<2>{}, Int<1>{});
+    if constexpr (FITS8) {
+      if (cut == kFewest) return go(Int<1>{}, Int<8>{}, Int<1>{});
+    }
+    if constexpr (F32) {
       return go(Int<4>{}, Int<2>{}, Int<1>{});
     } else {
       // Short histories of narrow rows: tiles of 32 keys leave registers for four workgroups a CU.  (2048 histories of up to 200 items, d 64:
       // 131 us, 143 with 64 keys; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
-      if constexpr (dp() <= 64) {
-        if (s->max_k <= 256) return go(Int<4>{}, Int<1>{}, Int<1>{});
-      }
+      if (dp() <= 64 && s->max_k <= 256) return go(Int<4>{}, Int<1>{}, Int<1>{});
       return go(Int<4>{}, Int<1>{}, Int<2>{});
     }
   });
@@ -925,17 +978,29 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     };
-    // fp32 rows of 128 columns need more registers than eight wavefronts of a CU have
-    constexpr bool WIDE_F32 = F32 && dp() > 96;
-    int rc;
-    if (WIDE_F32 || few_rows(s, a))
+    // (fp32 rows of 128 columns need more registers than eight wavefronts of a CU have)
+    constexpr bool WIDE_F32 = F32 && dp() > 96, FITS8 = !F32 || dp() <= 64;
+    const int cut = cut_of(s, a, FITS8);
+    int rc = DLRM_OK;
+    if (cut == kFewShort || (WIDE_F32 && cut == kManyShort))
+      rc = dq(Int<2>{}, Int<1>{});
+    else if (cut == kFew || (WIDE_F32 && cut == kMany))
       rc = dq(Int<2>{}, Int<2>{});
-    else if constexpr (!WIDE_F32)
-      rc = dq(Int<4>{}, Int<F32 ? 2 : 1>{});
+    else if (cut == kFewest) {
+      if constexpr (FITS8) rc = dq(Int<1>{}, Int<8>{});
+    } else if constexpr (!WIDE_F32) {
+      if constexpr (F32) {
+        rc = cut == kManyShort ? dq(Int<4>{}, Int<1>{}) : dq(Int<4>{}, Int<2>{});
+      } else {
+        rc = dq(Int<4>{}, Int<1>{});
+      }
+    }
     if (rc != DLRM_OK) return rc;
     a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
     // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
     // of up to 200 items, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
+    // (No more than 32 keys: no wavefront without any.  259 histories of one item or none, fp32, d 88: two wavefronts 75 us, one 42.)
+    if (s->max_k <= 32 && short_walks(s)) return dkv(Int<1>{}, Int<1>{});
     if (short_walks(s)) return dkv(Int<(!F32 && dp() > 64) ? 4 : 2>{}, Int<1>{});
     return dkv(Int<F32 ? 2 : 4>{}, Int<2>{});
   });

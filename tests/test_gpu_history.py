@@ -130,6 +130,34 @@ def test_norm_and_rotation_backward(i):
     assert torch.equal(dw[rows], first[rows])
 
 
+@pytest.mark.parametrize("dtype,d,Hq,Hk,layout", [("bf16", 8, 20, 4, "interleaved"), ("f16", 16, 3, 5, "half"), ("bf16", 24, 1, 1, "half"), ("f32", 8, 5, 2, "half")])
+def test_many_items_of_narrow_rows(dtype, d, Hq, Hk, layout):
+    g, dt, T, rot = gen(d), DT[dtype], 70001, 6
+    x = {"q": rand(g, T, Hq, d, dtype=dt), "k": rand(g, T, Hk, d, dtype=dt)}
+    dy = {n: rand(g, *x[n].shape, dtype=dt) for n in "qk"}
+    w = 1 + 0.1 * rand(g, 2, d)
+    pos, f = torch.arange(T, dtype=torch.int32) % 1000, hot.rope_frequencies(rot)
+    how = (pos, f, rot, layout, 1e-5, 1.0)
+    wd = w.to(DEV)
+    plan = hot.QkRope(pos.to(DEV), Hq, Hk, d, inv_freq=f.to(DEV), rot=rot, eps=1e-5, wq=wd[0], wk=wd[1],
+                      layout=hot.ROPE_HALF if layout == "half" else hot.ROPE_INTERLEAVED)
+    X, DY = ({n: placed(t[n], "packed") for n in "qk"} for t in (x, dy))
+    out, dx = ({n: torch.empty(T, x[n].shape[1], d, dtype=dt, device=DEV) for n in "qk"} for _ in range(2))
+    dw = torch.empty(2, d, device=DEV)
+    hot.dlrm_qk_rope_fwd(plan, X["q"], X["k"], out["q"], out["k"])
+    hot.dlrm_qk_rope_bwd(plan, X["q"], X["k"], DY["q"], DY["k"], dx["q"], dx["k"], dw[0], dw[1], hot.alloc_qk_rope_workspace(plan))
+    for j, n in enumerate("qk"):
+        y = ref.rope(x[n], w[j], *how)
+        ref.close(out[n], y, rope_bound(dt, x[n], w[j], y, 1.0, d), n)
+        want, dwn = ref.rope_grad(x[n], w[j], dy[n], *how)
+        r = 1 / torch.sqrt(x[n].double().square().mean(-1, keepdim=True) + 1e-5)
+        xn = (x[n].double() * r).abs()
+        gmag = 2 * dy[n].double().abs().amax(-1, keepdim=True) * w[j].double().abs().amax()
+        ref.close(dx[n], want, ref.UNIT[dt] * want.abs() + 2 * (d + 24) * ref.E32 * r * gmag * (1 + xn.amax(-1, keepdim=True)) + ref.TINY[dt], "d" + n)
+        # sums of a thousand terms a lane, then of the lanes and workgroups: n e32 times the terms is a bound on any of it
+        ref.close(dw[j], dwn, (d + 24 + 2000) * ref.E32 * (gmag * xn).sum((0, 1)) + 1e-30, "dw" + n)
+
+
 def test_no_items_leave_gradients_of_zero():
     plan = hot.QkRope(torch.empty(0, dtype=torch.int32, device=DEV), 2, 2, 16, wq=torch.ones(16, device=DEV), wk=torch.ones(16, device=DEV))
     e = torch.empty(0, 2, 16, device=DEV)
@@ -225,6 +253,17 @@ SEQ = [
     ("bf16", 24, 2, 1, [100, 3, 1], [20, 40, 0], True, True, False, 0.0, "rows"),  # rows that see nothing but a prefix, or nothing
     ("bf16", 128, 16, 1, [1] * 9, [1, 2, 3, 63, 64, 65, 0, 700, 5], True, False, False, 0.0, "rows"),   # one query each
     ("bf16", 56, 2, 2, [0, 0, 1, 0], None, True, False, False, 0.0, "rows"),
+    # few rows over many keys
+    ("f32", 40, 3, 1, [5, 70, 0], [700, 1300, 90], True, True, True, 20.0, "packed"),
+    ("f16", 80, 2, 1, [2, 1, 1, 1], [2694, 513, 0, 20], True, False, True, 0.0, "rows"),
+    ("bf16", 64, 4, 2, [600], None, True, False, False, 0.0, "heads"),
+    ("f32", 64, 2, 2, [3, 40], [600, 31], False, False, False, 0.0, "rows"),
+    ("f32", 88, 3, 3, [3, 40], [600, 1031], False, False, True, 0.0, "rows"),
+    ("bf16", 16, 5, 1, [9], [4000], True, False, False, 15.0, "rows"),
+    # no more than one tile of keys
+    ("f32", 88, 15, 3, [1, 0, 1, 1, 0] * 20, None, True, False, False, 0.0, "rows"),
+    ("f32", 128, 2, 2, [64, 3, 0, 17], None, True, False, True, 0.0, "packed"),
+    ("f16", 104, 4, 4, [3, 60, 0, 17], [40, 0, 3, 64], False, False, False, 9.0, "rows"),
 ]
 
 
@@ -282,6 +321,8 @@ MANY = [
     ("f32", 96, 8, 4, 24, 700, None, True, False, False, 0.0),
     ("f32", 128, 16, 2, 14, 600, None, True, False, True, 0.0),
     ("f32", 24, 4, 2, 700, 60, None, True, True, False, 20.0),
+    ("f32", 120, 4, 4, 900, 40, None, True, False, False, 0.0),
+    ("bf16", 112, 8, 1, 600, 40, 20, False, False, False, 0.0),
 ]
 
 
