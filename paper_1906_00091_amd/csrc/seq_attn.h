@@ -278,6 +278,13 @@ __device__ inline void own_rows(Op<DT>* f, const char* row, bool there, int d, i
   }
 }
 
+// The last step of a product over the columns has none below d where d <= DP - 16.  In fp32 it is left out, where its 8 products of 64 cycles would
+// add zeros (13 histories of up to 1999 items, d 72: forward 310 -> 290 us, queries' gradient 430 -> 392, keys' 560 -> 538).
+template <int DT, int STEPS>
+__device__ inline bool past_d(int st, int d) {
+  return DT == DLRM_F32 && st == STEPS - 1 && d <= 16 * st;
+}
+
 // What a sequence's rows may see: keys [0, vis(i)) for query i.
 struct Span {
   int nq, nk, shift, prefix, causal;  // shift: a query's place is i + shift
@@ -391,6 +398,11 @@ constexpr int fwd_resident(int dt, int dp, int groups, int parts, int sub) {
 }
 
 // Forward: tiles of keys and values go by, SUB x 32 keys for each part, two tiles in LDS.
+// 8 histories of 2048 to 4096 items, 16 query heads on 4, bf16, d 128, causal, capped: 490 us, 660 TFLOP/s of visible pairs (a large library product
+// of bf16 on the same card: 1203), bound by the exponentials and reciprocals beside the products: two wavefronts a SIMD, each of which can
+// multiply while the other does not.  2048 histories of up to 200 items, 4 heads, d 64, slopes: 127 us; a workgroup walks over four tiles and
+// waits for most of its time (four a CU hide part of it).  fp32, 13 histories of up to 1999 items, d 72: 290 us, 57 TFLOP/s of 154, and 70 with
+// the columns that pad 72 to 96.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, SUB> W;
@@ -439,7 +451,10 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       for (int u = 0; u < SUB; ++u) {
         s[u] = f32x16{};
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) s[u] = Op<DT>::mma(T::by_row(ks, 32 * u + (lane & 31), st, h), qf[st], s[u]);
+        for (int st = 0; st < STEPS; ++st) {
+          if (past_d<DT, STEPS>(st, a.d)) break;
+          s[u] = Op<DT>::mma(T::by_row(ks, 32 * u + (lane & 31), st, h), qf[st], s[u]);
+        }
       }
       __builtin_amdgcn_s_setprio(0);
       // with slopes the whole score, else what the factor c still goes to, in the multiply-add before the exponential
@@ -538,8 +553,9 @@ __device__ inline float lse2_of(float lse, bool there) { return !there || lse ==
 // ds = p (dp - delta) (a row with one key has dp = delta).  So delta is summed again on the way as sum p dp, in fp32: the kernel after this
 // one takes that; a row whose keys all lie in the first 32 has it before its first use here; and for the other rows what the rounding
 // of the output leaves is made up for by taking ds in two 16-bit parts, with a second product, where that costs little or is most needed: narrow
-// rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  2048 histories of up to 200 items in bf16, slopes: dq
-// 2.5e-3 off in one part, 2.0e-3 in two, 1.7e-3 being the rounding of dq itself.
+// rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  2048 histories of up to 200 items in bf16, slopes: the
+// outputs together are 2.5e-3 off (relative, all of them) in one part, 2.3e-3 in two, where rounding them alone makes 1.7e-3.
+// Bound as the forward is: the sizes above take 620 us (784 TFLOP/s), 209 us and 392 us (63 TFLOP/s).
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
@@ -599,6 +615,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
+        if (past_d<DT, STEPS>(st, a.d)) break;
         s = Op<DT>::mma(T::by_row(ks, lane & 31, st, h), qf[st], s);
         dp = Op<DT>::mma(T::by_row(vs, lane & 31, st, h), df[st], dp);
       }
@@ -676,6 +693,8 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
 // S = Q K^T and dP = dO V^T have the keys as columns; dV^T = dO^T P and dK^T = Q^T dS.
 // Two wavefronts share 32 keys, one for each half of a tile's 64 queries, and add their sums at the end: the keys that all
 // queries of a long sequence see are the longest work of all, and go by in half the steps.
+// The sizes above: 1010 us (640 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 229 us (latency of short
+// walks) and 538 us with 13 for the join (62 TFLOP/s).
 template <int DT, int DP, int GROUPS_, int PARTS_>
 struct Dkv {
   static constexpr int GROUPS = GROUPS_, PARTS = PARTS_, KEYS = 32 * GROUPS, THREADS = 64 * GROUPS * PARTS, BQ = 32 * PARTS;
@@ -776,6 +795,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
+        if (past_d<DT, STEPS>(st, a.d)) break;
         s = Op<DT>::mma(T::by_row(qs, lane & 31, st, h), kf[st], s);
         dp = Op<DT>::mma(T::by_row(os, lane & 31, st, h), W::V_LDS ? T::by_row(lds + W::V_AT, group * 32 + (lane & 31), st, h) : vf[W::V_LDS ? 0 : st], dp);
       }
