@@ -398,10 +398,10 @@ constexpr int fwd_resident(int dt, int dp, int groups, int parts, int sub) {
 }
 
 // Forward: tiles of keys and values go by, SUB x 32 keys for each part, two tiles in LDS.
-// 8 histories of 2048 to 4096 items, 16 query heads on 4, bf16, d 128, causal, capped: 490 us, 660 TFLOP/s of visible pairs (a large library product
+// 8 histories of 2048 to 4096 items, 16 query heads on 4, bf16, d 128, causal, capped: 485 us, 668 TFLOP/s of visible pairs (a large library product
 // of bf16 on the same card: 1203), bound by the exponentials and reciprocals beside the products: two wavefronts a SIMD, each of which can
 // multiply while the other does not.  2048 histories of up to 200 items, 4 heads, d 64, slopes: 127 us; a workgroup walks over four tiles and
-// waits for most of its time (four a CU hide part of it).  fp32, 13 histories of up to 1999 items, d 72: 290 us, 57 TFLOP/s of 154, and 70 with
+// waits for most of its time (four a CU hide part of it).  fp32, 13 histories of up to 1999 items, d 72: 283 us, 58 TFLOP/s of 154, and 72 with
 // the columns that pad 72 to 96.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
@@ -555,7 +555,7 @@ __device__ inline float lse2_of(float lse, bool there) { return !there || lse ==
 // of the output leaves is made up for by taking ds in two 16-bit parts, with a second product, where that costs little or is most needed: narrow
 // rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  2048 histories of up to 200 items in bf16, slopes: the
 // outputs together are 2.5e-3 off (relative, all of them) in one part, 2.3e-3 in two, where rounding them alone makes 1.7e-3.
-// Bound as the forward is: the sizes above take 620 us (784 TFLOP/s), 209 us and 392 us (63 TFLOP/s).
+// Bound as the forward is: the sizes above take 616 us (789 TFLOP/s), 210 us and 382 us (65 TFLOP/s).
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
@@ -693,8 +693,8 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
 // S = Q K^T and dP = dO V^T have the keys as columns; dV^T = dO^T P and dK^T = Q^T dS.
 // Two wavefronts share 32 keys, one for each half of a tile's 64 queries, and add their sums at the end: the keys that all
 // queries of a long sequence see are the longest work of all, and go by in half the steps.
-// The sizes above: 1010 us (640 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 229 us (latency of short
-// walks) and 538 us with 13 for the join (62 TFLOP/s).
+// The sizes above: 1000 us (648 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 230 us (latency of short
+// walks) and 521 us with 13 for the join (62 TFLOP/s).
 template <int DT, int DP, int GROUPS_, int PARTS_>
 struct Dkv {
   static constexpr int GROUPS = GROUPS_, PARTS = PARTS_, KEYS = 32 * GROUPS, THREADS = 64 * GROUPS * PARTS, BQ = 32 * PARTS;
@@ -932,16 +932,29 @@ __host__ inline int dkv_splits(const dlrm_seq_batch* s, int Hq, int Hk, int d, i
 }
 
 // How the rows' kernels are cut, by what there is of rows and keys (GROUPS x PARTS wavefronts; `sub` tiles of 32 keys to a part and step).
-// Short keys: no walk to share.  Few rows: two wavefronts to 32 rows where blocks of 128 rows would not give every CU two workgroups, and eight
-// where 32 rows to a workgroup would not give every CU one, if the walk is long and a step's keys fit into LDS.
-// Forward and backward together: 16 histories of 2694 items under one or two queries, f16, d 80: two wavefronts 116 us, eight 68; 2 of up to 1762
-// items, fp32, d 16: 141 and 89.  Forward and queries' gradient, 259 histories of one item or none, fp32, d 88: two parts 53 us, one 32.
-enum { kMany, kManyShort, kFew, kFewShort, kFewest };
-__host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool fits8) {
-  const int64_t rows = s->Tq * a.Hq, blocks = rows / 32 + (int64_t)s->B * a.Hk / 2;
-  if (s->max_k <= 64) return rows < 512 * 128 ? kFewShort : kManyShort;
-  if (fits8 && blocks <= 256 && s->max_k >= 512) return kFewest;
-  return rows < 512 * 128 ? kFew : kMany;
+//   k4x1: 16-bit types.  Wavefronts that share 32 rows pay for the join, and gain where the rows are too few to fill the device;
+//   k2x1: fp32, whose registers leave a SIMD one wavefront of most kernels: small workgroups begin and end on their own;
+//   k2x2, k4x2: long walks of few rows, which then take half the steps;
+//   k1x8: where 32 rows to a workgroup would not give every CU one, if the walk is long and a step's keys fit into LDS.
+// Measured, forward / queries' gradient in us:
+//   2048 histories of up to 200 items, 4 heads:  fp32, d 64: k4x2 672 / 1004, k2x2 457 / 626, k4x1 379 / 616, k2x1 373 / 501;
+//                                                bf16, d 128: k4x1 276 / 394, k2x1 366 / 445
+//   128 histories of up to 200 items, 4 heads, bf16, d 128: k2x2 40 / 50, k4x1 23 / 32;  40, fp32, d 64: k2x2 19 / 25, k2x1 27 / 34
+//   4 histories of 1000 to 1400 items, 4 heads, bf16, d 128: k2x2 40 / 36, k4x1 43 / 51;  8, 4 heads on 2: k2x2 59 / 61, k4x1 45 / 57
+//   64 of 1000 to 1400 items, 4 heads, fp32, d 64: k4x2 630 / 870, k2x1 561 / 763;  13 of up to 2000, 6 heads on 3: k4x2 194 / 266, k2x1 264 / 359
+//   2 of 3000 to 4000 items, 8 heads on 2, fp32, d 96: k2x2 552 / 690, k4x2 450 / 629;  4 of 1000 to 1400, 4 heads: k2x2 101 / 125, k4x2 151 / 211
+//   16 histories of 2694 items under one or two queries, f16, d 80, all kernels: k2x2 116, k1x8 68;  2 of up to 1762, fp32, d 16: 141 and 89.
+enum { k4x1, k4x1Short, k2x1, k2x2, k4x2, k1x8 };
+__host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool f32, bool fits8) {
+  const int64_t rows = s->Tq * a.Hq, blocks = rows / 32 + (int64_t)s->B * a.Hk / 2, fill = rows / 128;
+  const bool narrow = a.d <= (f32 ? 64 : 96);
+  if (s->max_k <= 64) return f32 || fill < 512 ? k2x1 : k4x1Short;
+  if (fits8 && blocks <= 256 && s->max_k >= 512) return k1x8;
+  if (f32) {
+    if (fill >= (s->max_k > 256 ? 1024 : narrow ? 512 : 256)) return k2x1;
+    return s->max_k <= 256 || fill < (narrow ? 512 : 384) ? k2x2 : k4x2;
+  }
+  return s->max_k > 256 && fill < (narrow ? 512 : 256) ? k2x2 : k4x1;
 }
 
 template <int DT>
@@ -956,19 +969,18 @@ int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       return DLRM_OK;
     };
     constexpr bool F32 = DT == DLRM_F32, FITS8 = !F32 || dp() <= 64;
-    const int cut = cut_of(s, a, FITS8);
-    if (cut == kFewShort) return go(Int<2>{}, Int<1>{}, Int<1>{});
-    if (cut == kManyShort) return go(Int<4>{}, Int<1>{}, Int<1>{});
-    if (cut == kFew) return go(Int<2>{}, Int<2>{}, Int<1>{});
+    const int cut = cut_of(s, a, F32, FITS8);
+    if (cut == k2x1) return go(Int<2>{}, Int<1>{}, Int<1>{});
+    if (cut == k2x2) return go(Int<2>{}, Int<2>{}, Int<1>{});
     if constexpr (FITS8) {
-      if (cut == kFewest) return go(Int<1>{}, Int<8>{}, Int<1>{});
+      if (cut == k1x8) return go(Int<1>{}, Int<8>{}, Int<1>{});
     }
     if constexpr (F32) {
       return go(Int<4>{}, Int<2>{}, Int<1>{});
     } else {
       // Short histories of narrow rows: tiles of 32 keys leave registers for four workgroups a CU.  (2048 histories of up to 200 items, d 64:
       // 131 us, 143 with 64 keys; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
-      if (dp() <= 64 && s->max_k <= 256) return go(Int<4>{}, Int<1>{}, Int<1>{});
+      if (cut == k4x1Short || (dp() <= 64 && s->max_k <= 256)) return go(Int<4>{}, Int<1>{}, Int<1>{});
       return go(Int<4>{}, Int<1>{}, Int<2>{});
     }
   });
@@ -998,31 +1010,39 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     };
-    // (fp32 rows of 128 columns need more registers than eight wavefronts of a CU have)
-    constexpr bool WIDE_F32 = F32 && dp() > 96, FITS8 = !F32 || dp() <= 64;
-    const int cut = cut_of(s, a, FITS8);
+    // Four groups of fp32 rows of more than 64 columns need more registers than there are: 13 histories of up to 2000 items, 6 heads on 3, d 96: four
+    // of two parts 384 us, two of one 374; d 128: two of two parts 551, of one 484.  (Nor would the keys' gradients with 128 columns fit, below.)
+    constexpr bool WIDE = F32 && dp() > 64, WIDEST = F32 && dp() > 96, FITS8 = !F32 || dp() <= 64;
+    const int cut = cut_of(s, a, F32, FITS8);
     int rc = DLRM_OK;
-    if (cut == kFewShort || (WIDE_F32 && cut == kManyShort))
+    if (cut == k2x1 || (WIDE && cut == k4x2))
       rc = dq(Int<2>{}, Int<1>{});
-    else if (cut == kFew || (WIDE_F32 && cut == kMany))
+    else if (cut == k2x2)
       rc = dq(Int<2>{}, Int<2>{});
-    else if (cut == kFewest) {
+    else if (cut == k1x8) {
       if constexpr (FITS8) rc = dq(Int<1>{}, Int<8>{});
-    } else if constexpr (!WIDE_F32) {
-      if constexpr (F32) {
-        rc = cut == kManyShort ? dq(Int<4>{}, Int<1>{}) : dq(Int<4>{}, Int<2>{});
-      } else {
-        rc = dq(Int<4>{}, Int<1>{});
-      }
+    } else if constexpr (!WIDE) {
+      rc = dq(Int<4>{}, Int<F32 ? 2 : 1>{});
     }
     if (rc != DLRM_OK) return rc;
     a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
     // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
-    // of up to 200 items, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
+    // of up to 200 items, bf16, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
     // (No more than 32 keys: no wavefront without any.  259 histories of one item or none, fp32, d 88: two wavefronts 75 us, one 42.)
-    if (s->max_k <= 32 && short_walks(s)) return dkv(Int<1>{}, Int<1>{});
-    if (short_walks(s)) return dkv(Int<(!F32 && dp() > 64) ? 4 : 2>{}, Int<1>{});
-    return dkv(Int<F32 ? 2 : 4>{}, Int<2>{});
+    const bool is_short = short_walks(s);
+    if constexpr (!WIDEST) {
+      if (is_short && s->max_k <= 32) return dkv(Int<1>{}, Int<1>{});
+    }
+    if constexpr (!F32) {
+      return is_short ? dkv(Int<(dp() > 64) ? 4 : 2>{}, Int<1>{}) : dkv(Int<4>{}, Int<2>{});
+    } else {
+      // 64 histories of 1000 to 1400 items, 4 heads: halved 1203 us with d 64 and 1651 with 96, not halved 1074 and 1485; with 128 columns, which
+      // leave no registers for the loads of a whole tile by two wavefronts, 2111 and 2980.
+      if constexpr (!WIDEST) {
+        if (is_short || s->Tk * a.Hk >= 131072) return dkv(Int<2>{}, Int<1>{});
+      }
+      return dkv(Int<2>{}, Int<2>{});
+    }
   });
 }
 

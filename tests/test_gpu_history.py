@@ -260,6 +260,11 @@ SEQ = [
     ("f32", 64, 2, 2, [3, 40], [600, 31], False, False, False, 0.0, "rows"),
     ("f32", 88, 3, 3, [3, 40], [600, 1031], False, False, True, 0.0, "rows"),
     ("bf16", 16, 5, 1, [9], [4000], True, False, False, 15.0, "rows"),
+    # fp32: many rows, and long walks of not so many
+    ("f32", 128, 4, 4, [130] * 70 + [0, 3], None, True, False, True, 0.0, "rows"),
+    ("f32", 72, 4, 1, [100, 0, 255] * 60, None, True, True, False, 0.0, "packed"),
+    ("f32", 24, 32, 32, [2100, 40, 30], None, True, False, False, 5.0, "rows"),
+    ("f32", 96, 32, 16, [1599, 40, 30], None, True, False, False, 0.0, "rows"),
     # no more than one tile of keys
     ("f32", 88, 15, 3, [1, 0, 1, 1, 0] * 20, None, True, False, False, 0.0, "rows"),
     ("f32", 128, 2, 2, [64, 3, 0, 17], None, True, False, True, 0.0, "packed"),
