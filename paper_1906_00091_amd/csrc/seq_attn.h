@@ -883,15 +883,15 @@ __global__ __launch_bounds__(256) void seq_attn_join_kernel(SeqArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Grid for n items in B sequences of at most `longest`, `per` rows an item, blocks of `rows` rows (see find_block); false: too large
-__host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, int per, int rows) {
+// Grid for n items in B sequences of at most `longest`, `per` rows an item, workgroups of `threads` for `rows` rows (see find_block); false: too large
+__host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, int per, int rows, int threads) {
   if ((int64_t)longest * per > 0x7fffffff - 1024) return false;
   const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B, walks = (int64_t)a.Hk * a.splits;
   // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
   // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
   a.by_block = each * a.B <= 3 * slots && a.B <= 65535 && each <= 65535;
   grid = a.by_block ? dim3((unsigned)walks, a.B, (unsigned)each) : dim3((unsigned)(slots * walks), 1, 1);
-  return (a.by_block ? each * a.B : slots) * walks < (int64_t)1 << 23;  // fewer than 2^32 threads
+  return (a.by_block ? each * a.B : slots) * walks < ((int64_t)1 << 32) / threads;
 }
 
 // Calls f with the padded width and the kind of score as compile-time constants.
@@ -963,7 +963,7 @@ int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
     auto go = [&](auto groups, auto parts, auto sub) -> int {
       dim3 grid;
       if (s->Tq == 0) return DLRM_OK;
-      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), 64 * groups() * parts())) return DLRM_ERR_BAD_SHAPE;
       hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid, dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
@@ -993,7 +993,7 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
     auto dq = [&](auto groups, auto parts) -> int {
       dim3 grid;
       if (s->Tq == 0) return DLRM_OK;
-      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), 64 * groups() * parts())) return DLRM_ERR_BAD_SHAPE;
       hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), grid,
                          dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
@@ -1002,7 +1002,7 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
     auto dkv = [&](auto groups, auto parts) -> int {
       dim3 grid;
       if (s->Tk == 0) return DLRM_OK;
-      if (!blocks_of(a, grid, s->Tk, s->max_k, 1, 32 * groups())) return DLRM_ERR_BAD_SHAPE;
+      if (!blocks_of(a, grid, s->Tk, s->max_k, 1, 32 * groups(), 64 * groups() * parts())) return DLRM_ERR_BAD_SHAPE;
       hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(64 * groups() * parts()), 0, st, a);
       DLRM_CHECK_LAUNCH();
       if (a.splits == 1) return DLRM_OK;
