@@ -948,6 +948,10 @@ enum { k4x1, k4x1Short, k2x1, k2x2, k4x2, k1x8 };
 __host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool f32, bool fits8) {
   const int64_t rows = s->Tq * a.Hq, blocks = rows / 32 + (int64_t)s->B * a.Hk / 2, fill = rows / 128;
   const bool narrow = a.d <= (f32 ? 64 : 96);
+  // a tile's rows are reached with 32-bit byte offsets: the 256 keys of k1x8 where the items' strides leave them below 2^32 (the other cuts'
+  // tiles have 128 rows at most, of 2^25 bytes at most: check_heads)
+  const int64_t st = a.k.st > a.v.st ? a.k.st : a.v.st;
+  fits8 = fits8 && 255 * st + 512 < ((int64_t)1 << 32);
   if (s->max_k <= 64) return f32 || fill < 512 ? k2x1 : k4x1Short;
   if (fits8 && blocks <= 256 && s->max_k >= 512) return k1x8;
   if (f32) {
