@@ -77,6 +77,10 @@ __device__ inline void lane_angles(const RopeArgs& a, int64_t t, int col0, float
   }
 }
 
+// The partner's part of a column's sum: s p, or what leaves the column as it is, bit for bit, where it is not rotated.  (Zero times the partner would not:
+// an infinity, or the column itself where it has no partner, would come out as NaN.)
+__device__ inline float partner_term(float s, float p, int c, int rot) { return c < rot ? s * p : -0.0f; }
+
 // The partners of this lane's E columns in a row as it was loaded; xs: this wavefront's buffer in LDS (kHalfAny).
 template <int DT, int MODE>
 __device__ inline void partners(u32x4 raw, const float* x, float* p, int lane, int col0, int rot, float* xs) {
@@ -205,7 +209,7 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_fwd_kernel(RopeArgs a) {
         r = 1.0f / sqrtf(group_sum<G>(ss) * inv_d + a.eps);
       }
 #pragma unroll
-      for (int j = 0; j < E; ++j) y[j] = r * fmaf(c[j], x[j], s[j] * p[j]);
+      for (int j = 0; j < E; ++j) y[j] = r * fmaf(c[j], x[j], partner_term(s[j], p[j], col0 + j, a.rot));
       char* dst = to(h);
       if (in && dst) store16(dst + cb, narrow<DT>(y));
     }
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(kRopeThreads, 4) void qk_rope_bwd_kernel(RopeArgs a
         Tab<DT>::widen(rd, dy);
         partners<DT, MODE>(rd, dy, g, lane, col0, a.rot, xs);
 #pragma unroll
-        for (int j = 0; j < E; ++j) g[j] = fmaf(L.c[j], dy[j], L.s[j] * g[j]);
+        for (int j = 0; j < E; ++j) g[j] = fmaf(L.c[j], dy[j], partner_term(L.s[j], g[j], col0 + j, a.rot));
         if (wp != nullptr) {
           float ss = 0.0f, sg = 0.0f, gw[E];
 #pragma unroll

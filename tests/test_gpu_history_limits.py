@@ -58,3 +58,49 @@ def test_keys_a_large_stride_apart(dtype, d, stride, slopes):
     want = ref.attention(q, k, v, qo.cpu(), ko.cpu(), True, None, sl, d ** -0.5, 0.0, do)
     for n, x in (("out", O), ("lse", lse), ("dq", DQ), ("dk", DK), ("dv", DV)):
         ref.close(x, want[n], want[n + "_tol"], n)
+
+
+# ------------------------------------------------------------------------------------------------ columns that are not rotated
+def bits(x):
+    return x.contiguous().view(torch.int32 if x.dtype == torch.float32 else torch.int16)
+
+
+@pytest.mark.parametrize("layout", [hot.ROPE_HALF, hot.ROPE_INTERLEAVED])
+@pytest.mark.parametrize("dtype,d,rot", [("f32", 16, 0), ("f16", 72, 20), ("bf16", 72, 64), ("bf16", 128, 0), ("f32", 40, 6), ("f16", 64, 32), ("bf16", 16, 16)])
+def test_columns_past_the_rotated_ones_keep_every_value(dtype, d, rot, layout):
+    """Without a norm they are copied, forward and backward, whatever they hold and whatever their neighbours hold."""
+    dt, T, Hq, Hk = DT[dtype], 40, 3, 2
+    g = gen(d + rot)
+    x = [rand(g, T, H, d, dtype=dt) for H in (Hq, Hk)]
+    odd = torch.tensor([INF, -INF, NAN, -0.0, 0.0, torch.finfo(dt).max, torch.finfo(dt).tiny], dtype=dt)
+    for t in x:
+        at = torch.rand(t.shape, generator=g) < 0.3
+        at[..., :rot] = False                      # (rotated columns are finite: what they become has to stay so)
+        t[at] = odd[torch.randint(0, len(odd), (int(at.sum()),), generator=g)]
+    pos = torch.arange(T, dtype=torch.int32, device=DEV)
+    plan = hot.QkRope(pos, Hq, Hk, d, inv_freq=hot.rope_frequencies(rot, device=DEV) if rot else None, rot=rot, layout=layout, mscale=1.5)
+    X = [t.to(DEV) for t in x]
+    fwd, bwd = ([torch.zeros_like(t) for t in X] for _ in range(2))
+    hot.dlrm_qk_rope_fwd(plan, X[0], X[1], fwd[0], fwd[1])
+    hot.dlrm_qk_rope_bwd(plan, X[0], X[1], X[0], X[1], bwd[0], bwd[1], None, None, None)
+    for a, b, c in zip(x, fwd, bwd):
+        nan = a[..., rot:].isnan()                 # (of a NaN only that it is one)
+        for y in (b.cpu(), c.cpu()):
+            assert torch.equal(y[..., rot:].isnan(), nan)
+            assert torch.equal(bits(y[..., rot:])[~nan], bits(a[..., rot:])[~nan])
+            assert torch.isfinite(y[..., :rot]).all()
+
+
+@pytest.mark.parametrize("layout", [hot.ROPE_HALF, hot.ROPE_INTERLEAVED])
+def test_an_infinite_column_of_a_gradient_stays_in_its_column(layout):
+    """With a norm: dy infinite in a column past the rotated ones makes its row's mean infinite, so the row; no other row, and dw in its column alone."""
+    g, T, d, rot = gen(3), 9, 32, 8
+    x, dy = rand(g, T, 1, d), rand(g, T, 1, d)
+    dy[4, 0, 21] = INF
+    w = 1 + 0.1 * rand(g, d)
+    plan = hot.QkRope(torch.arange(T, dtype=torch.int32, device=DEV), 1, 0, d, inv_freq=hot.rope_frequencies(rot, device=DEV), wq=w.to(DEV), layout=layout)
+    dx, dw = torch.zeros(T, 1, d, device=DEV), torch.zeros(d, device=DEV)
+    hot.dlrm_qk_rope_bwd(plan, x.to(DEV), None, dy.to(DEV), None, dx, None, dw, None, hot.alloc_qk_rope_workspace(plan))
+    rows, cols = torch.arange(T) != 4, torch.arange(d) != 21
+    assert torch.isfinite(dx.cpu()[rows]).all() and torch.isfinite(dw.cpu()[cols]).all()
+    assert float(dw[21]) == math.copysign(INF, float(x[4, 0, 21]))
