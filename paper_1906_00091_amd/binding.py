@@ -473,13 +473,13 @@ class QkRope:
             T = positions.numel()
         self.T, self.Hq, self.Hk, self.d = int(T), Hq, Hk, d
         self.positions, self.inv_freq, self.wq, self.wk = positions, inv_freq, wq, wk
-        self.c = _QkRopeC(self.T, Hq, Hk, d, F32, rot, layout, _vector("QkRope", positions, self.T, torch.int32),
-                          _vector("QkRope", inv_freq, rot // 2, torch.float32), _vector("QkRope", wq, d, torch.float32),
-                          _vector("QkRope", wk, d, torch.float32), eps, mscale)
+        arrays = (_vector("QkRope", positions, self.T, torch.int32), _vector("QkRope", inv_freq, rot // 2, torch.float32),
+                  _vector("QkRope", wq, d, torch.float32), _vector("QkRope", wk, d, torch.float32))
+        # one struct for each storage type, none written again: calls of several threads may use the plan at once
+        self.c = {t: _QkRopeC(self.T, Hq, Hk, d, t, rot, layout, *arrays, eps, mscale) for t in _ELEM}
 
     def ref(self, dtype: int):
-        self.c.dtype = dtype
-        return C.byref(self.c)
+        return C.byref(self.c[dtype])
 
 
 def rope_frequencies(rot: int, base: float = 10000.0, stretch: float = 1.0, keep_turns: Optional[float] = None,
@@ -529,9 +529,8 @@ def dlrm_qk_rope_bwd(rope: QkRope, q: torch.Tensor, k: Optional[torch.Tensor], d
 
 
 def alloc_qk_rope_workspace(rope: QkRope) -> torch.Tensor:
-    n = int(lib().dlrm_qk_rope_bwd_workspace_bytes(rope.ref(rope.c.dtype)))
     # (sized for any storage type: the widest rows take the most groups)
-    n = max([n] + [int(lib().dlrm_qk_rope_bwd_workspace_bytes(rope.ref(t))) for t in (F32, F16, BF16)])
+    n = max(int(lib().dlrm_qk_rope_bwd_workspace_bytes(rope.ref(t))) for t in (F32, F16, BF16))
     if n == 0:
         raise DlrmError("dlrm_qk_rope_bwd_workspace_bytes", -2)
     device = next((x.device for x in (rope.positions, rope.wq, rope.wk) if x is not None), None)
@@ -582,15 +581,19 @@ class SeqBatch:
         if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
             raise ValueError("SeqBatch: slopes are contiguous float32, one for each query head")
         self.Tq, self.Tk = int(Tq), int(Tk)
-        self.c = _SeqBatchC(self.B, int(causal), self.Tq, self.Tk, max_q, max_k, _vector("SeqBatch", q_off, self.B + 1, torch.int64),
-                            _vector("SeqBatch", k_off, self.B + 1, torch.int64), _vector("SeqBatch", prefix, self.B, torch.int32),
-                            _ptr(slopes), 0.0, cap)
+        self.fields = (self.B, int(causal), self.Tq, self.Tk, max_q, max_k, _vector("SeqBatch", q_off, self.B + 1, torch.int64),
+                       _vector("SeqBatch", k_off, self.B + 1, torch.int64), _vector("SeqBatch", prefix, self.B, torch.int32), _ptr(slopes))
+        self.cap = cap
+        self.c = {}  # a struct for each width of the heads, written once: calls of several threads may use the plan at once
 
     def ref(self, Hq: int, d: int):
         if self.slopes is not None and self.slopes.numel() != Hq:
             raise ValueError("SeqBatch: %d slopes for %d query heads" % (self.slopes.numel(), Hq))
-        self.c.scale = d ** -0.5 if self.scale is None else self.scale
-        return C.byref(self.c)
+        c = self.c.get(d)
+        if c is None:
+            # (of two threads that come here at once one's struct is kept, and the other's, the same values, lives as long as its reference)
+            c = self.c[d] = _SeqBatchC(*self.fields, d ** -0.5 if self.scale is None else self.scale, self.cap)
+        return C.byref(c)
 
 
 def dlrm_seq_attn_fwd(seq: SeqBatch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None):
