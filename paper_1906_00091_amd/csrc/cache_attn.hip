@@ -35,7 +35,7 @@ struct CacheArgs {
   const int32_t* table;
   const int32_t* lens;
   const float* slopes;
-  int B, Hq, Hk, d, cols, n_pages, page_shift, max_len;
+  int B, Hq, Hk, d, cols, n_pages, page_shift, max_len;  // max_len: the table's items at most
   int chunk, splits, blocks;  // keys of a chunk; chunks of a sequence; groups of 16 heads of a key head
   float scale, cap;
   float* po;  // [B][Hq][splits][d] unnormalised sums
@@ -115,6 +115,9 @@ __device__ inline float bent16(float z) {
   }
 }
 
+// items of sequence s that are read
+__device__ inline int length_of(const CacheArgs& a, int s) { return max(0, min(a.lens[s], a.max_len)); }
+
 template <int DT, int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
   constexpr int EB = Tab<DT>::EB, E = Tab<DT>::ELEMS, STEPS = DP / 32, NB = DP / 16;
@@ -132,8 +135,9 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
   const int head = hk * G + blk * kHeads + n;  // of this lane's column
   const bool head_there = blk * kHeads + n < G;
   // the chunk's page numbers and the queries are loaded beside the length, not after it
+  // (Keys are counted from the chunk's start: a cache may hold up to 2^31 - 1 items, and a sum past its end would leave 32 bits.)
   const int start = split * a.chunk, page0 = start >> a.page_shift;
-  const int most_pages = min(((start + a.chunk - 1) >> a.page_shift) + 1, a.cols) - page0;
+  const int most_pages = min(((start + min(a.chunk, a.max_len - start) - 1) >> a.page_shift) + 1, a.cols) - page0;
   for (int p = threadIdx.x; p < most_pages; p += 64 * WAVES) pages[p] = a.table[(int64_t)s * a.cols + page0 + p];
   Op16<DT> qf[STEPS];
   const char* qrow = row_of(a.q, s, head_there ? head : hk * G);
@@ -145,18 +149,17 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
   const float c = a.scale * kLog2e, slope = a.slopes && head_there ? a.slopes[head] * kLog2e : 0.0f;
   const bool bend = a.cap > 0.0f;
   const float zs = bend ? a.scale / a.cap : 0.0f, cl = a.cap * kLog2e;
-  const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
-  const int end = min(len, start + a.chunk), last_page = max(page0, (end - 1) >> a.page_shift);
-  if (start >= end && split > 0) return;  // the first chunk of an empty sequence gives zeros
+  const int len = length_of(a, s), n_keys = min(len - start, a.chunk);
+  if (n_keys <= 0 && split > 0) return;  // the first chunk of an empty sequence gives zeros
   __syncthreads();
 
   const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;
   const int64_t head_bytes = (int64_t)row_bytes << a.page_shift, page_bytes = head_bytes * a.Hk;
-  // Byte offset of key j's row in the cache; a key past the end, or on a page that is not there, gives the first row of the cache and false.
+  // Byte offset of the row of the chunk's key i; a key past the end, or on a page that is not there, gives the first row of the cache and false.
   // No load stands in a branch (the wait for it would come with the branch's end): what came for no reason is masked where it is used.
-  auto row_at = [&](int j, bool& there) -> int64_t {
-    const int p = pages[min(j >> a.page_shift, last_page) - page0];
-    there = j < end && p >= 0 && p < a.n_pages;
+  auto row_at = [&](int i, bool& there) -> int64_t {
+    const int j = start + min(i, n_keys - 1), p = pages[(j >> a.page_shift) - page0];
+    there = i < n_keys && p >= 0 && p < a.n_pages;
     return there ? p * page_bytes + hk * head_bytes + (int64_t)((j & mask) * row_bytes) : 0;
   };
   char* vs = lds + wave * kKeys * STRIDE;
@@ -190,9 +193,10 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
 #pragma unroll
   for (int b = 0; b < NB; ++b) o[b] = f32x4{0, 0, 0, 0};
   float m = -kInf, l = 0.0f;
-  int j0 = start + wave * kKeys;
-  if (j0 < end) fetch(j0);
-  for (; j0 < end; j0 += WAVES * kKeys) {
+  const int to_newest = len - 1 - start;  // from the chunk's first key
+  int j0 = wave * kKeys;
+  if (j0 < n_keys) fetch(j0);
+  for (; j0 < n_keys; j0 += WAVES * kKeys) {
     f32x4 sc[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -208,7 +212,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
       *reinterpret_cast<u32x4*>(vs + (id / CH) * STRIDE + (id % CH) * 16) = v_there >> i & 1 ? vf[i] : u32x4{0, 0, 0, 0};
     }
     const int jn = j0 + WAVES * kKeys;
-    if (jn < end) fetch(jn);
+    if (jn < n_keys) fetch(jn);
     float x[8];
     float top = -kInf;
 #pragma unroll
@@ -218,7 +222,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
         const int key = 4 * g + r;
         float y = sc[u][r];
         y = bend ? bent16<DT>(y * zs) * cl : y * c;
-        y -= slope * (float)(len - 1 - (j0 + 16 * u + key));
+        y -= slope * (float)(to_newest - (j0 + 16 * u + key));
         x[4 * u + r] = ((u ? have1 : have0) >> key) & 1 ? y : -kInf;
         top = fmaxf(top, x[4 * u + r]);
       }
@@ -322,8 +326,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
   __shared__ float factor[kJoinThreads];
   const int64_t row = blockIdx.x;
   const int s = (int)(row / a.Hq), head = (int)(row - (int64_t)s * a.Hq);
-  const int len = min(min(a.lens[s], a.max_len), a.cols << a.page_shift);
-  const int n = max(1, (len + a.chunk - 1) / a.chunk);
+  const int len = length_of(a, s), n = len > 0 ? (len - 1) / a.chunk + 1 : 1;
   const float* pm = a.pm + row * a.splits * 2;
   const float* po = a.po + row * a.splits * a.d;
   const int y = threadIdx.x >> 5, col = (threadIdx.x & 31) * 4, wave = wave_id();
@@ -409,7 +412,7 @@ static int splits_of(const dlrm_kv_cache* c, int Hq, int max_len) {
   const int64_t held = (int64_t)c->table_cols * c->page;
   if (max_len > held) max_len = (int)held;
   const int n = chunk_of(c, Hq, max_len);
-  return (max_len + n - 1) / n;
+  return (max_len - 1) / n + 1;
 }
 
 }  // namespace dlrm
@@ -449,7 +452,7 @@ extern "C" int32_t dlrm_cache_attn(const dlrm_kv_cache* c, const int32_t* lens, 
   const int64_t held = (int64_t)c->table_cols * c->page;
   a.max_len = max_len > held ? (int)held : max_len;
   a.chunk = chunk_of(c, Hq, a.max_len);
-  a.splits = (a.max_len + a.chunk - 1) / a.chunk;
+  a.splits = (a.max_len - 1) / a.chunk + 1;
   a.blocks = (Hq / c->Hk + kHeads - 1) / kHeads;
   a.scale = scale;
   a.cap = cap;

@@ -104,3 +104,33 @@ def test_an_infinite_column_of_a_gradient_stays_in_its_column(layout):
     rows, cols = torch.arange(T) != 4, torch.arange(d) != 21
     assert torch.isfinite(dx.cpu()[rows]).all() and torch.isfinite(dw.cpu()[cols]).all()
     assert float(dw[21]) == math.copysign(INF, float(x[4, 0, 21]))
+
+
+# ------------------------------------------------------------------------------------------------ the longest caches
+@pytest.mark.parametrize("page,cols,last", [(1024, (1 << 21) - 1, 1100), (1, (1 << 31) - 1, 700), (128, 1 << 23, 5)])
+def test_the_last_chunk_of_a_cache_of_two_billion_items(page, cols, last):
+    """One sequence whose table names the same two pages again and again: page 1 for the `last` columns, page 0 for all before.  The last ones' keys
+    carry half of the weight, so a chunk that is left out shows.  (128 x 2^23 items: 2^30, a length that divides.)"""
+    g, dt, H, d = gen(cols % 97), torch.float16, 1, 8
+    k, v = (rand(g, 2, H, page, d, dtype=dt) for _ in range(2))
+    k[..., 0] = 0.0
+    q = torch.zeros(1, H, d, dtype=dt)
+    q[0, 0, 0] = 1.0                                           # the score is scale times the key's first column
+    n = [(cols - last) * page, last * page]
+    k[1, :, :, 0] = math.log(n[0] / n[1])                      # (rounded to the type: the reference takes what it became)
+    v[1] += 4.0
+    table = torch.zeros(1, cols, dtype=torch.int32, device=DEV)
+    table[0, -last:] = 1
+    cache = hot.KvCache(k.to(DEV), v.to(DEV), table)
+    held = cols * page
+    out = torch.full((1, H, d), NAN, dtype=dt, device=DEV)
+    hot.dlrm_cache_attn(cache, torch.tensor([held], dtype=torch.int32, device=DEV), held, q.to(DEV), out, hot.alloc_cache_attn_workspace(cache, H, held), scale=1.0)
+    sc = k[:, 0, :, 0].double()                                # [page 0 or 1, item]
+    w = torch.exp(sc - sc.max()) * torch.tensor(n, dtype=torch.float64)[:, None] / page
+    p = w / w.sum()
+    want, mags = (p[..., None] * v[:, 0].double()).sum((0, 1)), (p[..., None] * v[:, 0].double().abs()).sum((0, 1))
+    # fp32 sums: a lane adds 8 weights a step, a chunk of 2^20 keys is 8192 steps of its four wavefronts, and a sequence up to 2^21 chunks
+    # that 512 threads add: at most 2^16 + 2^12 + 600 roundings on any path, in numerator and denominator each; the type's two roundings
+    tol = ref.UNIT[dt] * want.abs() + (ref.UNIT[dt] + 2 * (2 ** 16 + 2 ** 12 + 600) * ref.E32) * mags
+    ref.close(out[0, 0], want, tol, "out")
+    assert float(want.min()) > 1.0                             # (half of 4: without the last chunk the values' mean is near 0)
