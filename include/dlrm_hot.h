@@ -517,7 +517,8 @@ int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int
                           const float* lse, const dlrm_heads* dout, const dlrm_heads* dq, const dlrm_heads* dk,
                           const dlrm_heads* dv, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace dlrm_cache_attn needs for up to max_len cached items a sequence; 0 for an unsupported shape. */
+/* Bytes of workspace dlrm_cache_attn needs for up to max_len cached items a sequence, whatever smaller max_len a call then has; 0 for an
+ * unsupported shape. */
 size_t dlrm_cache_attn_workspace_bytes(const dlrm_kv_cache* cache, int32_t Hq, int32_t max_len);
 
 /*

@@ -389,15 +389,14 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
 // Keys of a chunk: 1024 workgroups, four a CU, and at least two tiles a wavefront.  (The 256 sequences above: 436 us with chunks for 1024 workgroups,
 // 474 for 2048, 498 for 4096, 537 for 8192, whose joins read more.  One sequence of 131072 items on 4 key heads, four workgroups if it were not
 // split: 48 us with its join.)
+constexpr int kWanted = 1024, kLeastChunk = 256;
+static int64_t groups_of(const dlrm_kv_cache* c, int Hq) { return (int64_t)c->B * c->Hk * ((Hq / c->Hk + kHeads - 1) / kHeads); }
+static int64_t most_of_chunk(const dlrm_kv_cache* c) { return (int64_t)(kTablePages - 1) * c->page; }  // (it need not start on a page)
 static int chunk_of(const dlrm_kv_cache* c, int Hq, int max_len) {
-  const int64_t rows = (int64_t)c->B * c->Hk * ((Hq / c->Hk + kHeads - 1) / kHeads);
-  const int64_t wanted = 1024;
-  int64_t n = (rows * max_len + wanted - 1) / wanted;
-  if (n < 256) n = 256;
-  const int64_t most = (int64_t)kTablePages * c->page;  // a chunk starts on a page where it is a multiple of the page
+  int64_t n = (groups_of(c, Hq) * max_len + kWanted - 1) / kWanted;
+  if (n < kLeastChunk) n = kLeastChunk;
   n = (n + 127) / 128 * 128;
-  if (n > most - c->page) n = most - c->page;
-  if (n < 1) n = 1;
+  if (n > most_of_chunk(c)) n = most_of_chunk(c);
   return (int)(n > max_len ? max_len : n);
 }
 
@@ -408,11 +407,14 @@ static int check_cache_attn(const dlrm_kv_cache* c, int Hq, int max_len) {
   return DLRM_OK;
 }
 
-static int splits_of(const dlrm_kv_cache* c, int Hq, int max_len) {
-  const int64_t held = (int64_t)c->table_cols * c->page;
-  if (max_len > held) max_len = (int)held;
-  const int n = chunk_of(c, Hq, max_len);
-  return (max_len - 1) / n + 1;
+// The most chunks that a bound of up to max_len gives a sequence.  (Chunks are rounded up, so a smaller bound may give more of them than max_len: 8
+// sequences, 16 query heads on 4, 33 chunks for 8256 items and 48 for 8000.)  A chunk has the fewest keys there are, as many as a page table's piece holds, or
+// enough for kWanted workgroups.
+static int64_t most_splits(const dlrm_kv_cache* c, int Hq, int max_len) {
+  const int64_t held = (int64_t)c->table_cols * c->page, n = max_len > held ? held : max_len;
+  const int64_t short_chunks = (n - 1) / kLeastChunk + 1, table_pieces = (n - 1) / most_of_chunk(c) + 1;
+  const int64_t workgroups = (kWanted - 1) / groups_of(c, Hq) + 1, most = workgroups > table_pieces ? workgroups : table_pieces;
+  return short_chunks < most ? short_chunks : most;
 }
 
 }  // namespace dlrm
@@ -421,7 +423,7 @@ using namespace dlrm;
 
 extern "C" size_t dlrm_cache_attn_workspace_bytes(const dlrm_kv_cache* c, int32_t Hq, int32_t max_len) {
   if (check_cache_attn(c, Hq, max_len) != DLRM_OK) return 0;
-  const size_t n = (size_t)c->B * Hq * splits_of(c, Hq, max_len) * (c->d + 2) * sizeof(float);
+  const size_t n = (size_t)c->B * Hq * most_splits(c, Hq, max_len) * (c->d + 2) * sizeof(float);
   return (n + 255) / 256 * 256;
 }
 

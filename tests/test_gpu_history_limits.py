@@ -134,3 +134,18 @@ def test_the_last_chunk_of_a_cache_of_two_billion_items(page, cols, last):
     tol = ref.UNIT[dt] * want.abs() + (ref.UNIT[dt] + 2 * (2 ** 16 + 2 ** 12 + 600) * ref.E32) * mags
     ref.close(out[0, 0], want, tol, "out")
     assert float(want.min()) > 1.0                             # (half of 4: without the last chunk the values' mean is near 0)
+
+
+def test_one_workspace_for_every_smaller_bound():
+    """A server's workspace, allocated for its longest history, with the bound of each call."""
+    g, B, Hq, Hk, d, page, top = gen(19), 8, 16, 4, 128, 64, 8256
+    cols = top // page
+    k, v = (torch.randn(B * cols, Hk, page, d, device=DEV).to(torch.bfloat16) for _ in range(2))
+    cache = hot.KvCache(k, v, torch.randperm(B * cols, generator=g).to(torch.int32).view(B, cols).to(DEV))
+    q = rand(g, B, Hq, d, dtype=torch.bfloat16).to(DEV)
+    ws = hot.alloc_cache_attn_workspace(cache, Hq, top)
+    for n in (8000, 8256, 1, 300, 4100, 8192):
+        lens, out, own = torch.full((B,), n, dtype=torch.int32, device=DEV), torch.empty_like(q), torch.empty_like(q)
+        hot.dlrm_cache_attn(cache, lens, n, q, out, ws)
+        hot.dlrm_cache_attn(cache, lens, n, q, own, hot.alloc_cache_attn_workspace(cache, Hq, n))
+        assert torch.equal(out, own) and torch.isfinite(out).all()
