@@ -5,6 +5,8 @@
 
 namespace dlrm {
 
+constexpr int64_t kLaunchThreads = (int64_t)1 << 31;  // of one launch at most, where a call may need several (the device's limit: 2^32 - 1)
+
 // one dlrm_heads on its way to a kernel, strides in bytes
 struct Rows {
   char* p;

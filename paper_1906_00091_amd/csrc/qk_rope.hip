@@ -452,16 +452,31 @@ static int head_splits(const dlrm_qk_rope* r, int heads) {
   return (int)(s < 1 ? 1 : s > heads ? heads : s);
 }
 
+// the forward's arguments for n items from item t0 on
+static RopeArgs items_of(RopeArgs a, int64_t t0, int64_t n) {
+  for (Rows* x : {&a.q, &a.k, &a.v, &a.qo, &a.ko})
+    if (x->p) x->p += t0 * x->st;
+  if (a.pos) a.pos += t0;
+  if (a.seqs) a.seqs += t0;
+  a.T = n;
+  return a;
+}
+
 template <bool CACHE>
 static int launch_fwd(const dlrm_qk_rope* r, RopeArgs a, hipStream_t st) {
   if (r->T == 0) return DLRM_OK;
   a.splits = head_splits(r, r->Hq + r->Hk * (CACHE ? 2 : 1));
   a.shift_v = r->Hk % a.splits;
-  const int64_t blocks = (r->T * a.splits * group_lanes(r) + kRopeThreads - 1) / kRopeThreads;
-  if (blocks > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;
+  const int lanes = a.splits * group_lanes(r);  // of an item
   return for_row_kind(r, a, [&](auto dt, auto md, auto g, auto split) {
-    hipLaunchKernelGGL((qk_rope_fwd_kernel<dt(), md(), g(), split(), CACHE>), dim3((unsigned)blocks), dim3(kRopeThreads), 0, st, a);
-    DLRM_CHECK_LAUNCH();
+    // a launch takes fewer than 2^32 threads: more items than that go in several
+    const int64_t each = kLaunchThreads / lanes;
+    for (int64_t t0 = 0; t0 < r->T; t0 += each) {
+      const RopeArgs b = items_of(a, t0, r->T - t0 < each ? r->T - t0 : each);
+      hipLaunchKernelGGL((qk_rope_fwd_kernel<dt(), md(), g(), split(), CACHE>), dim3((unsigned)((b.T * lanes + kRopeThreads - 1) / kRopeThreads)),
+                         dim3(kRopeThreads), 0, st, b);
+      DLRM_CHECK_LAUNCH();
+    }
     return (int)DLRM_OK;
   });
 }

@@ -149,3 +149,41 @@ def test_one_workspace_for_every_smaller_bound():
         hot.dlrm_cache_attn(cache, lens, n, q, out, ws)
         hot.dlrm_cache_attn(cache, lens, n, q, own, hot.alloc_cache_attn_workspace(cache, Hq, n))
         assert torch.equal(out, own) and torch.isfinite(out).all()
+
+
+# ------------------------------------------------------------------------------------------------ more threads than a launch takes
+def test_more_rows_than_one_launch_has_threads_for():
+    """2^28 rows of 72 bf16 columns are 2^32 lanes.  Rows and positions repeat, so the result does: it is compared, bit for bit, with a small call's."""
+    d, P, T, dt = 72, 1 << 16, (1 << 28) + 70003, torch.bfloat16
+    block = torch.randn(P, 1, d, device=DEV).to(dt)
+    pos = (torch.arange(T, device=DEV, dtype=torch.int32) & (P - 1))
+    w, f = torch.linspace(0.5, 1.5, d, device=DEV), hot.rope_frequencies(64, device=DEV)
+    want = torch.empty_like(block)
+    hot.dlrm_qk_rope_fwd(hot.QkRope(pos[:P], 1, 0, d, inv_freq=f, wq=w), block, None, want, None)
+    x = torch.empty(T, 1, d, dtype=dt, device=DEV)
+    for t in range(0, T, P):
+        x[t:t + P] = block[:min(P, T - t)]
+    hot.dlrm_qk_rope_fwd(hot.QkRope(pos, 1, 0, d, inv_freq=f, wq=w), x, None, x, None)
+    bad = torch.zeros((), dtype=torch.int64, device=DEV)
+    for t in range(0, T, P):
+        bad += (x[t:t + P] != want[:min(P, T - t)]).any()
+    assert int(bad) == 0
+
+
+def test_more_appended_items_than_one_launch_has_threads_for():
+    """2^28 items of one query, key and value of 72 bf16 columns, in sequences of 64.  The first and the last thousand sequences have pages, the others none."""
+    d, n_items, dt, page = 72, (1 << 28) + 6400, torch.bfloat16, 64
+    B = n_items // page
+    x = torch.randn(n_items, 1, 1, dtype=dt, device=DEV).expand(n_items, 1, 8).repeat(1, 1, 9)       # every row one value
+    pos = torch.arange(n_items, device=DEV, dtype=torch.int32) & (page - 1)
+    seqs = (torch.arange(n_items, device=DEV, dtype=torch.int32) >> 6)
+    table = torch.full((B, 1), -1, dtype=torch.int32, device=DEV)
+    table[:1000, 0] = torch.arange(1000, device=DEV, dtype=torch.int32)
+    table[-1000:, 0] = torch.arange(1000, 2000, device=DEV, dtype=torch.int32)
+    pool = torch.full((2, 2000, 1, page, d), 7.0, dtype=dt, device=DEV)
+    plan = hot.QkRope(pos, 1, 1, d)
+    q = torch.zeros(n_items, 1, d, dtype=dt, device=DEV)
+    hot.dlrm_qk_rope_append(plan, q, x, x, q, hot.KvCache(pool[0], pool[1], table), seqs)
+    for half, rows in ((slice(0, 1000), x[:64000]), (slice(1000, 2000), x[-64000:])):
+        for p in pool:
+            assert torch.equal(p[half].reshape(-1, 1, d), rows)
