@@ -526,7 +526,8 @@ size_t dlrm_cache_attn_workspace_bytes(const dlrm_kv_cache* cache, int32_t Hq, i
  * (its newest at lens[s] - 1, where the query stands).  Scores as for dlrm_seq_batch.  lens[s] <= 0 gives zeros; a length above
  * max_len or above the table's pages counts as that.  max_len: host upper bound on lens, >= 1.
  * The length is split over workgroups and their parts are joined by a second launch where one workgroup per sequence and key
- * head would leave the device empty.  slopes: [Hq] or NULL.  workspace: 256-byte aligned device memory; contents are scratch.
+ * head would leave the device empty.  One sequence may take up to 2^23 workgroups, its chunks (1024 at most, or one for every 1023 pages) times
+ * its key heads; more is DLRM_ERR_BAD_SHAPE.  slopes: [Hq] or NULL.  workspace: 256-byte aligned device memory; contents are scratch.
  */
 int32_t dlrm_cache_attn(const dlrm_kv_cache* cache, const int32_t* lens, int32_t max_len, int32_t Hq,
                         const dlrm_heads* q, const dlrm_heads* out, const float* slopes, float scale, float cap,

@@ -400,6 +400,20 @@ static int chunk_of(const dlrm_kv_cache* c, int Hq, int max_len) {
   return (int)(n > max_len ? max_len : n);
 }
 
+// the arguments for n sequences from sequence s0 on
+static CacheArgs sequences_of(CacheArgs a, int64_t s0, int64_t n) {
+  a.q.p += s0 * a.q.st;
+  a.out.p += s0 * a.out.st;
+  a.table += s0 * a.cols;
+  a.lens += s0;
+  if (a.po) {
+    a.po += s0 * a.Hq * a.splits * a.d;
+    a.pm += s0 * a.Hq * a.splits * 2;
+  }
+  a.B = (int)n;
+  return a;
+}
+
 static int check_cache_attn(const dlrm_kv_cache* c, int Hq, int max_len) {
   if (int st = check_cache(c)) return st;
   if (int st = check_head_shape(Hq, c->Hk, c->d, c->dtype)) return st;
@@ -458,8 +472,12 @@ extern "C" int32_t dlrm_cache_attn(const dlrm_kv_cache* c, const int32_t* lens, 
   a.blocks = (Hq / c->Hk + kHeads - 1) / kHeads;
   a.scale = scale;
   a.cap = cap;
-  const int64_t grid = (int64_t)a.splits * a.blocks * a.Hk * a.B;
-  if (grid > 0x7fffffff || (int64_t)a.B * Hq > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;
+  // a launch takes fewer than 2^32 threads: more sequences than that go in several
+  const int64_t per_seq = (int64_t)a.splits * a.blocks * a.Hk, join_per_seq = a.splits > 1 ? Hq : 0;
+  const int64_t most = 256 * per_seq > kJoinThreads * join_per_seq ? 256 * per_seq : kJoinThreads * join_per_seq;
+  const int64_t each = kLaunchThreads / most;
+  if (each == 0) return DLRM_ERR_BAD_SHAPE;
+  const int64_t grid = per_seq * a.B;
   if (a.splits > 1) {
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < dlrm_cache_attn_workspace_bytes(c, Hq, max_len))
       return DLRM_ERR_WORKSPACE;
@@ -473,14 +491,18 @@ extern "C" int32_t dlrm_cache_attn(const dlrm_kv_cache* c, const int32_t* lens, 
   hipStream_t st = static_cast<hipStream_t>(stream);
   auto by_type = [&](auto dt) {
     auto go = [&](auto dp) {
-      if (one_wave)
-        hipLaunchKernelGGL((cache_attn_kernel<dt(), dp(), 1>), dim3((unsigned)grid), dim3(64), 0, st, a);
-      else
-        hipLaunchKernelGGL((cache_attn_kernel<dt(), dp(), 4>), dim3((unsigned)grid), dim3(256), 0, st, a);
-      DLRM_CHECK_LAUNCH();
-      if (a.splits > 1) {
-        hipLaunchKernelGGL(cache_join_kernel<dt()>, dim3((unsigned)(a.B * Hq)), dim3(kJoinThreads), 0, st, a);
+      for (int64_t s0 = 0; s0 < a.B; s0 += each) {
+        const CacheArgs b = sequences_of(a, s0, a.B - s0 < each ? a.B - s0 : each);
+        const unsigned n = (unsigned)(per_seq * b.B);
+        if (one_wave)
+          hipLaunchKernelGGL((cache_attn_kernel<dt(), dp(), 1>), dim3(n), dim3(64), 0, st, b);
+        else
+          hipLaunchKernelGGL((cache_attn_kernel<dt(), dp(), 4>), dim3(n), dim3(256), 0, st, b);
         DLRM_CHECK_LAUNCH();
+        if (a.splits > 1) {
+          hipLaunchKernelGGL(cache_join_kernel<dt()>, dim3((unsigned)(b.B * Hq)), dim3(kJoinThreads), 0, st, b);
+          DLRM_CHECK_LAUNCH();
+        }
       }
       return (int)DLRM_OK;
     };

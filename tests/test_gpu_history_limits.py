@@ -187,3 +187,31 @@ def test_more_appended_items_than_one_launch_has_threads_for():
     for half, rows in ((slice(0, 1000), x[:64000]), (slice(1000, 2000), x[-64000:])):
         for p in pool:
             assert torch.equal(p[half].reshape(-1, 1, d), rows)
+
+
+@pytest.mark.parametrize("B,top,page,Hq,Hk,slopes", [((1 << 21) + 301, 512, 512, 8, 8, False), ((1 << 23) + 301, 16, 16, 8, 8, True), ((700 << 10) + 77, 2100, 1, 24, 8, False)])
+def test_more_sequences_than_one_launch_has_threads_for(B, top, page, Hq, Hk, slopes):
+    """Of four wavefronts each, of one, and in three chunks with a join.  Queries, lengths and tables repeat, so the result does: it is compared with a
+    small call's."""
+    g, d, P, dt, cols = gen(B % 1000), 8, 4096, torch.bfloat16, (top + page - 1) // page
+    k, v = (torch.randn(4 * cols, Hk, page, d, device=DEV).to(dt) for _ in range(2))
+    table = (torch.arange(P)[:, None] % 4 * cols + torch.arange(cols)).to(torch.int32).to(DEV)
+    lens = torch.randint(0, 4, (P,), generator=g).to(torch.int32)
+    lens[5::977] = top                                         # a few long ones: their walks and joins are whole
+    lens = lens.to(DEV)
+    q = torch.randn(P, Hq, d, device=DEV).to(dt)
+    sl = torch.linspace(0.1, 1.0, Hq, device=DEV) if slopes else None
+    n = (B + P - 1) // P
+    cache = hot.KvCache(k, v, table.repeat(n, 1)[:B].contiguous())
+    Q = q.repeat(n, 1, 1)[:B].contiguous()
+    out = torch.full_like(Q, NAN)
+    hot.dlrm_cache_attn(cache, lens.repeat(n)[:B].contiguous(), top, Q, out, hot.alloc_cache_attn_workspace(cache, Hq, top), slopes=sl)
+    part = out[:P].float()
+    for s in range(0, B, P):
+        assert torch.equal(out[s:s + P], out[:min(P, B - s)])
+    small = torch.empty_like(q)
+    c = hot.KvCache(k, v, table)
+    hot.dlrm_cache_attn(c, lens, top, q, small, hot.alloc_cache_attn_workspace(c, Hq, top), slopes=sl)
+    # (the small call may be cut otherwise: fp32 sums in another order, weights rounded from another maximum, one rounding of the result)
+    off = (part - small.float()).abs()
+    assert float((off - 4 * ref.UNIT[dt] * v.float().abs().max()).max()) <= 0 and float(part.abs().sum()) > 0

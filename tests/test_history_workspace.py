@@ -29,3 +29,14 @@ def test_lengths_whose_chunks_are_rounded_up(shape, lengths):
     """Pairs where the shorter bound is cut into more chunks than the longer one."""
     a, b = (need(*shape, n, cols=1 << 14) for n in lengths)
     assert b >= a
+
+
+def test_a_sequence_of_too_many_workgroups_is_refused():
+    """2^31 - 1 pages of one item and 16 key heads: 2^21 chunks times 16.  With 2 key heads the call is refused for its missing workspace alone."""
+    class HeadsC(C.Structure):
+        _fields_ = [("data", C.c_void_p), ("stride_t", C.c_int64), ("stride_h", C.c_int64)]
+    top = (1 << 31) - 1
+    for Hk, status in ((16, -2), (2, -4)):
+        c = binding._KvCacheC(0x10000, 0x10000, 0x10000, 1, top, 4, 1, Hk, 8, hot.BF16)
+        x = C.byref(HeadsC(0x10000, Hk * 8, 8))
+        assert hot.lib().dlrm_cache_attn(C.byref(c), 0x10000, top, Hk, x, x, None, 1.0, 0.0, None, 0, None) == status
