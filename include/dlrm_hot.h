@@ -486,7 +486,8 @@ typedef struct dlrm_seq_batch {
   int32_t B;             /* sequences, >= 1 */
   int32_t causal;        /* 0 or 1 */
   int64_t Tq, Tk;        /* host copies of q_off[B], k_off[B] */
-  int32_t max_q, max_k;  /* host upper bounds on a sequence's query / key items, >= 0 */
+  int32_t max_q, max_k;  /* host upper bounds on a sequence's query / key items, >= 0; loose ones (above Tq, Tk they count as these) may run slower.
+                          * max_q times the query heads of a key head, and max_k, <= 2^31 - 1025 */
   const int64_t* q_off;  /* [B+1], q_off[0] = 0, ascending */
   const int64_t* k_off;  /* [B+1]; the same array as q_off where every item attends over its own sequence */
   const int32_t* prefix; /* [B] or NULL; only with causal */

@@ -885,7 +885,6 @@ __global__ __launch_bounds__(256) void seq_attn_join_kernel(SeqArgs a) {
 // ---------------------------------------------------------------------------------------------------------------
 // Grid for n items in B sequences of at most `longest`, `per` rows an item, workgroups of `threads` for `rows` rows (see find_block); false: too large
 __host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, int per, int rows, int threads) {
-  if ((int64_t)longest * per > 0x7fffffff - 1024) return false;
   const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B, walks = (int64_t)a.Hk * a.splits;
   // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
   // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).

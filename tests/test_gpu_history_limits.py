@@ -215,3 +215,22 @@ def test_more_sequences_than_one_launch_has_threads_for(B, top, page, Hq, Hk, sl
     # (the small call may be cut otherwise: fp32 sums in another order, weights rounded from another maximum, one rounding of the result)
     off = (part - small.float()).abs()
     assert float((off - 4 * ref.UNIT[dt] * v.float().abs().max()).max()) <= 0 and float(part.abs().sum()) > 0
+
+
+# ------------------------------------------------------------------------------------------------ sequences: bounds
+@pytest.mark.parametrize("dtype,d,Hq,Hk", [("bf16", 64, 4, 2), ("f32", 32, 2, 2)])
+def test_bounds_that_say_nothing(dtype, d, Hq, Hk):
+    """2^31 - 1 for both: the results of exact bounds."""
+    g, dt, lens = gen(5), DT[dtype], [70, 0, 300, 1]
+    off, T = ref.offsets(lens).to(DEV), sum(lens)
+    q, do = (rand(g, T, Hq, d, dtype=dt).to(DEV) for _ in range(2))
+    k, v = (rand(g, T, Hk, d, dtype=dt).to(DEV) for _ in range(2))
+    want = ref.attention(q.cpu(), k.cpu(), v.cpu(), off.cpu(), off.cpu(), True, None, None, d ** -0.5, 0.0, do.cpu())
+    for top in ((1 << 31) - 1, 300):
+        seq = hot.SeqBatch(off, off, T, T, top, top)
+        out, dq, dk, dv = (torch.full_like(x, NAN) for x in (q, q, k, v))
+        lse = torch.empty(Hq, T, device=DEV)
+        hot.dlrm_seq_attn_fwd(seq, q, k, v, out, lse)
+        hot.dlrm_seq_attn_bwd(seq, q, k, v, out, lse, do, dq, dk, dv, hot.alloc_seq_attn_workspace(seq, Hq, Hk, d))
+        for n, x in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+            ref.close(x, want[n], want[n + "_tol"], n)
