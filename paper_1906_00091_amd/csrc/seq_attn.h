@@ -174,6 +174,7 @@ struct SeqArgs {
   int B, Hq, Hk, d, causal;
   int splits;    // workgroups that share a block of rows (keys' gradients)
   int by_block;  // the grid is (walk, sequence, block), else walks times slots
+  int slots, slot0;  // slots in all, and the first of this launch
   float scale, cap;
 };
 
@@ -182,7 +183,7 @@ struct SeqArgs {
 // Where all sequences fit into few blocks the grid is (walk, sequence, block), as many blocks as the longest may need: block by block
 // through all sequences, so with causal sequences the blocks of most work of every one of them start first.  Else it is walks times
 // slots: sequence s starts at slot off[s] * per / ROWS + s, which leaves it enough, and is found by all 64 lanes at once, each step
-// asking 64 places.  Workgroups past a sequence's rows end at once.
+// asking 64 places; more slots than a launch has threads for go in several.  Workgroups past a sequence's rows end at once.
 template <int ROWS>
 __device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per, bool last_first, int& walk, int& seq, int& row0) {
   const int walks = a.Hk * a.splits;
@@ -194,7 +195,7 @@ __device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per,
     row0 = (last_first ? gridDim.z - 1 - blockIdx.z : blockIdx.z) * ROWS;
     return;
   }
-  const int at = blockIdx.x / walks, slot = last_first ? gridDim.x / walks - 1 - at : at;
+  const int at = blockIdx.x / walks, slot = last_first ? a.slots - 1 - (a.slot0 + at) : a.slot0 + at;
   walk = blockIdx.x - at * walks;
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
@@ -883,14 +884,23 @@ __global__ __launch_bounds__(256) void seq_attn_join_kernel(SeqArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Grid for n items in B sequences of at most `longest`, `per` rows an item, workgroups of `threads` for `rows` rows (see find_block); false: too large
-__host__ inline bool blocks_of(SeqArgs& a, dim3& grid, int64_t n, int longest, int per, int rows, int threads) {
+// Launches for n items in B sequences of at most `longest`, `per` rows an item, workgroups of `threads` for `rows` rows (see find_block): calls
+// launch(grid), a.slot0 set, as often as it takes.
+template <typename F>
+__host__ inline int for_blocks(SeqArgs& a, int64_t n, int longest, int per, int rows, int threads, F launch) {
   const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B, walks = (int64_t)a.Hk * a.splits;
+  const int64_t most = kLaunchThreads / (threads * walks);  // slots of a launch
   // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
   // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
-  a.by_block = each * a.B <= 3 * slots && a.B <= 65535 && each <= 65535;
-  grid = a.by_block ? dim3((unsigned)walks, a.B, (unsigned)each) : dim3((unsigned)(slots * walks), 1, 1);
-  return (a.by_block ? each * a.B : slots) * walks < ((int64_t)1 << 32) / threads;
+  a.by_block = each * a.B <= 3 * slots && a.B <= 65535 && each <= 65535 && each * a.B <= most;
+  if (a.by_block) return launch(dim3((unsigned)walks, a.B, (unsigned)each));
+  if (slots > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;  // (of 32 rows at least: more than the memory has)
+  a.slots = (int)slots;
+  for (int64_t at = 0; at < slots; at += most) {
+    a.slot0 = (int)at;
+    if (int st = launch(dim3((unsigned)((slots - at < most ? slots - at : most) * walks)))) return st;
+  }
+  return DLRM_OK;
 }
 
 // Calls f with the padded width and the kind of score as compile-time constants.
@@ -964,12 +974,13 @@ template <int DT>
 int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
   return for_kind(a, [&](auto dp, auto kind) -> int {
     auto go = [&](auto groups, auto parts, auto sub) -> int {
-      dim3 grid;
       if (s->Tq == 0) return DLRM_OK;
-      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), 64 * groups() * parts())) return DLRM_ERR_BAD_SHAPE;
-      hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid, dim3(64 * groups() * parts()), 0, st, a);
-      DLRM_CHECK_LAUNCH();
-      return DLRM_OK;
+      constexpr int threads = 64 * groups() * parts();
+      return for_blocks(a, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), threads, [&](dim3 grid) -> int {
+        hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid, dim3(threads), 0, st, a);
+        DLRM_CHECK_LAUNCH();
+        return DLRM_OK;
+      });
     };
     constexpr bool F32 = DT == DLRM_F32, FITS8 = !F32 || dp() <= 64;
     const int cut = cut_of(s, a, F32, FITS8);
@@ -994,21 +1005,23 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
   return for_kind(a, [&](auto dp, auto kind) -> int {
     constexpr bool F32 = DT == DLRM_F32;
     auto dq = [&](auto groups, auto parts) -> int {
-      dim3 grid;
       if (s->Tq == 0) return DLRM_OK;
-      if (!blocks_of(a, grid, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), 64 * groups() * parts())) return DLRM_ERR_BAD_SHAPE;
-      hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), grid,
-                         dim3(64 * groups() * parts()), 0, st, a);
-      DLRM_CHECK_LAUNCH();
-      return DLRM_OK;
+      constexpr int threads = 64 * groups() * parts();
+      return for_blocks(a, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), threads, [&](dim3 grid) -> int {
+        hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(threads), 0, st, a);
+        DLRM_CHECK_LAUNCH();
+        return DLRM_OK;
+      });
     };
     auto dkv = [&](auto groups, auto parts) -> int {
-      dim3 grid;
       if (s->Tk == 0) return DLRM_OK;
-      if (!blocks_of(a, grid, s->Tk, s->max_k, 1, 32 * groups(), 64 * groups() * parts())) return DLRM_ERR_BAD_SHAPE;
-      hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(64 * groups() * parts()), 0, st, a);
-      DLRM_CHECK_LAUNCH();
-      if (a.splits == 1) return DLRM_OK;
+      constexpr int threads = 64 * groups() * parts();
+      const int rc = for_blocks(a, s->Tk, s->max_k, 1, 32 * groups(), threads, [&](dim3 grid) -> int {
+        hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(threads), 0, st, a);
+        DLRM_CHECK_LAUNCH();
+        return DLRM_OK;
+      });
+      if (rc != DLRM_OK || a.splits == 1) return rc;
       hipLaunchKernelGGL(seq_attn_join_kernel<DT>, dim3(div_up(a.Tk * a.Hk * (a.d / 8), 256), 2), dim3(256), 0, st, a);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;

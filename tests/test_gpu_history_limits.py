@@ -234,3 +234,35 @@ def test_bounds_that_say_nothing(dtype, d, Hq, Hk):
         hot.dlrm_seq_attn_bwd(seq, q, k, v, out, lse, do, dq, dk, dv, hot.alloc_seq_attn_workspace(seq, Hq, Hk, d))
         for n, x in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
             ref.close(x, want[n], want[n + "_tol"], n)
+
+
+@pytest.mark.parametrize("dtype,B,H", [("bf16", (1 << 20) + 301, 64), ("f32", (1 << 22) + 301, 8), ("f16", (1 << 26) + 301, 1)])
+def test_more_blocks_than_one_launch_has_threads_for(dtype, B, H):
+    """Histories of up to two items: 2^26 workgroups of one wavefront for the keys, and as many of two or more for the queries.  Rows and lengths repeat, so
+    the results do: they are compared, bit for bit, with the 64-bit form's of one round, and with each other."""
+    g, dt, d, P = gen(H), DT[dtype], 8, 64
+    lens = torch.randint(0, 3, (P,), generator=g)
+    lens[:2] = torch.tensor([2, 1])
+    n, rows = B // P, int(lens.sum())
+    all_lens = torch.cat([lens.repeat(n), lens[:B - n * P]])
+    off = torch.cat([torch.zeros(1, dtype=torch.int64), torch.cumsum(all_lens, 0)]).to(DEV)
+    T = int(off[-1])
+    small = [rand(g, rows, H, d, dtype=dt) for _ in range(4)]
+    q, k, v, do = (torch.cat([x.to(DEV).repeat(n, 1, 1), x[:T - n * rows].to(DEV)]) for x in small)
+    seq = hot.SeqBatch(off, off, T, T, 2, 2)
+    out, dq, dk, dv = (torch.full_like(x, NAN) for x in (q, q, k, v))
+    lse = torch.full((H, T), NAN, device=DEV)
+    hot.dlrm_seq_attn_fwd(seq, q, k, v, out, lse)
+    hot.dlrm_seq_attn_bwd(seq, q, k, v, out, lse, do, dq, dk, dv, hot.alloc_seq_attn_workspace(seq, H, H, d))
+    o = ref.offsets(lens.numpy())
+    want = ref.attention(*small[:3], o, o, True, None, None, d ** -0.5, 0.0, small[3])
+    for name, x in (("out", out), ("dq", dq), ("dk", dk), ("dv", dv), ("lse", lse.t())):
+        one = x[:rows]
+        if name != "lse":
+            ref.close(one, want[name], want[name + "_tol"], name)
+        else:
+            ref.close(one.t(), want[name], want[name + "_tol"], name)
+        whole = x[:n * rows].reshape(n, rows, *x.shape[1:])
+        for a in range(0, n, 1 << 14):
+            assert (whole[a:a + (1 << 14)] == one).all(), (name, a)
+        assert torch.equal(x[n * rows:], one[:T - n * rows]), name
