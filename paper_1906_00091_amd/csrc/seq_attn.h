@@ -418,7 +418,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
   Op<DT> qf[STEPS];
   own_rows<DT, STEPS>(qf, row_of(a.q, w.me.t, w.me.head), w.me.there, a.d, h);
   const Score<DT, KIND> sc(a, w.me.head);
-  const float place = (float)(w.me.i + sp.shift);
+  const int place = w.me.i + sp.shift;  // (distances are taken as integers: fp32 has no odd place past 2^24)
 
   f32x16 o[NB];
 #pragma unroll
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       // with slopes the whole score, else what the factor c still goes to, in the multiply-add before the exponential
       const float c = KIND & kSlopes ? 1.0f : sc.c;
       if constexpr (KIND != kPlain) {
-        const float away = place - (float)(j0 + 4 * h);
+        const float away = (float)(place - (j0 + 4 * h));
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -585,7 +585,8 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
   const int64_t at = (int64_t)w.me.head * a.Tq + w.me.t;
   const float lse = w.me.there ? a.lse[at] : 0.0f;
   const Score<DT, KIND> sc(a, w.me.head);
-  const float place = (float)(w.me.i + sp.shift), rest = lse2_of(lse, w.me.there) - sc.base;
+  const int place = w.me.i + sp.shift;
+  const float rest = lse2_of(lse, w.me.there) - sc.base;
 
   f32x16 g[NB];
 #pragma unroll
@@ -621,7 +622,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
         dp = Op<DT>::mma(T::by_row(vs, lane & 31, st, h), df[st], dp);
       }
       __builtin_amdgcn_s_setprio(0);
-      const float away = place - (float)(j0 + 4 * h);
+      const float away = (float)(place - (j0 + 4 * h));
       if (j0 == 0 && w.wave_full <= 32) {  // once a wavefront, and only the first of a sequence
         float all = 0.0f;
 #pragma unroll
@@ -801,7 +802,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
         dp = Op<DT>::mma(T::by_row(os, lane & 31, st, h), W::V_LDS ? T::by_row(lds + W::V_AT, group * 32 + (lane & 31), st, h) : vf[W::V_LDS ? 0 : st], dp);
       }
       __builtin_amdgcn_s_setprio(0);
-      const float away = (float)(i0 + sp.shift + 4 * h) - (float)j;
+      const float away = (float)(i0 + sp.shift + 4 * h - j);
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);

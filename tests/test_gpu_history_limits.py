@@ -266,3 +266,22 @@ def test_more_blocks_than_one_launch_has_threads_for(dtype, B, H):
         for a in range(0, n, 1 << 14):
             assert (whole[a:a + (1 << 14)] == one).all(), (name, a)
         assert torch.equal(x[n * rows:], one[:T - n * rows]), name
+
+
+@pytest.mark.parametrize("dtype,causal", [("f32", True), ("f32", False), ("bf16", True)])
+def test_distances_past_the_integers_of_fp32(dtype, causal):
+    """70 queries at the end of 2^24 + 6001 keys, slopes of 1/2 and 1/4: only the last keys weigh anything, and their distances are those of a short sequence."""
+    g, dt, nq, nk, H, d, last = gen(24), DT[dtype], 70, (1 << 24) + 6001, 2, 8, 4096
+    q, do = (rand(g, nq, H, d, dtype=dt) for _ in range(2))
+    k, v = (torch.randn(nk, H, d, device=DEV).to(dt) for _ in range(2))
+    sl = torch.tensor([0.5, 0.25])
+    seq = hot.SeqBatch(torch.tensor([0, nq], device=DEV), torch.tensor([0, nk], device=DEV), nq, nk, nq, nk, causal=causal, slopes=sl.to(DEV))
+    Q, DO = q.to(DEV), do.to(DEV)
+    out, dq, dk, dv = (torch.full_like(x, NAN) for x in (Q, Q, k, v))
+    lse = torch.empty(H, nq, device=DEV)
+    hot.dlrm_seq_attn_fwd(seq, Q, k, v, out, lse)
+    hot.dlrm_seq_attn_bwd(seq, Q, k, v, out, lse, DO, dq, dk, dv, hot.alloc_seq_attn_workspace(seq, H, H, d))
+    want = ref.attention(q, k[-last:].cpu(), v[-last:].cpu(), torch.tensor([0, nq]), torch.tensor([0, last]), causal, None, sl, d ** -0.5, 0.0, do)
+    for n, x in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk[-last:]), ("dv", dv[-last:])):
+        ref.close(x, want[n], want[n + "_tol"], n)
+    assert not dk[:-last].any() and not dv[:-last].any()
