@@ -539,9 +539,10 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
     if (w.part > 0) return;
   }
   if (!w.me.there) return;
-  store_rows<DT, NB>(o, l > 0.0f ? 1.0f / l : 0.0f, row_of(a.out, w.me.t, w.me.head), a.d, h);
+  // (a sum that is NaN is not a row that sees nothing: its lse is NaN too, and the backward's weights with it)
+  store_rows<DT, NB>(o, l == 0.0f ? 0.0f : 1.0f / l, row_of(a.out, w.me.t, w.me.head), a.d, h);
   if (a.lse && h == 0)
-    a.lse[(int64_t)w.me.head * a.Tq + w.me.t] = l > 0.0f ? (m + sc.base + __builtin_amdgcn_logf(l)) * kLn2 : -kInf;
+    a.lse[(int64_t)w.me.head * a.Tq + w.me.t] = l == 0.0f ? -kInf : (m + sc.base + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // a row's lse in powers of two, +inf (all weights 0) for a row that sees nothing or is not there

@@ -285,3 +285,26 @@ def test_distances_past_the_integers_of_fp32(dtype, causal):
     for n, x in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk[-last:]), ("dv", dv[-last:])):
         ref.close(x, want[n], want[n + "_tol"], n)
     assert not dk[:-last].any() and not dv[:-last].any()
+
+
+@pytest.mark.parametrize("dtype,d,n", [("f32", 32, 40), ("f16", 64, 40), ("bf16", 128, 40), ("bf16", 16, 700), ("f32", 96, 700)])
+@pytest.mark.parametrize("what", [NAN, INF])
+def test_a_query_that_is_not_finite_does_not_pass_for_one_that_sees_nothing(dtype, d, n, what):
+    """Its weights are NaN: so are its row, its lse and the gradients of the values that it sees, and nobody else's rows."""
+    g, dt, i = gen(d), DT[dtype], 21
+    q, k, v, do = (rand(g, n, 1, d, dtype=dt) for _ in range(4))
+    q[i, 0, 3] = what
+    k[:, 0, 3] = 1.0                                            # (the score is infinite or NaN, whatever the other columns give)
+    off = torch.tensor([0, n], device=DEV)
+    seq = hot.SeqBatch(off, off, n, n, n, n)
+    x = [t.to(DEV) for t in (q, k, v)]
+    out, dq, dk, dv = (torch.empty(n, 1, d, dtype=dt, device=DEV) for _ in range(4))
+    lse = torch.empty(1, n, device=DEV)
+    hot.dlrm_seq_attn_fwd(seq, *x, out, lse)
+    hot.dlrm_seq_attn_bwd(seq, *x, out, lse, do.to(DEV), dq, dk, dv, hot.alloc_seq_attn_workspace(seq, 1, 1, d))
+    mine = torch.arange(n, device=DEV) == i
+    for y in (out, dq):
+        assert y[i].isnan().all() and torch.isfinite(y[~mine]).all()
+    assert lse[0, i].isnan() and torch.isfinite(lse[0, ~mine]).all()
+    assert dv[:i + 1].isnan().all() and torch.isfinite(dv[i + 1:]).all()
+    assert dk[:i + 1].isnan().all()
