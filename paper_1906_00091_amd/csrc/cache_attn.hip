@@ -451,8 +451,8 @@ extern "C" int32_t dlrm_cache_attn(const dlrm_kv_cache* c, const int32_t* lens, 
   for (const dlrm_heads* x : {q, out})
     if (int st = check_heads(x, c->B, Hq, c->d, eb)) return st;
   CacheArgs a = {};
-  a.q = rows_of(q, eb);
-  a.out = rows_of(out, eb);
+  a.q = rows_of(q, c->B, Hq, c->d, eb);
+  a.out = rows_of(out, c->B, Hq, c->d, eb);
   a.k = static_cast<const char*>(c->k);
   a.v = static_cast<const char*>(c->v);
   a.table = c->table;

@@ -15,15 +15,16 @@ struct Rows {
 
 __device__ inline char* row_of(const Rows& r, int64_t t, int h) { return r.p + t * r.st + h * r.sh; }
 
-__host__ inline Rows rows_of(const dlrm_heads* x, int eb) {
-  return Rows{static_cast<char*>(x->data), x->stride_t * eb, x->stride_h * eb};
+// (the stride along an axis of one element means nothing, and is not passed on)
+__host__ inline Rows rows_of(const dlrm_heads* x, int64_t n, int H, int d, int eb) {
+  return Rows{static_cast<char*>(x->data), (n > 1 ? x->stride_t : d) * eb, (H > 1 ? x->stride_h : d) * eb};
 }
 
 // Checks a view of H heads of d columns, n items.
 __host__ inline int check_heads(const dlrm_heads* x, int64_t n, int H, int d, int eb) {
   if (!x || (!x->data && n > 0)) return DLRM_ERR_NULL;
   if (reinterpret_cast<uintptr_t>(x->data) & 15) return DLRM_ERR_BAD_SHAPE;
-  // (a stride along an axis of one element means nothing; a tile's rows are reached with 32-bit byte offsets)
+  // (as in rows_of; a tile's rows are reached with 32-bit byte offsets)
   const int64_t st = n > 1 ? x->stride_t : d, sh = H > 1 ? x->stride_h : d;
   if (st < d || sh < d || st > (1 << 23) || sh >= (int64_t)1 << 40) return DLRM_ERR_BAD_SHAPE;
   if (((st * eb) & 15) != 0 || ((sh * eb) & 15) != 0) return DLRM_ERR_BAD_SHAPE;

@@ -497,13 +497,13 @@ extern "C" int32_t dlrm_qk_rope_fwd(const dlrm_qk_rope* r, const dlrm_heads* q, 
   for (const dlrm_heads* x : {q, q_out})
     if (int st = check_heads(x, r->T, r->Hq, r->d, eb)) return st;
   RopeArgs a = rope_args(r);
-  a.q = rows_of(q, eb);
-  a.qo = rows_of(q_out, eb);
+  a.q = rows_of(q, r->T, r->Hq, r->d, eb);
+  a.qo = rows_of(q_out, r->T, r->Hq, r->d, eb);
   if (r->Hk > 0) {
     for (const dlrm_heads* x : {k, k_out})
       if (int st = check_heads(x, r->T, r->Hk, r->d, eb)) return st;
-    a.k = rows_of(k, eb);
-    a.ko = rows_of(k_out, eb);
+    a.k = rows_of(k, r->T, r->Hk, r->d, eb);
+    a.ko = rows_of(k_out, r->T, r->Hk, r->d, eb);
   }
   return launch_fwd<false>(r, a, static_cast<hipStream_t>(stream));
 }
@@ -521,10 +521,10 @@ extern "C" int32_t dlrm_qk_rope_append(const dlrm_qk_rope* r, const dlrm_heads* 
   for (const dlrm_heads* x : {k, v})
     if (int st = check_heads(x, r->T, r->Hk, r->d, eb)) return st;
   RopeArgs a = rope_args(r);
-  a.q = rows_of(q, eb);
-  a.qo = rows_of(q_out, eb);
-  a.k = rows_of(k, eb);
-  a.v = rows_of(v, eb);
+  a.q = rows_of(q, r->T, r->Hq, r->d, eb);
+  a.qo = rows_of(q_out, r->T, r->Hq, r->d, eb);
+  a.k = rows_of(k, r->T, r->Hk, r->d, eb);
+  a.v = rows_of(v, r->T, r->Hk, r->d, eb);
   a.ck = static_cast<char*>(c->k);
   a.cv = static_cast<char*>(c->v);
   a.table = c->table;
@@ -550,15 +550,15 @@ extern "C" int32_t dlrm_qk_rope_bwd(const dlrm_qk_rope* r, const dlrm_heads* q, 
   for (const dlrm_heads* x : {q, dq_out, dq})
     if (int st = check_heads(x, r->T, r->Hq, r->d, eb)) return st;
   RopeArgs a = rope_args(r);
-  a.q = rows_of(q, eb);
-  a.dqo = rows_of(dq_out, eb);
-  a.dq = rows_of(dq, eb);
+  a.q = rows_of(q, r->T, r->Hq, r->d, eb);
+  a.dqo = rows_of(dq_out, r->T, r->Hq, r->d, eb);
+  a.dq = rows_of(dq, r->T, r->Hq, r->d, eb);
   if (r->Hk > 0) {
     for (const dlrm_heads* x : {k, dk_out, dk})
       if (int st = check_heads(x, r->T, r->Hk, r->d, eb)) return st;
-    a.k = rows_of(k, eb);
-    a.dko = rows_of(dk_out, eb);
-    a.dk = rows_of(dk, eb);
+    a.k = rows_of(k, r->T, r->Hk, r->d, eb);
+    a.dko = rows_of(dk_out, r->T, r->Hk, r->d, eb);
+    a.dk = rows_of(dk, r->T, r->Hk, r->d, eb);
   }
   const bool norm = a.wq || a.wk;
   if ((a.wq && !dwq) || (a.wk && !dwk)) return DLRM_ERR_NULL;

@@ -57,10 +57,10 @@ extern "C" int32_t dlrm_seq_attn_fwd(const dlrm_seq_batch* batch, int32_t Hq, in
   for (const dlrm_heads* x : {k, v})
     if (int st = check_heads(x, s->Tk, Hk, d, eb)) return st;
   SeqArgs a = seq_args(s, Hq, Hk, d);
-  a.q = rows_of(q, eb);
-  a.k = rows_of(k, eb);
-  a.v = rows_of(v, eb);
-  a.out = rows_of(out, eb);
+  a.q = rows_of(q, s->Tq, Hq, d, eb);
+  a.k = rows_of(k, s->Tk, Hk, d, eb);
+  a.v = rows_of(v, s->Tk, Hk, d, eb);
+  a.out = rows_of(out, s->Tq, Hq, d, eb);
   a.lse = lse;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   switch (dtype) {
@@ -99,14 +99,14 @@ extern "C" int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* batch, int32_t Hq, in
       workspace_bytes < dlrm_seq_attn_bwd_workspace_bytes(batch, Hq, Hk, d, dtype))
     return DLRM_ERR_WORKSPACE;
   SeqArgs a = seq_args(s, Hq, Hk, d);
-  a.q = rows_of(q, eb);
-  a.k = rows_of(k, eb);
-  a.v = rows_of(v, eb);
-  a.out = rows_of(out, eb);
-  a.dout = rows_of(dout, eb);
-  a.dq = rows_of(dq, eb);
-  a.dk = rows_of(dk, eb);
-  a.dv = rows_of(dv, eb);
+  a.q = rows_of(q, s->Tq, Hq, d, eb);
+  a.k = rows_of(k, s->Tk, Hk, d, eb);
+  a.v = rows_of(v, s->Tk, Hk, d, eb);
+  a.out = rows_of(out, s->Tq, Hq, d, eb);
+  a.dout = rows_of(dout, s->Tq, Hq, d, eb);
+  a.dq = rows_of(dq, s->Tq, Hq, d, eb);
+  a.dk = rows_of(dk, s->Tk, Hk, d, eb);
+  a.dv = rows_of(dv, s->Tk, Hk, d, eb);
   a.lse = const_cast<float*>(lse);
   a.delta = static_cast<float*>(workspace);
   a.part = a.delta + delta_bytes(s, Hq) / sizeof(float);

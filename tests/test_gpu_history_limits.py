@@ -308,3 +308,25 @@ def test_a_query_that_is_not_finite_does_not_pass_for_one_that_sees_nothing(dtyp
     assert lse[0, i].isnan() and torch.isfinite(lse[0, ~mine]).all()
     assert dv[:i + 1].isnan().all() and torch.isfinite(dv[i + 1:]).all()
     assert dk[:i + 1].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("stride", [0, 1, 24])
+def test_the_stride_of_one_item_means_nothing(dtype, stride):
+    """One query over one key, whose value has an infinity: a product with rows that are not there would make it NaN."""
+    g, dt, d = gen(stride), DT[dtype], 40
+    rows = [rand(g, 1, 2, d, dtype=dt) for _ in range(4)]
+    rows[2][0, 1, 7] = INF
+    one = lambda x: x.to(DEV).as_strided((1, 2, d), (stride, d, 1))
+    q, k, v, do = (one(x) for x in rows)
+    out, dq, dk, dv = (one(torch.zeros(1, 2, d, dtype=dt)) for _ in range(4))
+    off = torch.tensor([0, 1], device=DEV)
+    seq, lse = hot.SeqBatch(off, off, 1, 1, 1, 1), torch.empty(2, 1, device=DEV)
+    hot.dlrm_seq_attn_fwd(seq, q, k, v, out, lse)
+    assert torch.equal(out, v)
+    hot.dlrm_seq_attn_bwd(seq, q, k, v, out, lse, do, dq, dk, dv, hot.alloc_seq_attn_workspace(seq, 2, 2, d))
+    assert torch.isfinite(dv).all() and torch.isfinite(dk[:, 0]).all() and torch.isfinite(dq[:, 0]).all()
+    plan = hot.QkRope(torch.zeros(1, dtype=torch.int32, device=DEV), 2, 2, d)
+    qo, ko = one(torch.zeros(1, 2, d, dtype=dt)), one(torch.zeros(1, 2, d, dtype=dt))
+    hot.dlrm_qk_rope_fwd(plan, q, v, qo, ko)
+    assert torch.equal(qo, q) and torch.equal(ko, v)
