@@ -124,6 +124,8 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
   constexpr int CH = DP * EB / 16, NV = kKeys * CH / DLRM_WAVE;  // chunks of a row; of a tile, per lane
   constexpr int STRIDE = DP * EB + 16;
   constexpr int OS = DP + 4;  // row of the joined sums
+  // fp16: weights, at most 1, are made 2^15 times as large, sums and all: those of a long cache's many keys are not lost below 2^-24
+  constexpr float LIFT = DT == DLRM_F16 ? 15.0f : 0.0f;
   constexpr int VBYTES = WAVES * kKeys * STRIDE, OBYTES = WAVES * kHeads * OS * 4;
   __shared__ __attribute__((aligned(16))) char lds[VBYTES > OBYTES ? VBYTES : OBYTES];
   __shared__ int pages[kTablePages];
@@ -236,7 +238,7 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
     for (int b = 0; b < NB; ++b) o[b] *= f;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-      x[r] = __builtin_amdgcn_exp2f(x[r] - ms);
+      x[r] = __builtin_amdgcn_exp2f(x[r] - (ms - LIFT));
       l += x[r];
     }
     const Op16<DT> p = op16_set<DT>(x);

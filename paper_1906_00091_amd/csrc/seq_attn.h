@@ -15,7 +15,9 @@
 //
 // fp32 operands run the same code: a fragment of 8 values a lane is 8 products of mfma 32x32x2 in place of one of 32x32x16.
 // With 16-bit types the weights and their gradients are rounded to that type before the second product, as the matrix cores
-// take it; sums of weights and all accumulators stay fp32.
+// take it; sums of weights and all accumulators stay fp32.  fp16 has few exponents (2^-14 to 2^15 at full precision), so there both are multiplied by
+// powers of two that the accumulators are divided by at the end: weights by one that takes the largest possible to 2^15, gradients by one that
+// follows the largest met so far (see Lift).
 #pragma once
 
 #include <type_traits>
@@ -244,6 +246,23 @@ struct Score {
     return FAST ? fmaf(y, y, y) : fmaf(-y, y, 1.0f);
   }
 };
+
+// fp16: log2 of what the weights are multiplied by where they are at most 2^8 (forward, see there) and 1 (gradients)
+template <int DT>
+constexpr float kWeightLift = DT == DLRM_F16 ? 7.0f : 0.0f;
+template <int DT>
+constexpr float kGradWeightLift = DT == DLRM_F16 ? 15.0f : 0.0f;
+
+// fp16: the power of two that takes a value of size `top` to 2^8, with room to grow below 2^15 and 22 binades above full precision's end
+__device__ inline float lift_for(float top) { return 8.0f - ceilf(__builtin_amdgcn_logf(top)); }
+__device__ inline float largest(const f32x16& x) {
+  float top = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(x[r]));
+  return top;
+}
+// whether a gradient of size `top` leaves fp16 (an infinity is not made finite)
+__device__ inline bool too_large(float top) { return top > 32768.0f && top < kInf; }
 
 // the other lane half's value
 __device__ inline float other_half(float v) { return __shfl_xor(v, 32, DLRM_WAVE); }
@@ -493,7 +512,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
         for (int b = 0; b < NB; ++b) o[b] *= f;
         m = m1;
       }
-      const float ms = m == -kInf ? 0.0f : m;  // nothing seen yet: every weight below is exp2(-inf)
+      const float ms = m == -kInf ? 0.0f : m - kWeightLift<DT>;  // nothing seen yet: every weight below is exp2(-inf)
 #pragma unroll
       for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -542,13 +561,21 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
   // (a sum that is NaN is not a row that sees nothing: its lse is NaN too, and the backward's weights with it)
   store_rows<DT, NB>(o, l == 0.0f ? 0.0f : 1.0f / l, row_of(a.out, w.me.t, w.me.head), a.d, h);
   if (a.lse && h == 0)
-    a.lse[(int64_t)w.me.head * a.Tq + w.me.t] = l == 0.0f ? -kInf : (m + sc.base + __builtin_amdgcn_logf(l)) * kLn2;
+    a.lse[(int64_t)w.me.head * a.Tq + w.me.t] = l == 0.0f ? -kInf : (m - kWeightLift<DT> + sc.base + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // a row's lse in powers of two, +inf (all weights 0) for a row that sees nothing or is not there
 __device__ inline float lse2_of(float lse, bool there) { return !there || lse == -kInf ? kInf : lse * kLog2e; }
 
 // ---------------------------------------------------------------------------------------------------------------
+// Wavefronts of a SIMD that the registers are to leave room for.  fp16 rows of up to 64 columns need one register more than three of them leave, for the
+// lift: kept to three (2048 histories of up to 200 items, slopes, forward and backward: 547 us, 586 with two; 535 without a lift), but for slopes and
+// a cap together, which would spill eleven.
+constexpr int dq_resident(int dt, int dp, int kind, int groups, int parts) {
+  if (dt == DLRM_F16 && dp <= 64 && groups == 4 && kind != (kSlopes | kBend)) return 3;
+  return groups == 4 || parts == 8 ? 2 : 1;
+}
+
 // Queries' gradient, and delta = <dout, out> of every row for the kernel after it.  As the forward, with
 // dP^T = V dO^T beside S^T and dQ^T = K^T dS^T.
 // The stored output is rounded where rows have 16 bits, and where few keys carry a row's weight that rounding shows in
@@ -559,7 +586,7 @@ __device__ inline float lse2_of(float lse, bool there) { return !there || lse ==
 // outputs together are 2.5e-3 off (relative, all of them) in one part, 2.3e-3 in two, where rounding them alone makes 1.7e-3.
 // Bound as the forward is: the sizes above take 616 us (789 TFLOP/s), 210 us and 382 us (65 TFLOP/s).
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
-__global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 : 1) void seq_attn_dq_kernel(SeqArgs a) {
+__global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROUPS, PARTS)) void seq_attn_dq_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
   constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   constexpr bool TWO = DT != DLRM_F32 && (DP <= 64 || (KIND & kSlopes) != 0);  // ds in two parts
@@ -573,21 +600,32 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
   Op<DT> qf[STEPS], df[STEPS];
   own_rows<DT, STEPS>(qf, row_of(a.q, w.me.t, w.me.head), w.me.there, a.d, h);
   own_rows<DT, STEPS>(df, row_of(a.dout, w.me.t, w.me.head), w.me.there, a.d, h);
-  float delta = 0.0f;
+  // fp16: ds is made 2^lift times as large.  |dp| <= |dout| |v|, so with 2^lift |dout| near 2^8 values of ordinary size stay far below 2^15, and weights
+  // down to 2^-22 above the subnormal numbers; where that does not do, the lift goes down (below).
+  constexpr bool LIFT = DT == DLRM_F16;
+  float delta = 0.0f, lift = 0.0f;
   {
     Op<DT> of[STEPS];
     own_rows<DT, STEPS>(of, row_of(a.out, w.me.t, w.me.head), w.me.there, a.d, h);
+    float square = 0.0f;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) delta += of[s].get(j) * df[s].get(j);
+      for (int j = 0; j < 8; ++j) {
+        delta += of[s].get(j) * df[s].get(j);
+        if constexpr (LIFT) square = fmaf(df[s].get(j), df[s].get(j), square);
+      }
     delta += other_half(delta);
+    if constexpr (LIFT) {
+      square += other_half(square);
+      if (square > 0.0f && square < kInf) lift = lift_for(sqrtf(square));
+    }
   }
   const int64_t at = (int64_t)w.me.head * a.Tq + w.me.t;
   const float lse = w.me.there ? a.lse[at] : 0.0f;
   const Score<DT, KIND> sc(a, w.me.head);
   const int place = w.me.i + sp.shift;
-  const float rest = lse2_of(lse, w.me.there) - sc.base;
+  float rest = lse2_of(lse, w.me.there) - sc.base - lift;  // (so p below is 2^lift times the weight)
 
   f32x16 g[NB];
 #pragma unroll
@@ -632,7 +670,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
           all += acc_row(r, h) < w.vis ? p * dp[r] : 0.0f;
         }
         all += other_half(all);
-        if (w.vis <= 32) delta = all;
+        if (w.vis <= 32) delta = all * (LIFT ? __builtin_amdgcn_exp2f(-lift) : 1.0f);
       }
       auto gradient = [&](auto masked) {
 #pragma unroll
@@ -649,6 +687,19 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
         gradient(Int<1>{});
       else
         gradient(Int<0>{});
+      if constexpr (LIFT) {
+        float top = largest(s);
+        if (__ballot(too_large(top))) {
+          top = fmaxf(top, other_half(top));
+          const float down = too_large(top) ? lift_for(top) : 0.0f, f = __builtin_amdgcn_exp2f(down);
+          lift += down;
+          rest -= down;
+          sum *= f;
+          s *= f;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) g[b] *= f;
+        }
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         Op<DT> ds, low;
@@ -671,6 +722,12 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, GROUPS == 4 || PARTS == 8 ? 2 
       tv.store(lds + ((t + 1) & (W::BUFS - 1)) * 2 * TILE + TILE);
     }
     __syncthreads();
+  }
+  if constexpr (LIFT) {
+    const float f = __builtin_amdgcn_exp2f(-lift);
+    sum *= f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) g[b] *= f;
   }
   sum += other_half(sum);
   if constexpr (PARTS > 1) {
@@ -760,6 +817,9 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     t += first % tiles;
   }
   const float base = Score<DT, KIND>(a, hk * G).base;
+  // fp16: p is 2^15 times the weight, ds made from it, and that times `f` for the product: from nothing met so far (any value is too large) down
+  constexpr bool LIFT = DT == DLRM_F16;
+  float f = LIFT ? 0x1p60f : 1.0f;
   auto fetch = [&]() {
     const int i0 = t * BQ;
     tq.load(row_of(a.q, q0 + i0, head), a.q.st, sp.nq - i0, a.d);
@@ -772,7 +832,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     if (threadIdx.x < 2 * BQ) {
       const bool row = t * BQ + srow < sp.nq;
       float* stat = reinterpret_cast<float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ;
-      stat[threadIdx.x] = threadIdx.x < BQ ? lse2_of(sraw, row) - base : row ? sraw : 0.0f;
+      stat[threadIdx.x] = threadIdx.x < BQ ? lse2_of(sraw, row) - base - kGradWeightLift<DT> : row ? sraw : 0.0f;
     }
   };
   if (all > 0) {
@@ -823,6 +883,17 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
         for (int r = 0; r < 16; ++r)
           if (i0 + acc_row(r, h) < from) s[r] = dp[r] = 0.0f;
       }
+      if constexpr (LIFT) {
+        float top = largest(dp);
+        if (__ballot(too_large(top * f))) {
+          top = fmaxf(top, other_half(top));
+          const float f1 = too_large(top * f) ? __builtin_amdgcn_exp2f(lift_for(top)) : f;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) gk[b] *= f1 / f;
+          f = f1;
+        }
+        dp *= f;
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         Op<DT> p, ds;
@@ -842,6 +913,13 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     }
     if (n + 1 < all) put(n + 1);
     __syncthreads();
+  }
+  if constexpr (LIFT) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      gk[b] *= 1.0f / f * __builtin_amdgcn_exp2f(-kGradWeightLift<DT>);
+      gv[b] *= __builtin_amdgcn_exp2f(-kGradWeightLift<DT>);
+    }
   }
   if constexpr (PARTS == 2) {  // one of the two gradients after the other
     const float ones[2] = {1.0f, 1.0f};
