@@ -212,23 +212,25 @@ __device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per,
 }
 
 // What a score is made of, fixed at compile time: without a cap and slopes an element costs a multiply-add and an exponential.
-enum { kPlain = 0, kSlopes = 1, kBend = 2 };  // bits
+enum { kPlain = 0, kSlopes = 1, kBend = 2, kLarge = 4 };  // bits; kLarge: a cap that 16-bit rows take as fp32 rows do (with kBend and, slopes or none, kSlopes)
 
 // The score of a product s is, in powers of two, c * y(s) + base - slope * |distance|:
 //   without a cap  y = s, c = scale log2 e, base = 0;
 //   with a cap     tanh(z) = 1 - 2 r, r = 1 / (exp(2 z) + 1): an exponential and a reciprocal; y = -r, c = 2 cap log2 e,
 //                  base = cap log2 e, and the derivative 1 - tanh^2 is 4 r (1 - r) = -4 (y + y^2);
 //   fp32 with cap  y = tanh(z) of the library, whose error near 0 is relative; c = cap log2 e, base = 0, derivative 1 - y^2.
+// The second form's r is off by up to 2^-23, the score by cap 2^-22 and, with what rounding `base` adds, less than cap 2^-21 whatever its size: an eighth of
+// what rounding the weight to 16 bits is at a cap of 128 (fp16) or 1024 (bf16).  Larger caps take the third form, in one cut of each kernel.
 // The derivative's constant factor goes into `grad`, which the gradients are multiplied by at the end, as scale does.
 template <int DT, int KIND>
 struct Score {
-  static constexpr bool BEND = (KIND & kBend) != 0, FAST = DT != DLRM_F32;
+  static constexpr bool BEND = (KIND & kBend) != 0, FAST = DT != DLRM_F32 && (KIND & kLarge) == 0;
   float zs, c, base, slope, grad;
   __device__ inline Score(const SeqArgs& a, int head) {
     zs = BEND ? a.scale / a.cap * (FAST ? 2.0f * kLog2e : 1.0f) : 0.0f;
     c = BEND ? a.cap * (FAST ? 2.0f * kLog2e : kLog2e) : a.scale * kLog2e;
     base = BEND && FAST ? a.cap * kLog2e : 0.0f;
-    slope = (KIND & kSlopes) ? a.slopes[head] * kLog2e : 0.0f;
+    slope = (KIND & kSlopes) && ((KIND & kLarge) == 0 || a.slopes) ? a.slopes[head] * kLog2e : 0.0f;
     grad = BEND && FAST ? -4.0f * a.scale : a.scale;
   }
   __device__ inline float y(float s) const {
@@ -984,9 +986,12 @@ __host__ inline int for_blocks(SeqArgs& a, int64_t n, int longest, int per, int 
 }
 
 // Calls f with the padded width and the kind of score as compile-time constants.
-template <typename F>
+template <int DT, typename F>
 __host__ inline int for_kind(const SeqArgs& a, F f) {
   auto by_kind = [&](auto dp) {
+    if constexpr (DT != DLRM_F32) {
+      if (a.cap > (DT == DLRM_F16 ? 128.0f : 1024.0f)) return f(dp, std::integral_constant<int, kSlopes | kBend | kLarge>{});
+    }
     switch ((a.slopes ? kSlopes : 0) | (a.cap > 0.0f ? kBend : 0)) {
       case kPlain: return f(dp, std::integral_constant<int, kPlain>{});
       case kSlopes: return f(dp, std::integral_constant<int, kSlopes>{});
@@ -1052,7 +1057,7 @@ __host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool f32, 
 
 template <int DT>
 int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  return for_kind(a, [&](auto dp, auto kind) -> int {
+  return for_kind<DT>(a, [&](auto dp, auto kind) -> int {
     auto go = [&](auto groups, auto parts, auto sub) -> int {
       if (s->Tq == 0) return DLRM_OK;
       constexpr int threads = 64 * groups() * parts();
@@ -1063,26 +1068,30 @@ int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       });
     };
     constexpr bool F32 = DT == DLRM_F32, FITS8 = !F32 || dp() <= 64;
-    const int cut = cut_of(s, a, F32, FITS8);
-    if (cut == k2x1) return go(Int<2>{}, Int<1>{}, Int<1>{});
-    if (cut == k2x2) return go(Int<2>{}, Int<2>{}, Int<1>{});
-    if constexpr (FITS8) {
-      if (cut == k1x8) return go(Int<1>{}, Int<8>{}, Int<1>{});
-    }
-    if constexpr (F32) {
-      return go(Int<4>{}, Int<2>{}, Int<1>{});
+    if constexpr ((kind() & kLarge) != 0) {
+      return go(Int<2>{}, Int<1>{}, Int<1>{});
     } else {
-      // Short histories of narrow rows: tiles of 32 keys leave registers for four workgroups a CU.  (2048 histories of up to 200 items, d 64:
-      // 131 us, 143 with 64 keys; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
-      if (cut == k4x1Short || (dp() <= 64 && s->max_k <= 256)) return go(Int<4>{}, Int<1>{}, Int<1>{});
-      return go(Int<4>{}, Int<1>{}, Int<2>{});
+      const int cut = cut_of(s, a, F32, FITS8);
+      if (cut == k2x1) return go(Int<2>{}, Int<1>{}, Int<1>{});
+      if (cut == k2x2) return go(Int<2>{}, Int<2>{}, Int<1>{});
+      if constexpr (FITS8) {
+        if (cut == k1x8) return go(Int<1>{}, Int<8>{}, Int<1>{});
+      }
+      if constexpr (F32) {
+        return go(Int<4>{}, Int<2>{}, Int<1>{});
+      } else {
+        // Short histories of narrow rows: tiles of 32 keys leave registers for four workgroups a CU.  (2048 histories of up to 200 items, d 64:
+        // 131 us, 143 with 64 keys; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
+        if (cut == k4x1Short || (dp() <= 64 && s->max_k <= 256)) return go(Int<4>{}, Int<1>{}, Int<1>{});
+        return go(Int<4>{}, Int<1>{}, Int<2>{});
+      }
     }
   });
 }
 
 template <int DT>
 int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  return for_kind(a, [&](auto dp, auto kind) -> int {
+  return for_kind<DT>(a, [&](auto dp, auto kind) -> int {
     constexpr bool F32 = DT == DLRM_F32;
     auto dq = [&](auto groups, auto parts) -> int {
       if (s->Tq == 0) return DLRM_OK;
@@ -1109,35 +1118,41 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
     // Four groups of fp32 rows of more than 64 columns need more registers than there are: 13 histories of up to 2000 items, 6 heads on 3, d 96: four
     // of two parts 384 us, two of one 374; d 128: two of two parts 551, of one 484.  (Nor would the keys' gradients with 128 columns fit, below.)
     constexpr bool WIDE = F32 && dp() > 64, WIDEST = F32 && dp() > 96, FITS8 = !F32 || dp() <= 64;
-    const int cut = cut_of(s, a, F32, FITS8);
-    int rc = DLRM_OK;
-    if (cut == k2x1 || (WIDE && cut == k4x2))
-      rc = dq(Int<2>{}, Int<1>{});
-    else if (cut == k2x2)
-      rc = dq(Int<2>{}, Int<2>{});
-    else if (cut == k1x8) {
-      if constexpr (FITS8) rc = dq(Int<1>{}, Int<8>{});
-    } else if constexpr (!WIDE) {
-      rc = dq(Int<4>{}, Int<F32 ? 2 : 1>{});
-    }
-    if (rc != DLRM_OK) return rc;
-    a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
-    // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
-    // of up to 200 items, bf16, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
-    // (No more than 32 keys: no wavefront without any.  259 histories of one item or none, fp32, d 88: two wavefronts 75 us, one 42.)
-    const bool is_short = short_walks(s);
-    if constexpr (!WIDEST) {
-      if (is_short && s->max_k <= 32) return dkv(Int<1>{}, Int<1>{});
-    }
-    if constexpr (!F32) {
-      return is_short ? dkv(Int<(dp() > 64) ? 4 : 2>{}, Int<1>{}) : dkv(Int<4>{}, Int<2>{});
+    if constexpr ((kind() & kLarge) != 0) {
+      if (int rc = dq(Int<2>{}, Int<1>{})) return rc;
+      a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
+      return dkv(Int<2>{}, Int<1>{});
     } else {
-      // 64 histories of 1000 to 1400 items, 4 heads: halved 1203 us with d 64 and 1651 with 96, not halved 1074 and 1485; with 128 columns, which
-      // leave no registers for the loads of a whole tile by two wavefronts, 2111 and 2980.
-      if constexpr (!WIDEST) {
-        if (is_short || s->Tk * a.Hk >= 131072) return dkv(Int<2>{}, Int<1>{});
+      const int cut = cut_of(s, a, F32, FITS8);
+      int rc = DLRM_OK;
+      if (cut == k2x1 || (WIDE && cut == k4x2))
+        rc = dq(Int<2>{}, Int<1>{});
+      else if (cut == k2x2)
+        rc = dq(Int<2>{}, Int<2>{});
+      else if (cut == k1x8) {
+        if constexpr (FITS8) rc = dq(Int<1>{}, Int<8>{});
+      } else if constexpr (!WIDE) {
+        rc = dq(Int<4>{}, Int<F32 ? 2 : 1>{});
       }
-      return dkv(Int<2>{}, Int<2>{});
+      if (rc != DLRM_OK) return rc;
+      a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
+      // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
+      // of up to 200 items, bf16, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
+      // (No more than 32 keys: no wavefront without any.  259 histories of one item or none, fp32, d 88: two wavefronts 75 us, one 42.)
+      const bool is_short = short_walks(s);
+      if constexpr (!WIDEST) {
+        if (is_short && s->max_k <= 32) return dkv(Int<1>{}, Int<1>{});
+      }
+      if constexpr (!F32) {
+        return is_short ? dkv(Int<(dp() > 64) ? 4 : 2>{}, Int<1>{}) : dkv(Int<4>{}, Int<2>{});
+      } else {
+        // 64 histories of 1000 to 1400 items, 4 heads: halved 1203 us with d 64 and 1651 with 96, not halved 1074 and 1485; with 128 columns, which
+        // leave no registers for the loads of a whole tile by two wavefronts, 2111 and 2980.
+        if constexpr (!WIDEST) {
+          if (is_short || s->Tk * a.Hk >= 131072) return dkv(Int<2>{}, Int<1>{});
+        }
+        return dkv(Int<2>{}, Int<2>{});
+      }
     }
   });
 }
