@@ -330,3 +330,28 @@ def test_the_stride_of_one_item_means_nothing(dtype, stride):
     qo, ko = one(torch.zeros(1, 2, d, dtype=dt)), one(torch.zeros(1, 2, d, dtype=dt))
     hot.dlrm_qk_rope_fwd(plan, q, v, qo, ko)
     assert torch.equal(qo, q) and torch.equal(ko, v)
+
+
+# ------------------------------------------------------------------------------------------------ digits
+def norm_off(got, want, dt):
+    """Distance from the exact result in the Euclidean norm over all rows, and that of the result rounded to the type."""
+    return float((got.double() - want).norm()), float((want.to(dt).double() - want).norm())
+
+
+@pytest.mark.parametrize("dtype,d,cap", [("bf16", 128, 0.0), ("f16", 64, 0.0), ("bf16", 40, 30.0)])
+def test_cached_attention_is_off_by_the_rounding_of_its_result(dtype, d, cap):
+    """The weights' own rounding (they are taken in two parts, to 2^-16 at least) and fp32 add less than a twentieth to it: 2^-16 / 2^-9 is an eightieth, a capped
+    score's 2^-16 as much again."""
+    dt, B, H, page, n = DT[dtype], 40, 4, 64, 1500
+    g = torch.Generator(device=DEV).manual_seed(d)
+    q = torch.randn(B, H, d, generator=g, device=DEV).to(dt)
+    cols = (n + page - 1) // page
+    k, v = (torch.randn(B * cols, 1, page, d, generator=g, device=DEV).to(dt) for _ in range(2))
+    cache = hot.KvCache(k, v, torch.arange(B * cols, dtype=torch.int32, device=DEV).view(B, cols))
+    out = torch.empty_like(q)
+    hot.dlrm_cache_attn(cache, torch.full((B,), n, dtype=torch.int32, device=DEV), n, q, out, hot.alloc_cache_attn_workspace(cache, H, n), cap=cap)
+    K, V = (x.double().view(B, cols * page, d)[:, :n] for x in (k, v))
+    x = torch.matmul(q.double(), K.transpose(1, 2).contiguous()) * d ** -0.5
+    want = torch.matmul(torch.softmax(cap * torch.tanh(x / cap) if cap else x, -1), V)
+    off, rounding = norm_off(out, want, dt)
+    assert off <= 1.05 * rounding, (off, rounding)
