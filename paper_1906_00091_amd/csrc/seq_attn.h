@@ -17,7 +17,9 @@
 // With 16-bit types the weights and their gradients are rounded to that type before the second product, as the matrix cores
 // take it; sums of weights and all accumulators stay fp32.  fp16 has few exponents (2^-14 to 2^15 at full precision), so there both are multiplied by
 // powers of two that the accumulators are divided by at the end: weights by one that takes the largest possible to 2^15, gradients by one that
-// follows the largest met so far (see Lift).
+// follows the largest met so far (lift_for).  Short walks of up to 64 columns wait for most of their time: they take weights and gradients in two parts, the
+// second what the first one's rounding leaves, so that a result's error is its own rounding (2048 histories of up to 200 items, bf16: out 1.9e-3 -> 1.6e-3
+// off, dk and dv 2.3e-3 -> 1.7e-3, for 2.5 % of the time).  Long walks would pay a quarter to a third for it (8 histories of up to 4096 items: 1865 -> 2480 us).
 #pragma once
 
 #include <type_traits>
@@ -429,6 +431,7 @@ template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, SUB> W;
   constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
+  constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && GROUPS == 4 && PARTS * SUB == 1;  // weights in two parts
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   __shared__ float stat[PARTS > 1 ? PARTS * GROUPS * 2 * 32 : 1];
@@ -519,15 +522,20 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       for (int u = 0; u < SUB; ++u)
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          Op<DT> p;
+          Op<DT> p, low;
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             const float e = __builtin_amdgcn_exp2f(fmaf(s[u][8 * g + r], c, -ms));
             l += e;
             p.set(r, e);
+            if constexpr (TWO) low.set(r, e - p.get(r));
           }
 #pragma unroll
-          for (int b = 0; b < NB; ++b) o[b] = Op<DT>::mma(T::by_column(vs, 32 * u + 16 * g, b, lane), p, o[b]);
+          for (int b = 0; b < NB; ++b) {
+            const Op<DT> vt = T::by_column(vs, 32 * u + 16 * g, b, lane);
+            o[b] = Op<DT>::mma(vt, p, o[b]);
+            if constexpr (TWO) o[b] = Op<DT>::mma(vt, low, o[b]);
+          }
         }
     }
     if (W::BUFS == 1) __syncthreads();
@@ -776,6 +784,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   typedef Dkv<DT, DP, GROUPS, PARTS> W;
   typedef typename W::T T;
   constexpr int BQ = W::BQ, STEPS = W::STEPS, NB = W::NB;
+  constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && PARTS == 1;  // weights and ds in two parts
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   const int G = a.Hq / a.Hk;
   int walk, seq, row0;
@@ -898,17 +907,25 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        Op<DT> p, ds;
+        Op<DT> p, ds, p_low, ds_low;
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
           p.set(r, s[8 * c + r]);
           ds.set(r, dp[8 * c + r]);
+          if constexpr (TWO) {
+            p_low.set(r, s[8 * c + r] - p.get(r));
+            ds_low.set(r, dp[8 * c + r] - ds.get(r));
+          }
         }
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-          gv[b] = Op<DT>::mma(T::by_column(os, 16 * c, b, lane), p, gv[b]);
-          gk[b] = Op<DT>::mma(T::by_column(qs, 16 * c, b, lane), ds, gk[b]);
+          const Op<DT> ot = T::by_column(os, 16 * c, b, lane);
+          gv[b] = Op<DT>::mma(ot, p, gv[b]);
+          if constexpr (TWO) gv[b] = Op<DT>::mma(ot, p_low, gv[b]);
+          const Op<DT> qt = T::by_column(qs, 16 * c, b, lane);
+          gk[b] = Op<DT>::mma(qt, ds, gk[b]);
+          if constexpr (TWO) gk[b] = Op<DT>::mma(qt, ds_low, gk[b]);
         }
         __builtin_amdgcn_s_setprio(0);
       }
