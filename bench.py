@@ -37,13 +37,23 @@ DR_SCALE = 2.0 ** -20
 
 
 def source_digest():
-    """Digest of the HIP sources and headers the library is built from: a traffic figure measured with
-    rocprofv3 counters is only quoted for the sources it was measured on."""
+    """Digest of the HIP sources and headers that the step's kernels are built from: a traffic figure measured with
+    rocprofv3 counters is only quoted for the sources it was measured on.  The operators that read a history in order are not
+    launched here: their translation units (those that include heads.h) and their part of the public header are left out."""
+    csrc, include = os.path.join(ROOT, "paper_1906_00091_amd", "csrc"), os.path.join(ROOT, "include")
+    text = {f: open(os.path.join(d, f)).read() for d in (csrc, include) for f in os.listdir(d)}
+
+    def with_included(f, seen):
+        if f in text and f not in seen:
+            seen.add(f)
+            for g in re.findall(r'^#include "([^"]+)"', text[f], flags=re.M):
+                with_included(g, seen)
+        return seen
+    units = [with_included(f, set()) for f in text if f.endswith(".hip")]
     h = hashlib.sha256()
-    for sub in (os.path.join("paper_1906_00091_amd", "csrc"), "include"):
-        for f in sorted(os.listdir(os.path.join(ROOT, sub))):
-            h.update(f.encode())
-            h.update(open(os.path.join(ROOT, sub, f), "rb").read())
+    for f in sorted(set().union(*(u for u in units if "heads.h" not in u))):
+        h.update(f.encode())
+        h.update(text[f].split("\n * A history in order.")[0].encode())
     return h.hexdigest()[:12]
 
 
