@@ -387,3 +387,25 @@ def test_short_histories_of_narrow_rows_are_off_by_the_rounding_of_their_results
     for n, x in got.items():
         err, rounding = norm_off(x, want[n], dt)
         assert err <= (1.42 if n == "dq" else 1.05) * rounding, (n, err, rounding)
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 32), ("f16", 64), ("bf16", 128), ("f32", 96)])
+def test_the_value_of_the_largest_score_by_far(dtype, d):
+    """Integer queries and keys, so that every type and fp32 hold the scores exactly; in rows whose largest score leads by 200 or more the others' weights are
+    below e^-200, and the row is that key's value to two roundings."""
+    g, dt, n = gen(d), DT[dtype], 300
+    q, k = (torch.randint(-16, 17, (n, 1, d), generator=g).to(dt) for _ in range(2))
+    v = rand(g, n, 1, d, dtype=dt)
+    off = torch.tensor([0, n], device=DEV)
+    out, lse = torch.empty(n, 1, d, dtype=dt, device=DEV), torch.empty(1, n, device=DEV)
+    hot.dlrm_seq_attn_fwd(hot.SeqBatch(off, off, n, n, n, n, scale=1.0), q.to(DEV), k.to(DEV), v.to(DEV), out, lse)
+    sc = (q[:, 0].double() @ k[:, 0].double().t()).masked_fill(torch.ones(n, n).triu(1).bool(), -math.inf)
+    top = sc.topk(2, -1)
+    clear = top.values[:, 0] - top.values[:, 1] >= 200
+    assert int(clear.sum()) >= 50
+    want = v[top.indices[:, 0], 0].double()
+    # (the exponent, up to 2^16, is rounded when the maximum is taken: the weight is 2^(2^-9) off 1 at most, and stands in the sum as it is; what a
+    # 16-bit weight is rounded by is u, and the result once more)
+    bound = (2 * ref.UNIT[dt] + 2.0 ** -22) * want.abs() + ref.TINY[dt]
+    assert ((out[:, 0].double().cpu() - want).abs() <= bound)[clear].all()
+    ref.close(lse[0].cpu()[clear], top.values[:, 0][clear], 4 * ref.E32 * top.values[:, 0][clear].abs() + 1e-30, "lse")
