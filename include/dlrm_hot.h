@@ -408,7 +408,8 @@ typedef struct dlrm_heads {
  *   n = x * w / sqrt(mean(x^2) + eps)                              (w = wq or wk; n = x where it is NULL)
  *   pair i < rot/2, angle a = positions[t] * inv_freq[i]:
  *   (y_a, y_b) = mscale * (n_a cos a - n_b sin a,  n_b cos a + n_a sin a);  columns >= rot: y = n
- * The angle is reduced in fp64, so it is exact at positions up to 2^31.  Every scaling of positions for
+ * The angle is reduced in fp64: off by 3 * 2^-53 of itself at most, 7e-7 radians at 2^31, less than sine and cosine in fp32 add below
+ * 2^29.  Every scaling of positions for
  * histories longer than those trained on is a choice of inv_freq and mscale by the caller.
  */
 typedef struct dlrm_qk_rope {

@@ -3,8 +3,8 @@
 // A row of d columns is held by a group of G lanes (a power of two), 16 bytes a lane; the sum of squares and the
 // backward's <g w, n> are joined by lane exchanges inside the group.  A group stays with one item and walks its heads, so that the
 // item's angles are reduced and their sines and cosines taken once, in registers, for all of its heads: the angle in turns is
-// position * frequency / 2 pi in fp64 (24 + 31 bits of product, exact; fp32 would be off by 1e-3 radians at position 2^14),
-// its fraction goes to sincospi in fp32.  In the half layout a column's partner lies rot/2 columns away: in another lane at the same
+// position * frequency / 2 pi in fp64 (1 / 2 pi and two products are rounded: off by 3 2^-53 of the angle at most, 7e-7 radians at 2^31; fp32 would be off
+// by 1e-3 radians at position 2^14), its fraction goes to sincospi in fp32.  In the half layout a column's partner lies rot/2 columns away: in another lane at the same
 // place of the chunk where rot/2 is a multiple of a chunk's columns (an exchange of the raw chunk), else anywhere (through LDS).
 // With p the partner of column j,  y_j = r (c_j w_j x_j + s_j w_p x_p):  the norm's weights go into the coefficients once an item, and
 // the exchange of the row as it was loaded does not wait for its norm.

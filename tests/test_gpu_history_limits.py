@@ -409,3 +409,33 @@ def test_the_value_of_the_largest_score_by_far(dtype, d):
     bound = (2 * ref.UNIT[dt] + 2.0 ** -22) * want.abs() + ref.TINY[dt]
     assert ((out[:, 0].double().cpu() - want).abs() <= bound)[clear].all()
     ref.close(lse[0].cpu()[clear], top.values[:, 0][clear], 4 * ref.E32 * top.values[:, 0][clear].abs() + 1e-30, "lse")
+
+
+# ------------------------------------------------------------------------------------------------ angles
+def angle(position, frequency):
+    """position * frequency modulo 2 pi, to 30 digits."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    two_pi = Decimal("6.28318530717958647692528676655900576839433879875021164194989")
+    x = Decimal(position) * Decimal(frequency)      # (both exact)
+    return float(x - (x / two_pi).to_integral_value() * two_pi)
+
+
+@pytest.mark.parametrize("layout", [hot.ROPE_HALF, hot.ROPE_INTERLEAVED])
+@pytest.mark.parametrize("top", [1 << 12, 1 << 24, 1 << 31])
+def test_angles_of_large_positions(layout, top):
+    """An angle is off by 3 2^-53 of itself (1 / 2 pi and two products in fp64) and what sine and cosine in fp32 add, 2^-22."""
+    T, rot = 50, 16
+    pos = [top - 1 - (7919 * i) % (top // 2) for i in range(T)]
+    f = hot.rope_frequencies(rot)
+    x = rand(gen(top % 1000), T, 1, rot)
+    y = torch.empty(T, 1, rot, device=DEV)
+    hot.dlrm_qk_rope_fwd(hot.QkRope(torch.tensor(pos, dtype=torch.int32, device=DEV), 1, 0, rot, inv_freq=f.to(DEV), layout=layout), x.to(DEV), None, y, None)
+    a = torch.tensor([[angle(p, float(w)) for w in f] for p in pos], dtype=torch.float64)
+    n = rot // 2
+    i, j = (torch.arange(n), torch.arange(n) + n) if layout == hot.ROPE_HALF else (2 * torch.arange(n), 2 * torch.arange(n) + 1)
+    u, v = x[:, 0, i].double(), x[:, 0, j].double()
+    got = y[:, 0].double().cpu()
+    off = 3 * 2.0 ** -53 * torch.tensor(pos, dtype=torch.float64)[:, None] * f.double() + 2.0 ** -22
+    for want, at in ((u * a.cos() - v * a.sin(), i), (v * a.cos() + u * a.sin(), j)):
+        assert ((got[:, at] - want).abs() <= off * (u.abs() + v.abs())).all()
