@@ -241,17 +241,13 @@ __global__ __launch_bounds__(64 * WAVES) void cache_attn_kernel(CacheArgs a) {
       x[r] = __builtin_amdgcn_exp2f(x[r] - (ms - LIFT));
       l += x[r];
     }
-    const Op16<DT> p = op16_set<DT>(x);
-    // 16-bit rows: what the rounding of the weights leaves, in a product of its own.  (The matrix cores wait for memory here: 256 sequences of up to 8192 items
-    // 414 -> 416 us, one of 131072 items 48 -> 49; the result's error 2.07e-3 -> 1.63e-3 of it in bf16, which is its own rounding.)
-    Op16<DT> p_low;
-    if constexpr (EB == 2) {
-      float left[8];
-      Tab<DT>::widen(p.v, left);
-#pragma unroll
-      for (int r = 0; r < 8; ++r) left[r] = x[r] - left[r];
-      p_low = op16_set<DT>(left);
-    }
+    // 16-bit rows: weights in two parts, each in a product of its own.  (The matrix cores wait for memory here: 256 sequences of up to 8192 items
+    // 413 -> 419 us, one of 131072 items 48.5 -> 49; the result's error 2.07e-3 -> 1.63e-3 of it in bf16, which is its own rounding.)
+    Op16<DT> p, p_low;
+    if constexpr (EB == 2)
+      two_parts<DT>(x, p.v, p_low.v);
+    else
+      p = op16_set<DT>(x);
     // the values' columns: rows 4g..4g+3 and 16+4g..16+4g+3 of the tile for lane group g
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();

@@ -54,6 +54,25 @@ __device__ inline u32x4 narrow(const float* f) {
   }
 }
 
+// A weight w >= 0 as the sum of two 16-bit numbers, 8 at a time: `high` is w rounded down, `low` what is left.  low is above zero wherever high is (by less than fp32's
+// rounding would add), so that both products with an infinite value are that infinity: zero times it, or an infinity less another, would be NaN.
+template <int DT>
+__device__ inline void two_parts(const float* w, u32x4& high, u32x4& low) {
+  constexpr float LEAST = DT == DLRM_F16 ? 0x1p-24f : 0x1p-126f;  // of fp16, subnormal numbers and all, and of the normal ones
+  if constexpr (DT == DLRM_F16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) high[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[2 * j], w[2 * j + 1]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) high[j] = __builtin_amdgcn_perm(f2u(w[2 * j + 1]), f2u(w[2 * j]), 0x07060302u);
+  }
+  float h[8], l[8];
+  Tab<DT>::widen(high, h);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) l[j] = fmaxf(w[j] - h[j], fminf(h[j], LEAST));
+  low = narrow<DT>(l);
+}
+
 int check_cache(const dlrm_kv_cache* c);  // qk_rope.hip
 
 }  // namespace dlrm

@@ -19,7 +19,7 @@
 // powers of two that the accumulators are divided by at the end: weights by one that takes the largest possible to 2^15, gradients by one that
 // follows the largest met so far (lift_for).  Short walks of up to 64 columns wait for most of their time: they take weights and gradients in two parts, the
 // second what the first one's rounding leaves, so that a result's error is its own rounding (2048 histories of up to 200 items, bf16: out 1.9e-3 -> 1.6e-3
-// off, dk and dv 2.3e-3 -> 1.7e-3, for 2.5 % of the time).  Long walks would pay a quarter to a third for it (8 histories of up to 4096 items: 1865 -> 2480 us).
+// off, dk and dv 2.3e-3 -> 1.7e-3, for 3 % of the time).  Long walks would pay a quarter to a third for it (8 histories of up to 4096 items: 1865 -> 2480 us).
 #pragma once
 
 #include <type_traits>
@@ -91,6 +91,14 @@ __device__ inline Op<DT> op_load(const char* p) {  // 8 consecutive values, 16-b
     o.v = *reinterpret_cast<const decltype(o.v)*>(p);
   }
   return o;
+}
+
+template <int DT>
+__device__ inline void op_two_parts(const float* w, Op<DT>& high, Op<DT>& low) {
+  u32x4 h, l;
+  two_parts<DT>(w, h, l);
+  high.v = __builtin_bit_cast(decltype(high.v), h);
+  low.v = __builtin_bit_cast(decltype(low.v), l);
 }
 
 // A tile of rows in LDS.  Rows are padded: row reads of 16 bytes by 16 and more consecutive rows, and column reads of 4 consecutive rows,
@@ -431,7 +439,7 @@ template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, SUB> W;
   constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
-  constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && GROUPS == 4 && PARTS * SUB == 1;  // weights in two parts
+  constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && PARTS * SUB == 1;  // weights in two parts
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   __shared__ float stat[PARTS > 1 ? PARTS * GROUPS * 2 * 32 : 1];
@@ -523,13 +531,14 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           Op<DT> p, low;
+          float e[8];
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[u][8 * g + r], c, -ms));
-            l += e;
-            p.set(r, e);
-            if constexpr (TWO) low.set(r, e - p.get(r));
+            e[r] = __builtin_amdgcn_exp2f(fmaf(s[u][8 * g + r], c, -ms));
+            l += e[r];
+            if constexpr (!TWO) p.set(r, e[r]);
           }
+          if constexpr (TWO) op_two_parts(e, p, low);
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const Op<DT> vt = T::by_column(vs, 32 * u + 16 * g, b, lane);
@@ -908,15 +917,17 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         Op<DT> p, ds, p_low, ds_low;
+        float w[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          p.set(r, s[8 * c + r]);
+          if constexpr (!TWO) p.set(r, s[8 * c + r]);
           ds.set(r, dp[8 * c + r]);
           if constexpr (TWO) {
-            p_low.set(r, s[8 * c + r] - p.get(r));
+            w[r] = s[8 * c + r];
             ds_low.set(r, dp[8 * c + r] - ds.get(r));
           }
         }
+        if constexpr (TWO) op_two_parts(w, p, p_low);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {

@@ -439,3 +439,44 @@ def test_angles_of_large_positions(layout, top):
     off = 3 * 2.0 ** -53 * torch.tensor(pos, dtype=torch.float64)[:, None] * f.double() + 2.0 ** -22
     for want, at in ((u * a.cos() - v * a.sin(), i), (v * a.cos() + u * a.sin(), j)):
         assert ((got[:, at] - want).abs() <= off * (u.abs() + v.abs())).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("f16", 32)])
+def test_a_few_short_histories_are_off_by_the_rounding_of_their_results(dtype, d):
+    """As above with next to no rows, which smaller workgroups take."""
+    dt, H = DT[dtype], 2
+    g = torch.Generator(device=DEV).manual_seed(d)
+    lens = [1 + (17 * i) % 64 for i in range(60)]
+    off, T = ref.offsets(lens), sum(lens)
+    q, k, v = (torch.randn(T, H, d, generator=g, device=DEV).to(dt) for _ in range(3))
+    out, want = torch.empty_like(q), torch.zeros(T, H, d, dtype=torch.float64, device=DEV)
+    hot.dlrm_seq_attn_fwd(hot.SeqBatch(off.to(DEV), off.to(DEV), T, T, 64, 64, causal=False), q, k, v, out)
+    for s, n in enumerate(lens):
+        I = slice(int(off[s]), int(off[s]) + n)
+        for h in range(H):
+            want[I, h] = torch.softmax(q[I, h].double() @ k[I, h].double().t() * d ** -0.5, -1) @ v[I, h].double()
+    err, rounding = norm_off(out, want, dt)
+    assert err <= 1.05 * rounding, (err, rounding)
+
+
+# ------------------------------------------------------------------------------------------------ infinite values
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,B,n", [(64, 3, 40), (64, 200, 64), (64, 40, 200), (128, 30, 152)])
+def test_an_infinite_value_is_an_infinite_column_of_who_sees_it(dtype, d, B, n):
+    """Every weight is above zero, so the columns are that infinity, and the others finite: sequences of every cut, and the cache."""
+    dt, H, page = DT[dtype], 2, 8
+    g = torch.Generator(device=DEV).manual_seed(d + n)
+    q, k, v = (torch.randn(B * n, H, d, generator=g, device=DEV).to(dt) for _ in range(3))
+    v[n // 2::n, :, 3], v[n - 1::n, :, 5] = INF, -INF
+    off = torch.arange(B + 1, device=DEV) * n
+    out = torch.empty_like(q)
+    hot.dlrm_seq_attn_fwd(hot.SeqBatch(off, off, B * n, B * n, n, n, causal=False), q, k, v, out)
+    one = q[::n].contiguous()
+    pages = lambda x: x.view(B * n // page, page, H, d).transpose(1, 2).contiguous()
+    cache = hot.KvCache(pages(k), pages(v), torch.arange(B * n // page, dtype=torch.int32, device=DEV).view(B, -1))
+    newest = torch.empty_like(one)
+    hot.dlrm_cache_attn(cache, torch.full((B,), n, dtype=torch.int32, device=DEV), n, one, newest, hot.alloc_cache_attn_workspace(cache, H, n))
+    cols = torch.ones(d, dtype=torch.bool, device=DEV)
+    cols[[3, 5]] = False
+    for x in (out, newest):
+        assert (x[..., 3] == INF).all() and (x[..., 5] == -INF).all() and torch.isfinite(x[..., cols]).all()
