@@ -372,7 +372,11 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) v[j] = loadf4(po + (int64_t)(i0 + (r + j * ROWS < m ? r + j * ROWS : r)) * a.d + col);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) sum += (r + j * ROWS < m ? factor[r + j * ROWS] : 0.0f) * v[j];
+        for (int j = 0; j < AHEAD; ++j) {
+          // (past the end both are zero: zero times the row that was loaded instead would be NaN where that holds an infinity)
+          const bool there = r + j * ROWS < m;
+          sum += (there ? factor[r + j * ROWS] : 0.0f) * (there ? v[j] : f32x4{0, 0, 0, 0});
+        }
       }
     }
     __syncthreads();

@@ -480,3 +480,10 @@ def test_an_infinite_value_is_an_infinite_column_of_who_sees_it(dtype, d, B, n):
     cols[[3, 5]] = False
     for x in (out, newest):
         assert (x[..., 3] == INF).all() and (x[..., 5] == -INF).all() and torch.isfinite(x[..., cols]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,B,n", [(32, 3, 600), (128, 40, 608), (64, 1, 9000)])
+def test_an_infinite_value_in_one_of_several_chunks(dtype, d, B, n):
+    """The parts of a long sequence, of attention over sequences and over the cache, are joined to the same infinities."""
+    test_an_infinite_value_is_an_infinite_column_of_who_sees_it(dtype, d, B, n)
