@@ -1055,7 +1055,8 @@ __host__ inline int dkv_splits(const dlrm_seq_batch* s, int Hq, int Hk, int d, i
 
 // How the rows' kernels are cut, by what there is of rows and keys (GROUPS x PARTS wavefronts; `sub` tiles of 32 keys to a part and step).
 //   k4x1: 16-bit types.  Wavefronts that share 32 rows pay for the join, and gain where the rows are too few to fill the device;
-//   k2x1: fp32, whose registers leave a SIMD one wavefront of most kernels: small workgroups begin and end on their own;
+//   k2x1: fp32, whose registers leave a SIMD one wavefront of most kernels: small workgroups begin and end on their own; and two tiles of keys at most;
+//   k4x1Short: two tiles at most under many wide rows: four groups read a tile once;
 //   k2x2, k4x2: long walks of few rows, which then take half the steps;
 //   k1x8: where 32 rows to a workgroup would not give every CU one, if the walk is long and a step's keys fit into LDS.
 // Measured, forward / queries' gradient in us:
@@ -1066,6 +1067,16 @@ __host__ inline int dkv_splits(const dlrm_seq_batch* s, int Hq, int Hk, int d, i
 //   64 of 1000 to 1400 items, 4 heads, fp32, d 64: k4x2 630 / 870, k2x1 561 / 763;  13 of up to 2000, 6 heads on 3: k4x2 194 / 266, k2x1 264 / 359
 //   2 of 3000 to 4000 items, 8 heads on 2, fp32, d 96: k2x2 552 / 690, k4x2 450 / 629;  4 of 1000 to 1400, 4 heads: k2x2 101 / 125, k4x2 151 / 211
 //   16 histories of 2694 items under one or two queries, f16, d 80, all kernels: k2x2 116, k1x8 68;  2 of up to 1762, fp32, d 16: 141 and 89.
+// Forward / the whole backward in us, 4 heads (8 in the first group):
+//   bf16, d 64: 16 histories of 300 to 700 items (2064 blocks of 32 rows) k2x2 18 / 64, k4x1 17 / 60;  4 of
+//   1500 to 2500 (2016) 46 / 124 and 46 / 139;  5 (2520) 49 / 163 and 50 / 166;  8 (4032) 72 / 229 and 57 / 214;  d 96: 16 of 300 to 700 30 / 77 and 23 / 71, 4
+//   of 1500 to 2500 60 / 146 and 65 / 164;  d 128: 4 of 300 to 700 21 / 53 and 20 / 58, 8 33 / 71 and 23 / 64, 13 46 / 98 and 26 / 79
+//   histories of 1 to 64 items: bf16, d 128, 256 of them k2x1 14 / 37, k4x1Short 13 / 35, 512 26 / 69 and 24 / 67, 2048 95 / 282 and 87 / 280;  d 64,
+//   2048 36 / 112 and 40 / 118;  fp16, d 32, 1024 16 / 45 and 18 / 47
+//   one query over 600 keys: bf16, d 64, k1x8 10 / 15, k2x2 14 / 21;  16 over 2000 to 4000, d 128: 51 / 163 and 97 / 137;  fp32, d 32: 53 / 93 and 118 / 155
+//   4 histories of 40 queries over 600 keys, fp32, d 64: k1x8 20 / 42, k2x2 32 / 56;  2 of 300 over 500 to 600, fp16, d 24: 9 / 18 and 11 / 23
+//   one of 1000 items, bf16, d 64: k1x8 11 / 34, k2x2 19 / 43;  8 of 200 queries over 2000 to 4000 keys (216 blocks), d 64: 31 / 71 and 74 / 110;  4 of 500 over
+//   500 to 600 (258 blocks: no longer k1x8) 10 / 29 and 13 / 33
 enum { k4x1, k4x1Short, k2x1, k2x2, k4x2, k1x8 };
 __host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool f32, bool fits8) {
   const int64_t rows = s->Tq * a.Hq, blocks = rows / 32 + (int64_t)s->B * a.Hk / 2, fill = rows / 128;
@@ -1074,7 +1085,7 @@ __host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool f32, 
   // tiles have 128 rows at most, of 2^25 bytes at most: check_heads)
   const int64_t st = a.k.st > a.v.st ? a.k.st : a.v.st;
   fits8 = fits8 && 255 * st + 512 < ((int64_t)1 << 32);
-  if (s->max_k <= 64) return f32 || fill < 512 ? k2x1 : k4x1Short;
+  if (s->max_k <= 64) return f32 || a.d <= 64 || fill < 512 ? k2x1 : k4x1Short;
   if (fits8 && blocks <= 256 && s->max_k >= 512) return k1x8;
   if (f32) {
     if (fill >= (s->max_k > 256 ? 1024 : narrow ? 512 : 256)) return k2x1;
