@@ -501,6 +501,10 @@ typedef struct dlrm_seq_batch {
  * Attention forward: q [Tq, Hq, d], k and v [Tk, Hk, d] -> out [Tq, Hq, d]; query head h reads key head
  * h / (Hq / Hk).  lse: fp32 [Hq, Tq], the logarithm of the softmax's denominator (-inf for a query that sees no key),
  * which the backward reads; NULL if it is not wanted.
+ * With 16-bit rows the weights, and in the backward the score gradients, are 16-bit numbers in the products that they go into.  Up to 64 columns and 256 keys
+ * (for the gradients of keys and values: queries) they are taken in two parts, and a result is off by its own rounding; else rounded once, and a result is off by up
+ * to one and a half times that.  dq takes its score gradients in two parts up to 64 columns, and with slopes.  In fp16 both are scaled by powers of two, so
+ * weights keep their digits down to 2^-21 of a row's largest, and score gradients down to 2^-22 of the upstream row (dq) or of a key's largest (dk).
  */
 int32_t dlrm_seq_attn_fwd(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int32_t d, int32_t dtype,
                           const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v, const dlrm_heads* out,

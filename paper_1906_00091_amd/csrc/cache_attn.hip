@@ -5,8 +5,8 @@
 // 8 consecutive columns of one key.  S^T = K Q^T leaves a lane four keys of one head, and those registers are, with the contracted
 // index permuted, what O^T = V^T P^T takes; values pass through a piece of LDS that belongs to the wavefront alone, to be read by
 // columns.  So the wavefronts of a workgroup run without a barrier, each with its own running maximum and sum, over
-// every fourth tile of 32 keys, and are joined once at the end.  256 sequences of up to 8192 items, 16 query heads on 4, bf16, d 128: 432 us for
-// 2.15 GB, 5.0 TB/s; a large copy on the same card moves 4.7.
+// every fourth tile of 32 keys, and are joined once at the end.  256 sequences of up to 8192 items, 16 query heads on 4, bf16, d 128, capped: 421 us for
+// 2.15 GB, 5.1 TB/s; a large copy on the same card moves 4.7.
 //
 // The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in
 // the order of the chunks.
@@ -399,9 +399,9 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(CacheArgs a) {
   }
 }
 
-// Keys of a chunk: 1024 workgroups, four a CU, and at least two tiles a wavefront.  (The 256 sequences above: 436 us with chunks for 1024 workgroups,
-// 474 for 2048, 498 for 4096, 537 for 8192, whose joins read more.  One sequence of 131072 items on 4 key heads, four workgroups if it were not
-// split: 48 us with its join.)
+// Keys of a chunk: 1024 workgroups, four a CU, and at least two tiles a wavefront.  (The 256 sequences above, weights in one part: 436 us with chunks for 1024
+// workgroups, 474 for 2048, 498 for 4096, 537 for 8192, whose joins read more.  One sequence of 131072 items on 4 key heads, four workgroups if it were not
+// split: 49 us with its join.)
 constexpr int kWanted = 1024, kLeastChunk = 256;
 static int64_t groups_of(const dlrm_kv_cache* c, int Hq) { return (int64_t)c->B * c->Hk * ((Hq / c->Hk + kHeads - 1) / kHeads); }
 static int64_t most_of_chunk(const dlrm_kv_cache* c) { return (int64_t)(kTablePages - 1) * c->page; }  // (it need not start on a page)

@@ -10,7 +10,7 @@
 // the exchange of the row as it was loaded does not wait for its norm.
 //
 // Bound by memory: every row is read and written once.  2048 histories of up to 200 items, 4 + 4 heads of 64 fp32 columns, normed, all rotated: forward
-// 152 us for 0.84 GB (5.5 TB/s), backward 252 us for 1.26 GB (5.0 TB/s); a large copy on the same card moves 4.7 TB/s, a read 5.7.
+// 151 us for 0.84 GB (5.6 TB/s), backward 249 us for 1.26 GB (5.1 TB/s); a large copy on the same card moves 4.7 TB/s, a read 5.7.
 // Few heads of narrow rows are bound by the angles instead (one head each of 16 columns of f16: 2.0 TB/s forward, 1.1 backward).
 #include <initializer_list>
 #include <type_traits>

@@ -430,10 +430,10 @@ constexpr int fwd_resident(int dt, int dp, int groups, int parts, int sub) {
 }
 
 // Forward: tiles of keys and values go by, SUB x 32 keys for each part, two tiles in LDS.
-// 8 histories of 2048 to 4096 items, 16 query heads on 4, bf16, d 128, causal, capped: 485 us, 668 TFLOP/s of visible pairs (a large library product
-// of bf16 on the same card: 1203), bound by the exponentials and reciprocals beside the products: two wavefronts a SIMD, each of which can
+// 8 histories of 2048 to 4096 items, 16 query heads on 4, bf16, d 128, causal, capped: 431 us, 752 TFLOP/s of visible pairs (a large library product
+// of bf16 on the same card: 1192), bound by the exponentials and reciprocals beside the products: two wavefronts a SIMD, each of which can
 // multiply while the other does not.  2048 histories of up to 200 items, 4 heads, d 64, slopes: 127 us; a workgroup walks over four tiles and
-// waits for most of its time (four a CU hide part of it).  fp32, 13 histories of up to 1999 items, d 72: 283 us, 58 TFLOP/s of 154, and 72 with
+// waits for most of its time (four a CU hide part of it).  fp32, 13 histories of up to 1999 items, d 72: 281 us, 59 TFLOP/s of 154, and 72 with
 // the columns that pad 72 to 96.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
@@ -601,9 +601,9 @@ constexpr int dq_resident(int dt, int dp, int kind, int groups, int parts) {
 // ds = p (dp - delta) (a row with one key has dp = delta).  So delta is summed again on the way as sum p dp, in fp32: the kernel after this
 // one takes that; a row whose keys all lie in the first 32 has it before its first use here; and for the other rows what the rounding
 // of the output leaves is made up for by taking ds in two 16-bit parts, with a second product, where that costs little or is most needed: narrow
-// rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  2048 histories of up to 200 items in bf16, slopes: the
-// outputs together are 2.5e-3 off (relative, all of them) in one part, 2.3e-3 in two, where rounding them alone makes 1.7e-3.
-// Bound as the forward is: the sizes above take 616 us (789 TFLOP/s), 210 us and 382 us (65 TFLOP/s).
+// rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  dq of the long histories above is 2.4e-3 off (relative, all of it) in one
+// part and 1.7e-3 in two, which is its own rounding; of 2048 histories of up to 200 items, slopes, 1.8e-3 in two.
+// Bound as the forward is: the sizes above take 576 us (844 TFLOP/s), 197 us and 379 us (66 TFLOP/s).
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROUPS, PARTS)) void seq_attn_dq_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
@@ -772,8 +772,8 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
 // S = Q K^T and dP = dO V^T have the keys as columns; dV^T = dO^T P and dK^T = Q^T dS.
 // Two wavefronts share 32 keys, one for each half of a tile's 64 queries, and add their sums at the end: the keys that all
 // queries of a long sequence see are the longest work of all, and go by in half the steps.
-// The sizes above: 1000 us (648 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 230 us (latency of short
-// walks) and 521 us with 13 for the join (62 TFLOP/s).
+// The sizes above: 885 us (733 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 229 us (latency of short
+// walks) and 518 us with 13 for the join (62 TFLOP/s).
 template <int DT, int DP, int GROUPS_, int PARTS_>
 struct Dkv {
   static constexpr int GROUPS = GROUPS_, PARTS = PARTS_, KEYS = 32 * GROUPS, THREADS = 64 * GROUPS * PARTS, BQ = 32 * PARTS;
@@ -1120,7 +1120,7 @@ int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
         return go(Int<4>{}, Int<2>{}, Int<1>{});
       } else {
         // Short histories of narrow rows: tiles of 32 keys leave registers for four workgroups a CU.  (2048 histories of up to 200 items, d 64:
-        // 131 us, 143 with 64 keys; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
+        // 127 us, 143 with 64 keys and weights in one part; 500 candidate lists against up to 1000 items, d 40: 48 us, 45.)
         if (cut == k4x1Short || (dp() <= 64 && s->max_k <= 256)) return go(Int<4>{}, Int<1>{}, Int<1>{});
         return go(Int<4>{}, Int<1>{}, Int<2>{});
       }
