@@ -473,13 +473,15 @@ class QkRope:
             T = positions.numel()
         self.T, self.Hq, self.Hk, self.d = int(T), Hq, Hk, d
         self.positions, self.inv_freq, self.wq, self.wk = positions, inv_freq, wq, wk
-        arrays = (_vector("QkRope", positions, self.T, torch.int32), _vector("QkRope", inv_freq, rot // 2, torch.float32),
-                  _vector("QkRope", wq, d, torch.float32), _vector("QkRope", wk, d, torch.float32))
-        # one struct for each storage type, none written again: calls of several threads may use the plan at once
-        self.c = {t: _QkRopeC(self.T, Hq, Hk, d, t, rot, layout, *arrays, eps, mscale) for t in _ELEM}
+        self.fields = (rot, layout, _vector("QkRope", positions, self.T, torch.int32), _vector("QkRope", inv_freq, rot // 2, torch.float32),
+                       _vector("QkRope", wq, d, torch.float32), _vector("QkRope", wk, d, torch.float32), eps, mscale)
+        self.c = {}  # a struct for each storage type, written once: calls of several threads may use the plan at once
 
     def ref(self, dtype: int):
-        return C.byref(self.c[dtype])
+        c = self.c.get(dtype)
+        if c is None:  # (as in SeqBatch.ref)
+            c = self.c[dtype] = _QkRopeC(self.T, self.Hq, self.Hk, self.d, dtype, *self.fields)
+        return C.byref(c)
 
 
 def rope_frequencies(rot: int, base: float = 10000.0, stretch: float = 1.0, keep_turns: Optional[float] = None,
