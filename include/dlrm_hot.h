@@ -523,6 +523,40 @@ int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int
                           const float* lse, const dlrm_heads* dout, const dlrm_heads* dq, const dlrm_heads* dk,
                           const dlrm_heads* dv, void* workspace, size_t workspace_bytes, void* stream);
 
+#define DLRM_MAX_BUCKETS 128
+
+/*
+ * A learned bias of scores by the buckets of relative places (host struct, device arrays).  The distance of a pair is the query's
+ * place less the key's, negative for keys behind the query; its bucket is the number of bounds that are at most the distance, and
+ * table[h][bucket] is added to the score (after the cap, beside the slopes): x + table[h * n + bucket].  Distances below bounds[0] are in bucket
+ * 0, those from bounds[n - 2] on in bucket n - 1.  A bias of -inf hides a bucket.
+ */
+typedef struct dlrm_rel_bias {
+  const float* table;    /* [Hq, n] */
+  const int32_t* bounds; /* [n - 1], ascending, no two the same; may be NULL for n == 1 */
+  int32_t n;             /* buckets, 1 .. DLRM_MAX_BUCKETS */
+} dlrm_rel_bias;
+
+/* dlrm_seq_attn_fwd with a learned bias.  (max_q + 31) times the query heads of a key head <= 2^31 - 1025. */
+int32_t dlrm_seq_attn_bias_fwd(const dlrm_seq_batch* seq, const dlrm_rel_bias* bias, int32_t Hq, int32_t Hk, int32_t d,
+                               int32_t dtype, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
+                               const dlrm_heads* out, float* lse, void* stream);
+
+/* Bytes of workspace dlrm_seq_attn_bias_bwd needs; 0 for an unsupported shape. */
+size_t dlrm_seq_attn_bias_bwd_workspace_bytes(const dlrm_seq_batch* seq, const dlrm_rel_bias* bias, int32_t Hq, int32_t Hk,
+                                              int32_t d, int32_t dtype);
+
+/*
+ * dlrm_seq_attn_bwd with a learned bias; out and lse as dlrm_seq_attn_bias_fwd wrote them.  dtable: fp32 [Hq, n], the gradient of the table, summed
+ * over all sequences (written, zeros where no pair is in a bucket).  Its sums are fp32 whatever the rows' type, in an order that depends on
+ * the arguments alone: bitwise reproducible.
+ */
+int32_t dlrm_seq_attn_bias_bwd(const dlrm_seq_batch* seq, const dlrm_rel_bias* bias, int32_t Hq, int32_t Hk, int32_t d,
+                               int32_t dtype, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
+                               const dlrm_heads* out, const float* lse, const dlrm_heads* dout, const dlrm_heads* dq,
+                               const dlrm_heads* dk, const dlrm_heads* dv, float* dtable, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /* Bytes of workspace dlrm_cache_attn needs for up to max_len cached items a sequence, whatever smaller max_len a call then has; 0 for an
  * unsupported shape. */
 size_t dlrm_cache_attn_workspace_bytes(const dlrm_kv_cache* cache, int32_t Hq, int32_t max_len);

@@ -5,6 +5,7 @@ if the library is missing or a call fails, an exception is raised."""
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 import threading
@@ -64,6 +65,10 @@ class _SeqBatchC(C.Structure):
         ("max_k", C.c_int32), ("q_off", C.c_void_p), ("k_off", C.c_void_p), ("prefix", C.c_void_p),
         ("slopes", C.c_void_p), ("scale", C.c_float), ("cap", C.c_float),
     ]
+
+
+class _RelBiasC(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("bounds", C.c_void_p), ("n", C.c_int32)]
 
 
 _lib = None
@@ -136,6 +141,13 @@ def lib() -> C.CDLL:
         L.dlrm_qk_rope_append.argtypes = [rp, hd, hd, hd, hd, kc, vp, vp]
         L.dlrm_seq_attn_fwd.restype = i32
         L.dlrm_seq_attn_fwd.argtypes = [sq, i32, i32, i32, i32, hd, hd, hd, hd, vp, vp]
+        rb = C.POINTER(_RelBiasC)
+        L.dlrm_seq_attn_bias_fwd.restype = i32
+        L.dlrm_seq_attn_bias_fwd.argtypes = [sq, rb, i32, i32, i32, i32, hd, hd, hd, hd, vp, vp]
+        L.dlrm_seq_attn_bias_bwd_workspace_bytes.restype = sz
+        L.dlrm_seq_attn_bias_bwd_workspace_bytes.argtypes = [sq, rb, i32, i32, i32, i32]
+        L.dlrm_seq_attn_bias_bwd.restype = i32
+        L.dlrm_seq_attn_bias_bwd.argtypes = [sq, rb, i32, i32, i32, i32, hd, hd, hd, hd, vp, hd, hd, hd, hd, vp, vp, sz, vp]
         L.dlrm_seq_attn_bwd_workspace_bytes.restype = sz
         L.dlrm_seq_attn_bwd_workspace_bytes.argtypes = [sq, i32, i32, i32, i32]
         L.dlrm_seq_attn_bwd.restype = i32
@@ -626,6 +638,75 @@ def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: Opt
     n = max(int(lib().dlrm_seq_attn_bwd_workspace_bytes(seq.ref(Hq, d), Hq, Hk, d, t)) for t in ((F32, F16, BF16) if dtype is None else (dtype,)))
     if n == 0:
         raise DlrmError("dlrm_seq_attn_bwd_workspace_bytes", -2)
+    return torch.empty(n, dtype=torch.uint8, device=seq.q_off.device)
+
+
+class RelBias:
+    """A learned bias of scores by buckets of relative places (dlrm_rel_bias).  table: fp32 [Hq, n]; bounds: int32 [n - 1], ascending (see
+    relative_bounds; None for one bucket)."""
+
+    def __init__(self, table: torch.Tensor, bounds: Optional[torch.Tensor]):
+        if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous():
+            raise ValueError("RelBias: the table is a contiguous float32 [query heads, buckets]")
+        self.Hq, self.n = (int(x) for x in table.shape)
+        if bounds is None and self.n != 1:
+            raise ValueError("RelBias: %d buckets have %d bounds" % (self.n, self.n - 1))
+        self.table, self.bounds = table, bounds
+        self.c = _RelBiasC(table.data_ptr(), _vector("RelBias", bounds, self.n - 1, torch.int32), self.n)
+
+    def ref(self, Hq: int):
+        if self.Hq != Hq:
+            raise ValueError("RelBias: a table of %d heads for %d query heads" % (self.Hq, Hq))
+        return C.byref(self.c)
+
+
+def relative_bounds(n: int, far: int, both: bool = False, device=None) -> torch.Tensor:
+    """Bounds of n buckets for RelBias: half of them for distances 0, 1, 2, ... alone, the others wider by equal factors, the last from `far` on.
+    With `both` half of the n are for keys behind the query: a distance of -x has a bucket of its own where x has."""
+    def up(m):
+        near = (m + 1) // 2
+        b = list(range(1, near + 1))
+        for k in range(1, m - near + 1):
+            b.append(max(b[-1] + 1, math.ceil(near * (max(far, near + 1) / near) ** (k / (m - near)))))
+        return b
+    if n < 1:
+        raise ValueError("relative_bounds: at least one bucket is needed")
+    m = n - 1
+    b = [1 - x for x in reversed(up(m // 2))] + up(m - m // 2) if both else up(m)
+    return torch.tensor(b, dtype=torch.int32, device=device)
+
+
+def dlrm_seq_attn_bias_fwd(seq: SeqBatch, bias: RelBias, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                           lse: Optional[torch.Tensor] = None):
+    """dlrm_seq_attn_fwd with a learned bias."""
+    fn = "dlrm_seq_attn_bias_fwd"
+    (_, Hq, d), dt = _first(fn, q)
+    Hk = _first(fn, k)[0][1]
+    rq, rk = (seq.Tq, Hq, d), (seq.Tk, Hk, d)
+    _check(fn, lib().dlrm_seq_attn_bias_fwd(seq.ref(Hq, d), bias.ref(Hq), Hq, Hk, d, dt, *_heads(fn, dt, ((q, rq), (k, rk), (v, rk), (out, rq))),
+                                            _vector(fn, lse, Hq * seq.Tq, torch.float32), _stream()))
+
+
+def dlrm_seq_attn_bias_bwd(seq: SeqBatch, bias: RelBias, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                           dout: torch.Tensor, dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, dtable: torch.Tensor, workspace: torch.Tensor):
+    """dlrm_seq_attn_bwd with a learned bias; out, lse: dlrm_seq_attn_bias_fwd's; dtable: fp32 [Hq, n], written."""
+    fn = "dlrm_seq_attn_bias_bwd"
+    (_, Hq, d), dt = _first(fn, q)
+    Hk = _first(fn, k)[0][1]
+    rq, rk = (seq.Tq, Hq, d), (seq.Tk, Hk, d)
+    h = _heads(fn, dt, ((q, rq), (k, rk), (v, rk), (out, rq), (dout, rq), (dq, rq), (dk, rk), (dv, rk)))
+    ws, ws_bytes = _workspace(workspace)
+    _check(fn, lib().dlrm_seq_attn_bias_bwd(seq.ref(Hq, d), bias.ref(Hq), Hq, Hk, d, dt, h[0], h[1], h[2], h[3],
+                                            _vector(fn, lse, Hq * seq.Tq, torch.float32), h[4], h[5], h[6], h[7],
+                                            _vector(fn, dtable, Hq * bias.n, torch.float32), ws, ws_bytes, _stream()))
+
+
+def alloc_seq_attn_bias_workspace(seq: SeqBatch, bias: RelBias, Hq: int, Hk: int, d: int, dtype: Optional[int] = None) -> torch.Tensor:
+    """For rows of one storage type, or of any."""
+    n = max(int(lib().dlrm_seq_attn_bias_bwd_workspace_bytes(seq.ref(Hq, d), bias.ref(Hq), Hq, Hk, d, t))
+            for t in ((F32, F16, BF16) if dtype is None else (dtype,)))
+    if n == 0:
+        raise DlrmError("dlrm_seq_attn_bias_bwd_workspace_bytes", -2)
     return torch.empty(n, dtype=torch.uint8, device=seq.q_off.device)
 
 

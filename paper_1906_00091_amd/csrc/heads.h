@@ -38,6 +38,12 @@ __host__ inline int check_head_shape(int Hq, int Hk, int d, int dtype) {
   return DLRM_OK;
 }
 
+__host__ inline int check_rel_bias(const dlrm_rel_bias* b) {
+  if (!b || !b->table) return DLRM_ERR_NULL;
+  if (b->n < 1 || b->n > DLRM_MAX_BUCKETS) return DLRM_ERR_BAD_SHAPE;
+  return b->n > 1 && !b->bounds ? DLRM_ERR_NULL : DLRM_OK;
+}
+
 // 16-byte chunk <- fp32 values, rounded to nearest-even once where the storage type has 16 bits
 template <int DT>
 __device__ inline u32x4 narrow(const float* f) {

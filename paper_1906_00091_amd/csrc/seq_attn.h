@@ -188,6 +188,12 @@ struct SeqArgs {
   int by_block;  // the grid is (walk, sequence, block), else walks times slots
   int slots, slot0;  // slots in all, and the first of this launch
   float scale, cap;
+  // a learned bias by buckets (else unused)
+  const float* table;     // [Hq, buckets]
+  const int32_t* bounds;  // [buckets - 1]
+  int buckets, bucket_steps;  // 2^bucket_steps >= buckets
+  float* bias_part;       // [Hq][bias_parts][buckets]: sums of the score gradients, of every wavefront of the keys' gradients
+  int64_t bias_parts;
 };
 
 // Workgroup -> walk (key head + Hk * split), sequence and first row, blocks of ROWS rows, `per` rows for each item of `off`.  A sequence with n rows needs
@@ -196,7 +202,13 @@ struct SeqArgs {
 // through all sequences, so with causal sequences the blocks of most work of every one of them start first.  Else it is walks times
 // slots: sequence s starts at slot off[s] * per / ROWS + s, which leaves it enough, and is found by all 64 lanes at once, each step
 // asking 64 places; more slots than a launch has threads for go in several.  Workgroups past a sequence's rows end at once.
-template <int ROWS>
+// BY_HEAD: blocks of ROWS / 32 units, a unit being 32 items under one of `per` heads; sequence s has ceil(n / 32) * per of them and the slots from
+// (off[s] / 32 + s) * per / (ROWS / 32) + s on.
+template <int ROWS, bool BY_HEAD>
+__host__ __device__ inline int64_t first_slot(int64_t off, int per, int s) {
+  return (BY_HEAD ? ((off >> 5) + s) * per / (ROWS / 32) : off * per / ROWS) + s;
+}
+template <int ROWS, bool BY_HEAD = false>
 __device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per, bool last_first, int& walk, int& seq, int& row0) {
   const int walks = a.Hk * a.splits;
   if (a.by_block) {
@@ -212,17 +224,17 @@ __device__ inline void find_block(const SeqArgs& a, const int64_t* off, int per,
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int step = (hi - lo + 63) >> 6, s = lo + lane_id() * step;
-    const bool before = s < hi && off[s] * per / ROWS + s <= slot;
+    const bool before = s < hi && first_slot<ROWS, BY_HEAD>(off[s], per, s) <= slot;
     const int n = __popcll(__ballot(before));  // >= 1: the first place always is
     hi = min(lo + n * step, hi);
     lo = lo + (n - 1) * step;
   }
   seq = __builtin_amdgcn_readfirstlane(lo);
-  row0 = (slot - (int)(off[seq] * per / ROWS) - seq) * ROWS;
+  row0 = (slot - (int)first_slot<ROWS, BY_HEAD>(off[seq], per, seq)) * ROWS;
 }
 
 // What a score is made of, fixed at compile time: without a cap and slopes an element costs a multiply-add and an exponential.
-enum { kPlain = 0, kSlopes = 1, kBend = 2, kLarge = 4 };  // bits; kLarge: a cap that 16-bit rows take as fp32 rows do (with kBend and, slopes or none, kSlopes)
+enum { kPlain = 0, kSlopes = 1, kBend = 2, kLarge = 4, kBias = 8 };  // bits; kLarge: a cap that 16-bit rows take as fp32 rows do (with kBend and, slopes or none, kSlopes)
 
 // The score of a product s is, in powers of two, c * y(s) + base - slope * |distance|:
 //   without a cap  y = s, c = scale log2 e, base = 0;
@@ -278,6 +290,71 @@ __device__ inline bool too_large(float top) { return top > 32768.0f && top < kIn
 
 // the other lane half's value
 __device__ inline float other_half(float v) { return __shfl_xor(v, 32, DLRM_WAVE); }
+
+// ---------------------------------------------------------------------------------------------------------------
+// A learned bias by buckets (kBias).  The bias of a pair goes by its distance alone, and a tile of 32 x 32 pairs of one head has 63 of them: a wavefront
+// finds the bucket of all at once, one distance a lane, by a binary search in LDS, puts their biases side by side in LDS, and each lane
+// reads its 16 from there, at offsets known at compile time.  So wavefronts with a bias hold 32 items of ONE head (not packed by heads as RowWork's
+// others are).  A tile whose distances lie in one bucket, as beyond the last bound, takes one value and no search.  Slopes go into the same
+// values.
+constexpr int kBuckets = DLRM_MAX_BUCKETS;
+
+// SUB tiles of a step lie 32 distances apart: their windows overlap, the last tile's first.
+template <int HEADS, int WAVES, int SUB>
+struct BiasLds {
+  int bounds[kBuckets];  // then the largest integer, up to a power of two of them
+  float rows[HEADS][kBuckets];
+  float window[WAVES][32 + 32 * SUB];
+};
+template <int HEADS, int WAVES, int SUB>
+__device__ inline BiasLds<HEADS, WAVES, SUB>& bias_lds() {
+  __shared__ BiasLds<HEADS, WAVES, SUB> lds;
+  return lds;
+}
+
+__device__ inline void load_bounds(const SeqArgs& a, int* bounds, int threads) {
+  for (int i = threadIdx.x; i < 1 << a.bucket_steps; i += threads) bounds[i] = i < a.buckets - 1 ? a.bounds[i] : 0x7fffffff;
+}
+// biases of a head in powers of two, by `threads` threads of which this is number `id`
+__device__ inline void load_biases(const SeqArgs& a, int head, float* row, int id, int threads) {
+  for (int i = id; i < a.buckets; i += threads) row[i] = a.table[(int64_t)head * a.buckets + i] * kLog2e;
+}
+__device__ inline void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+struct Bias {
+  const int* bounds;
+  int n, steps, first, last;  // first and last: the outer bounds
+  __device__ inline Bias(const SeqArgs& a, const int* bounds_)
+      : bounds(bounds_), n(a.buckets), steps(a.bucket_steps), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
+  // how many bounds are at most `away`
+  __device__ inline int bucket_of(int away) const {
+    int b = 0;
+    for (int step = 1 << steps >> 1; step > 0; step >>= 1) b += bounds[b + step - 1] <= away ? step : 0;
+    return b;
+  }
+  // Looks at the distances from `least` on, this lane's `least` + lane.  True where all have one bias, which `flat` then is; else they go to `window`.
+  // bucket: this lane's.  row: the head's biases; slope: the head's, in powers of two.
+  __device__ inline bool look(int least, const float* row, float slope, float* window, int& bucket, float& flat) const {
+    if (slope == 0.0f && (least >= last || least + 63 < first)) {
+      bucket = least >= last ? n - 1 : 0;
+      flat = row[bucket];
+      return true;
+    }
+    const int away = least + lane_id();  // (64 of them: the last belongs to the neighbour's window)
+    bucket = bucket_of(away);
+    const float v = fmaf(-slope, fabsf((float)away), row[bucket]);
+    flat = v;
+    if (slope == 0.0f && __ballot(bucket != __builtin_amdgcn_readfirstlane(bucket)) == 0) return true;
+    wave_fence();
+    window[lane_id()] = v;
+    wave_fence();
+    return false;
+  }
+};
+__device__ inline float slope_of(const SeqArgs& a, int head) { return a.slopes ? a.slopes[head] * kLog2e : 0.0f; }
 
 // Rows t of an accumulator set acc^T [DP columns x 32 rows]: row lane % 32, columns 32 b + 8 g + 4 h + 0..3.
 template <int DT, int NB>
@@ -353,9 +430,10 @@ struct MyRow {
   int i, head;
   bool there;
 };
-template <int GROUPS, int PARTS>
+template <int GROUPS, int PARTS, bool BY_HEAD = false>
 struct RowWork {
   int seq, row0, group, part, hk, G;
+  int item0, head;  // BY_HEAD: the wavefront's first item, and its head
   int64_t q0, k0;
   Span sp;
   MyRow me;
@@ -363,8 +441,29 @@ struct RowWork {
   __device__ inline bool find(const SeqArgs& a) {
     constexpr int ROWS = 32 * GROUPS;
     G = a.Hq / a.Hk;
-    find_block<ROWS>(a, a.q_off, G, true, hk, seq, row0);  // late rows see most keys
+    find_block<ROWS, BY_HEAD>(a, a.q_off, G, true, hk, seq, row0);  // late rows see most keys
     sp = span_of(a, seq, q0, k0);
+    if constexpr (BY_HEAD) {
+      const int units = (sp.nq + 31) / 32 * G, unit0 = row0 / 32;
+      if (unit0 >= units) return false;
+      const int wave = __builtin_amdgcn_readfirstlane(wave_id());
+      group = wave % GROUPS;
+      part = wave / GROUPS;
+      const int unit = unit0 + group, last = min(unit0 + GROUPS, units) - 1;
+      const bool any = unit < units;
+      item0 = any ? unit / G * 32 : 0;
+      head = hk * G + (any ? unit % G : 0);
+      const int i = item0 + (lane_id() & 31);
+      me.there = any && i < sp.nq;
+      me.i = me.there ? i : 0;
+      me.head = head;
+      me.t = q0 + me.i;
+      vis = me.there ? sp.vis(i) : 0;
+      wave_vis = any ? sp.vis(min(item0 + 31, sp.nq - 1)) : 0;
+      wave_full = any ? sp.vis(item0) : 0;
+      end = sp.vis(min(last / G * 32 + 31, sp.nq - 1));
+      return true;
+    }
     const int rows = sp.nq * G;
     if (row0 >= rows) return false;
     group = wave_id() % GROUPS;
@@ -440,10 +539,11 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
   typedef Walk<DT, DP, GROUPS, PARTS, SUB> W;
   constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && PARTS * SUB == 1;  // weights in two parts
+  constexpr bool BIAS = (KIND & kBias) != 0;
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   __shared__ float stat[PARTS > 1 ? PARTS * GROUPS * 2 * 32 : 1];
-  RowWork<GROUPS, PARTS> w;
+  RowWork<GROUPS, PARTS, BIAS> w;
   if (!w.find(a)) return;
   const Span& sp = w.sp;
   const int lane = lane_id(), h = lane >> 5;
@@ -467,6 +567,19 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
     tk.store(lds);
     tv.store(lds + TILE);
   }
+  const int* bounds = nullptr;
+  const float* biases = nullptr;
+  float* window = nullptr;
+  float slope = 0.0f;
+  if constexpr (BIAS) {
+    auto& bl = bias_lds<GROUPS, GROUPS * PARTS, SUB>();
+    load_bounds(a, bl.bounds, THREADS);
+    if (w.part == 0) load_biases(a, w.head, bl.rows[w.group], lane, DLRM_WAVE);
+    bounds = bl.bounds;
+    biases = bl.rows[w.group];
+    window = bl.window[w.group + GROUPS * w.part];
+    slope = slope_of(a, w.head);
+  }
   __syncthreads();
   for (int t = 0; t < tiles; ++t) {
     const int jt = t * BK;
@@ -479,6 +592,15 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       const char* ks = lds + (t & (W::BUFS - 1)) * 2 * TILE + 32 * SUB * w.part * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 s[SUB];
+      float flat[SUB];
+      bool is_flat[SUB];
+      if constexpr (BIAS) {
+        const Bias bias(a, bounds);
+        int bucket;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+          is_flat[u] = bias.look(w.item0 + sp.shift - (j0 + 32 * u + 31), biases, slope, window + 32 * (SUB - 1 - u), bucket, flat[u]);
+      }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
@@ -491,8 +613,20 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       }
       __builtin_amdgcn_s_setprio(0);
       // with slopes the whole score, else what the factor c still goes to, in the multiply-add before the exponential
-      const float c = KIND & kSlopes ? 1.0f : sc.c;
-      if constexpr (KIND != kPlain) {
+      const float c = KIND & (kSlopes | kBias) ? 1.0f : sc.c;
+      if constexpr (BIAS) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+          const float* at = window + 32 * (SUB - 1 - u) + (lane & 31) + 31 - 4 * h;
+          if (is_flat[u]) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(sc.y(s[u][r]), sc.c, flat[u]);
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(sc.y(s[u][r]), sc.c, at[-acc_row(r, 0)]);
+          }
+        }
+      } else if constexpr (KIND != kPlain) {
         const float away = (float)(place - (j0 + 4 * h));
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
@@ -609,10 +743,11 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
   constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
   constexpr bool TWO = DT != DLRM_F32 && (DP <= 64 || (KIND & kSlopes) != 0);  // ds in two parts
+  constexpr bool BIAS = (KIND & kBias) != 0;
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
-  __shared__ float sums[PARTS > 1 ? PARTS * GROUPS * 32 : 1];
-  RowWork<GROUPS, PARTS> w;
+  __shared__ float sums[PARTS > 1 ? (BIAS ? 2 : 1) * PARTS * GROUPS * 32 : 1];
+  RowWork<GROUPS, PARTS, BIAS> w;
   if (!w.find(a)) return;
   const Span& sp = w.sp;
   const int lane = lane_id(), h = lane >> 5;
@@ -649,7 +784,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
   f32x16 g[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) g[b] = f32x16{};
-  float sum = 0.0f;  // of p dp
+  float sum = 0.0f, mass = 0.0f;  // of p dp; with a bias: of p
   const char* kb = row_of(a.k, w.k0, w.hk);
   const char* vb = row_of(a.v, w.k0, w.hk);
   const int tiles = (w.end + BK - 1) / BK;
@@ -659,6 +794,19 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
     tv.load(vb, a.v.st, sp.nk, a.d);
     tk.store(lds);
     tv.store(lds + TILE);
+  }
+  const int* bounds = nullptr;
+  const float* biases = nullptr;
+  float* window = nullptr;
+  float slope = 0.0f;
+  if constexpr (BIAS) {
+    auto& bl = bias_lds<GROUPS, GROUPS * PARTS, 1>();
+    load_bounds(a, bl.bounds, THREADS);
+    if (w.part == 0) load_biases(a, w.head, bl.rows[w.group], lane, DLRM_WAVE);
+    bounds = bl.bounds;
+    biases = bl.rows[w.group];
+    window = bl.window[w.group + GROUPS * w.part];
+    slope = slope_of(a, w.head);
   }
   __syncthreads();
   for (int t = 0; t < tiles; ++t) {
@@ -672,6 +820,12 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
       const char* ks = lds + (t & (W::BUFS - 1)) * 2 * TILE + 32 * w.part * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 s = {}, dp = {};
+      float flat = 0.0f;
+      bool is_flat = false;
+      if constexpr (BIAS) {
+        int bucket;
+        is_flat = Bias(a, bounds).look(w.item0 + sp.shift - (j0 + 31), biases, slope, window, bucket, flat);
+      }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
@@ -681,31 +835,49 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
       }
       __builtin_amdgcn_s_setprio(0);
       const float away = (float)(place - (j0 + 4 * h));
+      const float* at_bias = BIAS ? window + (lane & 31) + 31 - 4 * h : nullptr;
+      auto exponent = [&](float y, int r, auto one_bias) {
+        if constexpr (BIAS) return fmaf(y, sc.c, (one_bias() ? flat : at_bias[-acc_row(r, 0)]) - rest);
+        return sc.exponent(y, away - (float)acc_row(r, 0), rest);
+      };
       if (j0 == 0 && w.wave_full <= 32) {  // once a wavefront, and only the first of a sequence
         float all = 0.0f;
+        if (BIAS && is_flat) {
+          wave_fence();
+          window[lane] = flat;
+          wave_fence();
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(sc.exponent(sc.y(s[r]), away - (float)acc_row(r, 0), rest));
+          const float p = __builtin_amdgcn_exp2f(exponent(sc.y(s[r]), r, Int<0>{}));
           all += acc_row(r, h) < w.vis ? p * dp[r] : 0.0f;
         }
         all += other_half(all);
         if (w.vis <= 32) delta = all * (LIFT ? __builtin_amdgcn_exp2f(-lift) : 1.0f);
       }
-      auto gradient = [&](auto masked) {
+      auto gradient = [&](auto masked, auto one_bias) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float y = sc.y(s[r]);
-          float p = __builtin_amdgcn_exp2f(sc.exponent(y, away - (float)acc_row(r, 0), rest)), x = dp[r];
+          float p = __builtin_amdgcn_exp2f(exponent(y, r, one_bias)), x = dp[r];
           if (masked() && j0 + acc_row(r, h) >= w.vis) p = x = 0.0f;
           sum = fmaf(p, x, sum);
+          if constexpr (BIAS) mass += p;
           s[r] = p * (x - delta);
           if constexpr ((KIND & kBend) != 0) s[r] *= sc.derivative(y);
         }
       };
-      if (j0 + 32 > w.wave_full)
-        gradient(Int<1>{});
-      else
-        gradient(Int<0>{});
+      if (BIAS && is_flat) {
+        if (j0 + 32 > w.wave_full)
+          gradient(Int<1>{}, Int<1>{});
+        else
+          gradient(Int<0>{}, Int<1>{});
+      } else {
+        if (j0 + 32 > w.wave_full)
+          gradient(Int<1>{}, Int<0>{});
+        else
+          gradient(Int<0>{}, Int<0>{});
+      }
       if constexpr (LIFT) {
         float top = largest(s);
         if (__ballot(too_large(top))) {
@@ -714,6 +886,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
           lift += down;
           rest -= down;
           sum *= f;
+          mass *= f;
           s *= f;
 #pragma unroll
           for (int b = 0; b < NB; ++b) g[b] *= f;
@@ -745,13 +918,16 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
   if constexpr (LIFT) {
     const float f = __builtin_amdgcn_exp2f(-lift);
     sum *= f;
+    mass *= f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) g[b] *= f;
   }
   sum += other_half(sum);
+  if constexpr (BIAS) mass += other_half(mass);
   if constexpr (PARTS > 1) {
     float* st = sums + w.group * 32 + (lane & 31);
     if (h == 0) st[w.part * GROUPS * 32] = sum;
+    if (BIAS && h == 0) st[(PARTS + w.part) * GROUPS * 32] = mass;
     float ones[PARTS];
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) ones[p] = 1.0f;
@@ -760,8 +936,17 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
     sum = 0.0f;
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) sum += st[p * GROUPS * 32];
+    if constexpr (BIAS) {
+      mass = 0.0f;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) mass += st[(PARTS + p) * GROUPS * 32];
+    }
   }
   if (!w.me.there) return;
+  // With a bias delta is divided by the sum of the weights as they are made here and after this, which is off from 1 by the rounding of lse.  A row's score
+  // gradients then sum to zero in each head's table too; else delta times that rounding would stay in the bucket that has most of the weight (one
+  // history of 506 items, two buckets: the table's gradient 5e-6 -> 1e-6 off).
+  if constexpr (BIAS) sum = mass == 0.0f ? 0.0f : sum / mass;
   if (h == 0) a.delta[at] = sum;
   store_rows<DT, NB>(g, sc.grad, row_of(a.dq, w.me.t, w.me.head), a.d, h);
 }
@@ -788,12 +973,110 @@ struct Dkv {
   static constexpr int LDS = PARTS == 1 || BYTES > JOIN ? BYTES : JOIN;
 };
 
+// Gradient of the learned bias: a pair's is its score gradient, and a bucket's the sum of its pairs' of all sequences.  It is summed here, where delta is the
+// fp32 sum of p dp, so it has fp32's digits whatever the rows' type.  A tile's 1024 score gradients are added up by distance in LDS, where the lanes
+// of one addition have 32 distances and the two lane halves places of their own: none meets another, and the order of the sums is the order of the
+// program.  Then neighbouring distances of one bucket are summed over the lanes and added to the wavefront's sum of that bucket.  Tiles in
+// one bucket are summed in a register.  A wavefront leaves the sums of each head in memory, seq_attn_bias_join_kernel adds them up in a fixed order.
+template <bool BIAS, int WAVES>
+struct BiasSums {
+  __device__ inline BiasSums(const SeqArgs&, int, int, float) {}
+  __device__ inline void finish(int) {}
+};
+template <int WAVES>
+struct BiasSums<true, WAVES> {
+  struct Lds : BiasLds<2, WAVES, 1> {
+    float by_distance[WAVES][2][DLRM_WAVE];
+    float by_bucket[WAVES][kBuckets];
+  };
+  const SeqArgs& a;
+  const float unit;
+  int64_t slot;
+  int head;          // of the sums now held
+  float run = 0.0f;  // this lane's, of tiles in bucket `run_of`
+  int run_of = 0;
+  __device__ static inline Lds& lds() {
+    __shared__ Lds x;
+    return x;
+  }
+  __device__ static inline int wave() { return __builtin_amdgcn_readfirstlane(wave_id()); }
+  __device__ static inline float* window() { return lds().window[wave()]; }
+  __device__ static inline float* distances() { return lds().by_distance[wave()][0]; }
+  __device__ static inline float* buckets() { return lds().by_bucket[wave()]; }
+  __device__ inline BiasSums(const SeqArgs& args, int split, int head0, float unit_) : a(args), unit(unit_), head(head0) {
+    const int64_t block = a.by_block ? (int64_t)blockIdx.z * gridDim.y + blockIdx.y : a.slot0 + blockIdx.x / (a.Hk * a.splits);
+    slot = (block * a.splits + split) * WAVES + wave();
+    for (int i = lane_id(); i < a.buckets; i += DLRM_WAVE) buckets()[i] = 0.0f;
+    distances()[lane_id()] = distances()[DLRM_WAVE + lane_id()] = 0.0f;
+    wave_fence();
+  }
+  template <bool FLAT>
+  __device__ inline void add(int at, float v) {
+    if constexpr (FLAT)
+      run += v;
+    else
+      __hip_atomic_fetch_add(distances() + (lane_id() >> 5) * DLRM_WAVE + at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+  }
+  // before a tile in one bucket
+  __device__ inline void begin(int bucket) {
+    if (bucket != run_of) give_run();
+    run_of = bucket;
+  }
+  // after any other; bucket: this lane's distance's
+  __device__ inline void gather(int bucket) {
+    const int lane = lane_id();
+    wave_fence();
+    float v = distances()[lane] + distances()[DLRM_WAVE + lane];
+    distances()[lane] = distances()[DLRM_WAVE + lane] = 0.0f;
+    wave_fence();
+    const int before = __shfl_up(bucket, 1, DLRM_WAVE);
+    const uint64_t starts = __ballot(lane == 0 || bucket != before);
+    const int start = 63 - __clzll(starts & (~0ull >> (63 - lane)));
+    const bool ends = lane == 63 || (starts >> (lane + 1) & 1);
+    v = segment_scan(v, start);
+    if (ends) buckets()[bucket] += v;
+    wave_fence();
+  }
+  // sum of v over the lanes from `start` to this one
+  __device__ static inline float segment_scan(float v, int start) {
+    const int lane = lane_id();
+    auto step = [&](float t, bool take) { v += take ? t : 0.0f; };
+    step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x111, 0xf, 0xf, false)), lane - start >= 1);  // row_shr:1 (rows of 16 lanes)
+    step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x112, 0xf, 0xf, false)), lane - start >= 2);  // row_shr:2
+    step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x114, 0xf, 0xf, false)), lane - start >= 4);  // row_shr:4
+    step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x118, 0xf, 0xf, false)), lane - start >= 8);  // row_shr:8
+    step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x142, 0xa, 0xf, false)), start < (lane & 48));  // row_bcast:15 into rows 1 and 3
+    step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x143, 0xc, 0xf, false)), start < 32);           // row_bcast:31 into rows 2 and 3
+    return v;
+  }
+  __device__ inline void give_run() {
+    const float all = segment_scan(run, 0);
+    if (lane_id() == 63) buckets()[run_of] += all;
+    wave_fence();
+    run = 0.0f;
+  }
+  // the sums of all heads before `to` are complete
+  __device__ inline void turn_to(int to) {
+    for (; head < to; ++head) {
+      give_run();
+      float* at = a.bias_part + ((int64_t)head * a.bias_parts + slot) * a.buckets;
+      for (int i = lane_id(); i < a.buckets; i += DLRM_WAVE) {
+        at[i] = buckets()[i] * unit;
+        buckets()[i] = 0.0f;
+      }
+      wave_fence();
+    }
+  }
+  __device__ inline void finish(int end) { turn_to(end); }
+};
+
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void seq_attn_dkv_kernel(SeqArgs a) {
   typedef Dkv<DT, DP, GROUPS, PARTS> W;
   typedef typename W::T T;
   constexpr int BQ = W::BQ, STEPS = W::STEPS, NB = W::NB;
   constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && PARTS == 1;  // weights and ds in two parts
+  constexpr bool BIAS = (KIND & kBias) != 0;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   const int G = a.Hq / a.Hk;
   int walk, seq, row0;
@@ -801,7 +1084,12 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   const int split = a.splits == 1 ? 0 : walk / a.Hk, hk = walk - split * a.Hk;
   int64_t q0, k0;
   const Span sp = span_of(a, seq, q0, k0);
-  if (row0 >= sp.nk) return;
+  // (with a bias: every wavefront of the launch leaves its sums for each of its heads, zeros where it has none)
+  BiasSums<BIAS, W::GROUPS * PARTS> sums(a, split, hk * G, DT == DLRM_F16 ? 0x1p-15f : 1.0f);
+  if (row0 >= sp.nk) {
+    sums.finish(hk * G + G);
+    return;
+  }
   const int lane = lane_id(), h = lane >> 5, group = wave_id() % W::GROUPS, part = wave_id() / W::GROUPS;
   const int w0 = row0 + group * 32, j = w0 + (lane & 31);
   const bool there = j < sp.nk;
@@ -837,6 +1125,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     t += first % tiles;
   }
   const float base = Score<DT, KIND>(a, hk * G).base;
+  int loaded = -1;  // head of the biases that were put into LDS last
   // fp16: p is 2^15 times the weight, ds made from it, and that times `f` for the product: from nothing met so far (any value is too large) down
   constexpr bool LIFT = DT == DLRM_F16;
   float f = LIFT ? 0x1p60f : 1.0f;
@@ -854,7 +1143,12 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       float* stat = reinterpret_cast<float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ;
       stat[threadIdx.x] = threadIdx.x < BQ ? lse2_of(sraw, row) - base - kGradWeightLift<DT> : row ? sraw : 0.0f;
     }
+    if constexpr (BIAS) {
+      if (head != loaded) load_biases(a, head, sums.lds().rows[head & 1], threadIdx.x, W::THREADS);
+      loaded = head;
+    }
   };
+  if constexpr (BIAS) load_bounds(a, sums.lds().bounds, W::THREADS);
   if (all > 0) {
     fetch();
     put(0);
@@ -875,6 +1169,13 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       const char* os = qs + W::TILE;
       const float* stat = reinterpret_cast<const float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ + 32 * part + 4 * h;
       f32x16 s = {}, dp = {};
+      float flat = 0.0f;
+      bool is_flat = false;
+      int bucket = 0;
+      if constexpr (BIAS) {
+        sums.turn_to(at);
+        is_flat = Bias(a, sums.lds().bounds).look(i0 + sp.shift - (w0 + 31), sums.lds().rows[at & 1], slope_of(a, at), sums.window(), bucket, flat);
+      }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
@@ -884,19 +1185,38 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       }
       __builtin_amdgcn_s_setprio(0);
       const float away = (float)(i0 + sp.shift + 4 * h - j);
+      auto gradient = [&](auto one_bias) {
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);
-        const f32x4 del = *reinterpret_cast<const f32x4*>(stat + BQ + 8 * r4);
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);
+          const f32x4 del = *reinterpret_cast<const f32x4*>(stat + BQ + 8 * r4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 4 * r4 + i;
-          const float y = sc.y(s[r]);
-          const float p = __builtin_amdgcn_exp2f(sc.exponent(y, away + (float)acc_row(r, 0), rest[i]));
-          dp[r] = p * (dp[r] - del[i]);
-          if constexpr ((KIND & kBend) != 0) dp[r] *= sc.derivative(y);
-          s[r] = p;
+          for (int i = 0; i < 4; ++i) {
+            const int r = 4 * r4 + i;
+            const float y = sc.y(s[r]);
+            float e;
+            if constexpr (BIAS)
+              e = fmaf(y, sc.c, (one_bias() ? flat : sums.window()[acc_row(r, h) + 31 - (lane & 31)]) - rest[i]);
+            else
+              e = sc.exponent(y, away + (float)acc_row(r, 0), rest[i]);
+            const float p = __builtin_amdgcn_exp2f(e);
+            dp[r] = p * (dp[r] - del[i]);
+            if constexpr (BIAS) sums.template add<one_bias()>(acc_row(r, h) + 31 - (lane & 31), i0 + acc_row(r, h) >= from ? dp[r] : 0.0f);
+            if constexpr ((KIND & kBend) != 0) dp[r] *= sc.derivative(y);
+            s[r] = p;
+          }
         }
+      };
+      if constexpr (BIAS) {
+        if (is_flat) {
+          sums.begin(bucket);
+          gradient(Int<1>{});
+        } else {
+          gradient(Int<0>{});
+          sums.gather(bucket);
+        }
+      } else {
+        gradient(Int<0>{});
       }
       if (i0 < wave_full) {
 #pragma unroll
@@ -944,6 +1264,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     if (n + 1 < all) put(n + 1);
     __syncthreads();
   }
+  sums.finish(hk * G + G);
   if constexpr (LIFT) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -994,33 +1315,51 @@ __global__ __launch_bounds__(256) void seq_attn_join_kernel(SeqArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Launches for n items in B sequences of at most `longest`, `per` rows an item, workgroups of `threads` for `rows` rows (see find_block): calls
-// launch(grid), a.slot0 set, as often as it takes.
+// How the blocks of n items in B sequences of at most `longest` are laid out, `per` rows an item, workgroups of `threads` for 32 * groups rows (see find_block).
+struct Blocks {
+  int64_t each, slots, walks, most;  // most: slots of a launch
+  bool by_block;
+  __host__ inline Blocks(int B, int64_t n, int longest, int per, int groups, int threads, int64_t walks_, bool by_head) : walks(walks_) {
+    const int64_t rows = 32 * groups;
+    each = by_head ? (((int64_t)longest + 31) / 32 * per + groups - 1) / groups : ((int64_t)longest * per + rows - 1) / rows;
+    slots = (by_head ? ((n >> 5) + B) * per / groups : n * per / rows) + B;
+    most = kLaunchThreads / (threads * walks);
+    // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
+    // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
+    by_block = each * B <= 3 * slots && B <= 65535 && each <= 65535 && each * B <= most;
+  }
+};
+// Calls launch(grid), a.slot0 set, as often as it takes.
 template <typename F>
-__host__ inline int for_blocks(SeqArgs& a, int64_t n, int longest, int per, int rows, int threads, F launch) {
-  const int64_t each = ((int64_t)longest * per + rows - 1) / rows, slots = n * per / rows + a.B, walks = (int64_t)a.Hk * a.splits;
-  const int64_t most = kLaunchThreads / (threads * walks);  // slots of a launch
-  // Block by block while at most two in three are empty: an empty workgroup ends in under two microseconds, while histories one after
-  // the other leave the last and longest blocks for the end (8 histories of 2048 to 4096 items: 31 % of the device idle).
-  a.by_block = each * a.B <= 3 * slots && a.B <= 65535 && each <= 65535 && each * a.B <= most;
-  if (a.by_block) return launch(dim3((unsigned)walks, a.B, (unsigned)each));
-  if (slots > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;  // (of 32 rows at least: more than the memory has)
-  a.slots = (int)slots;
-  for (int64_t at = 0; at < slots; at += most) {
+__host__ inline int for_blocks(SeqArgs& a, const Blocks& b, F launch) {
+  a.by_block = b.by_block;
+  if (b.by_block) return launch(dim3((unsigned)b.walks, a.B, (unsigned)b.each));
+  if (b.slots > 0x7fffffff) return DLRM_ERR_BAD_SHAPE;  // (of 32 rows at least: more than the memory has)
+  a.slots = (int)b.slots;
+  for (int64_t at = 0; at < b.slots; at += b.most) {
     a.slot0 = (int)at;
-    if (int st = launch(dim3((unsigned)((slots - at < most ? slots - at : most) * walks)))) return st;
+    if (int st = launch(dim3((unsigned)((b.slots - at < b.most ? b.slots - at : b.most) * b.walks)))) return st;
   }
   return DLRM_OK;
 }
 
+// Caps that 16-bit rows take as fp32 rows do.  With a bias smaller ones too: its gradient is fp32, and a score's error is one of the weights that it is made of
+// (a cap of 30 leaves it 2e-6 off).
+__host__ inline bool large_cap(float cap, int dtype, bool bias) {
+  return dtype != DLRM_F32 && cap > (bias ? 64.0f : dtype == DLRM_F16 ? 128.0f : 1024.0f);
+}
+
 // Calls f with the padded width and the kind of score as compile-time constants.
-template <int DT, typename F>
+template <int DT, bool BIAS, typename F>
 __host__ inline int for_kind(const SeqArgs& a, F f) {
   auto by_kind = [&](auto dp) {
     if constexpr (DT != DLRM_F32) {
-      if (a.cap > (DT == DLRM_F16 ? 128.0f : 1024.0f)) return f(dp, std::integral_constant<int, kSlopes | kBend | kLarge>{});
+      if (large_cap(a.cap, DT, BIAS)) return f(dp, std::integral_constant<int, (BIAS ? kBias : kSlopes) | kBend | kLarge>{});
     }
-    switch ((a.slopes ? kSlopes : 0) | (a.cap > 0.0f ? kBend : 0)) {
+    if constexpr (BIAS) {
+      if (a.cap > 0.0f) return f(dp, std::integral_constant<int, kBias | kBend>{});
+      return f(dp, std::integral_constant<int, kBias>{});
+    } else switch ((a.slopes ? kSlopes : 0) | (a.cap > 0.0f ? kBend : 0)) {
       case kPlain: return f(dp, std::integral_constant<int, kPlain>{});
       case kSlopes: return f(dp, std::integral_constant<int, kSlopes>{});
       case kBend: return f(dp, std::integral_constant<int, kBend>{});
@@ -1052,6 +1391,33 @@ __host__ inline int dkv_splits(const dlrm_seq_batch* s, int Hq, int Hk, int d, i
   while (n > 1 && n * bytes > (int64_t)256 << 20) --n;
   return n;
 }
+
+// How the keys' gradients are cut: GROUPS x PARTS wavefronts.
+// Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
+// of up to 200 items, bf16, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
+// (No more than 32 keys: no wavefront without any.  259 histories of one item or none, fp32, d 88: two wavefronts 75 us, one 42.)
+// fp32: 64 histories of 1000 to 1400 items, 4 heads: halved 1203 us with d 64 and 1651 with 96, not halved 1074 and 1485; with 128 columns, which
+// leave no registers for the loads of a whole tile by two wavefronts, 2111 and 2980.
+struct KeysCut {
+  int groups, parts;
+};
+__host__ inline KeysCut dkv_cut(const dlrm_seq_batch* s, int Hk, int d, int dtype, bool bias) {
+  const bool f32 = dtype == DLRM_F32, is_short = short_walks(s), widest = f32 && d > 96;
+  if (large_cap(s->cap, dtype, bias)) return {2, 1};
+  if (!widest && is_short && s->max_k <= 32) return {1, 1};
+  if (!f32) return is_short ? KeysCut{d > 64 ? 4 : 2, 1} : KeysCut{4, 2};
+  return {2, !widest && (is_short || s->Tk * Hk >= 131072) ? 1 : 2};
+}
+// Wavefronts that leave sums of the bias's gradient, for each head, and workgroups that add them up before the last one does.  (2048 histories of up to 200 items
+// leave 16384 for each of 4 heads, which one workgroup a head took 30 us for.)
+__host__ inline int64_t bias_parts(const dlrm_seq_batch* s, int Hk, int d, int dtype, int splits) {
+  if (s->Tk == 0) return 0;
+  const KeysCut cut = dkv_cut(s, Hk, d, dtype, true);
+  const int waves = cut.groups * cut.parts;
+  const Blocks b(s->B, s->Tk, s->max_k, 1, cut.groups, 64 * waves, (int64_t)Hk * splits, false);
+  return (b.by_block ? b.each * s->B : b.slots) * splits * waves;
+}
+__host__ inline int64_t bias_chunks(int64_t parts) { return parts <= 512 ? 1 : parts < 256 * 256 ? (parts + 255) / 256 : 256; }
 
 // How the rows' kernels are cut, by what there is of rows and keys (GROUPS x PARTS wavefronts; `sub` tiles of 32 keys to a part and step).
 //   k4x1: 16-bit types.  Wavefronts that share 32 rows pay for the join, and gain where the rows are too few to fill the device;
@@ -1094,13 +1460,13 @@ __host__ inline int cut_of(const dlrm_seq_batch* s, const SeqArgs& a, bool f32, 
   return s->max_k > 256 && fill < (narrow ? 512 : 256) ? k2x2 : k4x1;
 }
 
-template <int DT>
+template <int DT, bool BIAS>
 int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  return for_kind<DT>(a, [&](auto dp, auto kind) -> int {
+  return for_kind<DT, BIAS>(a, [&](auto dp, auto kind) -> int {
     auto go = [&](auto groups, auto parts, auto sub) -> int {
       if (s->Tq == 0) return DLRM_OK;
       constexpr int threads = 64 * groups() * parts();
-      return for_blocks(a, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), threads, [&](dim3 grid) -> int {
+      return for_blocks(a, Blocks(a.B, s->Tq, s->max_q, a.Hq / a.Hk, groups(), threads, a.Hk, BIAS), [&](dim3 grid) -> int {
         hipLaunchKernelGGL((seq_attn_fwd_kernel<DT, dp(), kind(), groups(), parts(), sub()>), grid, dim3(threads), 0, st, a);
         DLRM_CHECK_LAUNCH();
         return DLRM_OK;
@@ -1128,14 +1494,14 @@ int launch_seq_fwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
   });
 }
 
-template <int DT>
+template <int DT, bool BIAS>
 int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
-  return for_kind<DT>(a, [&](auto dp, auto kind) -> int {
+  return for_kind<DT, BIAS>(a, [&](auto dp, auto kind) -> int {
     constexpr bool F32 = DT == DLRM_F32;
     auto dq = [&](auto groups, auto parts) -> int {
       if (s->Tq == 0) return DLRM_OK;
       constexpr int threads = 64 * groups() * parts();
-      return for_blocks(a, s->Tq, s->max_q, a.Hq / a.Hk, 32 * groups(), threads, [&](dim3 grid) -> int {
+      return for_blocks(a, Blocks(a.B, s->Tq, s->max_q, a.Hq / a.Hk, groups(), threads, a.Hk, BIAS), [&](dim3 grid) -> int {
         hipLaunchKernelGGL((seq_attn_dq_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(threads), 0, st, a);
         DLRM_CHECK_LAUNCH();
         return DLRM_OK;
@@ -1144,7 +1510,7 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
     auto dkv = [&](auto groups, auto parts) -> int {
       if (s->Tk == 0) return DLRM_OK;
       constexpr int threads = 64 * groups() * parts();
-      const int rc = for_blocks(a, s->Tk, s->max_k, 1, 32 * groups(), threads, [&](dim3 grid) -> int {
+      const int rc = for_blocks(a, Blocks(a.B, s->Tk, s->max_k, 1, groups(), threads, (int64_t)a.Hk * a.splits, false), [&](dim3 grid) -> int {
         hipLaunchKernelGGL((seq_attn_dkv_kernel<DT, dp(), kind(), groups(), parts()>), grid, dim3(threads), 0, st, a);
         DLRM_CHECK_LAUNCH();
         return DLRM_OK;
@@ -1175,20 +1541,15 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
       }
       if (rc != DLRM_OK) return rc;
       a.splits = dkv_splits(s, a.Hq, a.Hk, a.d, DT);
-      // Short histories: few steps, so nothing is gained by halving them, and small workgroups hide each other's starts.  (2048 histories
-      // of up to 200 items, bf16, d 64: two wavefronts of one part 217 us, four 242, eight of two parts 391; 8 of up to 4096, d 128: 1789, 1163, 1038.)
-      // (No more than 32 keys: no wavefront without any.  259 histories of one item or none, fp32, d 88: two wavefronts 75 us, one 42.)
-      const bool is_short = short_walks(s);
+      const KeysCut keys = dkv_cut(s, a.Hk, a.d, DT, BIAS);
       if constexpr (!WIDEST) {
-        if (is_short && s->max_k <= 32) return dkv(Int<1>{}, Int<1>{});
+        if (keys.groups == 1) return dkv(Int<1>{}, Int<1>{});
       }
       if constexpr (!F32) {
-        return is_short ? dkv(Int<(dp() > 64) ? 4 : 2>{}, Int<1>{}) : dkv(Int<4>{}, Int<2>{});
+        return keys.parts == 1 ? dkv(Int<(dp() > 64) ? 4 : 2>{}, Int<1>{}) : dkv(Int<4>{}, Int<2>{});
       } else {
-        // 64 histories of 1000 to 1400 items, 4 heads: halved 1203 us with d 64 and 1651 with 96, not halved 1074 and 1485; with 128 columns, which
-        // leave no registers for the loads of a whole tile by two wavefronts, 2111 and 2980.
         if constexpr (!WIDEST) {
-          if (is_short || s->Tk * a.Hk >= 131072) return dkv(Int<2>{}, Int<1>{});
+          if (keys.parts == 1) return dkv(Int<2>{}, Int<1>{});
         }
         return dkv(Int<2>{}, Int<2>{});
       }
@@ -1196,11 +1557,17 @@ int launch_seq_bwd(const dlrm_seq_batch* s, SeqArgs a, hipStream_t st) {
   });
 }
 
-extern template int launch_seq_fwd<DLRM_F32>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
-extern template int launch_seq_fwd<DLRM_F16>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
-extern template int launch_seq_fwd<DLRM_BF16>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
-extern template int launch_seq_bwd<DLRM_F32>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
-extern template int launch_seq_bwd<DLRM_F16>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
-extern template int launch_seq_bwd<DLRM_BF16>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_fwd<DLRM_F32, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_fwd<DLRM_F32, true>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_fwd<DLRM_F16, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_fwd<DLRM_F16, true>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_fwd<DLRM_BF16, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_fwd<DLRM_BF16, true>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_bwd<DLRM_F32, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_bwd<DLRM_F32, true>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_bwd<DLRM_F16, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_bwd<DLRM_F16, true>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_bwd<DLRM_BF16, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+extern template int launch_seq_bwd<DLRM_BF16, true>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
 
 }  // namespace dlrm

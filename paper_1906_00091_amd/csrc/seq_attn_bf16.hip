@@ -2,6 +2,6 @@
 #include "seq_attn.h"
 
 namespace dlrm {
-template int launch_seq_fwd<DLRM_BF16>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
-template int launch_seq_bwd<DLRM_BF16>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+template int launch_seq_fwd<DLRM_BF16, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
+template int launch_seq_bwd<DLRM_BF16, false>(const dlrm_seq_batch*, SeqArgs, hipStream_t);
 }  // namespace dlrm

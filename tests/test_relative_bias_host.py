@@ -1,0 +1,134 @@
+"""The learned relative position bias without a GPU: what the library and the binding refuse, the bounds, the workspaces, and the tests' own 64-bit form
+against differences."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_1906_00091_amd as hot
+from paper_1906_00091_amd import binding
+
+import bias_ref as ref
+from history_ref import offsets
+from test_history_host import BAD_HEADS, BAD_SEQ, BAD_SHAPE, DTYPE, NULL, P, SHAPE, WORKSPACE, heads, seq  # noqa: F401
+
+
+def bias(**kw):
+    a = dict(table=P, bounds=P, n=32)
+    a.update(kw)
+    return binding._RelBiasC(**a)
+
+
+BAD_BIAS = [(dict(table=None), NULL), (dict(bounds=None), NULL), (dict(n=0), SHAPE), (dict(n=-1), SHAPE), (dict(n=129), SHAPE)]
+
+
+def fwd(s=None, b=None, shape=(4, 2, 64, hot.BF16), lse=P, **kw):
+    h = {n: heads() for n in ("q", "k", "v", "o")}
+    h.update(kw)
+    return hot.lib().dlrm_seq_attn_bias_fwd(s, b, *shape, h["q"], h["k"], h["v"], h["o"], lse, None)
+
+
+def bwd(s=None, b=None, shape=(4, 2, 64, hot.BF16), lse=P, dtable=P, ws=P, n=1 << 40, **kw):
+    h = {n_: heads() for n_ in ("q", "k", "v", "o", "do", "dq", "dk", "dv")}
+    h.update(kw)
+    return hot.lib().dlrm_seq_attn_bias_bwd(s, b, *shape, h["q"], h["k"], h["v"], h["o"], lse, h["do"], h["dq"], h["dk"], h["dv"], dtable, ws, n, None)
+
+
+@pytest.mark.parametrize("call", [fwd, bwd])
+def test_refusals(call):
+    assert call(None, bias()) == NULL and call(seq(), None) == NULL
+    for kw, want in BAD_SEQ:
+        assert call(seq(**kw), bias()) == want, kw
+    for kw, want in BAD_BIAS:
+        assert call(seq(), bias(**kw)) == want, kw
+    for shape, want in BAD_SHAPE:
+        assert call(seq(), bias(), shape) == want, shape
+    for n in ("q", "k", "v", "o"):
+        for kw, want in BAD_HEADS:
+            assert call(seq(), bias(), **{n: heads(**kw)}) == want, (n, kw)
+    # 32 items of one head to a wavefront: the last ones of each head may be empty, and rows are counted in 32 bits
+    assert call(seq(Tq=2 ** 31 - 1, max_q=2 ** 30, Tk=1), bias()) == SHAPE
+
+
+def test_refusals_of_the_backward():
+    for n in ("do", "dq", "dk", "dv"):
+        for kw, want in BAD_HEADS:
+            assert bwd(seq(), bias(), **{n: heads(**kw)}) == want, (n, kw)
+    assert bwd(seq(), bias(), lse=None) == NULL and bwd(seq(), bias(), dtable=None) == NULL
+    need = hot.lib().dlrm_seq_attn_bias_bwd_workspace_bytes(C.byref(seq()), C.byref(bias()), 4, 2, 64, hot.BF16)
+    assert need >= 256
+    for ws, n in ((None, need), (P + 128, need), (P, need - 1)):
+        assert bwd(seq(), bias(), ws=ws, n=n) == WORKSPACE
+
+
+def test_workspace_of_unsupported_shapes_is_none():
+    need = hot.lib().dlrm_seq_attn_bias_bwd_workspace_bytes
+    assert need(C.byref(seq(B=0)), C.byref(bias()), 4, 2, 64, hot.BF16) == 0
+    assert need(C.byref(seq()), C.byref(bias(n=0)), 4, 2, 64, hot.BF16) == 0
+    assert need(C.byref(seq()), None, 4, 2, 64, hot.BF16) == 0
+    assert need(C.byref(seq()), C.byref(bias()), 4, 3, 64, hot.BF16) == 0
+    # what is kept grows with the buckets, and holds at least the unbiased backward's
+    s = seq(B=2048, Tq=200000, Tk=200000, max_q=200, max_k=200)
+    sizes = [need(C.byref(s), C.byref(bias(n=n)), 4, 4, 64, hot.BF16) for n in (1, 32, 128)]
+    assert sizes[0] < sizes[1] < sizes[2] and sizes[0] >= hot.lib().dlrm_seq_attn_bwd_workspace_bytes(C.byref(s), 4, 4, 64, hot.BF16)
+
+
+def test_binding_refuses():
+    t = torch.zeros(4, 8)
+    b = torch.arange(1, 8, dtype=torch.int32)
+    for table, bounds in ((t.double(), b), (t[:, ::2], b[:3]), (t[0], b), (t, b.long()), (t, b[:6]), (t, None)):
+        with pytest.raises(ValueError):
+            hot.RelBias(table, bounds)
+    assert hot.RelBias(t[:, :1].contiguous(), None).n == 1
+    off = torch.tensor([0, 4])
+    s = hot.SeqBatch(off, off, 4, 4, 4, 4)
+    x, x2 = torch.zeros(4, 4, 8), torch.zeros(4, 2, 8)
+    with pytest.raises(ValueError, match="4 heads for 2"):
+        hot.dlrm_seq_attn_bias_fwd(s, hot.RelBias(t, b), x2, x2, x2, x2)
+    with pytest.raises(ValueError):
+        hot.dlrm_seq_attn_bias_bwd(s, hot.RelBias(t, b), x, x, x, x, torch.zeros(4, 4), x, x, x, x, torch.zeros(4, 7), None)
+
+
+@pytest.mark.parametrize("both", [False, True])
+@pytest.mark.parametrize("n,far", [(1, 5), (2, 1), (3, 100), (8, 16), (32, 128), (33, 300), (64, 2048), (128, 10), (128, 100000)])
+def test_bounds(n, far, both):
+    b = hot.relative_bounds(n, far, both).tolist()
+    assert len(b) == n - 1 and all(x < y for x, y in zip(b, b[1:]))
+    up = [x for x in b if x > 0]
+    assert up[:1] == [1] * bool(up)
+    if not both:
+        assert up == b
+    else:  # a distance of -x has a bucket of its own where x has
+        down = [1 - x for x in b if x <= 0]
+        assert len(down) == (n - 1) // 2 and len(up) == n - 1 - len(down)
+        near = (len(down) + 1) // 2
+        assert sorted(down)[:near] == up[:near] or len(up) != len(down)
+    if len(up) >= 4 and far > 4 * len(up):
+        assert up[-1] in (far, far + 1)
+
+
+@pytest.mark.parametrize("causal,slopes,cap", [(True, False, 0.0), (False, True, 0.0), (True, True, 2.0)])
+def test_the_64_bit_form_against_differences(causal, slopes, cap):
+    g = torch.Generator().manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)
+    lens, klens, Hq, Hk, d = [3, 0, 6], [5, 2, 4], 4, 2, 8
+    qo, ko = offsets(lens), offsets(klens)
+    x = {"q": rand(9, Hq, d), "k": rand(11, Hk, d), "v": rand(11, Hk, d), "table": rand(Hq, 5)}
+    bounds, do = torch.tensor([-2, 0, 1, 3]), rand(9, Hq, d)
+    sl = rand(Hq).abs() if slopes else None
+    pre = torch.tensor([2, 1, 3]) if causal else None
+    ref.UNIT.setdefault(torch.float64, 2.0 ** -53)
+    ref.TINY.setdefault(torch.float64, 0.0)
+
+    def run(y, dout=None):
+        return ref.attention(y["q"], y["k"], y["v"], qo, ko, causal, pre, sl, y["table"], bounds, 0.3, cap, dout)
+    got = run(x, do)
+    for n in x:
+        grad = got["d" + n]
+        for at in range(0, x[n].numel(), 7):
+            sides = []
+            for step in (1e-5, -1e-5):
+                y = {m: t.clone() for m, t in x.items()}
+                y[n].view(-1)[at] += step
+                sides.append(float((run(y)["out"] * do).sum()))
+            assert abs((sides[0] - sides[1]) / 2e-5 - float(grad.view(-1)[at])) < 1e-8, (n, at)
