@@ -573,6 +573,45 @@ int32_t dlrm_cache_attn(const dlrm_kv_cache* cache, const int32_t* lens, int32_t
                         const dlrm_heads* q, const dlrm_heads* out, const float* slopes, float scale, float cap,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* Bytes of workspace dlrm_cache_attn_bias needs for up to max_len cached items a sequence; 0 for an unsupported shape. */
+size_t dlrm_cache_attn_bias_workspace_bytes(const dlrm_kv_cache* cache, int32_t Hq, int32_t max_len);
+
+/* dlrm_cache_attn with a learned bias. */
+int32_t dlrm_cache_attn_bias(const dlrm_kv_cache* cache, const int32_t* lens, int32_t max_len, const dlrm_rel_bias* bias,
+                             int32_t Hq, const dlrm_heads* q, const dlrm_heads* out, const float* slopes, float scale,
+                             float cap, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * New items of cached sequences that are not in the cache (host struct, device arrays): sequence s has the items [off[s], off[s+1]), numbered
+ * from 0 within it.  Item i sees the sequence's cached items, and item j of its own sequence where j <= i <= last[j]: with the items of
+ * a tree in depth-first order and last[j] the last one below j, an item sees itself and those on its way to the root.  last[j] = j: items that see
+ * no other; last NULL: every item sees those before it (a chain, or a piece of a prompt); last[j] < j: nobody sees j.
+ */
+typedef struct dlrm_new_items {
+  int64_t T;                /* items of all sequences, host copy of off[B] */
+  int32_t max_items;        /* host upper bound on a sequence's items, >= 1; items past it are neither answered nor seen */
+  const int64_t* off;       /* [B+1], off[0] = 0, ascending */
+  const int32_t* last;      /* [T] or NULL */
+  const int32_t* positions; /* [T] places, >= 0, that distances of slopes and bias go by (the length of the cache plus the depth in the tree); may be NULL without these */
+} dlrm_new_items;
+
+/* Bytes of workspace dlrm_cache_tree_attn needs for up to max_len cached items a sequence, whatever smaller max_len a call then has; 0 for
+ * an unsupported shape. */
+size_t dlrm_cache_tree_attn_workspace_bytes(const dlrm_kv_cache* cache, const dlrm_new_items* items, int32_t Hq, int32_t max_len);
+
+/*
+ * Attention of new items over the cache and over one another: q, out [T, Hq, d]; k, v [T, Hk, d] are the new items' keys and values, which the cache does not
+ * hold and does not get (dlrm_qk_rope_append stores those that are kept).  Scores as for dlrm_seq_batch, with bias or NULL; cached item j stands at place j,
+ * a new one at its position.  lens and max_len as for dlrm_cache_attn, but the items of lens[s] all come before the new ones, and max_len may be 0.  An item that
+ * sees nothing gets zeros; values that are not finite may show in items of the same sequence they are hidden from.
+ * max_len plus max_items, and max_items times Hq, <= 2^31 - 1025.
+ * workspace: 256-byte aligned device memory; contents are scratch.
+ */
+int32_t dlrm_cache_tree_attn(const dlrm_kv_cache* cache, const int32_t* lens, int32_t max_len, const dlrm_new_items* items,
+                             int32_t Hq, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
+                             const dlrm_heads* out, const dlrm_rel_bias* bias, const float* slopes, float scale, float cap,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,5 +10,6 @@ from .binding import (  # noqa: F401
     dlrm_place_dense, dlrm_emb_bag_bwd_sgd_timed, dlrm_emb_bag_bwd_adagrad_timed, dlrm_table_init_hash, dlrm_validate_csr, lib, status_string, version,
     ROPE_HALF, ROPE_INTERLEAVED, KvCache, QkRope, SeqBatch, alloc_cache_attn_workspace, alloc_qk_rope_workspace, alloc_seq_attn_workspace,
     RelBias, alloc_seq_attn_bias_workspace, dlrm_seq_attn_bias_bwd, dlrm_seq_attn_bias_fwd, relative_bounds,
+    NewItems, alloc_cache_attn_bias_workspace, alloc_cache_tree_attn_workspace, dlrm_cache_attn_bias, dlrm_cache_tree_attn, tree_order,
     dlrm_cache_attn, dlrm_qk_rope_append, dlrm_qk_rope_bwd, dlrm_qk_rope_fwd, dlrm_seq_attn_bwd, dlrm_seq_attn_fwd, rope_frequencies,
 )

@@ -71,6 +71,10 @@ class _RelBiasC(C.Structure):
     _fields_ = [("table", C.c_void_p), ("bounds", C.c_void_p), ("n", C.c_int32)]
 
 
+class _NewItemsC(C.Structure):
+    _fields_ = [("T", C.c_int64), ("max_items", C.c_int32), ("off", C.c_void_p), ("last", C.c_void_p), ("positions", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -148,6 +152,15 @@ def lib() -> C.CDLL:
         L.dlrm_seq_attn_bias_bwd_workspace_bytes.argtypes = [sq, rb, i32, i32, i32, i32]
         L.dlrm_seq_attn_bias_bwd.restype = i32
         L.dlrm_seq_attn_bias_bwd.argtypes = [sq, rb, i32, i32, i32, i32, hd, hd, hd, hd, vp, hd, hd, hd, hd, vp, vp, sz, vp]
+        ni = C.POINTER(_NewItemsC)
+        L.dlrm_cache_attn_bias_workspace_bytes.restype = sz
+        L.dlrm_cache_attn_bias_workspace_bytes.argtypes = [kc, i32, i32]
+        L.dlrm_cache_attn_bias.restype = i32
+        L.dlrm_cache_attn_bias.argtypes = [kc, vp, i32, rb, i32, hd, hd, vp, f32, f32, vp, sz, vp]
+        L.dlrm_cache_tree_attn_workspace_bytes.restype = sz
+        L.dlrm_cache_tree_attn_workspace_bytes.argtypes = [kc, ni, i32, i32]
+        L.dlrm_cache_tree_attn.restype = i32
+        L.dlrm_cache_tree_attn.argtypes = [kc, vp, i32, ni, i32, hd, hd, hd, hd, rb, vp, f32, f32, vp, sz, vp]
         L.dlrm_seq_attn_bwd_workspace_bytes.restype = sz
         L.dlrm_seq_attn_bwd_workspace_bytes.argtypes = [sq, i32, i32, i32, i32]
         L.dlrm_seq_attn_bwd.restype = i32
@@ -727,4 +740,86 @@ def alloc_cache_attn_workspace(cache: KvCache, Hq: int, max_len: int) -> torch.T
     n = int(lib().dlrm_cache_attn_workspace_bytes(cache.ref(), Hq, max_len))
     if n == 0:
         raise DlrmError("dlrm_cache_attn_workspace_bytes", -2)
+    return torch.empty(n, dtype=torch.uint8, device=cache.table.device)
+
+
+def dlrm_cache_attn_bias(cache: KvCache, lens: torch.Tensor, max_len: int, bias: RelBias, q: torch.Tensor, out: torch.Tensor,
+                         workspace: Optional[torch.Tensor], slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None, cap: float = 0.0):
+    """dlrm_cache_attn with a learned bias."""
+    fn = "dlrm_cache_attn_bias"
+    Hq = _first(fn, q)[0][1]
+    rows = (cache.B, Hq, cache.d)
+    a, b = _heads(fn, cache.dtype, ((q, rows), (out, rows)))
+    ws, ws_bytes = _workspace(workspace)
+    _check(fn, lib().dlrm_cache_attn_bias(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, bias.ref(Hq), Hq, a, b,
+                                          _vector(fn, slopes, Hq, torch.float32), cache.d ** -0.5 if scale is None else scale, cap, ws, ws_bytes,
+                                          _stream()))
+
+
+def alloc_cache_attn_bias_workspace(cache: KvCache, Hq: int, max_len: int) -> torch.Tensor:
+    n = int(lib().dlrm_cache_attn_bias_workspace_bytes(cache.ref(), Hq, max_len))
+    if n == 0:
+        raise DlrmError("dlrm_cache_attn_bias_workspace_bytes", -2)
+    return torch.empty(n, dtype=torch.uint8, device=cache.table.device)
+
+
+class NewItems:
+    """New items of cached sequences that the cache does not hold (dlrm_new_items).  off: int64 [B + 1]; T: its last element; max_items: bound on a
+    sequence's items; last: int32 [T], the last item of its sequence that sees item j (None: all after it do; see tree_order); positions: int32 [T],
+    places that distances go by, for slopes and a bias."""
+
+    def __init__(self, off: torch.Tensor, T: int, max_items: int, last: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+        self.B, self.T, self.max_items = int(off.numel()) - 1, int(T), int(max_items)
+        self.off, self.last, self.positions = off, last, positions
+        self.c = _NewItemsC(self.T, self.max_items, _vector("NewItems", off, self.B + 1, torch.int64), _vector("NewItems", last, self.T, torch.int32),
+                            _vector("NewItems", positions, self.T, torch.int32))
+
+    def ref(self, B: int):
+        if self.B != B:
+            raise ValueError("NewItems: items of %d sequences for a cache of %d" % (self.B, B))
+        return C.byref(self.c)
+
+
+def tree_order(parents: Sequence[int]):
+    """(order, last, depth) of one sequence's items given by the parent of each, -1 where it is drafted right after the cache: item order[i] of the
+    caller is item i of NewItems, in depth-first order, last[i] is the last one below it, depth[i] how many items it has above it.  Lists on the host."""
+    children, roots = [[] for _ in parents], []
+    for i, p in enumerate(parents):
+        if not -1 <= p < len(parents):
+            raise ValueError("tree_order: item %d has parent %d of %d items" % (i, p, len(parents)))
+        (roots if p < 0 else children[p]).append(i)
+    order, last, depth, todo = [], [], [], [(i, 0) for i in reversed(roots)]
+    while todo:
+        i, deep = todo.pop()
+        if i < 0:  # all below item ~i are placed
+            last[~i] = len(order) - 1
+            continue
+        todo.append((~len(order), 0))
+        order.append(i)
+        last.append(0)
+        depth.append(deep)
+        todo.extend((c, deep + 1) for c in reversed(children[i]))
+    if len(order) != len(parents):
+        raise ValueError("tree_order: items that are their own ancestors")
+    return order, last, depth
+
+
+def dlrm_cache_tree_attn(cache: KvCache, lens: torch.Tensor, max_len: int, items: NewItems, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                         out: torch.Tensor, workspace: Optional[torch.Tensor], bias: Optional[RelBias] = None, slopes: Optional[torch.Tensor] = None,
+                         scale: Optional[float] = None, cap: float = 0.0):
+    """q, out: [T, Hq, d]; k, v: [T, Hk, d], the new items' own; lens: int32 [B], items of every sequence in the cache, which all come before the new ones."""
+    fn = "dlrm_cache_tree_attn"
+    Hq = _first(fn, q)[0][1]
+    rq, rk = (items.T, Hq, cache.d), (items.T, cache.Hk, cache.d)
+    ws, ws_bytes = _workspace(workspace)
+    _check(fn, lib().dlrm_cache_tree_attn(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, items.ref(cache.B), Hq,
+                                          *_heads(fn, cache.dtype, ((q, rq), (k, rk), (v, rk), (out, rq))), None if bias is None else bias.ref(Hq),
+                                          _vector(fn, slopes, Hq, torch.float32), cache.d ** -0.5 if scale is None else scale, cap, ws, ws_bytes,
+                                          _stream()))
+
+
+def alloc_cache_tree_attn_workspace(cache: KvCache, Hq: int, max_len: int, items: NewItems) -> torch.Tensor:
+    n = int(lib().dlrm_cache_tree_attn_workspace_bytes(cache.ref(), items.ref(cache.B), Hq, max_len))
+    if n == 0:
+        raise DlrmError("dlrm_cache_tree_attn_workspace_bytes", -2)
     return torch.empty(n, dtype=torch.uint8, device=cache.table.device)

@@ -1,0 +1,437 @@
+// Attention of several new items of every sequence over a paged cache and over one another, and of one new item with a learned bias.
+//
+// As the attention of one new item: a key row is loaded once, straight from its page into the registers that the product takes it in, S^T = K Q^T leaves a
+// lane four keys of one column, and those registers are what O^T = V^T P^T takes; values pass through a piece of LDS of the wavefront's own.  The columns
+// are (item, head) pairs of one key head, 16 to a tile and NT tiles to a wavefront, so that a key is read from memory once for up to 16 NT of them; the
+// workgroups of a sequence's further columns read it from the L2 of their die, which they share.  New items are keys behind the cached ones: key j of a
+// sequence is item j of the cache, or row j - len of the new ones, and only the address of its row differs.
+//
+// The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in the order of the chunks.
+#pragma once
+
+#include <initializer_list>
+
+#include "cache_ops.h"
+
+namespace dlrm {
+
+struct TreeArgs {
+  Rows q, out, new_k, new_v;
+  const char* k;
+  const char* v;
+  const int32_t* pages;
+  const int32_t* lens;
+  const int64_t* off;  // [B + 1] of the new items; NULL: one a sequence, at the place of the newest cached item
+  const int32_t* last;
+  const int32_t* positions;
+  const float* slopes;
+  const float* table;  // [Hq, buckets] or NULL
+  const int32_t* bounds;
+  int buckets, bucket_steps, bias_rows;  // bias_rows: heads whose biases a workgroup needs
+  int B, Hq, Hk, d, cols, n_pages, page_shift, max_len, max_items;  // max_len: the table's items at most
+  int chunk, splits, blocks;  // keys of a chunk; chunks of a sequence; groups of 16 NT columns of a key head
+  int seq0;                   // first sequence of this launch
+  float scale, cap;
+  float* po;  // [T * Hq][splits][d] unnormalised sums
+  float* pm;  // [T * Hq][splits][2] maximum (powers of two), sum of weights
+};
+
+// A sequence's new items and keys.
+struct TreeSeq {
+  int64_t t0;      // its first new item
+  int n, len, total;  // new items; cached items that are read; keys
+  __device__ inline TreeSeq(const TreeArgs& a, int s) {
+    len = max(0, min(a.lens[s], a.max_len));
+    if (a.off) {
+      t0 = a.off[s];
+      n = (int)min(a.off[s + 1] - t0, (int64_t)a.max_items);
+      total = len + n;
+    } else {
+      t0 = s;
+      n = 1;
+      total = len;
+    }
+  }
+};
+
+template <int DT, int DP, int NT, bool LARGE, bool TREE>
+__global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
+  constexpr int WAVES = 4, COLS = 16 * NT;
+  constexpr int EB = Tab<DT>::EB, E = Tab<DT>::ELEMS, STEPS = DP / 32, NB = DP / 16;
+  constexpr int CH = DP * EB / 16, NV = kKeys * CH / DLRM_WAVE;  // chunks of a row; of a tile, per lane
+  constexpr int STRIDE = DP * EB + 16;
+  constexpr int OS = DP + 4;  // row of the joined sums
+  // fp16: weights are at most 2^8 (below) and made 2^7 times as large, sums and all: those of a long cache's many keys are not lost below 2^-24
+  constexpr float LIFT = DT == DLRM_F16 ? 7.0f : 0.0f;
+  constexpr int VBYTES = WAVES * kKeys * STRIDE, OBYTES = WAVES * 16 * OS * 4;
+  __shared__ __attribute__((aligned(16))) char lds[VBYTES > OBYTES ? VBYTES : OBYTES];
+  __shared__ int pages[kTablePages];
+  __shared__ float stat[WAVES][2][16];
+  __shared__ int bounds[DLRM_MAX_BUCKETS];
+  extern __shared__ float biases[];  // [bias_rows][buckets], in powers of two
+
+  // Workgroups go to the 8 dies in turn: those of one sequence, key head and chunk, which read the same keys, lie 8 apart.
+  const int in_eight = blockIdx.x % (8 * a.blocks), blk = in_eight / 8;
+  const int unit = blockIdx.x / (8 * a.blocks) * 8 + in_eight % 8;
+  if (unit >= a.B * a.Hk * a.splits) return;
+  const int split = unit % a.splits, hk = unit / a.splits % a.Hk, s = a.seq0 + unit / a.splits / a.Hk;
+  const int G = a.Hq / a.Hk, c0 = blk * COLS;
+  const int lane = lane_id(), g = lane >> 4, n = lane & 15, wave = wave_id();
+  const TreeSeq me(a, s);
+  const int start = split * a.chunk, n_keys = min(me.total - start, a.chunk), n_cached = min(max(me.len - start, 0), max(n_keys, 0));
+  if (c0 >= me.n * G || (n_keys <= 0 && split > 0)) return;  // the first chunk of rows that see nothing gives zeros
+
+  const int page0 = start >> a.page_shift;
+  const int n_pages = n_cached > 0 ? ((start + n_cached - 1) >> a.page_shift) + 1 - page0 : 0;
+  for (int p = threadIdx.x; p < n_pages; p += 256) pages[p] = a.pages[(int64_t)s * a.cols + page0 + p];
+  if (a.table) {
+    load_bounds(bounds, a.bounds, a.buckets, a.bucket_steps, 256);
+    for (int id = threadIdx.x; id < a.bias_rows * a.buckets; id += 256) {
+      const int row = id / a.buckets, h = a.bias_rows == G ? row : (c0 + row) % G;
+      biases[id] = a.table[(int64_t)(hk * G + h) * a.buckets + id - row * a.buckets] * kLog2e;
+    }
+  }
+  // this lane's columns
+  Op16<DT> qf[NT][STEPS];
+  int item[NT], place[NT];
+  float slope[NT];
+  const float* bias_row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int c = c0 + 16 * t + n;
+    const bool there = c < me.n * G;
+    const int i = there ? c / G : 0, head = hk * G + (there ? c - i * G : 0);
+    item[t] = i;
+    place[t] = !TREE ? me.len - 1 : a.positions ? a.positions[me.t0 + i] : 0;
+    slope[t] = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
+    bias_row[t] = biases + (a.bias_rows == G ? head - hk * G : there ? c - c0 : 0) * a.buckets;
+    const char* row = row_of(a.q, me.t0 + i, head);
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      qf[t][st] = op16_zero<DT>();
+      if (there && 32 * st + 8 * g < a.d) qf[t][st] = op16_load<DT>(row + (32 * st + 8 * g) * EB);
+    }
+  }
+  const bool bend = a.cap > 0.0f;
+  const float zs = bend ? a.scale / a.cap : 0.0f, scale2 = (bend ? a.cap : a.scale) * kLog2e;
+  const int first_bound = a.table && a.buckets > 1 ? a.bounds[0] : 0, last_bound = a.table && a.buckets > 1 ? a.bounds[a.buckets - 2] : -0x7fffffff - 1;
+  __syncthreads();
+
+  const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;
+  const int64_t head_bytes = (int64_t)row_bytes << a.page_shift, page_bytes = head_bytes * a.Hk;
+  // The rows of the chunk's key i; a key past the end, or on a page that is not there, gives the cache's first row and false.  No load stands in a branch (the wait
+  // for it would come with the branch's end): what came for no reason is masked where it is used.
+  struct Where {
+    const char* k;
+    const char* v;
+    bool there;
+  };
+  auto row_at = [&](int i) -> Where {
+    const int at = min(i, n_cached - 1), j = start + max(at, 0), p = n_cached > 0 ? pages[(j >> a.page_shift) - page0] : -1;
+    bool there = i < n_cached && p >= 0 && p < a.n_pages;
+    const int64_t off = there ? p * page_bytes + hk * head_bytes + (int64_t)((j & mask) * row_bytes) : 0;
+    Where w = {a.k + off, a.v + off, there};
+    if constexpr (TREE) {
+      const bool fresh = i >= n_cached && i < n_keys;
+      const int64_t t = me.t0 + (fresh ? start + i - me.len : 0);
+      w.k = fresh ? row_of(a.new_k, t, hk) : w.k;
+      w.v = fresh ? row_of(a.new_v, t, hk) : w.v;
+      w.there = there || fresh;
+    }
+    return w;
+  };
+  char* vs = lds + wave * kKeys * STRIDE;
+  Op16<DT> kf[2][STEPS];
+  u32x4 vf[NV];
+  bool seen[2];
+  uint32_t v_there = 0;  // bit i: chunk i of the values
+  // columns past d: another chunk of the same row; the query's zeros there cancel the key's, and the values' are never written out
+  int kcol[STEPS];
+#pragma unroll
+  for (int st = 0; st < STEPS; ++st) kcol[st] = min(32 * st + 8 * g, a.d - 8) * EB;
+  auto fetch = [&](int j0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const Where w = row_at(j0 + 16 * u + n);
+      seen[u] = w.there;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) kf[u][st] = op16_load<DT>(w.k + kcol[st]);
+    }
+    v_there = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int id = lane + i * DLRM_WAVE, r = id / CH, cc = min(id % CH, a.d / E - 1);
+      const Where w = row_at(j0 + r);
+      v_there |= w.there ? 1u << i : 0u;
+      vf[i] = load16(w.v + cc * 16);
+    }
+  };
+
+  f32x4 o[NT][NB];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    m[t] = -kInf;
+    l[t] = 0.0f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) o[t][b] = f32x4{0, 0, 0, 0};
+  }
+  int j0 = wave * kKeys;
+  if (j0 < n_keys) fetch(j0);
+  for (; j0 < n_keys; j0 += WAVES * kKeys) {
+    f32x4 sc[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        sc[t][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) sc[t][u] = Op16<DT>::mma(kf[u][st], qf[t][st], sc[t][u]);
+      }
+    // which of the four keys of each register set are there: their lanes know
+    const uint64_t have0 = __ballot(seen[0]), have1 = __ballot(seen[1]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int id = lane + i * DLRM_WAVE;
+      *reinterpret_cast<u32x4*>(vs + (id / CH) * STRIDE + (id % CH) * 16) = v_there >> i & 1 ? vf[i] : u32x4{0, 0, 0, 0};
+    }
+    const int jn = j0 + WAVES * kKeys;
+    if (jn < n_keys) fetch(jn);
+    const int first_key = start + j0 + 4 * g;  // of this lane: first_key + 16 u + r
+    const bool any_new = TREE && j0 + kKeys > n_cached;
+    Op16<DT> p[NT], p_low[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[4 * u + r] = (bend ? bent16<LARGE>(sc[t][u][r] * zs) : sc[t][u][r]) * scale2;
+      if (any_new) {
+        // keys among the new items: places of their own, and a key that is not on the way to this lane's item is hidden
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = first_key + 16 * (e >> 2) + (e & 3), u = key - me.len;
+          int away = place[t] - key;
+          if (u >= 0) {
+            const int64_t at = me.t0 + min(u, me.n - 1);
+            const int last = a.last ? a.last[at] : me.n - 1;
+            if (a.positions) away = place[t] - a.positions[at];
+            if (u > item[t] || item[t] > last) x[e] = -kInf;
+          }
+          if (a.table) x[e] += bias_row[t][bucket_of(bounds, a.bucket_steps, away)];
+          x[e] -= slope[t] * fabsf((float)away);
+        }
+      } else {
+        const int away = place[t] - first_key;  // of this lane's first key; its last stands at away - 19
+        if (a.table) {
+          if (__ballot(away - 19 < last_bound) == 0) {
+            const float b = bias_row[t][a.buckets - 1];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += b;
+          } else {
+            const int far = bucket_of(bounds, a.bucket_steps, away), near = bucket_of(bounds, a.bucket_steps, away - 19);
+            if (__ballot(far - near > 1) == 0) {  // at most one bound among the lane's distances
+              const float bf = bias_row[t][far], bn = bias_row[t][near];
+              const int bound = bounds[near];  // (the largest integer behind the last bound)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] += away - (16 * (e >> 2) + (e & 3)) >= bound ? bf : bn;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] += bias_row[t][bucket_of(bounds, a.bucket_steps, away - (16 * (e >> 2) + (e & 3)))];
+            }
+          }
+        }
+        if (a.slopes) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] -= slope[t] * fabsf((float)(away - (16 * (e >> 2) + (e & 3))));
+        }
+      }
+      float top = -kInf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = ((e >> 2 ? have1 : have0) >> (4 * g + (e & 3))) & 1 ? x[e] : -kInf;
+        top = fmaxf(top, x[e]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, DLRM_WAVE));
+      top = fmaxf(top, __shfl_xor(top, 32, DLRM_WAVE));
+      // The sums are rescaled only where a maximum grew by more than 2^8: until then weights of up to 2^8 are as good as weights of up to 1.
+      if (__ballot(top > m[t] + 8.0f)) {
+        const float m1 = fmaxf(m[t], top), f = __builtin_amdgcn_exp2f(m[t] - (m1 == -kInf ? 0.0f : m1));
+        m[t] = m1;
+        l[t] *= f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[t][b] *= f;
+      }
+      const float ms = (m[t] == -kInf ? 0.0f : m[t]) - LIFT;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = __builtin_amdgcn_exp2f(x[e] - ms);
+        l[t] += x[e];
+      }
+      // 16-bit rows: weights in two parts, each in a product of its own
+      if constexpr (EB == 2)
+        two_parts<DT>(x, p[t].v, p_low[t].v);
+      else
+        p[t] = op16_set<DT>(x);
+    }
+    // the values' columns: rows 4g..4g+3 and 16+4g..16+4g+3 of the tile for lane group g
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      Op16<DT> vt;
+      if constexpr (EB == 2) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const char* q = vs + (4 * g + (n >> 2)) * STRIDE + (16 * b + 4 * (n & 3)) * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 16 * STRIDE));
+        const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+        vt.v = u32x4{l2.x, l2.y, h2.x, h2.y};
+      } else {
+        const char* q = vs + 4 * g * STRIDE + (16 * b + n) * 4;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          vt.f[j] = *reinterpret_cast<const float*>(q + j * STRIDE);
+          vt.f[4 + j] = *reinterpret_cast<const float*>(q + (16 + j) * STRIDE);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        o[t][b] = Op16<DT>::mma(vt, p[t], o[t][b]);
+        if constexpr (EB == 2) o[t][b] = Op16<DT>::mma(vt, p_low[t], o[t][b]);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  // join the wavefronts, 16 columns at a time: a thread takes 4 columns of a row
+  float* os = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (c0 + 16 * t >= me.n * G) break;
+    l[t] += __shfl_xor(l[t], 16, DLRM_WAVE);
+    l[t] += __shfl_xor(l[t], 32, DLRM_WAVE);
+    __syncthreads();  // every wavefront is done with its values, and with the sums before
+    if (g == 0) {
+      stat[wave][0][n] = m[t];
+      stat[wave][1][n] = l[t];
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) *reinterpret_cast<f32x4*>(os + (wave * 16 + n) * OS + 16 * b + 4 * g) = o[t][b];
+    __syncthreads();
+    const int per_row = a.d / 4, rows = min(16, me.n * G - c0 - 16 * t);
+    for (int id = threadIdx.x; id < rows * per_row; id += 256) {
+      const int r = id / per_row, col = id % per_row * 4, c = c0 + 16 * t + r, i = c / G, head = hk * G + c - i * G;
+      float top = -kInf;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) top = fmaxf(top, stat[w][0][r]);
+      const float ms = top == -kInf ? 0.0f : top;
+      f32x4 sum = {0, 0, 0, 0};
+      float total = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(stat[w][0][r] - ms);
+        total += f * stat[w][1][r];
+        sum += f * *reinterpret_cast<const f32x4*>(os + (w * 16 + r) * OS + col);
+      }
+      if (a.splits == 1) {
+        store4<DT>(row_of(a.out, me.t0 + i, head) + col * EB, sum * (total == 0.0f ? 0.0f : 1.0f / total));
+      } else {
+        const int64_t at = ((me.t0 + i) * a.Hq + head) * a.splits + split;
+        *reinterpret_cast<f32x4*>(a.po + at * a.d + col) = sum;
+        if (col == 0) {
+          a.pm[at * 2] = top;
+          a.pm[at * 2 + 1] = total;
+        }
+      }
+    }
+  }
+}
+
+// Joins the chunks of a row (new item, head): a wavefront a row, half of it every second chunk, 4 columns a lane, four chunks of each half in flight.
+template <int DT>
+__global__ __launch_bounds__(256) void cache_tree_join_kernel(TreeArgs a) {
+  constexpr int AHEAD = 4;
+  const int rows = a.max_items * a.Hq, row = blockIdx.x * 4 + wave_id();  // of this sequence
+  const int s = a.seq0 + blockIdx.y;
+  const TreeSeq me(a, s);
+  if (row >= rows || row >= me.n * a.Hq) return;
+  const int i = row / a.Hq, head = row - i * a.Hq, n = me.total > 0 ? (me.total - 1) / a.chunk + 1 : 1;
+  const int64_t at = ((me.t0 + i) * a.Hq + head) * a.splits;
+  const float* pm = a.pm + at * 2;
+  const float* po = a.po + at * a.d;
+  const int lane = lane_id(), half = lane >> 5, col = (lane & 31) * 4;
+  float top = -kInf;
+  for (int c = lane; c < n; c += DLRM_WAVE) top = fmaxf(top, pm[2 * c]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, DLRM_WAVE));
+  const float ms = top == -kInf ? 0.0f : top;
+  f32x4 sum = {0, 0, 0, 0};
+  float total = 0.0f;
+  for (int c0 = half; c0 < n; c0 += 2 * AHEAD) {
+    f32x4 v[AHEAD];
+    float f[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int c = c0 + 2 * j, there = c < n ? c : c0;
+      v[j] = loadf4(po + (int64_t)there * a.d + min(col, a.d - 4));
+      f[j] = __builtin_amdgcn_exp2f(pm[2 * there] - ms);
+      total += c < n ? f[j] * pm[2 * there + 1] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) sum += c0 + 2 * j < n ? f[j] * v[j] : f32x4{0, 0, 0, 0};
+  }
+  total += __shfl_xor(total, 32, DLRM_WAVE);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], 32, DLRM_WAVE);
+  if (half != 0 || col >= a.d) return;
+  store4<DT>(row_of(a.out, me.t0 + i, head) + col * Tab<DT>::EB, sum * (total == 0.0f ? 0.0f : 1.0f / total));
+}
+
+struct TreeLaunch {
+  int tiles;  // of 16 columns to a wavefront
+  int64_t each;  // sequences of a launch
+  unsigned lds;  // bytes for the biases
+};
+template <int DT>
+int launch_cache_tree(const TreeArgs& a, const TreeLaunch& how, hipStream_t st) {
+  auto with = [&](auto dp, auto nt, auto large, auto tree) -> int {
+    for (int64_t s0 = 0; s0 < a.B; s0 += how.each) {
+      TreeArgs b = a;
+      b.seq0 = (int)s0;
+      b.B = (int)(a.B - s0 < how.each ? a.B - s0 : how.each);
+      const int64_t eights = ((int64_t)b.B * a.Hk * a.splits + 7) / 8;
+      hipLaunchKernelGGL((cache_tree_kernel<DT, dp(), nt(), large(), tree()>), dim3((unsigned)(eights * 8 * a.blocks)), dim3(256), how.lds, st, b);
+      DLRM_CHECK_LAUNCH();
+      if (a.splits == 1) continue;
+      hipLaunchKernelGGL(cache_tree_join_kernel<DT>, dim3(div_up((int64_t)a.max_items * a.Hq, 4), (unsigned)b.B), dim3(256), 0, st, b);
+      DLRM_CHECK_LAUNCH();
+    }
+    return DLRM_OK;
+  };
+  auto by_tiles = [&](auto dp, auto large) -> int {
+    using T = std::integral_constant<bool, true>;
+    if (!a.off) return with(dp, std::integral_constant<int, 1>{}, large, std::integral_constant<bool, false>{});
+    if (how.tiles == 1) return with(dp, std::integral_constant<int, 1>{}, large, T{});
+    if constexpr (DT != DLRM_F32) {
+      if (how.tiles == 4) return with(dp, std::integral_constant<int, 4>{}, large, T{});
+    }
+    return with(dp, std::integral_constant<int, 2>{}, large, T{});
+  };
+  auto by_cap = [&](auto dp) -> int {
+    if constexpr (DT != DLRM_F32) {
+      if (a.cap <= (DT == DLRM_F16 ? 128.0f : 1024.0f)) return by_tiles(dp, std::integral_constant<bool, false>{});
+    }
+    return by_tiles(dp, std::integral_constant<bool, true>{});
+  };
+  if (a.d <= 32) return by_cap(std::integral_constant<int, 32>{});
+  if (a.d <= 64) return by_cap(std::integral_constant<int, 64>{});
+  if (a.d <= 96) return by_cap(std::integral_constant<int, 96>{});
+  return by_cap(std::integral_constant<int, 128>{});
+}
+
+extern template int launch_cache_tree<DLRM_F32>(const TreeArgs&, const TreeLaunch&, hipStream_t);
+extern template int launch_cache_tree<DLRM_F16>(const TreeArgs&, const TreeLaunch&, hipStream_t);
+extern template int launch_cache_tree<DLRM_BF16>(const TreeArgs&, const TreeLaunch&, hipStream_t);
+
+}  // namespace dlrm

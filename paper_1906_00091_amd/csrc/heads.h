@@ -60,6 +60,18 @@ __device__ inline u32x4 narrow(const float* f) {
   }
 }
 
+// 4 columns of a row
+template <int DT>
+__device__ inline void store4(char* to, f32x4 v) {
+  if constexpr (DT == DLRM_F32) {
+    *reinterpret_cast<f32x4*>(to) = v;
+  } else {
+    const float y[8] = {v[0], v[1], v[2], v[3], 0, 0, 0, 0};
+    const u32x4 r = narrow<DT>(y);
+    *reinterpret_cast<u32x2*>(to) = u32x2{r.x, r.y};
+  }
+}
+
 // A weight w >= 0 as the sum of two 16-bit numbers, 8 at a time: `high` is w rounded down, `low` what is left.  low is above zero wherever high is (by less than fp32's
 // rounding would add), so that both products with an infinite value are that infinity: zero times it, or an infinity less another, would be NaN.
 template <int DT>
@@ -77,6 +89,17 @@ __device__ inline void two_parts(const float* w, u32x4& high, u32x4& low) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) l[j] = fmaxf(w[j] - h[j], fminf(h[j], LEAST));
   low = narrow<DT>(l);
+}
+
+// The bucket of a distance: how many of the bounds are at most it.  bounds: 2^steps - 1 of them at least, the largest integer past those that there are; found by
+// halves, so bounds that do not ascend give some bucket too, none past the last.
+__device__ inline int bucket_of(const int* bounds, int steps, int away) {
+  int b = 0;
+  for (int step = 1 << steps >> 1; step > 0; step >>= 1) b += bounds[b + step - 1] <= away ? step : 0;
+  return b;
+}
+__device__ inline void load_bounds(int* to, const int32_t* bounds, int n, int steps, int threads) {
+  for (int i = threadIdx.x; i < 1 << steps; i += threads) to[i] = i < n - 1 ? bounds[i] : 0x7fffffff;
 }
 
 int check_cache(const dlrm_kv_cache* c);  // qk_rope.hip

@@ -312,9 +312,6 @@ __device__ inline BiasLds<HEADS, WAVES, SUB>& bias_lds() {
   return lds;
 }
 
-__device__ inline void load_bounds(const SeqArgs& a, int* bounds, int threads) {
-  for (int i = threadIdx.x; i < 1 << a.bucket_steps; i += threads) bounds[i] = i < a.buckets - 1 ? a.bounds[i] : 0x7fffffff;
-}
 // biases of a head in powers of two, by `threads` threads of which this is number `id`
 __device__ inline void load_biases(const SeqArgs& a, int head, float* row, int id, int threads) {
   for (int i = id; i < a.buckets; i += threads) row[i] = a.table[(int64_t)head * a.buckets + i] * kLog2e;
@@ -329,12 +326,6 @@ struct Bias {
   int n, steps, first, last;  // first and last: the outer bounds
   __device__ inline Bias(const SeqArgs& a, const int* bounds_)
       : bounds(bounds_), n(a.buckets), steps(a.bucket_steps), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
-  // how many bounds are at most `away`
-  __device__ inline int bucket_of(int away) const {
-    int b = 0;
-    for (int step = 1 << steps >> 1; step > 0; step >>= 1) b += bounds[b + step - 1] <= away ? step : 0;
-    return b;
-  }
   // Looks at the distances from `least` on, this lane's `least` + lane.  True where all have one bias, which `flat` then is; else they go to `window`.
   // bucket: this lane's.  row: the head's biases; slope: the head's, in powers of two.
   __device__ inline bool look(int least, const float* row, float slope, float* window, int& bucket, float& flat) const {
@@ -344,7 +335,7 @@ struct Bias {
       return true;
     }
     const int away = least + lane_id();  // (64 of them: the last belongs to the neighbour's window)
-    bucket = bucket_of(away);
+    bucket = bucket_of(bounds, steps, away);
     const float v = fmaf(-slope, fabsf((float)away), row[bucket]);
     flat = v;
     if (slope == 0.0f && __ballot(bucket != __builtin_amdgcn_readfirstlane(bucket)) == 0) return true;
@@ -573,7 +564,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
   float slope = 0.0f;
   if constexpr (BIAS) {
     auto& bl = bias_lds<GROUPS, GROUPS * PARTS, SUB>();
-    load_bounds(a, bl.bounds, THREADS);
+    load_bounds(bl.bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
     if (w.part == 0) load_biases(a, w.head, bl.rows[w.group], lane, DLRM_WAVE);
     bounds = bl.bounds;
     biases = bl.rows[w.group];
@@ -801,7 +792,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
   float slope = 0.0f;
   if constexpr (BIAS) {
     auto& bl = bias_lds<GROUPS, GROUPS * PARTS, 1>();
-    load_bounds(a, bl.bounds, THREADS);
+    load_bounds(bl.bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
     if (w.part == 0) load_biases(a, w.head, bl.rows[w.group], lane, DLRM_WAVE);
     bounds = bl.bounds;
     biases = bl.rows[w.group];
@@ -1148,7 +1139,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       loaded = head;
     }
   };
-  if constexpr (BIAS) load_bounds(a, sums.lds().bounds, W::THREADS);
+  if constexpr (BIAS) load_bounds(sums.lds().bounds, a.bounds, a.buckets, a.bucket_steps, W::THREADS);
   if (all > 0) {
     fetch();
     put(0);
