@@ -293,10 +293,11 @@ __device__ inline float other_half(float v) { return __shfl_xor(v, 32, DLRM_WAVE
 
 // ---------------------------------------------------------------------------------------------------------------
 // A learned bias by buckets (kBias).  The bias of a pair goes by its distance alone, and a tile of 32 x 32 pairs of one head has 63 of them: a wavefront
-// finds the bucket of all at once, one distance a lane, by a binary search in LDS, puts their biases side by side in LDS, and each lane
+// finds the buckets of all at once, one distance a lane, by a binary search in LDS, puts their biases side by side in LDS (the tile's window), and each lane
 // reads its 16 from there, at offsets known at compile time.  So wavefronts with a bias hold 32 items of ONE head (not packed by heads as RowWork's
-// others are).  A tile whose distances lie in one bucket, as beyond the last bound, takes one value and no search.  Slopes go into the same
-// values.
+// others are).  Beyond the outer bounds there is one bias and no search.  Slopes go into the same values.  Without a cap the window holds bias / scale,
+// and the product of queries and keys starts from it; with one the bias is added to the bent score.  (No branch chooses between one bias and several for
+// the elements: two copies of that code spilled 95 registers of the keys' gradients, 8 histories of up to 4096 items 885 -> 4540 us.)
 constexpr int kBuckets = DLRM_MAX_BUCKETS;
 
 // SUB tiles of a step lie 32 distances apart: their windows overlap, the last tile's first.
@@ -312,9 +313,9 @@ __device__ inline BiasLds<HEADS, WAVES, SUB>& bias_lds() {
   return lds;
 }
 
-// biases of a head in powers of two, by `threads` threads of which this is number `id`
-__device__ inline void load_biases(const SeqArgs& a, int head, float* row, int id, int threads) {
-  for (int i = id; i < a.buckets; i += threads) row[i] = a.table[(int64_t)head * a.buckets + i] * kLog2e;
+// biases of a head times `unit`, by `threads` threads of which this is number `id`
+__device__ inline void load_biases(const SeqArgs& a, int head, float unit, float* row, int id, int threads) {
+  for (int i = id; i < a.buckets; i += threads) row[i] = a.table[(int64_t)head * a.buckets + i] * unit;
 }
 __device__ inline void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -323,29 +324,74 @@ __device__ inline void wave_fence() {
 
 struct Bias {
   const int* bounds;
+  const float* row;  // the head's biases
+  float* window;
+  float* behind = nullptr;  // keys' gradients: the same, -inf for keys behind the query
+  float slope;       // the head's, in the biases' unit
   int n, steps, first, last;  // first and last: the outer bounds
-  __device__ inline Bias(const SeqArgs& a, const int* bounds_)
-      : bounds(bounds_), n(a.buckets), steps(a.bucket_steps), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
-  // Looks at the distances from `least` on, this lane's `least` + lane.  True where all have one bias, which `flat` then is; else they go to `window`.
-  // bucket: this lane's.  row: the head's biases; slope: the head's, in powers of two.
-  __device__ inline bool look(int least, const float* row, float slope, float* window, int& bucket, float& flat) const {
-    if (slope == 0.0f && (least >= last || least + 63 < first)) {
-      bucket = least >= last ? n - 1 : 0;
-      flat = row[bucket];
-      return true;
-    }
+  int even = -1;     // the bucket that the whole window is filled with, or -1
+  __device__ inline Bias(const SeqArgs& a, const int* bounds_, float* window_)
+      : bounds(bounds_), window(window_), n(a.buckets), steps(a.bucket_steps), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
+  __device__ inline void head(const SeqArgs& a, int h, float unit, const float* row_) {
+    row = row_;
+    slope = a.slopes ? a.slopes[h] * unit : 0.0f;
+    even = -1;
+  }
+  // Fills `to` with the biases of the distances from `least` on and returns the bucket of this lane's, `least` + lane; `one` becomes whether all
+  // have the same bucket.
+  __device__ inline int fill(int least, float* to, bool& one) const {
     const int away = least + lane_id();  // (64 of them: the last belongs to the neighbour's window)
-    bucket = bucket_of(bounds, steps, away);
+    const int bucket = bucket_of(bounds, steps, away);
+    one = __ballot(bucket != __builtin_amdgcn_readfirstlane(bucket)) == 0;
     const float v = fmaf(-slope, fabsf((float)away), row[bucket]);
-    flat = v;
-    if (slope == 0.0f && __ballot(bucket != __builtin_amdgcn_readfirstlane(bucket)) == 0) return true;
+    to[lane_id()] = v;
+    if (behind) behind[lane_id()] = away < 0 ? -kInf : v;
+    return bucket;
+  }
+  __device__ inline int look(int least, bool& one) {
+    if (slope == 0.0f && (!behind || least >= 0) && (least >= last || least + 63 < first)) {
+      const int bucket = least >= last ? n - 1 : 0;
+      one = true;
+      if (bucket != even) {
+        wave_fence();
+        window[lane_id()] = row[bucket];
+        if (behind) behind[lane_id()] = row[bucket];
+        wave_fence();
+        even = bucket;
+      }
+      return bucket;
+    }
+    even = -1;
     wave_fence();
-    window[lane_id()] = v;
+    const int bucket = fill(least, window, one);
     wave_fence();
-    return false;
+    return bucket;
+  }
+  // SUB = 2: the windows of two tiles of keys, 32 distances apart
+  __device__ inline void look_wide(int least) {
+    if (slope == 0.0f && (least >= last || least + 95 < first)) {
+      const int bucket = least >= last ? n - 1 : 0;
+      if (bucket != even) {
+        wave_fence();
+        window[lane_id()] = window[32 + lane_id()] = row[bucket];
+        wave_fence();
+        even = bucket;
+      }
+      return;
+    }
+    even = -1;
+    bool one;
+    wave_fence();
+    fill(least, window, one);
+    fill(least + 32, window + 32, one);
+    wave_fence();
   }
 };
-__device__ inline float slope_of(const SeqArgs& a, int head) { return a.slopes ? a.slopes[head] * kLog2e : 0.0f; }
+// what the biases in LDS are multiplied by: powers of two of the score with a cap, the product's own unit without
+template <int KIND>
+__device__ inline float bias_unit(const SeqArgs& a) {
+  return (KIND & kBend) != 0 ? kLog2e : 1.0f / a.scale;
+}
 
 // Rows t of an accumulator set acc^T [DP columns x 32 rows]: row lane % 32, columns 32 b + 8 g + 4 h + 0..3.
 template <int DT, int NB>
@@ -473,6 +519,22 @@ struct RowWork {
   }
 };
 
+// The bias of a wavefront's rows, its LDS filled but not waited for; nothing where there is none.
+struct NoBias {};
+template <int KIND, int GROUPS, int PARTS, int SUB, typename Work>
+__device__ inline auto bias_of(const SeqArgs& a, const Work& w) {
+  if constexpr ((KIND & kBias) != 0) {
+    auto& bl = bias_lds<GROUPS, GROUPS * PARTS, SUB>();
+    load_bounds(bl.bounds, a.bounds, a.buckets, a.bucket_steps, 64 * GROUPS * PARTS);
+    if (w.part == 0) load_biases(a, w.head, bias_unit<KIND>(a), bl.rows[w.group], lane_id(), DLRM_WAVE);
+    Bias b(a, bl.bounds, bl.window[w.group + GROUPS * w.part]);
+    b.head(a, w.head, bias_unit<KIND>(a), bl.rows[w.group]);
+    return b;
+  } else {
+    return NoBias{};
+  }
+}
+
 // x of part 0 becomes x f[0] + (x of part 1) f[1] + ..., through LDS; LDS has to be free.
 template <int NB, int GROUPS, int PARTS>
 __device__ inline void join_parts(f32x16* x, char* lds, int group, int part, const float* f) {
@@ -558,19 +620,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
     tk.store(lds);
     tv.store(lds + TILE);
   }
-  const int* bounds = nullptr;
-  const float* biases = nullptr;
-  float* window = nullptr;
-  float slope = 0.0f;
-  if constexpr (BIAS) {
-    auto& bl = bias_lds<GROUPS, GROUPS * PARTS, SUB>();
-    load_bounds(bl.bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
-    if (w.part == 0) load_biases(a, w.head, bl.rows[w.group], lane, DLRM_WAVE);
-    bounds = bl.bounds;
-    biases = bl.rows[w.group];
-    window = bl.window[w.group + GROUPS * w.part];
-    slope = slope_of(a, w.head);
-  }
+  auto bias = bias_of<KIND, GROUPS, PARTS, SUB>(a, w);
   __syncthreads();
   for (int t = 0; t < tiles; ++t) {
     const int jt = t * BK;
@@ -583,19 +633,24 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       const char* ks = lds + (t & (W::BUFS - 1)) * 2 * TILE + 32 * SUB * w.part * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 s[SUB];
-      float flat[SUB];
-      bool is_flat[SUB];
+      const float* near = nullptr;  // this lane's biases of the last tile: those of rows 32 u + acc_row at near[32 (SUB - 1 - u) - acc_row]
       if constexpr (BIAS) {
-        const Bias bias(a, bounds);
-        int bucket;
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-          is_flat[u] = bias.look(w.item0 + sp.shift - (j0 + 32 * u + 31), biases, slope, window + 32 * (SUB - 1 - u), bucket, flat[u]);
+        bool one;
+        near = bias.window + (lane & 31) + 31 - 4 * h;
+        if constexpr (SUB == 1) {
+          bias.look(w.item0 + sp.shift - (j0 + 31), one);
+        } else {
+          bias.look_wide(w.item0 + sp.shift - (j0 + 32 * SUB - 1));
+        }
       }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         s[u] = f32x16{};
+        if constexpr (BIAS && (KIND & kBend) == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = near[32 * (SUB - 1 - u) - acc_row(r, 0)];
+        }
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
           if (past_d<DT, STEPS>(st, a.d)) break;
@@ -604,20 +659,13 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       }
       __builtin_amdgcn_s_setprio(0);
       // with slopes the whole score, else what the factor c still goes to, in the multiply-add before the exponential
-      const float c = KIND & (kSlopes | kBias) ? 1.0f : sc.c;
-      if constexpr (BIAS) {
+      const float c = KIND & kSlopes || (BIAS && KIND & kBend) ? 1.0f : sc.c;
+      if constexpr (BIAS && (KIND & kBend) != 0) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
-          const float* at = window + 32 * (SUB - 1 - u) + (lane & 31) + 31 - 4 * h;
-          if (is_flat[u]) {
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(sc.y(s[u][r]), sc.c, flat[u]);
-          } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(sc.y(s[u][r]), sc.c, at[-acc_row(r, 0)]);
-          }
-        }
-      } else if constexpr (KIND != kPlain) {
+          for (int r = 0; r < 16; ++r) s[u][r] = fmaf(sc.y(s[u][r]), sc.c, near[32 * (SUB - 1 - u) - acc_row(r, 0)]);
+      } else if constexpr (KIND != kPlain && !BIAS) {
         const float away = (float)(place - (j0 + 4 * h));
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
@@ -786,19 +834,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
     tk.store(lds);
     tv.store(lds + TILE);
   }
-  const int* bounds = nullptr;
-  const float* biases = nullptr;
-  float* window = nullptr;
-  float slope = 0.0f;
-  if constexpr (BIAS) {
-    auto& bl = bias_lds<GROUPS, GROUPS * PARTS, 1>();
-    load_bounds(bl.bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
-    if (w.part == 0) load_biases(a, w.head, bl.rows[w.group], lane, DLRM_WAVE);
-    bounds = bl.bounds;
-    biases = bl.rows[w.group];
-    window = bl.window[w.group + GROUPS * w.part];
-    slope = slope_of(a, w.head);
-  }
+  auto bias = bias_of<KIND, GROUPS, PARTS, 1>(a, w);
   __syncthreads();
   for (int t = 0; t < tiles; ++t) {
     const int jt = t * BK;
@@ -811,11 +847,15 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
       const char* ks = lds + (t & (W::BUFS - 1)) * 2 * TILE + 32 * w.part * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 s = {}, dp = {};
-      float flat = 0.0f;
-      bool is_flat = false;
+      const float* near = nullptr;  // this lane's biases: that of row acc_row at near[-acc_row]
       if constexpr (BIAS) {
-        int bucket;
-        is_flat = Bias(a, bounds).look(w.item0 + sp.shift - (j0 + 31), biases, slope, window, bucket, flat);
+        bool one;
+        near = bias.window + (lane & 31) + 31 - 4 * h;
+        bias.look(w.item0 + sp.shift - (j0 + 31), one);
+        if constexpr ((KIND & kBend) == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = near[-acc_row(r, 0)];
+        }
       }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -826,31 +866,25 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
       }
       __builtin_amdgcn_s_setprio(0);
       const float away = (float)(place - (j0 + 4 * h));
-      const float* at_bias = BIAS ? window + (lane & 31) + 31 - 4 * h : nullptr;
-      auto exponent = [&](float y, int r, auto one_bias) {
-        if constexpr (BIAS) return fmaf(y, sc.c, (one_bias() ? flat : at_bias[-acc_row(r, 0)]) - rest);
+      auto exponent = [&](float y, int r) {
+        if constexpr (BIAS) return fmaf(y, sc.c, (KIND & kBend) != 0 ? near[-acc_row(r, 0)] - rest : -rest);
         return sc.exponent(y, away - (float)acc_row(r, 0), rest);
       };
       if (j0 == 0 && w.wave_full <= 32) {  // once a wavefront, and only the first of a sequence
         float all = 0.0f;
-        if (BIAS && is_flat) {
-          wave_fence();
-          window[lane] = flat;
-          wave_fence();
-        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float p = __builtin_amdgcn_exp2f(exponent(sc.y(s[r]), r, Int<0>{}));
+          const float p = __builtin_amdgcn_exp2f(exponent(sc.y(s[r]), r));
           all += acc_row(r, h) < w.vis ? p * dp[r] : 0.0f;
         }
         all += other_half(all);
         if (w.vis <= 32) delta = all * (LIFT ? __builtin_amdgcn_exp2f(-lift) : 1.0f);
       }
-      auto gradient = [&](auto masked, auto one_bias) {
+      auto gradient = [&](auto masked) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float y = sc.y(s[r]);
-          float p = __builtin_amdgcn_exp2f(exponent(y, r, one_bias)), x = dp[r];
+          float p = __builtin_amdgcn_exp2f(exponent(y, r)), x = dp[r];
           if (masked() && j0 + acc_row(r, h) >= w.vis) p = x = 0.0f;
           sum = fmaf(p, x, sum);
           if constexpr (BIAS) mass += p;
@@ -858,17 +892,10 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
           if constexpr ((KIND & kBend) != 0) s[r] *= sc.derivative(y);
         }
       };
-      if (BIAS && is_flat) {
-        if (j0 + 32 > w.wave_full)
-          gradient(Int<1>{}, Int<1>{});
-        else
-          gradient(Int<0>{}, Int<1>{});
-      } else {
-        if (j0 + 32 > w.wave_full)
-          gradient(Int<1>{}, Int<0>{});
-        else
-          gradient(Int<0>{}, Int<0>{});
-      }
+      if (j0 + 32 > w.wave_full)
+        gradient(Int<1>{});
+      else
+        gradient(Int<0>{});
       if constexpr (LIFT) {
         float top = largest(s);
         if (__ballot(too_large(top))) {
@@ -965,60 +992,109 @@ struct Dkv {
 };
 
 // Gradient of the learned bias: a pair's is its score gradient, and a bucket's the sum of its pairs' of all sequences.  It is summed here, where delta is the
-// fp32 sum of p dp, so it has fp32's digits whatever the rows' type.  A tile's 1024 score gradients are added up by distance in LDS, where the lanes
-// of one addition have 32 distances and the two lane halves places of their own: none meets another, and the order of the sums is the order of the
-// program.  Then neighbouring distances of one bucket are summed over the lanes and added to the wavefront's sum of that bucket.  Tiles in
-// one bucket are summed in a register.  A wavefront leaves the sums of each head in memory, seq_attn_bias_join_kernel adds them up in a fixed order.
+// fp32 sum of p dp, so it has fp32's digits whatever the rows' type.  A tile's score gradients are summed by distance without leaving the registers: rows of
+// a tile lie in the accumulators' registers and keys in lanes, so a lane shift by as many lanes as the row has (DPP, within 16 lanes) lines up the pairs of one
+// distance, and what a shift moves out of its 16 lanes is summed as well, shifted the other way; after 32 additions three registers hold all.  These
+// go on being added to while tiles lie in one bucket; else they go through LDS to one distance a lane, neighbouring distances of a bucket are summed over
+// the lanes and added to the wavefront's sum of that bucket.  A wavefront leaves the sums of each head in memory, and seq_attn_bias_join_kernel adds them
+// up.  Every order is the program's.  (Additions in LDS, ds_add_f32 at 64 places without a conflict, took 270 cycles each: 8 histories of up to 4096
+// items 5040 us in all.)
+// Keys behind the query are left out by a bias of -inf, for keys past the prefix; lanes without a key read nothing but that.
 template <bool BIAS, int WAVES>
 struct BiasSums {
   __device__ inline BiasSums(const SeqArgs&, int, int, float) {}
   __device__ inline void finish(int) {}
+  __device__ inline NoBias bias() const { return {}; }
 };
 template <int WAVES>
 struct BiasSums<true, WAVES> {
   struct Lds : BiasLds<2, WAVES, 1> {
-    float by_distance[WAVES][2][DLRM_WAVE];
+    float behind[WAVES][DLRM_WAVE];
+    float none[DLRM_WAVE];  // -inf
+    float by_distance[WAVES][4][84];
     float by_bucket[WAVES][kBuckets];
   };
   const SeqArgs& a;
   const float unit;
   int64_t slot;
-  int head;          // of the sums now held
-  float run = 0.0f;  // this lane's, of tiles in bucket `run_of`
-  int run_of = 0;
+  int head;       // of the sums now held
+  int held = -1;  // the bucket of the distances whose sums wait to be gathered, -1 for none
+  // Sums by distance, d = row + 31 - key within the tile: lane x of the 16 lanes of lane half h and key half k has d = {62, 46, 46, 30} - x + 4 h - 16 k.
+  float in_high = 0.0f, out_high = 0.0f, in_low = 0.0f, out_low = 0.0f;
   __device__ static inline Lds& lds() {
     __shared__ Lds x;
     return x;
   }
   __device__ static inline int wave() { return __builtin_amdgcn_readfirstlane(wave_id()); }
   __device__ static inline float* window() { return lds().window[wave()]; }
-  __device__ static inline float* distances() { return lds().by_distance[wave()][0]; }
   __device__ static inline float* buckets() { return lds().by_bucket[wave()]; }
   __device__ inline BiasSums(const SeqArgs& args, int split, int head0, float unit_) : a(args), unit(unit_), head(head0) {
     const int64_t block = a.by_block ? (int64_t)blockIdx.z * gridDim.y + blockIdx.y : a.slot0 + blockIdx.x / (a.Hk * a.splits);
     slot = (block * a.splits + split) * WAVES + wave();
     for (int i = lane_id(); i < a.buckets; i += DLRM_WAVE) buckets()[i] = 0.0f;
-    distances()[lane_id()] = distances()[DLRM_WAVE + lane_id()] = 0.0f;
+    for (int i = lane_id(); i < 4 * 84; i += DLRM_WAVE) lds().by_distance[wave()][0][i] = 0.0f;
+    lds().none[lane_id()] = -kInf;
     wave_fence();
   }
-  template <bool FLAT>
-  __device__ inline void add(int at, float v) {
-    if constexpr (FLAT)
-      run += v;
+  template <int CTRL>
+  __device__ static inline float shifted(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+  }
+  // The score gradient of accumulator register r; r is known at compile time.
+  __device__ inline void add(int r, float v) {
+    constexpr int RIGHT = 0x110, LEFT = 0x100;  // row_shr, row_shl
+    switch (r) {
+#define DLRM_AT(R, ROW, IN, OUT)             \
+  case R:                                    \
+    IN += shifted<RIGHT + 15 - (ROW)>(v);    \
+    OUT += shifted<LEFT + 1 + (ROW)>(v);     \
+    asm("" : "+v"(IN), "+v"(OUT));           \
+    break;
+      DLRM_AT(0, 0, in_low, out_low)
+      DLRM_AT(1, 1, in_low, out_low)
+      DLRM_AT(2, 2, in_low, out_low)
+      DLRM_AT(3, 3, in_low, out_low)
+      DLRM_AT(4, 8, in_low, out_low)
+      DLRM_AT(5, 9, in_low, out_low)
+      DLRM_AT(6, 10, in_low, out_low)
+      DLRM_AT(7, 11, in_low, out_low)
+      DLRM_AT(8, 0, in_high, out_high)
+      DLRM_AT(9, 1, in_high, out_high)
+      DLRM_AT(10, 2, in_high, out_high)
+      DLRM_AT(11, 3, in_high, out_high)
+      DLRM_AT(12, 8, in_high, out_high)
+      DLRM_AT(13, 9, in_high, out_high)
+      DLRM_AT(14, 10, in_high, out_high)
+      DLRM_AT(15, 11, in_high, out_high)
+#undef DLRM_AT
+    }
+  }
+  // Before a tile whose distances have one bucket or several: sums of tiles in one bucket are gathered when that changes.
+  __device__ inline void begin(bool one, int bucket) {
+    if (held >= 0 && !(one && bucket == held)) {
+      gather(held);
+      held = -1;
+    }
+  }
+  __device__ inline void end(bool one, int bucket) {
+    if (one)
+      held = bucket;
     else
-      __hip_atomic_fetch_add(distances() + (lane_id() >> 5) * DLRM_WAVE + at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+      gather(bucket);
   }
-  // before a tile in one bucket
-  __device__ inline void begin(int bucket) {
-    if (bucket != run_of) give_run();
-    run_of = bucket;
-  }
-  // after any other; bucket: this lane's distance's
+  // Adds the sums by distance to those by bucket; bucket: this lane's distance's
   __device__ inline void gather(int bucket) {
     const int lane = lane_id();
+    // distance d of the tile is at place d + 4 - 4 h + 16 k of the row of its 16 lanes, zeros around them
+    float* at = lds().by_distance[wave()][lane >> 4] + 4 - (lane & 15);
     wave_fence();
-    float v = distances()[lane] + distances()[DLRM_WAVE + lane];
-    distances()[lane] = distances()[DLRM_WAVE + lane] = 0.0f;
+    at[62] = in_high;
+    at[46] = out_high + in_low;
+    at[30] = out_low;
+    wave_fence();
+    in_high = out_high = in_low = out_low = 0.0f;
+    const float* from = lds().by_distance[wave()][0] + 4 + lane;
+    float v = (from[0] + from[84 + 16]) + (from[2 * 84 - 4] + from[3 * 84 + 12]);
     wave_fence();
     const int before = __shfl_up(bucket, 1, DLRM_WAVE);
     const uint64_t starts = __ballot(lane == 0 || bucket != before);
@@ -1040,16 +1116,10 @@ struct BiasSums<true, WAVES> {
     step(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, (int)f2u(v), 0x143, 0xc, 0xf, false)), start < 32);           // row_bcast:31 into rows 2 and 3
     return v;
   }
-  __device__ inline void give_run() {
-    const float all = segment_scan(run, 0);
-    if (lane_id() == 63) buckets()[run_of] += all;
-    wave_fence();
-    run = 0.0f;
-  }
   // the sums of all heads before `to` are complete
   __device__ inline void turn_to(int to) {
     for (; head < to; ++head) {
-      give_run();
+      begin(false, 0);
       float* at = a.bias_part + ((int64_t)head * a.bias_parts + slot) * a.buckets;
       for (int i = lane_id(); i < a.buckets; i += DLRM_WAVE) {
         at[i] = buckets()[i] * unit;
@@ -1059,6 +1129,11 @@ struct BiasSums<true, WAVES> {
     }
   }
   __device__ inline void finish(int end) { turn_to(end); }
+  __device__ inline Bias bias() const {
+    Bias b(a, lds().bounds, lds().window[wave()]);
+    if (a.causal) b.behind = lds().behind[wave()];
+    return b;
+  }
 };
 
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
@@ -1116,7 +1191,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     t += first % tiles;
   }
   const float base = Score<DT, KIND>(a, hk * G).base;
-  int loaded = -1;  // head of the biases that were put into LDS last
+  int loaded = -1, turned = -1;  // heads: of the biases that were put into LDS last, and of those in use
   // fp16: p is 2^15 times the weight, ds made from it, and that times `f` for the product: from nothing met so far (any value is too large) down
   constexpr bool LIFT = DT == DLRM_F16;
   float f = LIFT ? 0x1p60f : 1.0f;
@@ -1135,10 +1210,11 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       stat[threadIdx.x] = threadIdx.x < BQ ? lse2_of(sraw, row) - base - kGradWeightLift<DT> : row ? sraw : 0.0f;
     }
     if constexpr (BIAS) {
-      if (head != loaded) load_biases(a, head, sums.lds().rows[head & 1], threadIdx.x, W::THREADS);
+      if (head != loaded) load_biases(a, head, bias_unit<KIND>(a), sums.lds().rows[head & 1], threadIdx.x, W::THREADS);
       loaded = head;
     }
   };
+  auto bias = sums.bias();
   if constexpr (BIAS) load_bounds(sums.lds().bounds, a.bounds, a.buckets, a.bucket_steps, W::THREADS);
   if (all > 0) {
     fetch();
@@ -1160,12 +1236,22 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       const char* os = qs + W::TILE;
       const float* stat = reinterpret_cast<const float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ + 32 * part + 4 * h;
       f32x16 s = {}, dp = {};
-      float flat = 0.0f;
-      bool is_flat = false;
+      const float* near = nullptr;  // this lane's biases: that of row acc_row at near[acc_row]
+      bool one = false;
       int bucket = 0;
       if constexpr (BIAS) {
-        sums.turn_to(at);
-        is_flat = Bias(a, sums.lds().bounds).look(i0 + sp.shift - (w0 + 31), sums.lds().rows[at & 1], slope_of(a, at), sums.window(), bucket, flat);
+        if (at != turned) {
+          sums.turn_to(at);
+          bias.head(a, at, bias_unit<KIND>(a), sums.lds().rows[at & 1]);
+          turned = at;
+        }
+        near = (!there ? sums.lds().none : bias.behind && j >= sp.prefix ? bias.behind : bias.window) + 31 - (lane & 31) + 4 * h;
+        bucket = bias.look(i0 + sp.shift - (w0 + 31), one);
+        sums.begin(one, __builtin_amdgcn_readfirstlane(bucket));
+        if constexpr ((KIND & kBend) == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = near[acc_row(r, 0)];
+        }
       }
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -1176,38 +1262,25 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       }
       __builtin_amdgcn_s_setprio(0);
       const float away = (float)(i0 + sp.shift + 4 * h - j);
-      auto gradient = [&](auto one_bias) {
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);
-          const f32x4 del = *reinterpret_cast<const f32x4*>(stat + BQ + 8 * r4);
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);
+        const f32x4 del = *reinterpret_cast<const f32x4*>(stat + BQ + 8 * r4);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = 4 * r4 + i;
-            const float y = sc.y(s[r]);
-            float e;
-            if constexpr (BIAS)
-              e = fmaf(y, sc.c, (one_bias() ? flat : sums.window()[acc_row(r, h) + 31 - (lane & 31)]) - rest[i]);
-            else
-              e = sc.exponent(y, away + (float)acc_row(r, 0), rest[i]);
-            const float p = __builtin_amdgcn_exp2f(e);
-            dp[r] = p * (dp[r] - del[i]);
-            if constexpr (BIAS) sums.template add<one_bias()>(acc_row(r, h) + 31 - (lane & 31), i0 + acc_row(r, h) >= from ? dp[r] : 0.0f);
-            if constexpr ((KIND & kBend) != 0) dp[r] *= sc.derivative(y);
-            s[r] = p;
-          }
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * r4 + i;
+          const float y = sc.y(s[r]);
+          float e;
+          if constexpr (BIAS)
+            e = fmaf(y, sc.c, (KIND & kBend) != 0 ? near[acc_row(r, 0)] - rest[i] : -rest[i]);
+          else
+            e = sc.exponent(y, away + (float)acc_row(r, 0), rest[i]);
+          const float p = __builtin_amdgcn_exp2f(e);
+          dp[r] = p * (dp[r] - del[i]);
+          if constexpr (BIAS) sums.add(r, dp[r]);
+          if constexpr ((KIND & kBend) != 0) dp[r] *= sc.derivative(y);
+          s[r] = p;
         }
-      };
-      if constexpr (BIAS) {
-        if (is_flat) {
-          sums.begin(bucket);
-          gradient(Int<1>{});
-        } else {
-          gradient(Int<0>{});
-          sums.gather(bucket);
-        }
-      } else {
-        gradient(Int<0>{});
       }
       if (i0 < wave_full) {
 #pragma unroll
@@ -1251,6 +1324,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
         }
         __builtin_amdgcn_s_setprio(0);
       }
+      if constexpr (BIAS) sums.end(one, bucket);  // (here, where the tile's registers are free)
     }
     if (n + 1 < all) put(n + 1);
     __syncthreads();
