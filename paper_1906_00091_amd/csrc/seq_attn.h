@@ -244,9 +244,11 @@ enum { kPlain = 0, kSlopes = 1, kBend = 2, kLarge = 4, kBias = 8 };  // bits; kL
 // The second form's r is off by up to 2^-23, the score by cap 2^-22 and, with what rounding `base` adds, less than cap 2^-21 whatever its size: an eighth of
 // what rounding the weight to 16 bits is at a cap of 128 (fp16) or 1024 (bf16).  Larger caps take the third form, in one cut of each kernel.
 // The derivative's constant factor goes into `grad`, which the gradients are multiplied by at the end, as scale does.
+// With a bias a cap takes the third form in every type, y by bend() below: the bias's gradient is fp32, and a score's error is one of the weights that it is made
+// of (8 histories of up to 4096 items, cap 30: 1.8e-6 off by the second form).
 template <int DT, int KIND>
 struct Score {
-  static constexpr bool BEND = (KIND & kBend) != 0, FAST = DT != DLRM_F32 && (KIND & kLarge) == 0;
+  static constexpr bool BEND = (KIND & kBend) != 0, BENT = (KIND & kBias) != 0, FAST = DT != DLRM_F32 && (KIND & (kLarge | kBias)) == 0;
   float zs, c, base, slope, grad;
   __device__ inline Score(const SeqArgs& a, int head) {
     zs = BEND ? a.scale / a.cap * (FAST ? 2.0f * kLog2e : 1.0f) : 0.0f;
@@ -256,7 +258,7 @@ struct Score {
     grad = BEND && FAST ? -4.0f * a.scale : a.scale;
   }
   __device__ inline float y(float s) const {
-    if constexpr (!BEND) return s;
+    if constexpr (!BEND || BENT) return s;
     if constexpr (FAST) return __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(s * zs));
     return tanhf(s * zs);
   }
@@ -270,6 +272,35 @@ struct Score {
     return FAST ? fmaf(y, y, y) : fmaf(-y, y, 1.0f);
   }
 };
+
+// tanh(s zs) of a tile of products, relative error 1.2e-7: a polynomial in z^2 for tanh(z) / z up to 0.625 (fitted at Chebyshev points; 9.5e-8), 1 - 2 / (exp(2 |z|) + 1)
+// beyond.  Scores mostly lie far below their cap, so a wavefront whose products all do takes the polynomial alone, which is also less work than an
+// exponential and a reciprocal.
+__device__ inline void bend(f32x16& s, float zs) {
+  constexpr float END = 0.625f;
+  auto near_zero = [](float z) {
+    const float u = z * z;
+    float p = fmaf(u, -0.00566477536f, 0.02059568f);
+    p = fmaf(u, p, -0.0537226793f);
+    p = fmaf(u, p, 0.133311502f);
+    p = fmaf(u, p, -0.333332616f);
+    return z * fmaf(u, p, 1.0f);
+  };
+  float top = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[r]));
+  if (__ballot(!(top * zs <= END))) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float z = s[r] * zs, a = fabsf(z);
+      const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(a * (2.0f * kLog2e)) + 1.0f);
+      s[r] = a <= END ? near_zero(z) : __builtin_copysignf(t, z);
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = near_zero(s[r] * zs);
+  }
+}
 
 // fp16: log2 of what the weights are multiplied by where they are at most 2^8 (forward, see there) and 1 (gradients)
 template <int DT>
@@ -662,9 +693,11 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       const float c = KIND & kSlopes || (BIAS && KIND & kBend) ? 1.0f : sc.c;
       if constexpr (BIAS && (KIND & kBend) != 0) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+        for (int u = 0; u < SUB; ++u) {
+          bend(s[u], sc.zs);
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[u][r] = fmaf(sc.y(s[u][r]), sc.c, near[32 * (SUB - 1 - u) - acc_row(r, 0)]);
+        }
       } else if constexpr (KIND != kPlain && !BIAS) {
         const float away = (float)(place - (j0 + 4 * h));
 #pragma unroll
@@ -866,6 +899,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
       }
       __builtin_amdgcn_s_setprio(0);
       const float away = (float)(place - (j0 + 4 * h));
+      if constexpr (BIAS && (KIND & kBend) != 0) bend(s, sc.zs);
       auto exponent = [&](float y, int r) {
         if constexpr (BIAS) return fmaf(y, sc.c, (KIND & kBend) != 0 ? near[-acc_row(r, 0)] - rest : -rest);
         return sc.exponent(y, away - (float)acc_row(r, 0), rest);
@@ -1262,6 +1296,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       }
       __builtin_amdgcn_s_setprio(0);
       const float away = (float)(i0 + sp.shift + 4 * h - j);
+      if constexpr (BIAS && (KIND & kBend) != 0) bend(s, sc.zs);
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const f32x4 rest = *reinterpret_cast<const f32x4*>(stat + 8 * r4);
@@ -1408,18 +1443,17 @@ __host__ inline int for_blocks(SeqArgs& a, const Blocks& b, F launch) {
   return DLRM_OK;
 }
 
-// Caps that 16-bit rows take as fp32 rows do.  With a bias smaller ones too: its gradient is fp32, and a score's error is one of the weights that it is made of
-// (a cap of 30 leaves it 2e-6 off).
+// Caps that 16-bit rows take as fp32 rows do; with a bias all do.
 __host__ inline bool large_cap(float cap, int dtype, bool bias) {
-  return dtype != DLRM_F32 && cap > (bias ? 64.0f : dtype == DLRM_F16 ? 128.0f : 1024.0f);
+  return dtype != DLRM_F32 && !bias && cap > (dtype == DLRM_F16 ? 128.0f : 1024.0f);
 }
 
 // Calls f with the padded width and the kind of score as compile-time constants.
 template <int DT, bool BIAS, typename F>
 __host__ inline int for_kind(const SeqArgs& a, F f) {
   auto by_kind = [&](auto dp) {
-    if constexpr (DT != DLRM_F32) {
-      if (large_cap(a.cap, DT, BIAS)) return f(dp, std::integral_constant<int, (BIAS ? kBias : kSlopes) | kBend | kLarge>{});
+    if constexpr (DT != DLRM_F32 && !BIAS) {
+      if (large_cap(a.cap, DT, BIAS)) return f(dp, std::integral_constant<int, kSlopes | kBend | kLarge>{});
     }
     if constexpr (BIAS) {
       if (a.cap > 0.0f) return f(dp, std::integral_constant<int, kBias | kBend>{});
