@@ -17,7 +17,8 @@ SOURCES = ["bwd_reduce_sgd.hip", "bwd_reduce_adagrad.hip", "bwd_reduce_sgd_weigh
            "emb_bwd.hip", "emb_fwd.hip", "interact.hip", "pooled_interact.hip", "util.hip",
            "qk_rope.hip", "seq_attn_f32.hip", "seq_attn_f16.hip", "seq_attn_bf16.hip", "seq_attn_bias_f32.hip", "seq_attn_bias_f16.hip",
            "seq_attn_bias_bf16.hip", "seq_attn.hip", "cache_attn.hip",
-           "cache_tree_f32.hip", "cache_tree_f16.hip", "cache_tree_bf16.hip", "cache_tree.hip"]
+           "cache_tree_f32.hip", "cache_tree_f16.hip", "cache_tree_bf16.hip", "cache_wide_f32.hip", "cache_wide_f16.hip",
+           "cache_wide_bf16.hip", "cache_tree.hip"]
 CEIL_LIB = os.path.join(PKG, "libdlrm_ceilings.so")
 CEIL_SOURCES = ["ceilings.hip"]
 

@@ -9,50 +9,10 @@
 // The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in the order of the chunks.
 #pragma once
 
-#include <initializer_list>
-
 #include "cache_ops.h"
+#include "tree_args.h"
 
 namespace dlrm {
-
-struct TreeArgs {
-  Rows q, out, new_k, new_v;
-  const char* k;
-  const char* v;
-  const int32_t* pages;
-  const int32_t* lens;
-  const int64_t* off;  // [B + 1] of the new items; NULL: one a sequence, at the place of the newest cached item
-  const int32_t* last;
-  const int32_t* positions;
-  const float* slopes;
-  const float* table;  // [Hq, buckets] or NULL
-  const int32_t* bounds;
-  int buckets, bucket_steps, bias_rows;  // bias_rows: heads whose biases a workgroup needs
-  int B, Hq, Hk, d, cols, n_pages, page_shift, max_len, max_items;  // max_len: the table's items at most
-  int chunk, splits, blocks;  // keys of a chunk; chunks of a sequence; groups of 16 NT columns of a key head
-  int seq0;                   // first sequence of this launch
-  float scale, cap;
-  float* po;  // [T * Hq][splits][d] unnormalised sums
-  float* pm;  // [T * Hq][splits][2] maximum (powers of two), sum of weights
-};
-
-// A sequence's new items and keys.
-struct TreeSeq {
-  int64_t t0;      // its first new item
-  int n, len, total;  // new items; cached items that are read; keys
-  __device__ inline TreeSeq(const TreeArgs& a, int s) {
-    len = max(0, min(a.lens[s], a.max_len));
-    if (a.off) {
-      t0 = a.off[s];
-      n = (int)min(a.off[s + 1] - t0, (int64_t)a.max_items);
-      total = len + n;
-    } else {
-      t0 = s;
-      n = 1;
-      total = len;
-    }
-  }
-};
 
 template <int DT, int DP, int NT, bool LARGE, bool TREE>
 __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
@@ -70,10 +30,8 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
   __shared__ int bounds[DLRM_MAX_BUCKETS];
   extern __shared__ float biases[];  // [bias_rows][buckets], in powers of two
 
-  // Workgroups go to the 8 dies in turn: those of one sequence, key head and chunk, which read the same keys, lie 8 apart.
-  const int in_eight = blockIdx.x % (8 * a.blocks), blk = in_eight / 8;
-  const int unit = blockIdx.x / (8 * a.blocks) * 8 + in_eight % 8;
-  if (unit >= a.B * a.Hk * a.splits) return;
+  int unit, blk;
+  if (!place_of(a, unit, blk)) return;
   const int split = unit % a.splits, hk = unit / a.splits % a.Hk, s = a.seq0 + unit / a.splits / a.Hk;
   const int G = a.Hq / a.Hk, c0 = blk * COLS;
   const int lane = lane_id(), g = lane >> 4, n = lane & 15, wave = wave_id();
@@ -388,34 +346,19 @@ __global__ __launch_bounds__(256) void cache_tree_join_kernel(TreeArgs a) {
   store4<DT>(row_of(a.out, me.t0 + i, head) + col * Tab<DT>::EB, sum * (total == 0.0f ? 0.0f : 1.0f / total));
 }
 
-struct TreeLaunch {
-  int tiles;  // of 16 columns to a wavefront
-  int64_t each;  // sequences of a launch
-  unsigned lds;  // bytes for the biases
-};
 template <int DT>
 int launch_cache_tree(const TreeArgs& a, const TreeLaunch& how, hipStream_t st) {
   auto with = [&](auto dp, auto nt, auto large, auto tree) -> int {
-    for (int64_t s0 = 0; s0 < a.B; s0 += how.each) {
-      TreeArgs b = a;
-      b.seq0 = (int)s0;
-      b.B = (int)(a.B - s0 < how.each ? a.B - s0 : how.each);
-      const int64_t eights = ((int64_t)b.B * a.Hk * a.splits + 7) / 8;
-      hipLaunchKernelGGL((cache_tree_kernel<DT, dp(), nt(), large(), tree()>), dim3((unsigned)(eights * 8 * a.blocks)), dim3(256), how.lds, st, b);
+    return for_sequences(a, how, [&](const TreeArgs& b) -> int {
+      hipLaunchKernelGGL((cache_tree_kernel<DT, dp(), nt(), large(), tree()>), dim3(grid_of(b)), dim3(256), how.lds, st, b);
       DLRM_CHECK_LAUNCH();
-      if (a.splits == 1) continue;
-      hipLaunchKernelGGL(cache_tree_join_kernel<DT>, dim3(div_up((int64_t)a.max_items * a.Hq, 4), (unsigned)b.B), dim3(256), 0, st, b);
-      DLRM_CHECK_LAUNCH();
-    }
-    return DLRM_OK;
+      return DLRM_OK;
+    });
   };
   auto by_tiles = [&](auto dp, auto large) -> int {
     using T = std::integral_constant<bool, true>;
     if (!a.off) return with(dp, std::integral_constant<int, 1>{}, large, std::integral_constant<bool, false>{});
     if (how.tiles == 1) return with(dp, std::integral_constant<int, 1>{}, large, T{});
-    if constexpr (DT != DLRM_F32) {
-      if (how.tiles == 4) return with(dp, std::integral_constant<int, 4>{}, large, T{});
-    }
     return with(dp, std::integral_constant<int, 2>{}, large, T{});
   };
   auto by_cap = [&](auto dp) -> int {
@@ -424,14 +367,18 @@ int launch_cache_tree(const TreeArgs& a, const TreeLaunch& how, hipStream_t st) 
     }
     return by_tiles(dp, std::integral_constant<bool, true>{});
   };
-  if (a.d <= 32) return by_cap(std::integral_constant<int, 32>{});
-  if (a.d <= 64) return by_cap(std::integral_constant<int, 64>{});
-  if (a.d <= 96) return by_cap(std::integral_constant<int, 96>{});
-  return by_cap(std::integral_constant<int, 128>{});
+  int rc = DLRM_OK;
+  if (how.tiles > 2) rc = launch_cache_wide<DT>(a, how, st);
+  else if (a.d <= 32) rc = by_cap(std::integral_constant<int, 32>{});
+  else if (a.d <= 64) rc = by_cap(std::integral_constant<int, 64>{});
+  else if (a.d <= 96) rc = by_cap(std::integral_constant<int, 96>{});
+  else rc = by_cap(std::integral_constant<int, 128>{});
+  if (rc != DLRM_OK || a.splits == 1) return rc;
+  return for_sequences(a, how, [&](const TreeArgs& b) -> int {
+    hipLaunchKernelGGL(cache_tree_join_kernel<DT>, dim3(div_up((int64_t)a.max_items * a.Hq, 4), (unsigned)b.B), dim3(256), 0, st, b);
+    DLRM_CHECK_LAUNCH();
+    return DLRM_OK;
+  });
 }
-
-extern template int launch_cache_tree<DLRM_F32>(const TreeArgs&, const TreeLaunch&, hipStream_t);
-extern template int launch_cache_tree<DLRM_F16>(const TreeArgs&, const TreeLaunch&, hipStream_t);
-extern template int launch_cache_tree<DLRM_BF16>(const TreeArgs&, const TreeLaunch&, hipStream_t);
 
 }  // namespace dlrm

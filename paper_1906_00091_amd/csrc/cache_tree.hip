@@ -1,17 +1,20 @@
 // Attention of new items over a paged cache: entry points and argument checks (the kernels: cache_tree.h).
-#include "cache_tree.h"
+#include "tree_args.h"
+
+#include <math.h>
+
+#include <initializer_list>
 
 using namespace dlrm;
 
 // Tiles of 16 columns to a wavefront: as many as the items' columns fill, up to what the registers hold; one where `max_items` is 0, for one item that is in the cache.
 static int tiles_of(const dlrm_kv_cache* c, int Hq, int max_items) {
   const int64_t n = (int64_t)max_items * (Hq / c->Hk);
-  if (n <= 16) return 1;
-  return n <= 32 || c->dtype == DLRM_F32 ? 2 : 4;
+  return n <= 16 ? 1 : n <= 32 ? 2 : n <= 64 ? 4 : 8;
 }
 
 // Keys of a chunk: 1024 workgroups, and at least two tiles a wavefront.
-constexpr int kWanted = 1024, kLeastChunk = 256;
+constexpr int kWanted = 1024, kLeastChunk = 256, kTablePages = 1024;
 static int64_t blocks_of(const dlrm_kv_cache* c, int Hq, int max_items) {
   const int cols = 16 * tiles_of(c, Hq, max_items);
   return ((int64_t)(max_items < 1 ? 1 : max_items) * (Hq / c->Hk) + cols - 1) / cols;
@@ -89,7 +92,7 @@ static int run(const dlrm_kv_cache* c, const int32_t* lens, int max_len, int max
     a.bucket_steps = ilog2_ceil(bias->n);
     const int G = Hq / c->Hk;
     a.bias_rows = G < 16 * how.tiles ? G : 16 * how.tiles;
-    how.lds = (unsigned)(a.bias_rows * bias->n * sizeof(float));
+    how.lds = (unsigned)(a.bias_rows * (bias->n | 1) * sizeof(float));
   }
   // a launch takes fewer than 2^32 threads, and the joining one 65535 sequences: more than that go in several
   const int64_t per_seq = (int64_t)a.splits * a.Hk * blocks;
