@@ -30,9 +30,8 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
   __shared__ int bounds[DLRM_MAX_BUCKETS];
   extern __shared__ float biases[];  // [bias_rows][buckets], in powers of two
 
-  int unit, blk;
-  if (!place_of(a, unit, blk)) return;
-  const int split = unit % a.splits, hk = unit / a.splits % a.Hk, s = a.seq0 + unit / a.splits / a.Hk;
+  int s, hk, split, blk;
+  if (!place_of(a, s, hk, split, blk)) return;
   const int G = a.Hq / a.Hk, c0 = blk * COLS;
   const int lane = lane_id(), g = lane >> 4, n = lane & 15, wave = wave_id();
   const TreeSeq me(a, s);

@@ -1,8 +1,9 @@
 // Attention of several new items of every sequence over a paged cache and over one another, for more than 32 columns ((item, head) pairs of a key head).
 //
-// The forward of attention over sequences, with a paged cache for keys: wavefronts of 32 columns, tiles of keys and values that the workgroup's four
-// wavefronts bring to LDS together, products of 32 x 32 whose accumulators' columns are the wavefront's own.  GROUPS wavefronts have columns of their own, PARTS share
-// 32 columns, each with its 32 keys of a tile, and join at the end.  New items are keys behind the cached ones, as in cache_tree.h.
+// The forward of attention over sequences, with a paged cache for keys: wavefronts of 32 columns, tiles of 64 keys and values that the workgroup's WAVES
+// wavefronts bring to LDS together, products of 32 x 32 whose accumulators' columns are the wavefront's own.  Where a block's columns are no more than half of what the
+// workgroup holds, two wavefronts share 32 of them, each with half of a tile's keys, and join at the end.  New items are keys behind the cached
+// ones, as in cache_tree.h.
 #pragma once
 
 #include "seq_attn.h"
@@ -12,35 +13,43 @@ namespace dlrm {
 
 constexpr int kWidePages = 1024;  // pages of a chunk, at most
 
-template <int DT, int DP, int GROUPS, int PARTS, bool BEND>
-__global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel(TreeArgs a) {
-  static_assert(GROUPS * PARTS == 4, "a workgroup is four wavefronts");
+template <int DT, int DP, int WAVES, bool BEND>
+__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel(TreeArgs a) {
   typedef Tile<DT, DP> T;
-  constexpr int EB = Tab<DT>::EB, STEPS = DP / 16, NB = DP / 32, THREADS = 256, BK = 32 * PARTS;
+  constexpr int EB = Tab<DT>::EB, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * WAVES, BK = 64;
   constexpr int CH = DP * EB / 16, N = (BK * CH + THREADS - 1) / THREADS;  // chunks of 16 bytes: of a row; of a tile, per thread
-  constexpr int TILE = BK * T::STRIDE, BUFS = 4 * TILE > 70 * 1024 ? 1 : 2;
-  constexpr int JOIN = (PARTS - 1) * GROUPS * DP / 2 * DLRM_WAVE * 4, BYTES = 2 * BUFS * TILE > JOIN ? 2 * BUFS * TILE : JOIN;
+  constexpr int TILE = BK * T::STRIDE, BUFS = 4 * TILE > (DT == DLRM_F32 || WAVES == 8 ? 120 : 70) * 1024 ? 1 : 2;
+  constexpr int HALF = WAVES / 2, JOIN = HALF * DP / 2 * DLRM_WAVE * 4, BYTES = 2 * BUFS * TILE > JOIN ? 2 * BUFS * TILE : JOIN;
   __shared__ __attribute__((aligned(16))) char lds[BYTES];
   __shared__ int pages[kWidePages];
-  __shared__ float stat[PARTS > 1 ? PARTS * GROUPS * 2 * 32 : 1];
+  __shared__ float stat[HALF][2][2][32];  // of a group: part, maximum or sum, column
   __shared__ int bounds[kBuckets];
-  __shared__ int window[4][DLRM_WAVE];          // buckets of a tile's distances
-  __shared__ __attribute__((aligned(16))) int fresh[4][2][32];  // of a tile's keys among the new items: last, place
+  __shared__ int window[WAVES][DLRM_WAVE];  // buckets of a tile's distances
+  __shared__ __attribute__((aligned(16))) int fresh[WAVES][2][32];  // of a tile's keys among the new items: last, place
   extern __shared__ float biases[];             // [bias_rows][buckets | 1], in powers of two
 
-  int unit, blk;
-  if (!place_of(a, unit, blk)) return;
-  const int split = unit % a.splits, hk = unit / a.splits % a.Hk, s = a.seq0 + unit / a.splits / a.Hk;
-  const int G = a.Hq / a.Hk, c0 = blk * 32 * GROUPS;
-  const int lane = lane_id(), h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(wave_id()), group = wave % GROUPS, part = wave / GROUPS;
+  int s, hk, split, blk;
+  if (!place_of(a, s, hk, split, blk)) return;
+  const int G = a.Hq / a.Hk, c0 = blk * 32 * WAVES;
+  const int lane = lane_id(), h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(wave_id());
   const TreeSeq me(a, s);
   const int start = split * a.chunk, n_keys = min(me.total - start, a.chunk), n_cached = min(max(me.len - start, 0), max(n_keys, 0));
   const int columns = me.n * G;
   if (c0 >= columns || (n_keys <= 0 && split > 0)) return;  // the first chunk of rows that see nothing gives zeros
 
+  // (the wavefronts that have work are spread over the four SIMDs: wavefront i is on SIMD i % 4)
+  const bool shared = columns - c0 <= 32 * HALF;
+  const int sharing = columns - c0 <= 64 ? 2 : HALF;  // groups that share
+  const int group = shared ? wave % sharing : wave, part = shared ? wave / sharing : 0;
+
   const int page0 = start >> a.page_shift;
   const int n_pages = n_cached > 0 ? ((start + n_cached - 1) >> a.page_shift) + 1 - page0 : 0;
-  for (int p = threadIdx.x; p < n_pages; p += THREADS) pages[p] = a.pages[(int64_t)s * a.cols + page0 + p];
+  bool gone = false;
+  for (int p = threadIdx.x; p < n_pages; p += THREADS) {
+    const int page = a.pages[(int64_t)s * a.cols + page0 + p];
+    pages[p] = page;
+    gone = gone || page < 0 || page >= a.n_pages;
+  }
   const int row_floats = a.buckets | 1;
   if (a.table) {
     load_bounds(bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
@@ -51,7 +60,7 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
   }
   // this lane's column
   const int c = c0 + 32 * group + (lane & 31);
-  const bool mine = c < columns;
+  const bool mine = c < columns && part < 2;
   const int item = mine ? c / G : 0, head = hk * G + (mine ? c - item * G : 0);
   const int64_t t = me.t0 + item;
   const int place = a.positions ? a.positions[t] : 0;
@@ -71,7 +80,7 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
   low = __builtin_amdgcn_readfirstlane(low);
   high = __builtin_amdgcn_readfirstlane(high);
   const bool close = high - low <= 32;  // one window of 64 distances is enough for a tile
-  __syncthreads();
+  const bool whole = __syncthreads_or(gone) == 0;  // every page of the chunk is there
 
   const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;
   const int64_t head_bytes = (int64_t)row_bytes << a.page_shift, page_bytes = head_bytes * a.Hk;
@@ -91,10 +100,16 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
     for (int i = 0; i < N; ++i) {
       const int id = threadIdx.x + i * THREADS, r = j0 + id / CH, cc = id % CH;
       int64_t off;
-      const bool old = cached_at(r, off), young = r >= n_cached && r < n_keys, in_row = cc * Tab<DT>::ELEMS < a.d;
-      const int64_t at = me.t0 + (young ? start + r - me.len : 0);
-      const char* k = young ? row_of(a.new_k, at, hk) : a.k + off;
-      const char* v = young ? row_of(a.new_v, at, hk) : a.v + off;
+      const bool old = cached_at(r, off), in_row = cc * Tab<DT>::ELEMS < a.d;
+      const char* k = a.k + off;
+      const char* v = a.v + off;
+      bool young = false;
+      if (j0 + BK > n_cached) {  // (the same for all threads)
+        young = r >= n_cached && r < n_keys;
+        const int64_t at = me.t0 + (young ? start + r - me.len : 0);
+        k = young ? row_of(a.new_k, at, hk) : k;
+        v = young ? row_of(a.new_v, at, hk) : v;
+      }
       there |= (old || young) && in_row ? 1u << i : 0u;
       kv[0][i] = load16(k + (in_row ? cc * 16 : 0));
       kv[1][i] = load16(v + (in_row ? cc * 16 : 0));
@@ -116,7 +131,7 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
   for (int b = 0; b < NB; ++b) o[b] = f32x16{};
   float m = -kInf, l = 0.0f;
   const int tiles = n_keys > 0 ? (n_keys + BK - 1) / BK : 0;
-  const bool busy = c0 + 32 * group < columns;
+  const bool busy = c0 + 32 * group < columns && part < 2;
   if (tiles > 0) {
     fetch(0);
     put(lds);
@@ -124,9 +139,10 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
   __syncthreads();
   for (int tile = 0; tile < tiles; ++tile) {
     if (tile + 1 < tiles) fetch((tile + 1) * BK);
-    const int j0 = tile * BK + 32 * part;
-    if (busy && j0 < n_keys) {
-      const char* ks = lds + (tile & (BUFS - 1)) * 2 * TILE + 32 * part * T::STRIDE;
+    for (int sub = part; sub < 2; sub += shared ? 2 : 1) {
+      const int j0 = tile * BK + 32 * sub;
+      if (!busy || j0 >= n_keys) break;
+      const char* ks = lds + (tile & (BUFS - 1)) * 2 * TILE + 32 * sub * T::STRIDE;
       const char* vs = ks + TILE;
       f32x16 x = {};
       __builtin_amdgcn_s_setprio(1);
@@ -138,9 +154,12 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
       __builtin_amdgcn_s_setprio(0);
       if constexpr (BEND) bend(x, zs);
       // which keys are there (bit i: key i of the tile)
-      int64_t off;
       const int ki = j0 + (lane & 31);
-      const uint32_t have = (uint32_t)__ballot(cached_at(ki, off) || (ki >= n_cached && ki < n_keys));
+      uint32_t have = j0 + 32 <= n_keys ? 0xffffffffu : (1u << (n_keys - j0)) - 1;
+      if (!whole) {
+        int64_t off;
+        have = (uint32_t)__ballot(cached_at(ki, off) || (ki >= n_cached && ki < n_keys));
+      }
       const int key0 = start + j0;  // of the tile's first key
       float cc = scale2;
       if (j0 + 32 > n_cached) {
@@ -181,7 +200,7 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
           for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], scale2, y);
         } else if (close) {
           wave_fence();
-          window[wave][lane] = bucket_of(bounds, a.bucket_steps, low - (key0 + 31) + lane);
+          window[wave][lane] = buckets_from(bounds, a.buckets, low - (key0 + 31), window[wave]);
           wave_fence();
           const int* at = window[wave] + (place - low) + 31 - 4 * h;
 #pragma unroll
@@ -238,25 +257,17 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
     __syncthreads();
   }
   l += other_half(l);
-  if constexpr (PARTS > 1) {
-    float* st = stat + group * PARTS * 64 + (lane & 31);
-    if (h == 0) {
-      st[part * 64] = m;
-      st[part * 64 + 32] = l;
+  if (shared) {
+    if (h == 0 && part < 2) {
+      stat[group][part][0][lane] = m;
+      stat[group][part][1][lane] = l;
     }
     __syncthreads();
-    float top = -kInf, f[PARTS];
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) top = fmaxf(top, st[p * 64]);
-    const float ts = top == -kInf ? 0.0f : top;
-    l = 0.0f;
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-      f[p] = __builtin_amdgcn_exp2f(st[p * 64] - ts);
-      l = fmaf(st[p * 64 + 32], f[p], l);
-    }
-    m = top;
-    join_parts<NB, GROUPS, PARTS>(o, lds, group, part, f);
+    const float m0 = stat[group][0][0][lane & 31], m1 = stat[group][1][0][lane & 31];
+    m = fmaxf(m0, m1);
+    const float ms = m == -kInf ? 0.0f : m, f[2] = {__builtin_amdgcn_exp2f(m0 - ms), __builtin_amdgcn_exp2f(m1 - ms)};
+    l = stat[group][0][1][lane & 31] * f[0] + stat[group][1][1][lane & 31] * f[1];
+    join_parts<NB, HALF, 2>(o, lds, group, part == 1 ? 1 : part == 0 ? 0 : -1, f);
     if (part > 0) return;
   }
   if (!mine) return;
@@ -274,23 +285,27 @@ __global__ __launch_bounds__(256, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel
 
 template <int DT>
 int launch_cache_wide(const TreeArgs& a, const TreeLaunch& how, hipStream_t st) {
-  auto with = [&](auto dp, auto groups, auto bend) -> int {
+  auto with = [&](auto dp, auto waves, auto bend) -> int {
     return for_sequences(a, how, [&](const TreeArgs& b) -> int {
-      hipLaunchKernelGGL((cache_wide_kernel<DT, dp(), groups(), 4 / groups(), bend()>), dim3(grid_of(b)), dim3(256), how.lds, st, b);
+      hipLaunchKernelGGL((cache_wide_kernel<DT, dp(), waves(), bend()>), dim3(grid_of(b)), dim3(64 * waves()), how.lds, st, b);
       DLRM_CHECK_LAUNCH();
       return DLRM_OK;
     });
   };
-  auto by_cap = [&](auto dp) -> int {
-    using Yes = std::integral_constant<bool, true>;
-    using No = std::integral_constant<bool, false>;
-    if (how.tiles == 4) return a.cap > 0.0f ? with(dp, Int<2>{}, Yes{}) : with(dp, Int<2>{}, No{});
-    return a.cap > 0.0f ? with(dp, Int<4>{}, Yes{}) : with(dp, Int<4>{}, No{});
+  auto by_cap = [&](auto dp, auto waves) -> int {
+    if (a.cap > 0.0f) return with(dp, waves, std::integral_constant<bool, true>{});
+    return with(dp, waves, std::integral_constant<bool, false>{});
   };
-  if (a.d <= 32) return by_cap(Int<32>{});
-  if (a.d <= 64) return by_cap(Int<64>{});
-  if (a.d <= 96) return by_cap(Int<96>{});
-  return by_cap(Int<128>{});
+  auto by_size = [&](auto dp) -> int {
+    if constexpr (DT != DLRM_F32) {
+      if (how.tiles == 16) return by_cap(dp, Int<8>{});
+    }
+    return by_cap(dp, Int<4>{});
+  };
+  if (a.d <= 32) return by_size(Int<32>{});
+  if (a.d <= 64) return by_size(Int<64>{});
+  if (a.d <= 96) return by_size(Int<96>{});
+  return by_size(Int<128>{});
 }
 
 }  // namespace dlrm

@@ -98,6 +98,35 @@ __device__ inline int bucket_of(const int* bounds, int steps, int away) {
   for (int step = 1 << steps >> 1; step > 0; step >>= 1) b += bounds[b + step - 1] <= away ? step : 0;
   return b;
 }
+// orders a wavefront's own accesses of LDS, which the compiler takes for those of one lane
+__device__ inline void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The buckets of 64 neighbouring distances, least + lane, by a wavefront: the bounds up to `least` are counted, and those among the distances mark their places in
+// `marks` (64 places in LDS of the wavefront's own), which are counted up to each lane's.  Two round trips through LDS, where halving takes one for each step.
+template <typename T>
+__device__ inline int buckets_from(const int* bounds, int n, int least, T* marks) {
+  const int lane = lane_id();
+  int base = 0;
+  wave_fence();
+  marks[lane] = T(0);
+  wave_fence();
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (64 * half >= n - 1) break;
+    const int b = 64 * half + lane < n - 1 ? bounds[64 * half + lane] : 0x7fffffff;
+    base += __popcll(__ballot(b <= least));
+    const uint32_t at = (uint32_t)b - (uint32_t)least;  // (the bound past all others is 2^31 - 1: no difference of integers)
+    if (at - 1u < 63u) marks[at] = T(1);
+  }
+  wave_fence();
+  const bool mark = marks[lane] != T(0);
+  wave_fence();
+  const uint64_t all = __ballot(mark);
+  return base + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+}
 __device__ inline void load_bounds(int* to, const int32_t* bounds, int n, int steps, int threads) {
   for (int i = threadIdx.x; i < 1 << steps; i += threads) to[i] = i < n - 1 ? bounds[i] : 0x7fffffff;
 }

@@ -348,10 +348,6 @@ __device__ inline BiasLds<HEADS, WAVES, SUB>& bias_lds() {
 __device__ inline void load_biases(const SeqArgs& a, int head, float unit, float* row, int id, int threads) {
   for (int i = id; i < a.buckets; i += threads) row[i] = a.table[(int64_t)head * a.buckets + i] * unit;
 }
-__device__ inline void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
 
 struct Bias {
   const int* bounds;
@@ -359,10 +355,10 @@ struct Bias {
   float* window;
   float* behind = nullptr;  // keys' gradients: the same, -inf for keys behind the query
   float slope;       // the head's, in the biases' unit
-  int n, steps, first, last;  // first and last: the outer bounds
+  int n, first, last;  // first and last: the outer bounds
   int even = -1;     // the bucket that the whole window is filled with, or -1
   __device__ inline Bias(const SeqArgs& a, const int* bounds_, float* window_)
-      : bounds(bounds_), window(window_), n(a.buckets), steps(a.bucket_steps), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
+      : bounds(bounds_), window(window_), n(a.buckets), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
   __device__ inline void head(const SeqArgs& a, int h, float unit, const float* row_) {
     row = row_;
     slope = a.slopes ? a.slopes[h] * unit : 0.0f;
@@ -372,7 +368,7 @@ struct Bias {
   // have the same bucket.
   __device__ inline int fill(int least, float* to, bool& one) const {
     const int away = least + lane_id();  // (64 of them: the last belongs to the neighbour's window)
-    const int bucket = bucket_of(bounds, steps, away);
+    const int bucket = buckets_from(bounds, n, least, to);
     one = __ballot(bucket != __builtin_amdgcn_readfirstlane(bucket)) == 0;
     const float v = fmaf(-slope, fabsf((float)away), row[bucket]);
     to[lane_id()] = v;
@@ -558,7 +554,8 @@ __device__ inline auto bias_of(const SeqArgs& a, const Work& w) {
     auto& bl = bias_lds<GROUPS, GROUPS * PARTS, SUB>();
     load_bounds(bl.bounds, a.bounds, a.buckets, a.bucket_steps, 64 * GROUPS * PARTS);
     if (w.part == 0) load_biases(a, w.head, bias_unit<KIND>(a), bl.rows[w.group], lane_id(), DLRM_WAVE);
-    Bias b(a, bl.bounds, bl.window[w.group + GROUPS * w.part]);
+    const int wave = w.group + GROUPS * w.part;
+    Bias b(a, bl.bounds, bl.window[wave]);
     b.head(a, w.head, bias_unit<KIND>(a), bl.rows[w.group]);
     return b;
   } else {
