@@ -273,9 +273,9 @@ struct Score {
   }
 };
 
-// tanh(s zs) of a tile of products, relative error 1.2e-7: a polynomial in z^2 for tanh(z) / z up to 0.625 (fitted at Chebyshev points; 9.5e-8), 1 - 2 / (exp(2 |z|) + 1)
-// beyond.  Scores mostly lie far below their cap, so a wavefront whose products all do takes the polynomial alone, which is also less work than an
-// exponential and a reciprocal.
+// tanh(s zs) of a tile of products, relative error 1.2e-7: polynomials in z^2 for tanh(z) / z up to 0.25 and 0.625 (fitted at Chebyshev points; 9.2e-8, 9.5e-8),
+// 1 - 2 / (exp(2 |z|) + 1) beyond.  Scores mostly lie far below their cap, so a wavefront whose products all do takes the first polynomial alone, which is also
+// less work than an exponential and a reciprocal.
 __device__ inline void bend(f32x16& s, float zs) {
   constexpr float END = 0.625f;
   auto near_zero = [](float z) {
@@ -289,7 +289,7 @@ __device__ inline void bend(f32x16& s, float zs) {
   float top = 0.0f;
 #pragma unroll
   for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[r]));
-  if (__ballot(!(top * zs <= END))) {
+  if (__ballot(!(top * zs <= 0.25f))) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const float z = s[r] * zs, a = fabsf(z);
@@ -298,7 +298,10 @@ __device__ inline void bend(f32x16& s, float zs) {
     }
   } else {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = near_zero(s[r] * zs);
+    for (int r = 0; r < 16; ++r) {
+      const float z = s[r] * zs, u = z * z;
+      s[r] = z * fmaf(u, fmaf(u, fmaf(u, -0.051329013f, 0.133231446f), -0.333332062f), 1.0f);
+    }
   }
 }
 
@@ -1008,15 +1011,19 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
 // queries of a long sequence see are the longest work of all, and go by in half the steps.
 // The sizes above: 885 us (733 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 229 us (latency of short
 // walks) and 518 us with 13 for the join (62 TFLOP/s).
-template <int DT, int DP, int GROUPS_, int PARTS_>
+template <int DT, int DP, bool BIAS, int GROUPS_, int PARTS_>
 struct Dkv {
   static constexpr int GROUPS = GROUPS_, PARTS = PARTS_, KEYS = 32 * GROUPS, THREADS = 64 * GROUPS * PARTS, BQ = 32 * PARTS;
   static constexpr int STEPS = DP / 16, NB = DP / 32;
   // Wide 16-bit rows: the values' operands are read from LDS again for every tile, or the accumulators and both operands would
   // not fit the registers of two wavefronts per SIMD.
   static constexpr bool V_LDS = DT != DLRM_F32 && DP > 64;
+  // With a bias some of the keys' operands too, which else are spilled, and a reload waits for the tile that is on its way (8 histories of up to 4096
+  // items, d 128, cap: 1918 us with 81 registers spilled).
+  static constexpr int K_LDS = BIAS && V_LDS && PARTS == 2 ? (DP > 96 ? 5 : 3) : 0;  // steps
+  static constexpr int K_STRIDE = 32 * K_LDS + 16, K_BYTES = K_LDS > 0 ? KEYS * K_STRIDE : 0;
   typedef Tile<DT, DP> T;
-  static constexpr int TILE = BQ * T::STRIDE, V_AT = 4 * TILE, STAT_AT = V_AT + (V_LDS ? KEYS * T::STRIDE : 0);
+  static constexpr int TILE = BQ * T::STRIDE, V_AT = 4 * TILE, K_AT = V_AT + (V_LDS ? KEYS * T::STRIDE : 0), STAT_AT = K_AT + K_BYTES;
   static constexpr int BYTES = STAT_AT + 2 * 2 * BQ * 4;
   static constexpr int JOIN = GROUPS * NB * 16 * DLRM_WAVE * 4;  // one of the two sums of half the wavefronts
   static constexpr int LDS = PARTS == 1 || BYTES > JOIN ? BYTES : JOIN;
@@ -1169,11 +1176,11 @@ struct BiasSums<true, WAVES> {
 
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void seq_attn_dkv_kernel(SeqArgs a) {
-  typedef Dkv<DT, DP, GROUPS, PARTS> W;
+  constexpr bool BIAS = (KIND & kBias) != 0;
+  typedef Dkv<DT, DP, BIAS, GROUPS, PARTS> W;
   typedef typename W::T T;
   constexpr int BQ = W::BQ, STEPS = W::STEPS, NB = W::NB;
   constexpr bool TWO = DT != DLRM_F32 && DP <= 64 && PARTS == 1;  // weights and ds in two parts
-  constexpr bool BIAS = (KIND & kBias) != 0;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
   const int G = a.Hq / a.Hk;
   int walk, seq, row0;
@@ -1190,8 +1197,25 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
   const int lane = lane_id(), h = lane >> 5, group = wave_id() % W::GROUPS, part = wave_id() / W::GROUPS;
   const int w0 = row0 + group * 32, j = w0 + (lane & 31);
   const bool there = j < sp.nk;
-  Op<DT> kf[STEPS], vf[W::V_LDS ? 1 : STEPS];
-  own_rows<DT, STEPS>(kf, row_of(a.k, k0 + j, hk), there, a.d, h);
+  Op<DT> kf[STEPS - W::K_LDS], vf[W::V_LDS ? 1 : STEPS];
+  char* const k_lds = lds + W::K_AT + (group * 32 + (lane & 31)) * W::K_STRIDE + 8 * h * Tab<DT>::EB;  // of this lane's key
+  {
+    Op<DT> all[STEPS];
+    own_rows<DT, STEPS>(all, row_of(a.k, k0 + j, hk), there, a.d, h);
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      if (st >= W::K_LDS)
+        kf[st - (st >= W::K_LDS ? W::K_LDS : 0)] = all[st];
+      else if constexpr (W::K_LDS > 0)
+        if (part == 0) *reinterpret_cast<u32x4*>(k_lds + 32 * st) = __builtin_bit_cast(u32x4, all[st].v);
+    }
+  }
+  auto key_at = [&](int st) {
+    if constexpr (W::K_LDS > 0) {
+      if (st < W::K_LDS) return op_load<DT>(k_lds + 32 * st);
+    }
+    return kf[st - (st >= W::K_LDS ? W::K_LDS : 0)];
+  };
   if constexpr (W::V_LDS) {
     Staged<DT, DP, W::KEYS, W::THREADS> t(a.v.st, a.d);
     t.load(row_of(a.v, k0 + row0, hk), a.v.st, sp.nk - row0, a.d);
@@ -1288,7 +1312,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) {
         if (past_d<DT, STEPS>(st, a.d)) break;
-        s = Op<DT>::mma(T::by_row(qs, lane & 31, st, h), kf[st], s);
+        s = Op<DT>::mma(T::by_row(qs, lane & 31, st, h), key_at(st), s);
         dp = Op<DT>::mma(T::by_row(os, lane & 31, st, h), W::V_LDS ? T::by_row(lds + W::V_AT, group * 32 + (lane & 31), st, h) : vf[W::V_LDS ? 0 : st], dp);
       }
       __builtin_amdgcn_s_setprio(0);
