@@ -200,7 +200,8 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void cache_wide
           for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], scale2, y);
         } else if (close) {
           wave_fence();
-          window[wave][lane] = buckets_from(bounds, a.buckets, low - (key0 + 31), window[wave]);
+          uint64_t starts;
+          window[wave][lane] = buckets_from(bounds, a.buckets, low - (key0 + 31), window[wave], starts);
           wave_fence();
           const int* at = window[wave] + (place - low) + 31 - 4 * h;
 #pragma unroll

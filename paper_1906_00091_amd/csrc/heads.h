@@ -105,9 +105,9 @@ __device__ inline void wave_fence() {
 }
 
 // The buckets of 64 neighbouring distances, least + lane, by a wavefront: the bounds up to `least` are counted, and those among the distances mark their places in
-// `marks` (64 places in LDS of the wavefront's own), which are counted up to each lane's.  Two round trips through LDS, where halving takes one for each step.
+// `marks` (64 places in LDS of the wavefront's own), which are counted up to each lane's; starts: the lanes, but the first, whose bucket is not the one before's.  Two round trips through LDS, where halving takes one for each step.
 template <typename T>
-__device__ inline int buckets_from(const int* bounds, int n, int least, T* marks) {
+__device__ inline int buckets_from(const int* bounds, int n, int least, T* marks, uint64_t& starts) {
   const int lane = lane_id();
   int base = 0;
   wave_fence();
@@ -124,8 +124,8 @@ __device__ inline int buckets_from(const int* bounds, int n, int least, T* marks
   wave_fence();
   const bool mark = marks[lane] != T(0);
   wave_fence();
-  const uint64_t all = __ballot(mark);
-  return base + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+  starts = __ballot(mark);
+  return base + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(starts >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)starts, 0));
 }
 __device__ inline void load_bounds(int* to, const int32_t* bounds, int n, int steps, int threads) {
   for (int i = threadIdx.x; i < 1 << steps; i += threads) to[i] = i < n - 1 ? bounds[i] : 0x7fffffff;

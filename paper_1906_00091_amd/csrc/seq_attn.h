@@ -367,21 +367,19 @@ struct Bias {
     slope = a.slopes ? a.slopes[h] * unit : 0.0f;
     even = -1;
   }
-  // Fills `to` with the biases of the distances from `least` on and returns the bucket of this lane's, `least` + lane; `one` becomes whether all
-  // have the same bucket.
-  __device__ inline int fill(int least, float* to, bool& one) const {
+  // Fills `to` with the biases of the distances from `least` on and returns the bucket of this lane's, `least` + lane; starts: see buckets_from.
+  __device__ inline int fill(int least, float* to, uint64_t& starts) const {
     const int away = least + lane_id();  // (64 of them: the last belongs to the neighbour's window)
-    const int bucket = buckets_from(bounds, n, least, to);
-    one = __ballot(bucket != __builtin_amdgcn_readfirstlane(bucket)) == 0;
+    const int bucket = buckets_from(bounds, n, least, to, starts);
     const float v = fmaf(-slope, fabsf((float)away), row[bucket]);
     to[lane_id()] = v;
     if (behind) behind[lane_id()] = away < 0 ? -kInf : v;
     return bucket;
   }
-  __device__ inline int look(int least, bool& one) {
+  __device__ inline int look(int least, uint64_t& starts) {
     if (slope == 0.0f && (!behind || least >= 0) && (least >= last || least + 63 < first)) {
       const int bucket = least >= last ? n - 1 : 0;
-      one = true;
+      starts = 0;
       if (bucket != even) {
         wave_fence();
         window[lane_id()] = row[bucket];
@@ -393,7 +391,7 @@ struct Bias {
     }
     even = -1;
     wave_fence();
-    const int bucket = fill(least, window, one);
+    const int bucket = fill(least, window, starts);
     wave_fence();
     return bucket;
   }
@@ -410,10 +408,10 @@ struct Bias {
       return;
     }
     even = -1;
-    bool one;
+    uint64_t starts;
     wave_fence();
-    fill(least, window, one);
-    fill(least + 32, window + 32, one);
+    fill(least, window, starts);
+    fill(least + 32, window + 32, starts);
     wave_fence();
   }
 };
@@ -666,10 +664,10 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
       f32x16 s[SUB];
       const float* near = nullptr;  // this lane's biases of the last tile: those of rows 32 u + acc_row at near[32 (SUB - 1 - u) - acc_row]
       if constexpr (BIAS) {
-        bool one;
+        uint64_t starts;
         near = bias.window + (lane & 31) + 31 - 4 * h;
         if constexpr (SUB == 1) {
-          bias.look(w.item0 + sp.shift - (j0 + 31), one);
+          bias.look(w.item0 + sp.shift - (j0 + 31), starts);
         } else {
           bias.look_wide(w.item0 + sp.shift - (j0 + 32 * SUB - 1));
         }
@@ -882,9 +880,9 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
       f32x16 s = {}, dp = {};
       const float* near = nullptr;  // this lane's biases: that of row acc_row at near[-acc_row]
       if constexpr (BIAS) {
-        bool one;
+        uint64_t starts;
         near = bias.window + (lane & 31) + 31 - 4 * h;
-        bias.look(w.item0 + sp.shift - (j0 + 31), one);
+        bias.look(w.item0 + sp.shift - (j0 + 31), starts);
         if constexpr ((KIND & kBend) == 0) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = near[-acc_row(r, 0)];
@@ -1020,7 +1018,7 @@ struct Dkv {
   static constexpr bool V_LDS = DT != DLRM_F32 && DP > 64;
   // With a bias some of the keys' operands too, which else are spilled, and a reload waits for the tile that is on its way (8 histories of up to 4096
   // items, d 128, cap: 1918 us with 81 registers spilled).
-  static constexpr int K_LDS = BIAS && V_LDS && PARTS == 2 ? (DP > 96 ? 5 : 3) : 0;  // steps
+  static constexpr int K_LDS = BIAS && V_LDS && PARTS == 2 ? (DP > 96 ? 6 : 3) : 0;  // steps
   static constexpr int K_STRIDE = 32 * K_LDS + 16, K_BYTES = K_LDS > 0 ? KEYS * K_STRIDE : 0;
   typedef Tile<DT, DP> T;
   static constexpr int TILE = BQ * T::STRIDE, V_AT = 4 * TILE, K_AT = V_AT + (V_LDS ? KEYS * T::STRIDE : 0), STAT_AT = K_AT + K_BYTES;
@@ -1032,9 +1030,9 @@ struct Dkv {
 // Gradient of the learned bias: a pair's is its score gradient, and a bucket's the sum of its pairs' of all sequences.  It is summed here, where delta is the
 // fp32 sum of p dp, so it has fp32's digits whatever the rows' type.  A tile's score gradients are summed by distance without leaving the registers: rows of
 // a tile lie in the accumulators' registers and keys in lanes, so a lane shift by as many lanes as the row has (DPP, within 16 lanes) lines up the pairs of one
-// distance, and what a shift moves out of its 16 lanes is summed as well, shifted the other way; after 32 additions three registers hold all.  These
-// go on being added to while tiles lie in one bucket; else they go through LDS to one distance a lane, neighbouring distances of a bucket are summed over
-// the lanes and added to the wavefront's sum of that bucket.  A wavefront leaves the sums of each head in memory, and seq_attn_bias_join_kernel adds them
+// distance, and what a shift moves out of its 16 lanes is summed as well, shifted the other way; after 32 additions four registers hold all.  Where
+// a tile has no bound among its distances, or one, a lane tells its sums apart by itself; else they go through LDS to one distance a lane, and neighbouring
+// distances of a bucket are summed over the lanes and added to the wavefront's sum of that bucket.  A wavefront leaves the sums of each head in memory, and seq_attn_bias_join_kernel adds them
 // up.  Every order is the program's.  (Additions in LDS, ds_add_f32 at 64 places without a conflict, took 270 cycles each: 8 histories of up to 4096
 // items 5040 us in all.)
 // Keys behind the query are left out by a bias of -inf, for keys past the prefix; lanes without a key read nothing but that.
@@ -1046,17 +1044,19 @@ struct BiasSums {
 };
 template <int WAVES>
 struct BiasSums<true, WAVES> {
+  static constexpr int kLane16 = 67;
   struct Lds : BiasLds<2, WAVES, 1> {
     float behind[WAVES][DLRM_WAVE];
     float none[DLRM_WAVE];  // -inf
-    float by_distance[WAVES][4][84];
+    float by_distance[WAVES][4 * kLane16 + 17];  // a row for each 16 lanes, zeros around the distances that they have; the zeros of two rows are the same ones
     float by_bucket[WAVES][kBuckets];
   };
   const SeqArgs& a;
   const float unit;
   int64_t slot;
   int head;       // of the sums now held
-  int held = -1;  // the bucket of the distances whose sums wait to be gathered, -1 for none
+  int held = 0;       // the bucket that `run`, summed over the lanes, goes to
+  float run = 0.0f;
   // Sums by distance, d = row + 31 - key within the tile: lane x of the 16 lanes of lane half h and key half k has d = {62, 46, 46, 30} - x + 4 h - 16 k.
   float in_high = 0.0f, out_high = 0.0f, in_low = 0.0f, out_low = 0.0f;
   __device__ static inline Lds& lds() {
@@ -1070,7 +1070,7 @@ struct BiasSums<true, WAVES> {
     const int64_t block = a.by_block ? (int64_t)blockIdx.z * gridDim.y + blockIdx.y : a.slot0 + blockIdx.x / (a.Hk * a.splits);
     slot = (block * a.splits + split) * WAVES + wave();
     for (int i = lane_id(); i < a.buckets; i += DLRM_WAVE) buckets()[i] = 0.0f;
-    for (int i = lane_id(); i < 4 * 84; i += DLRM_WAVE) lds().by_distance[wave()][0][i] = 0.0f;
+    for (int i = lane_id(); i < 4 * kLane16 + 17; i += DLRM_WAVE) lds().by_distance[wave()][i] = 0.0f;
     lds().none[lane_id()] = -kInf;
     wave_fence();
   }
@@ -1107,36 +1107,54 @@ struct BiasSums<true, WAVES> {
 #undef DLRM_AT
     }
   }
-  // Before a tile whose distances have one bucket or several: sums of tiles in one bucket are gathered when that changes.
-  __device__ inline void begin(bool one, int bucket) {
-    if (held >= 0 && !(one && bucket == held)) {
-      gather(held);
-      held = -1;
+  __device__ inline void give_run() {
+    const float all = segment_scan(run, 0);
+    if (lane_id() == 63) buckets()[held] += all;
+    wave_fence();
+    run = 0.0f;
+  }
+  // After a tile; bucket: this lane's distance's, which the lane before has too but where `starts` says not.  Sums of a tile in one bucket wait in the lanes,
+  // and where one bound lies within a tile, as far from the query where buckets are wide, the lanes' sums are told apart by their distances.
+  __device__ inline void end(int bucket, uint64_t starts) {
+    const uint64_t all = starts;
+    starts &= ~(1ull << 63);  // (63 distances)
+    const int first = __builtin_amdgcn_readfirstlane(bucket);
+    if (starts & (starts - 1)) {
+      gather(bucket, all);
+      return;
     }
+    if (first != held) {
+      give_run();
+      held = first;
+    }
+    if (starts == 0) {
+      run += (in_high + out_low) + (in_low + out_high);
+    } else {
+      const int lane = lane_id(), bound = __ffsll((unsigned long long)starts) - 1, from = 4 * (lane >> 5) - (lane & 16) - (lane & 15);
+      const bool a0 = from + 62 < bound, a1 = from + 46 < bound, a2 = from + 30 < bound;
+      const float mid = in_low + out_high;
+      run += ((a0 ? in_high : 0.0f) + (a2 ? out_low : 0.0f)) + (a1 ? mid : 0.0f);
+      give_run();
+      run = ((a0 ? 0.0f : in_high) + (a2 ? 0.0f : out_low)) + (a1 ? 0.0f : mid);
+      held = first + 1;
+    }
+    in_high = out_high = in_low = out_low = 0.0f;
   }
-  __device__ inline void end(bool one, int bucket) {
-    if (one)
-      held = bucket;
-    else
-      gather(bucket);
-  }
-  // Adds the sums by distance to those by bucket; bucket: this lane's distance's
-  __device__ inline void gather(int bucket) {
+  // Adds the sums by distance to those by bucket
+  __device__ inline void gather(int bucket, uint64_t starts) {
     const int lane = lane_id();
     // distance d of the tile is at place d + 4 - 4 h + 16 k of the row of its 16 lanes, zeros around them
-    float* at = lds().by_distance[wave()][lane >> 4] + 4 - (lane & 15);
+    float* at = lds().by_distance[wave()] + (lane >> 4) * kLane16 + 4 - (lane & 15);
     wave_fence();
     at[62] = in_high;
     at[46] = out_high + in_low;
     at[30] = out_low;
     wave_fence();
     in_high = out_high = in_low = out_low = 0.0f;
-    const float* from = lds().by_distance[wave()][0] + 4 + lane;
-    float v = (from[0] + from[84 + 16]) + (from[2 * 84 - 4] + from[3 * 84 + 12]);
+    const float* from = lds().by_distance[wave()] + 4 + lane;
+    float v = (from[0] + from[kLane16 + 16]) + (from[2 * kLane16 - 4] + from[3 * kLane16 + 12]);
     wave_fence();
-    const int before = __shfl_up(bucket, 1, DLRM_WAVE);
-    const uint64_t starts = __ballot(lane == 0 || bucket != before);
-    const int start = 63 - __clzll(starts & (~0ull >> (63 - lane)));
+    const int start = 63 - __clzll((starts | 1) & (~0ull >> (63 - lane)));
     const bool ends = lane == 63 || (starts >> (lane + 1) & 1);
     v = segment_scan(v, start);
     if (ends) buckets()[bucket] += v;
@@ -1157,7 +1175,7 @@ struct BiasSums<true, WAVES> {
   // the sums of all heads before `to` are complete
   __device__ inline void turn_to(int to) {
     for (; head < to; ++head) {
-      begin(false, 0);
+      give_run();
       float* at = a.bias_part + ((int64_t)head * a.bias_parts + slot) * a.buckets;
       for (int i = lane_id(); i < a.buckets; i += DLRM_WAVE) {
         at[i] = buckets()[i] * unit;
@@ -1292,7 +1310,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
       const float* stat = reinterpret_cast<const float*>(lds + W::STAT_AT) + (n & 1) * 2 * BQ + 32 * part + 4 * h;
       f32x16 s = {}, dp = {};
       const float* near = nullptr;  // this lane's biases: that of row acc_row at near[acc_row]
-      bool one = false;
+      uint64_t starts = 0;
       int bucket = 0;
       if constexpr (BIAS) {
         if (at != turned) {
@@ -1301,8 +1319,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
           turned = at;
         }
         near = (!there ? sums.lds().none : bias.behind && j >= sp.prefix ? bias.behind : bias.window) + 31 - (lane & 31) + 4 * h;
-        bucket = bias.look(i0 + sp.shift - (w0 + 31), one);
-        sums.begin(one, __builtin_amdgcn_readfirstlane(bucket));
+        bucket = bias.look(i0 + sp.shift - (w0 + 31), starts);
         if constexpr ((KIND & kBend) == 0) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = near[acc_row(r, 0)];
@@ -1380,7 +1397,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
         }
         __builtin_amdgcn_s_setprio(0);
       }
-      if constexpr (BIAS) sums.end(one, bucket);  // (here, where the tile's registers are free)
+      if constexpr (BIAS) sums.end(bucket, starts);  // (here, where the tile's registers are free)
     }
     if (n + 1 < all) put(n + 1);
     __syncthreads();
