@@ -28,25 +28,23 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
   __shared__ int pages[kTablePages];
   __shared__ float stat[WAVES][2][16];
   __shared__ int bounds[DLRM_MAX_BUCKETS];
-  extern __shared__ float biases[];  // [bias_rows][buckets], in powers of two
+  __shared__ int window[WAVES][DLRM_WAVE];  // buckets of a tile's distances
+  extern __shared__ float biases[];         // [bias_rows][buckets | 1], in powers of two
 
   int s, hk, split, blk;
   if (!place_of(a, s, hk, split, blk)) return;
   const int G = a.Hq / a.Hk, c0 = blk * COLS;
   const int lane = lane_id(), g = lane >> 4, n = lane & 15, wave = wave_id();
+  const int start = split * a.chunk, page0 = start >> a.page_shift, n_pages = pages_of_chunk(a, start);
+  for (int p = threadIdx.x; p < n_pages; p += 256) pages[p] = a.pages[(int64_t)s * a.cols + page0 + p];
   const TreeSeq me(a, s);
-  const int start = split * a.chunk, n_keys = min(me.total - start, a.chunk), n_cached = min(max(me.len - start, 0), max(n_keys, 0));
+  const int n_keys = min(me.total - start, a.chunk), n_cached = min(max(me.len - start, 0), max(n_keys, 0));
   if (c0 >= me.n * G || (n_keys <= 0 && split > 0)) return;  // the first chunk of rows that see nothing gives zeros
 
-  const int page0 = start >> a.page_shift;
-  const int n_pages = n_cached > 0 ? ((start + n_cached - 1) >> a.page_shift) + 1 - page0 : 0;
-  for (int p = threadIdx.x; p < n_pages; p += 256) pages[p] = a.pages[(int64_t)s * a.cols + page0 + p];
+  const int row_floats = a.buckets | 1;
   if (a.table) {
     load_bounds(bounds, a.bounds, a.buckets, a.bucket_steps, 256);
-    for (int id = threadIdx.x; id < a.bias_rows * a.buckets; id += 256) {
-      const int row = id / a.buckets, h = a.bias_rows == G ? row : (c0 + row) % G;
-      biases[id] = a.table[(int64_t)(hk * G + h) * a.buckets + id - row * a.buckets] * kLog2e;
-    }
+    load_biases(a, hk, c0, biases, row_floats, WAVES);
   }
   // this lane's columns
   Op16<DT> qf[NT][STEPS];
@@ -61,7 +59,7 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
     item[t] = i;
     place[t] = !TREE ? me.len - 1 : a.positions ? a.positions[me.t0 + i] : 0;
     slope[t] = a.slopes ? a.slopes[head] * kLog2e : 0.0f;
-    bias_row[t] = biases + (a.bias_rows == G ? head - hk * G : there ? c - c0 : 0) * a.buckets;
+    bias_row[t] = biases + (a.bias_rows == G ? head - hk * G : there ? c - c0 : 0) * row_floats;
     const char* row = row_of(a.q, me.t0 + i, head);
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) {
@@ -71,7 +69,23 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
   }
   const bool bend = a.cap > 0.0f;
   const float zs = bend ? a.scale / a.cap : 0.0f, scale2 = (bend ? a.cap : a.scale) * kLog2e;
-  const int first_bound = a.table && a.buckets > 1 ? a.bounds[0] : 0, last_bound = a.table && a.buckets > 1 ? a.bounds[a.buckets - 2] : -0x7fffffff - 1;
+  const int last_bound = a.table && a.buckets > 1 ? a.bounds[a.buckets - 2] : -0x7fffffff - 1;
+  // places of the wavefront's columns (one of no column counts as the first)
+  int low = place[0], high = place[0];
+  if constexpr (TREE) {
+#pragma unroll
+    for (int t = 1; t < NT; ++t) {
+      low = min(low, place[t]);
+      high = max(high, place[t]);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+      low = min(low, __shfl_xor(low, o, DLRM_WAVE));
+      high = max(high, __shfl_xor(high, o, DLRM_WAVE));
+    }
+  }
+  low = __builtin_amdgcn_readfirstlane(low);
+  const bool close = __builtin_amdgcn_readfirstlane(high) - low <= 32;  // one window of 64 distances is enough for a tile
   __syncthreads();
 
   const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;
@@ -156,6 +170,14 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
     if (jn < n_keys) fetch(jn);
     const int first_key = start + j0 + 4 * g;  // of this lane: first_key + 16 u + r
     const bool any_new = TREE && j0 + kKeys > n_cached;
+    const bool far = low - (start + j0 + 31) >= last_bound;
+    if (a.table && !any_new && !far && close) {
+      uint64_t starts;
+      const int b = buckets_from(bounds, a.buckets, low - (start + j0 + 31), window[wave], starts);
+      wave_fence();
+      window[wave][lane] = b;
+      wave_fence();
+    }
     Op16<DT> p[NT], p_low[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -182,21 +204,17 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
       } else {
         const int away = place[t] - first_key;  // of this lane's first key; its last stands at away - 19
         if (a.table) {
-          if (__ballot(away - 19 < last_bound) == 0) {
+          if (far) {
             const float b = bias_row[t][a.buckets - 1];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] += b;
+          } else if (close) {
+            const int* at = window[wave] + (place[t] - low) + 31 - 4 * g;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += bias_row[t][at[-(16 * (e >> 2) + (e & 3))]];
           } else {
-            const int far = bucket_of(bounds, a.bucket_steps, away), near = bucket_of(bounds, a.bucket_steps, away - 19);
-            if (__ballot(far - near > 1) == 0) {  // at most one bound among the lane's distances
-              const float bf = bias_row[t][far], bn = bias_row[t][near];
-              const int bound = bounds[near];  // (the largest integer behind the last bound)
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] += away - (16 * (e >> 2) + (e & 3)) >= bound ? bf : bn;
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] += bias_row[t][bucket_of(bounds, a.bucket_steps, away - (16 * (e >> 2) + (e & 3)))];
-            }
+            for (int e = 0; e < 8; ++e) x[e] += bias_row[t][bucket_of(bounds, a.bucket_steps, away - (16 * (e >> 2) + (e & 3)))];
           }
         }
         if (a.slopes) {

@@ -13,8 +13,10 @@ namespace dlrm {
 
 constexpr int kWidePages = 1024;  // pages of a chunk, at most
 
+// Registers leave room for four wavefronts a SIMD up to 64 columns, two workgroups of eight a CU: 25 of them are spilled for it (500 candidate lists over up to 1000
+// items, fp16, d 40: 89 us, 115 with one workgroup).
 template <int DT, int DP, int WAVES, bool BEND>
-__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void cache_wide_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) void cache_wide_kernel(TreeArgs a) {
   typedef Tile<DT, DP> T;
   constexpr int EB = Tab<DT>::EB, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * WAVES, BK = 64;
   constexpr int CH = DP * EB / 16, N = (BK * CH + THREADS - 1) / THREADS;  // chunks of 16 bytes: of a row; of a tile, per thread
@@ -32,8 +34,10 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void cache_wide
   if (!place_of(a, s, hk, split, blk)) return;
   const int G = a.Hq / a.Hk, c0 = blk * 32 * WAVES;
   const int lane = lane_id(), h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const int start = split * a.chunk, page0 = start >> a.page_shift, n_pages = pages_of_chunk(a, start);
+  for (int p = threadIdx.x; p < n_pages; p += THREADS) pages[p] = a.pages[(int64_t)s * a.cols + page0 + p];
   const TreeSeq me(a, s);
-  const int start = split * a.chunk, n_keys = min(me.total - start, a.chunk), n_cached = min(max(me.len - start, 0), max(n_keys, 0));
+  const int n_keys = min(me.total - start, a.chunk), n_cached = min(max(me.len - start, 0), max(n_keys, 0));
   const int columns = me.n * G;
   if (c0 >= columns || (n_keys <= 0 && split > 0)) return;  // the first chunk of rows that see nothing gives zeros
 
@@ -42,21 +46,12 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : 2) void cache_wide
   const int sharing = columns - c0 <= 64 ? 2 : HALF;  // groups that share
   const int group = shared ? wave % sharing : wave, part = shared ? wave / sharing : 0;
 
-  const int page0 = start >> a.page_shift;
-  const int n_pages = n_cached > 0 ? ((start + n_cached - 1) >> a.page_shift) + 1 - page0 : 0;
-  bool gone = false;
-  for (int p = threadIdx.x; p < n_pages; p += THREADS) {
-    const int page = a.pages[(int64_t)s * a.cols + page0 + p];
-    pages[p] = page;
-    gone = gone || page < 0 || page >= a.n_pages;
-  }
+  bool gone = false;  // a page that the sequence has (each thread looks at those that it loaded)
+  for (int p = threadIdx.x; n_cached > 0 && p <= ((start + n_cached - 1) >> a.page_shift) - page0; p += THREADS) gone = gone || pages[p] < 0 || pages[p] >= a.n_pages;
   const int row_floats = a.buckets | 1;
   if (a.table) {
     load_bounds(bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
-    for (int id = threadIdx.x; id < a.bias_rows * a.buckets; id += THREADS) {
-      const int row = id / a.buckets, b = id - row * a.buckets, head = a.bias_rows == G ? row : (c0 + row) % G;
-      biases[row * row_floats + b] = a.table[(int64_t)(hk * G + head) * a.buckets + b] * kLog2e;
-    }
+    load_biases(a, hk, c0, biases, row_floats, WAVES);
   }
   // this lane's column
   const int c = c0 + 32 * group + (lane & 31);

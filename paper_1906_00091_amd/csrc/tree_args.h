@@ -56,6 +56,20 @@ int launch_cache_tree(const TreeArgs& a, const TreeLaunch& how, hipStream_t st);
 template <int DT>
 int launch_cache_wide(const TreeArgs& a, const TreeLaunch& how, hipStream_t st);
 
+// Page numbers of the chunk from `start` on, loaded beside the length and not after it: as many as the bound on it may need.
+__device__ inline int pages_of_chunk(const TreeArgs& a, int start) {
+  return start >= a.max_len ? 0 : ((start + min(a.chunk, a.max_len - start) - 1) >> a.page_shift) + 1 - (start >> a.page_shift);
+}
+// The biases of the heads that a block's columns (from c0 on) have, in powers of two: row `row` of the block's is that of head `row` of the key head's, or of column
+// c0 + row where these are fewer.  A wavefront a row.
+__device__ inline void load_biases(const TreeArgs& a, int hk, int c0, float* to, int stride, int waves) {
+  const int G = a.Hq / a.Hk;
+  for (int row = wave_id(); row < a.bias_rows; row += waves) {
+    const float* from = a.table + (int64_t)(hk * G + (a.bias_rows == G ? row : (c0 + row) % G)) * a.buckets;
+    for (int b = lane_id(); b < a.buckets; b += DLRM_WAVE) to[row * stride + b] = from[b] * 1.44269504088896340736f;
+  }
+}
+
 // kernels take `each` sequences a launch: go(arguments for them)
 template <typename F>
 __host__ inline int for_sequences(const TreeArgs& a, const TreeLaunch& how, F go) {
