@@ -1,12 +1,16 @@
 // Attention of several new items of every sequence over a paged cache and over one another, and of one new item with a learned bias.
 //
+// Up to 32 columns ((item, head) pairs of a key head); more: cache_wide.h.
+//
 // As the attention of one new item: a key row is loaded once, straight from its page into the registers that the product takes it in, S^T = K Q^T leaves a
-// lane four keys of one column, and those registers are what O^T = V^T P^T takes; values pass through a piece of LDS of the wavefront's own.  The columns
-// are (item, head) pairs of one key head, 16 to a tile and NT tiles to a wavefront, so that a key is read from memory once for up to 16 NT of them; the
-// workgroups of a sequence's further columns read it from the L2 of their die, which they share.  New items are keys behind the cached ones: key j of a
-// sequence is item j of the cache, or row j - len of the new ones, and only the address of its row differs.
+// lane four keys of one column, and those registers are what O^T = V^T P^T takes; values pass through a piece of LDS of the wavefront's own.  16 columns
+// are a tile, and a wavefront has NT of them.  New items are keys behind the cached ones: key j of a sequence is item j of the cache, or row j - len of the new
+// ones, and only the address of its row differs.
 //
 // The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in the order of the chunks.
+//
+// Bound by memory where there is enough of it: 256 sequences of up to 8192 items under one item with a bias of 64 buckets, 16 query heads on 4, bf16, d 128, capped:
+// 407 us for 2.15 GB, 5.3 TB/s.  64 sequences of up to 200 items: 10 us, a launch and a chain of loads (length, page, key, value); 64 of up to 200 under trees of 8: 12 us.
 #pragma once
 
 #include "cache_ops.h"
@@ -85,7 +89,7 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
     }
   }
   low = __builtin_amdgcn_readfirstlane(low);
-  const bool close = __builtin_amdgcn_readfirstlane(high) - low <= 32;  // one window of 64 distances is enough for a tile
+  const bool close = (uint32_t)__builtin_amdgcn_readfirstlane(high) - (uint32_t)low <= 32;  // one window of 64 distances is enough for a tile
   __syncthreads();
 
   const int row_bytes = a.d * EB, mask = (1 << a.page_shift) - 1;

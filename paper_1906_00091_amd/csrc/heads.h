@@ -127,6 +127,9 @@ __device__ inline int buckets_from(const int* bounds, int n, int least, T* marks
   starts = __ballot(mark);
   return base + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(starts >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)starts, 0));
 }
+// A bias times `unit`; one that is there to hide its bucket (the lowest number of a type, or any so low that a row of nothing else would leave fp32 no digit of its
+// scores) is -inf.
+__device__ inline float bias_in(float t, float unit) { return t <= DLRM_BIAS_HIDES ? -__builtin_inff() : t * unit; }
 __device__ inline void load_bounds(int* to, const int32_t* bounds, int n, int steps, int threads) {
   for (int i = threadIdx.x; i < 1 << steps; i += threads) to[i] = i < n - 1 ? bounds[i] : 0x7fffffff;
 }

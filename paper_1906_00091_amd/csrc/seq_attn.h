@@ -349,7 +349,7 @@ __device__ inline BiasLds<HEADS, WAVES, SUB>& bias_lds() {
 
 // biases of a head times `unit`, by `threads` threads of which this is number `id`
 __device__ inline void load_biases(const SeqArgs& a, int head, float unit, float* row, int id, int threads) {
-  for (int i = id; i < a.buckets; i += threads) row[i] = a.table[(int64_t)head * a.buckets + i] * unit;
+  for (int i = id; i < a.buckets; i += threads) row[i] = bias_in(a.table[(int64_t)head * a.buckets + i], unit);
 }
 
 struct Bias {

@@ -66,7 +66,7 @@ __device__ inline void load_biases(const TreeArgs& a, int hk, int c0, float* to,
   const int G = a.Hq / a.Hk;
   for (int row = wave_id(); row < a.bias_rows; row += waves) {
     const float* from = a.table + (int64_t)(hk * G + (a.bias_rows == G ? row : (c0 + row) % G)) * a.buckets;
-    for (int b = lane_id(); b < a.buckets; b += DLRM_WAVE) to[row * stride + b] = from[b] * 1.44269504088896340736f;
+    for (int b = lane_id(); b < a.buckets; b += DLRM_WAVE) to[row * stride + b] = bias_in(from[b], 1.44269504088896340736f);
   }
 }
 

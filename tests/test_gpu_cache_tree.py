@@ -83,6 +83,8 @@ def tree_of(g, n, kind):
         return list(range(n)), [0] * n
     if kind in ("chain", "none"):
         return [n - 1] * n, list(range(n))
+    if kind == "far apart":   # places all over, as of items whose distances are not what they stand behind
+        return list(range(n)), torch.randint(0, 900, (n,), generator=g).tolist()
     if kind == "hidden":   # nobody sees the odd ones
         return [j - 1 if j % 2 else n - 1 for j in range(n)], list(range(n))
     rng = random.Random(int(torch.randint(1 << 30, (1,), generator=g)))
@@ -106,6 +108,11 @@ TREES = [
     ("f16", 5, 1, 104, 128, [20000, 50], [13, 14], "tree", False, 0.0, 20, "both", "heads"),
     ("f16", 4, 2, 64, 16, [130, 20], [40, 65], "chain", False, 300.0, 5, "edges", "rows"),
     ("f16", 4, 1, 128, 64, [1025, 3], [200, 100], "none", False, 0.0, 5, "far", "rows"),
+    ("bf16", 33, 1, 128, 16, [300, 45, 17], [8, 3, 1], "tree", False, 0.0, 128, "one by one", "rows"),   # the most biases in LDS: 33 heads of 128
+    ("f32", 64, 1, 96, 16, [200, 31], [2, 3], "chain", False, 0.0, 128, "log", "packed"),
+    ("bf16", 4, 2, 64, 32, [3000, 2000], [90, 70], "far apart", False, 0.0, 30, "log", "rows"),          # places too far from each other for one window
+    ("f32", 2, 2, 32, 8, [400, 20], [12, 5], "far apart", True, 0.0, 30, "log", "rows"),
+    ("bf16", 8, 4, 128, 64, [700, 64], [130, 33], "tree", False, 15.0, 40, "log", "heads"),
 ]
 
 
@@ -341,3 +348,32 @@ def test_a_graph_of_calls_over_the_cache_replays_like_eager_calls():
         step()
         torch.cuda.synchronize()
         assert torch.equal(got[0], out) and torch.equal(got[1], one)
+
+
+def test_a_bias_that_hides_and_caps_far_below_the_scores():
+    """Buckets hidden by -inf and by the lowest number; scores many times the cap."""
+    g, Hq, Hk, d = gen(12), 6, 3, 72
+    for dt in (torch.float32, torch.bfloat16):
+        c = Paged(g, [300, 40, 0], 20, 16, Hk, d, dt)
+        new = [3, 25, 2]
+        last, pos = [], []
+        for m, n in zip(c.lens, new):
+            l, depth = tree_of(g, n, "tree")
+            last += list(l)
+            pos += [m + y for y in depth]
+        last, pos = torch.tensor(last, dtype=torch.int32), torch.tensor(pos, dtype=torch.int32)
+        x = {n: rand(g, 30, H, d, dtype=dt) * 3 for n, H in (("q", Hq), ("k", Hk), ("v", Hk))}
+        table, bounds = rand(g, Hq, 6), torch.tensor([1, 2, 5, 20, 100], dtype=torch.int32)
+        table[0, 1], table[2, :3], table[5] = -math.inf, torch.finfo(torch.float32).min, -math.inf
+        items = hot.NewItems(offsets(new).to(DEV), 30, 25, last=last.to(DEV), positions=pos.to(DEV))
+        out = run_tree(c, x, items, hot.RelBias(table.to(DEV), bounds.to(DEV)), None, 0.5, "rows")
+        table = torch.where(table <= -60000.0, torch.full_like(table, -math.inf), table)
+        check_tree(c, new, x, (pos, last, None, table, bounds, d ** -0.5, 0.5), out)
+        assert not out[:, 5].any()
+        q = x["q"][:3]
+        ws = hot.alloc_cache_attn_bias_workspace(c.cache, Hq, 300)
+        one = torch.full_like(q, NAN).to(DEV)
+        hot.dlrm_cache_attn_bias(c.cache, c.dlens, 300, hot.RelBias(table.to(DEV), bounds.to(DEV)), q.to(DEV), one, ws, cap=0.5)
+        for s, m in enumerate(c.lens):
+            want, tol = ref.cached(q[s:s + 1], c.k[s], c.v[s], None, None, torch.tensor([m - 1]), None, None, table, bounds, d ** -0.5, 0.5)
+            close(one[s:s + 1], want, tol, "sequence %d" % s)

@@ -257,3 +257,31 @@ def test_a_graph_of_forward_and_backward_replays_like_eager_calls():
         torch.cuda.synchronize()
         for a, b in zip(got, (out, lse, dq, dk, dv, dtable)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("lowest", [torch.finfo(torch.float32).min, -1e9, torch.finfo(torch.float16).min, -60000.0])
+def test_the_lowest_numbers_hide_their_buckets_too(lowest):
+    """As -inf does: a row of nothing else has zeros, and no gradients; the greatest number that does not hide is a bias."""
+    g, lens = gen(6), [1, 30, 80]
+    x = {n: rand(g, 111, 2, 32) for n in ("q", "k", "v", "do")}
+    bounds, off = torch.tensor([1, 3, 10], dtype=torch.int32), offsets(lens)
+    table = rand(g, 2, 4)
+    table[:, 0] = table[0, 2] = lowest
+    seq = hot.SeqBatch(off.to(DEV), off.to(DEV), 111, 111, 80, 80)
+    got = run(x, seq, hot.RelBias(table.to(DEV), bounds.to(DEV)), "rows")
+    hidden = torch.where(table <= -60000.0, torch.full_like(table, -math.inf), table)
+    want = ref.attention(x["q"], x["k"], x["v"], off, off, True, None, None, hidden, bounds, 32 ** -0.5, 0.0, x["do"])
+    for n in got:
+        close(got[n], want[n], want[n + "_tol"], n)
+    assert not got["dtable"][:, 0].any() and not got["out"][0].any()
+
+
+def test_bounds_that_do_not_ascend_stay_within_the_table():
+    """What they mean is not said; every pair has some bucket of the table, and results are finite."""
+    g = gen(7)
+    off = offsets([90, 200])
+    x = {n: rand(g, 290, 2, 16, dtype=torch.bfloat16) for n in ("q", "k", "v", "do")}
+    bounds = torch.tensor([9, 3, 3, 150, -40, 20, 2 ** 31 - 1, -2 ** 31], dtype=torch.int64).to(torch.int32)
+    bias = hot.RelBias(rand(g, 2, 9).to(DEV), bounds.to(DEV))
+    got = run(x, hot.SeqBatch(off.to(DEV), off.to(DEV), 290, 290, 200, 200, causal=False), bias, "rows")
+    assert all(torch.isfinite(t).all() for t in got.values())
