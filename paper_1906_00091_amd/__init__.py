@@ -1,7 +1,7 @@
 """DLRM sparse hot path on one MI355X: pooled embedding lookup, dot interaction,
 their backward and the fused sparse SGD update; and histories read in order:
 norms with rotary positions, attention over CSR sequences and over a paged
-cache.  Hand-written HIP kernels behind a C ABI (include/dlrm_hot.h).  This package is the thin binding."""
+cache, with a learned relative position bias and for trees of new items.  Hand-written HIP kernels behind a C ABI (include/dlrm_hot.h).  This package is the thin binding."""
 from .binding import (  # noqa: F401
     BF16, BWD_ATOMIC, BWD_AUTO, BWD_SORT, BWD_SORT_PREPARED, BWD_SORT_PREPARED_FLAT, F16, F32, FWD_AUTO, FWD_FUSED, FWD_SPLIT, DlrmError, SparseBatch, alloc_workspace,
     dlrm_emb_bag_bwd_adagrad, dlrm_emb_bag_bwd_export_groups, dlrm_emb_bag_bwd_route_counts, ROUTE_NAMES, dlrm_emb_bag_bwd_prepare, dlrm_emb_bag_bwd_prepared_oversized, dlrm_emb_bag_bwd_sgd, dlrm_emb_bag_bwd_sgd_noalloc, NOALLOC_SCRATCH_BYTES,

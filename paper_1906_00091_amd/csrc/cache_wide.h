@@ -7,9 +7,9 @@
 //
 // Weights are 16-bit numbers in their product, in one part: bound by arithmetic, this would pay a third for two, and a result is off by up to one and a half times its
 // rounding (bf16 2.1e-3, rounding alone 1.7e-3).  128 sequences of up to 8192 items with trees of up to 60, 16 query heads on 4, bf16, d 128, a bias of 64 buckets, capped:
-// 553 us and 37 for the join, 218 TFLOP/s of visible pairs; with 60 items to 8192 each 1050 us and 490 TFLOP/s (vector work 60 % of the time, matrix cores 21 %, one after
-// the other for the most part).  The difference is rows of no column in a wavefront's 32 and wavefronts with none in a workgroup.  One sequence of
-// 131072 items under 64: 104 us and 14, 660 TFLOP/s.
+// 543 us and 36 for the join, 238 TFLOP/s of visible pairs; with 60 items to 8192 each 1116 us in all, 462 TFLOP/s (vector work 60 % of the time, matrix cores 21 %, one
+// after the other for the most part).  The difference is rows of no column in a wavefront's 32 and wavefronts with none in a workgroup.  One sequence of
+// 131072 items under 64: 117 us in all, 590 TFLOP/s.
 #pragma once
 
 #include "seq_attn.h"
