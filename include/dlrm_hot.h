@@ -605,7 +605,8 @@ size_t dlrm_cache_tree_attn_workspace_bytes(const dlrm_kv_cache* cache, const dl
  * hold and does not get (dlrm_qk_rope_append stores those that are kept).  Scores as for dlrm_seq_batch, with bias or NULL; cached item j stands at place j,
  * a new one at its position.  lens and max_len as for dlrm_cache_attn, but the items of lens[s] all come before the new ones, and max_len may be 0.  An item that
  * sees nothing gets zeros; values that are not finite may show in items of the same sequence they are hidden from.
- * max_len plus max_items, and max_items times Hq, <= 2^31 - 1025.
+ * max_len plus max_items, and max_items times Hq, <= 2^31 - 1025.  One sequence may take up to 2^22 workgroups, its chunks (as for dlrm_cache_attn) times its key heads
+ * times the blocks of 16 to 256 pairs of an item and a head that these have; more is DLRM_ERR_BAD_SHAPE.
  * workspace: 256-byte aligned device memory; contents are scratch.
  */
 int32_t dlrm_cache_tree_attn(const dlrm_kv_cache* cache, const int32_t* lens, int32_t max_len, const dlrm_new_items* items,

@@ -377,3 +377,43 @@ def test_a_bias_that_hides_and_caps_far_below_the_scores():
         for s, m in enumerate(c.lens):
             want, tol = ref.cached(q[s:s + 1], c.k[s], c.v[s], None, None, torch.tensor([m - 1]), None, None, table, bounds, d ** -0.5, 0.5)
             close(one[s:s + 1], want, tol, "sequence %d" % s)
+
+
+def test_drafts_are_run_in_a_tree_and_a_path_of_them_is_kept():
+    """Drafts of every user in one call; the items on the way to one of them are then stored, and that item alone, run over the cache, is what it was in the tree."""
+    g, Hq, Hk, d, page = gen(21), 8, 4, 128, 32
+    lens, new = [70, 1, 300], [24, 5, 17]
+    c = Paged(g, lens, 12, page, Hk, d, torch.bfloat16)
+    B, T, starts = 3, sum(new), offsets(new)
+    pool = torch.full((2, 36, Hk, page, d), NAN, dtype=torch.bfloat16, device=DEV)
+    cache = hot.KvCache(pool[0], pool[1], torch.randperm(36, generator=g).to(torch.int32).view(3, 12).to(DEV))
+    bias = hot.RelBias(torch.randn(Hq, 40, device=DEV), hot.relative_bounds(40, 200, device=DEV))
+    rope = lambda pos: hot.QkRope(pos.to(torch.int32).to(DEV), Hq, Hk, d, inv_freq=hot.rope_frequencies(d, device=DEV))
+
+    def store(users, pos, q, k, v):
+        hot.dlrm_qk_rope_append(rope(pos), q, k, v, torch.empty_like(q), cache, users.to(torch.int32).to(DEV))
+    for s, n in enumerate(lens):
+        store(torch.full((n,), s), torch.arange(n), rand(g, n, Hq, d, dtype=torch.bfloat16).to(DEV), c.k[s].to(DEV), c.v[s].to(DEV))
+    parents = [[-1] + [int(torch.randint(-1, i, (1,), generator=g)) for i in range(1, n)] for n in new]
+    order, last, depth = zip(*(hot.tree_order(p) for p in parents))
+    pos = torch.tensor([m + y for m, x in zip(lens, depth) for y in x])
+    q, k, v = (rand(g, T, H, d, dtype=torch.bfloat16).to(DEV) for H in (Hq, Hk, Hk))   # in depth-first order
+    qr, kr, out = torch.empty_like(q), torch.empty_like(k), torch.empty_like(q)
+    hot.dlrm_qk_rope_fwd(rope(pos), q, k, qr, kr)
+    items = hot.NewItems(starts.to(DEV), T, max(new), last=torch.tensor(sum(last, []), dtype=torch.int32, device=DEV), positions=pos.to(torch.int32).to(DEV))
+    dl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    hot.dlrm_cache_tree_attn(cache, dl, max(lens), items, qr, kr, v, out, hot.alloc_cache_tree_attn_workspace(cache, Hq, max(lens), items), bias=bias, cap=30.0)
+    ends = [max(range(n), key=lambda i: x[i]) for n, x in zip(new, depth)]   # the deepest draft of each
+    path = [[j for j in range(e + 1) if l[j] >= e] for e, l in zip(ends, last)]
+    assert [len(x) for x in path] == [depth[s][ends[s]] + 1 for s in range(B)]
+    rows = torch.tensor([int(starts[s]) + j for s in range(B) for j in path[s]])
+    users = torch.tensor([s for s in range(B) for _ in path[s]])
+    a = rows.to(DEV)
+    store(users, pos[rows], q[a], k[a], v[a])
+    now = [m + len(x) for m, x in zip(lens, path)]
+    at = torch.tensor([int(starts[s]) + ends[s] for s in range(B)], device=DEV)
+    one = torch.empty(B, Hq, d, dtype=torch.bfloat16, device=DEV)
+    hot.dlrm_cache_attn_bias(cache, torch.tensor(now, dtype=torch.int32, device=DEV), max(now), bias, qr[at], one,
+                             hot.alloc_cache_attn_bias_workspace(cache, Hq, max(now)), cap=30.0)
+    # both round one number to bf16, and the tree's weights are rounded once more
+    close(one, out[at].double().cpu(), (2 ** -7 * out[at].double().abs() + 2 ** -8 * 4.5).cpu(), "the kept draft")

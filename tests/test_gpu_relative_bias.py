@@ -81,6 +81,13 @@ CASES = [
     ("f16", 8, 4, 96, [300, 301], [120, 500], True, True, False, 10.0, 31, "both", "wide"),
     ("bf16", 2, 2, 32, [0] * 40 + [600, 3] + [0] * 40, None, True, False, False, 0.0, 9, "log", "rows"),   # few of many sequences have rows
     ("bf16", 1, 1, 64, [520, 300], [100, 90], True, False, False, 0.0, 8, "log", "packed"),              # queries before the first key see none
+    # enough rows for two tiles of keys a step, and for the cuts of fp32 between few rows and many
+    ("bf16", 8, 4, 64, [300, 270] * 16, None, True, False, True, 0.0, 40, "log", "packed"),
+    ("f16", 8, 8, 40, [290] * 30, [280, 310, 257] * 10, False, False, False, 20.0, 60, "both", "rows"),
+    ("bf16", 16, 4, 128, [300, 130, 290] * 5, None, True, True, False, 0.0, 128, "one by one", "rows"),
+    ("bf16", 16, 2, 104, [280, 300] * 4, None, True, False, False, 30.0, 64, "log", "rows"),
+    ("f32", 8, 2, 32, [300] * 30, None, True, False, False, 0.0, 33, "both", "packed"),
+    ("f32", 2, 1, 24, [3, 2, 1], [700, 900, 640], False, False, False, 5.0, 90, "both", "rows"),
 ]
 
 
