@@ -538,7 +538,7 @@ typedef struct dlrm_rel_bias {
   int32_t n;             /* buckets, 1 .. DLRM_MAX_BUCKETS */
 } dlrm_rel_bias;
 
-/* dlrm_seq_attn_fwd with a learned bias.  (max_q + 31) times the query heads of a key head <= 2^31 - 1025. */
+/* dlrm_seq_attn_fwd with a learned bias.  (max_q + 31) times the query heads of a key head <= 2^31 - 1025; the scale from 2^-64 to 2^64. */
 int32_t dlrm_seq_attn_bias_fwd(const dlrm_seq_batch* seq, const dlrm_rel_bias* bias, int32_t Hq, int32_t Hk, int32_t d,
                                int32_t dtype, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
                                const dlrm_heads* out, float* lse, void* stream);
@@ -605,8 +605,8 @@ size_t dlrm_cache_tree_attn_workspace_bytes(const dlrm_kv_cache* cache, const dl
  * hold and does not get (dlrm_qk_rope_append stores those that are kept).  Scores as for dlrm_seq_batch, with bias or NULL; cached item j stands at place j,
  * a new one at its position.  lens and max_len as for dlrm_cache_attn, but the items of lens[s] all come before the new ones, and max_len may be 0.  An item that
  * sees nothing gets zeros; values that are not finite may show in items of the same sequence they are hidden from.
- * max_len plus max_items, and max_items times Hq, <= 2^31 - 1025.  One sequence may take up to 2^22 workgroups, its chunks (as for dlrm_cache_attn) times its key heads
- * times the blocks of 16 to 256 pairs of an item and a head that these have; more is DLRM_ERR_BAD_SHAPE.
+ * max_len plus max_items, and max_items times Hq, <= 2^31 - 1025.  One sequence may take nearly 2^22 workgroups, its chunks (as for dlrm_cache_attn) times its key heads
+ * times the blocks of 16 to 256 pairs of an item and a head that these have, and where it has several chunks max_items times Hq may be 2^25; more is DLRM_ERR_BAD_SHAPE.
  * workspace: 256-byte aligned device memory; contents are scratch.
  */
 int32_t dlrm_cache_tree_attn(const dlrm_kv_cache* cache, const int32_t* lens, int32_t max_len, const dlrm_new_items* items,

@@ -50,6 +50,8 @@ static int check_bias(const dlrm_rel_bias* b, const dlrm_seq_batch* s, int Hq, i
   if (int st = check_rel_bias(b)) return st;
   // (wavefronts hold 32 items of one head: the last ones of every head may be empty)
   if ((int64_t)(s->max_q + 31) * (Hq / Hk) > kMostRows) return DLRM_ERR_BAD_SHAPE;
+  // (products start from bias / scale, which has to be a number)
+  if (s->scale < 0x1p-64f || s->scale > 0x1p64f) return DLRM_ERR_BAD_SHAPE;
   return DLRM_OK;
 }
 

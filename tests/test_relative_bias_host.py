@@ -50,6 +50,15 @@ def test_refusals(call):
     assert call(seq(Tq=2 ** 31 - 1, max_q=2 ** 30, Tk=1), bias()) == SHAPE
 
 
+@pytest.mark.parametrize("call", [fwd, bwd])
+def test_scales_whose_inverse_leaves_fp32(call):
+    """Without a cap the scores' products start from the bias by the scale: 1 / scale and a bias of 60000 times it have to be numbers."""
+    for scale in (2.0 ** -149, 2.0 ** -129, 2.0 ** -65, 2.0 ** 65, 2.0 ** 127):
+        assert call(seq(scale=scale), bias()) == SHAPE, scale
+        assert call(seq(scale=scale, cap=5.0), bias()) == SHAPE, scale
+    assert hot.lib().dlrm_seq_attn_bias_bwd_workspace_bytes(C.byref(seq(scale=2.0 ** -129)), C.byref(bias()), 4, 2, 64, hot.BF16) == 0
+
+
 def test_refusals_of_the_backward():
     for n in ("do", "dq", "dk", "dv"):
         for kw, want in BAD_HEADS:
