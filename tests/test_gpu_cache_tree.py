@@ -417,3 +417,33 @@ def test_drafts_are_run_in_a_tree_and_a_path_of_them_is_kept():
                              hot.alloc_cache_attn_bias_workspace(cache, Hq, max(now)), cap=30.0)
     # both round one number to bf16, and the tree's weights are rounded once more
     close(one, out[at].double().cpu(), (2 ** -7 * out[at].double().abs() + 2 ** -8 * 4.5).cpu(), "the kept draft")
+
+
+def test_calls_on_two_streams_at_once_are_what_they_are_alone():
+    """Each with a workspace of its own, on streams other than the tensors'."""
+    g, Hq, Hk, d = gen(33), 8, 2, 128
+    c = Paged(g, [9000, 40, 700], 150, 64, Hk, d, torch.bfloat16)
+    new, T = [20, 1, 37], 58
+    last = torch.tensor(sum((tree_of(g, m, "tree")[0] for m in new), []), dtype=torch.int32, device=DEV)
+    pos = torch.arange(T, dtype=torch.int32, device=DEV) + 9000
+    items = hot.NewItems(offsets(new).to(DEV), T, 37, last=last, positions=pos)
+    bias = hot.RelBias(torch.randn(Hq, 50, device=DEV), hot.relative_bounds(50, 3000, device=DEV))
+    x = [[rand(g, T, H, d, dtype=torch.bfloat16).to(DEV) for H in (Hq, Hk, Hk)] for _ in range(2)]
+
+    def step(i, out, one, ws, ws1):
+        hot.dlrm_cache_tree_attn(c.cache, c.dlens, 9000, items, *x[i], out, ws, bias=bias)
+        hot.dlrm_cache_attn_bias(c.cache, c.dlens, 9000, bias, x[i][0][:3], one, ws1)
+
+    room = lambda: (torch.full((T, Hq, d), NAN, dtype=torch.bfloat16, device=DEV), torch.full((3, Hq, d), NAN, dtype=torch.bfloat16, device=DEV),
+                    hot.alloc_cache_tree_attn_workspace(c.cache, Hq, 9000, items), hot.alloc_cache_attn_bias_workspace(c.cache, Hq, 9000))
+    alone, both, streams = [room(), room()], [room(), room()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in range(2):
+        step(i, *alone[i])
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                step(i, *both[i])
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

@@ -292,3 +292,34 @@ def test_bounds_that_do_not_ascend_stay_within_the_table():
     bias = hot.RelBias(rand(g, 2, 9).to(DEV), bounds.to(DEV))
     got = run(x, hot.SeqBatch(off.to(DEV), off.to(DEV), 290, 290, 200, 200, causal=False), bias, "rows")
     assert all(torch.isfinite(t).all() for t in got.values())
+
+
+def test_calls_on_two_streams_at_once_are_what_they_are_alone():
+    """Each with a workspace of its own, on streams other than the tensors'."""
+    g, lens = gen(52), [400, 3, 130, 257]
+    off, T = offsets(lens).to(DEV), sum(lens)
+    seq = hot.SeqBatch(off, off, T, T, 400, 400)
+    bias = hot.RelBias(torch.randn(4, 32, device=DEV), hot.relative_bounds(32, 100, device=DEV))
+    heads = (4, 2, 2, 4)
+    x = [[rand(g, T, H, 64, dtype=torch.bfloat16).to(DEV) for H in heads] for _ in range(2)]
+
+    def step(i, out, lse, dq, dk, dv, dtable, ws):
+        q, k, v, do = x[i]
+        hot.dlrm_seq_attn_bias_fwd(seq, bias, q, k, v, out, lse)
+        hot.dlrm_seq_attn_bias_bwd(seq, bias, q, k, v, out, lse, do, dq, dk, dv, dtable, ws)
+
+    def room():
+        mk = lambda H: torch.empty(T, H, 64, dtype=torch.bfloat16, device=DEV)
+        return mk(4), torch.empty(4, T, device=DEV), mk(4), mk(2), mk(2), torch.empty(4, 32, device=DEV), hot.alloc_seq_attn_bias_workspace(seq, bias, 4, 2, 64)
+    alone, both, streams = [room(), room()], [room(), room()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for i in range(2):
+        step(i, *alone[i])
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                step(i, *both[i])
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        for y, z in zip(a[:-1], b[:-1]):
+            assert torch.equal(y, z)
