@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
             if (a.positions) away = place[t] - a.positions[at];
             if (u > item[t] || item[t] > last) x[e] = -kInf;
           }
-          if (a.table) x[e] += bias_row[t][bucket_of(bounds, a.bucket_steps, away)];
+          if (a.table) x[e] += bias_row[t][bucket_of(bounds, a.buckets, a.bucket_steps, away)];
           x[e] -= slope[t] * fabsf((float)away);
         }
       } else {
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
             for (int e = 0; e < 8; ++e) x[e] += bias_row[t][at[-(16 * (e >> 2) + (e & 3))]];
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += bias_row[t][bucket_of(bounds, a.bucket_steps, away - (16 * (e >> 2) + (e & 3)))];
+            for (int e = 0; e < 8; ++e) x[e] += bias_row[t][bucket_of(bounds, a.buckets, a.bucket_steps, away - (16 * (e >> 2) + (e & 3)))];
           }
         }
         if (a.slopes) {

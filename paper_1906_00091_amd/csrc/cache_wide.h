@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) 
         for (int r = 0; r < 16; ++r) {
           const int key = key0 + acc_row(r, h) - me.len;
           float y = x[r] * scale2;
-          if (a.table) y += bias_row[b[r]];
+          if (a.table) y += bias_row[min(b[r], a.buckets - 1)];
           if (a.slopes) y -= slope * fabsf((float)(place - fresh[wave][1][acc_row(r, h)]));
           x[r] = key >= 0 && (key > item || item > fresh[wave][0][acc_row(r, h)]) ? -kInf : y;
         }
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) 
 #pragma unroll
             for (int r = 0; r < 16; ++r) b[r] += bounds[b[r] + step - 1] <= place - key0 - acc_row(r, h) ? step : 0;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], scale2, bias_row[b[r]]);
+          for (int r = 0; r < 16; ++r) x[r] = fmaf(x[r], scale2, bias_row[min(b[r], a.buckets - 1)]);  // (as in bucket_of)
         }
         if (a.slopes) {
           const int away = place - key0 - 4 * h;

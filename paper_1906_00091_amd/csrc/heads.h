@@ -91,12 +91,12 @@ __device__ inline void two_parts(const float* w, u32x4& high, u32x4& low) {
   low = narrow<DT>(l);
 }
 
-// The bucket of a distance: how many of the bounds are at most it.  bounds: 2^steps - 1 of them at least, the largest integer past those that there are; found by
-// halves, so bounds that do not ascend give some bucket too, none past the last.
-__device__ inline int bucket_of(const int* bounds, int steps, int away) {
+// The bucket of a distance: how many of the n - 1 bounds are at most it.  bounds: 2^steps - 1 of them at least, the largest integer past those that there are, which a
+// distance may reach: what that adds is taken off.  Found by halves, so bounds that do not ascend give some bucket too, none past the last.
+__device__ inline int bucket_of(const int* bounds, int n, int steps, int away) {
   int b = 0;
   for (int step = 1 << steps >> 1; step > 0; step >>= 1) b += bounds[b + step - 1] <= away ? step : 0;
-  return b;
+  return min(b, n - 1);
 }
 // orders a wavefront's own accesses of LDS, which the compiler takes for those of one lane
 __device__ inline void wave_fence() {
@@ -116,10 +116,11 @@ __device__ inline int buckets_from(const int* bounds, int n, int least, T* marks
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     if (64 * half >= n - 1) break;
-    const int b = 64 * half + lane < n - 1 ? bounds[64 * half + lane] : 0x7fffffff;
-    base += __popcll(__ballot(b <= least));
-    const uint32_t at = (uint32_t)b - (uint32_t)least;  // (the bound past all others is 2^31 - 1: no difference of integers)
-    if (at - 1u < 63u) marks[at] = T(1);
+    const int i = 64 * half + lane, b = bounds[i];  // (the array has room for two halves)
+    const bool is = i < n - 1, below = b <= least;
+    base += __popcll(__ballot(is && below));
+    const uint32_t at = (uint32_t)b - (uint32_t)least;  // (below 2^32 where b is not below)
+    if (is && !below && at < 64u) marks[at] = T(1);
   }
   wave_fence();
   const bool mark = marks[lane] != T(0);
