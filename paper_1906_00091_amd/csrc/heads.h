@@ -106,10 +106,11 @@ __device__ inline void wave_fence() {
 
 // The buckets of 64 neighbouring distances, least + lane, by a wavefront: the bounds up to `least` are counted, and those among the distances mark their places in
 // `marks` (64 places in LDS of the wavefront's own), which are counted up to each lane's; starts: the lanes, but the first, whose bucket is not the one before's.  Two round trips through LDS, where halving takes one for each step.
+// A bound that is there several times has one mark, and counts as often as it is there: each but the first of it is added to the lanes from its place on.
 template <typename T>
 __device__ inline int buckets_from(const int* bounds, int n, int least, T* marks, uint64_t& starts) {
   const int lane = lane_id();
-  int base = 0;
+  int base = 0, more = 0, before = least;  // before: the bound before a half's first
   wave_fence();
   marks[lane] = T(0);
   wave_fence();
@@ -120,13 +121,18 @@ __device__ inline int buckets_from(const int* bounds, int n, int least, T* marks
     const bool is = i < n - 1, below = b <= least;
     base += __popcll(__ballot(is && below));
     const uint32_t at = (uint32_t)b - (uint32_t)least;  // (below 2^32 where b is not below)
-    if (is && !below && at < 64u) marks[at] = T(1);
+    const bool here = is && !below && at < 64u;
+    if (here) marks[at] = T(1);
+    const int left = __builtin_amdgcn_update_dpp(before, b, 0x138, 0xf, 0xf, false);  // wave_shr:1
+    for (uint64_t again = __ballot(here && b == left); again != 0; again &= again - 1)
+      more += lane >= __builtin_amdgcn_readlane((int)at, __builtin_ctzll(again));
+    before = __builtin_amdgcn_readlane(b, 63);
   }
   wave_fence();
   const bool mark = marks[lane] != T(0);
   wave_fence();
   starts = __ballot(mark);
-  return base + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(starts >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)starts, 0));
+  return base + more + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(starts >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)starts, 0));
 }
 // A bias times `unit`; one that is there to hide its bucket (the lowest number of a type, or any so low that a row of nothing else would leave fp32 no digit of its
 // scores) is -inf.

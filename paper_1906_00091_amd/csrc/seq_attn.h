@@ -1137,7 +1137,7 @@ struct BiasSums<true, WAVES> {
       run += ((a0 ? in_high : 0.0f) + (a2 ? out_low : 0.0f)) + (a1 ? mid : 0.0f);
       give_run();
       run = ((a0 ? 0.0f : in_high) + (a2 ? 0.0f : out_low)) + (a1 ? 0.0f : mid);
-      held = first + 1;
+      held = __builtin_amdgcn_readlane(bucket, bound);
     }
     in_high = out_high = in_low = out_low = 0.0f;
   }
