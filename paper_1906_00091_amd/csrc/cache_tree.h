@@ -46,9 +46,11 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
   if (c0 >= me.n * G || (n_keys <= 0 && split > 0)) return;  // the first chunk of rows that see nothing gives zeros
 
   const int row_floats = a.buckets | 1;
+  bool by_marks = true;
   if (a.table) {
     load_bounds(bounds, a.bounds, a.buckets, a.bucket_steps, 256);
     load_biases(a, hk, c0, biases, row_floats, WAVES);
+    by_marks = bounds_differ(a.bounds, a.buckets);
   }
   // this lane's columns
   Op16<DT> qf[NT][STEPS];
@@ -89,6 +91,7 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
     }
   }
   low = __builtin_amdgcn_readfirstlane(low);
+  by_marks = by_marks && low <= kWindowEnd;
   const bool close = (uint32_t)__builtin_amdgcn_readfirstlane(high) - (uint32_t)low <= 32;  // one window of 64 distances is enough for a tile
   __syncthreads();
 
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(256) void cache_tree_kernel(TreeArgs a) {
     const bool far = low - (start + j0 + 31) >= last_bound;
     if (a.table && !any_new && !far && close) {
       uint64_t starts;
-      const int b = buckets_from(bounds, a.buckets, low - (start + j0 + 31), window[wave], starts);
+      const int b = buckets_from(bounds, a.buckets, a.bucket_steps, by_marks, low - (start + j0 + 31), window[wave], starts);
       wave_fence();
       window[wave][lane] = b;
       wave_fence();

@@ -55,9 +55,11 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) 
   bool gone = false;  // a page that the sequence has (each thread looks at those that it loaded)
   for (int p = threadIdx.x; n_cached > 0 && p <= ((start + n_cached - 1) >> a.page_shift) - page0; p += THREADS) gone = gone || pages[p] < 0 || pages[p] >= a.n_pages;
   const int row_floats = a.buckets | 1;
+  bool by_marks = true;
   if (a.table) {
     load_bounds(bounds, a.bounds, a.buckets, a.bucket_steps, THREADS);
     load_biases(a, hk, c0, biases, row_floats, WAVES);
+    by_marks = bounds_differ(a.bounds, a.buckets);
   }
   // this lane's column
   const int c = c0 + 32 * group + (lane & 31);
@@ -79,6 +81,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) 
     high = max(high, __shfl_xor(high, o, DLRM_WAVE));
   }
   low = __builtin_amdgcn_readfirstlane(low);
+  by_marks = by_marks && low <= kWindowEnd;
   high = __builtin_amdgcn_readfirstlane(high);
   const bool close = (uint32_t)high - (uint32_t)low <= 32;  // one window of 64 distances is enough for a tile
   const bool whole = __syncthreads_or(gone) == 0;  // every page of the chunk is there
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) 
         } else if (close) {
           wave_fence();
           uint64_t starts;
-          window[wave][lane] = buckets_from(bounds, a.buckets, low - (key0 + 31), window[wave], starts);
+          window[wave][lane] = buckets_from(bounds, a.buckets, a.bucket_steps, by_marks, low - (key0 + 31), window[wave], starts);
           wave_fence();
           const int* at = window[wave] + (place - low) + 31 - 4 * h;
 #pragma unroll

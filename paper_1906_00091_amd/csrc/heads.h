@@ -104,35 +104,53 @@ __device__ inline void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The buckets of 64 neighbouring distances, least + lane, by a wavefront: the bounds up to `least` are counted, and those among the distances mark their places in
-// `marks` (64 places in LDS of the wavefront's own), which are counted up to each lane's; starts: the lanes, but the first, whose bucket is not the one before's.  Two round trips through LDS, where halving takes one for each step.
-// A bound that is there several times has one mark, and counts as often as it is there: each but the first of it is added to the lanes from its place on.
+// Whether no bound is there twice, for a wavefront.
+__device__ inline bool bounds_differ(const int32_t* bounds, int n) {
+  uint64_t same = 0;
+  int before = 0;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (64 * half >= n - 1) break;
+    const int i = 64 * half + lane_id(), b = bounds[min(i, n - 2)];
+    const int left = __builtin_amdgcn_update_dpp(before, b, 0x138, 0xf, 0xf, false);  // wave_shr:1
+    same |= __ballot(b == left && i > 0 && i < n - 1);
+    before = __builtin_amdgcn_readlane(b, 63);
+  }
+  return same == 0;
+}
+constexpr int kWindowEnd = 0x7fffffff - 64;  // the last distance that a window by marks may start from
+
+// The buckets of 64 neighbouring distances, least + lane, by a wavefront; starts: the lanes, but the first, whose bucket is not the one before's.  By marks, where no bound is
+// there twice and least <= kWindowEnd (else a window would meet the largest integer behind the bounds): the bounds up to `least` are counted, and those among the
+// distances mark their places in `marks` (64 places in LDS of the wavefront's own), which are counted up to each lane's.  Two round trips through LDS, where halving
+// takes one for each step.
 template <typename T>
-__device__ inline int buckets_from(const int* bounds, int n, int least, T* marks, uint64_t& starts) {
+__device__ inline int buckets_from(const int* bounds, int n, int steps, bool by_marks, int least, T* marks, uint64_t& starts) {
   const int lane = lane_id();
-  int base = 0, more = 0, before = least;  // before: the bound before a half's first
+  if (__builtin_expect(!by_marks, 0)) {
+    const int bucket = bucket_of(bounds, n, steps, (int)((uint32_t)least + lane));
+    const int before = __shfl_up(bucket, 1, DLRM_WAVE);
+    starts = __ballot(lane > 0 && bucket != before);
+    wave_fence();
+    return bucket;
+  }
+  int base = 0;
   wave_fence();
   marks[lane] = T(0);
   wave_fence();
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     if (64 * half >= n - 1) break;
-    const int i = 64 * half + lane, b = bounds[i];  // (the array has room for two halves)
-    const bool is = i < n - 1, below = b <= least;
-    base += __popcll(__ballot(is && below));
-    const uint32_t at = (uint32_t)b - (uint32_t)least;  // (below 2^32 where b is not below)
-    const bool here = is && !below && at < 64u;
-    if (here) marks[at] = T(1);
-    const int left = __builtin_amdgcn_update_dpp(before, b, 0x138, 0xf, 0xf, false);  // wave_shr:1
-    for (uint64_t again = __ballot(here && b == left); again != 0; again &= again - 1)
-      more += lane >= __builtin_amdgcn_readlane((int)at, __builtin_ctzll(again));
-    before = __builtin_amdgcn_readlane(b, 63);
+    const int b = 64 * half + lane < n - 1 ? bounds[64 * half + lane] : 0x7fffffff;
+    base += __popcll(__ballot(b <= least));
+    const uint32_t at = (uint32_t)b - (uint32_t)least;  // (the bound past all others is 2^31 - 1: no difference of integers)
+    if (at - 1u < 63u) marks[at] = T(1);
   }
   wave_fence();
   const bool mark = marks[lane] != T(0);
   wave_fence();
   starts = __ballot(mark);
-  return base + more + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(starts >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)starts, 0));
+  return base + mark + __builtin_amdgcn_mbcnt_hi((uint32_t)(starts >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)starts, 0));
 }
 // A bias times `unit`; one that is there to hide its bucket (the lowest number of a type, or any so low that a row of nothing else would leave fp32 no digit of its
 // scores) is -inf.

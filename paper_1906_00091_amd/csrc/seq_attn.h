@@ -358,10 +358,12 @@ struct Bias {
   float* window;
   float* behind = nullptr;  // keys' gradients: the same, -inf for keys behind the query
   float slope;       // the head's, in the biases' unit
-  int n, first, last;  // first and last: the outer bounds
+  int n, steps, first, last;  // first and last: the outer bounds
+  bool by_marks = true;  // see buckets_from (distances here end before kWindowEnd)
   int even = -1;     // the bucket that the whole window is filled with, or -1
   __device__ inline Bias(const SeqArgs& a, const int* bounds_, float* window_)
-      : bounds(bounds_), window(window_), n(a.buckets), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
+      : bounds(bounds_), window(window_), n(a.buckets), steps(a.bucket_steps), first(n > 1 ? a.bounds[0] : 0), last(n > 1 ? a.bounds[n - 2] : -0x7fffffff - 1) {}
+  __device__ inline void ready() { by_marks = bounds_differ(bounds, n); }  // once the bounds are there
   __device__ inline void head(const SeqArgs& a, int h, float unit, const float* row_) {
     row = row_;
     slope = a.slopes ? a.slopes[h] * unit : 0.0f;
@@ -370,7 +372,7 @@ struct Bias {
   // Fills `to` with the biases of the distances from `least` on and returns the bucket of this lane's, `least` + lane; starts: see buckets_from.
   __device__ inline int fill(int least, float* to, uint64_t& starts) const {
     const int away = least + lane_id();  // (64 of them: the last belongs to the neighbour's window)
-    const int bucket = buckets_from(bounds, n, least, to, starts);
+    const int bucket = buckets_from(bounds, n, steps, by_marks, least, to, starts);
     const float v = fmaf(-slope, fabsf((float)away), row[bucket]);
     to[lane_id()] = v;
     if (behind) behind[lane_id()] = away < 0 ? -kInf : v;
@@ -652,6 +654,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, P
   }
   auto bias = bias_of<KIND, GROUPS, PARTS, SUB>(a, w);
   __syncthreads();
+  if constexpr (BIAS) bias.ready();
   for (int t = 0; t < tiles; ++t) {
     const int jt = t * BK;
     if (t + 1 < tiles) {
@@ -868,6 +871,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
   }
   auto bias = bias_of<KIND, GROUPS, PARTS, 1>(a, w);
   __syncthreads();
+  if constexpr (BIAS) bias.ready();
   for (int t = 0; t < tiles; ++t) {
     const int jt = t * BK;
     if (t + 1 < tiles) {
@@ -1295,6 +1299,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, DT == DLRM_F32 ? 1 : 2) void s
     put(0);
   }
   __syncthreads();
+  if constexpr (BIAS) bias.ready();
   for (int n = 0; n < all; ++n) {
     const int at = head, i0 = t * BQ + 32 * part;
     if (n + 1 < all) {
