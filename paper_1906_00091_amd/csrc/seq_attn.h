@@ -809,14 +809,14 @@ constexpr int dq_resident(int dt, int dp, int kind, int groups, int parts) {
 // ds = p (dp - delta) (a row with one key has dp = delta).  So delta is summed again on the way as sum p dp, in fp32: the kernel after this
 // one takes that; a row whose keys all lie in the first 32 has it before its first use here; and for the other rows what the rounding
 // of the output leaves is made up for by taking ds in two 16-bit parts, with a second product, where that costs little or is most needed: narrow
-// rows (5 %), and slopes, which leave a row few keys of weight (128 columns: 22 %).  dq of the long histories above is 2.4e-3 off (relative, all of it) in one
-// part and 1.7e-3 in two, which is its own rounding; of 2048 histories of up to 200 items, slopes, 1.8e-3 in two.
-// Bound as the forward is: the sizes above take 576 us (844 TFLOP/s), 197 us and 379 us (66 TFLOP/s); with a learned bias 672, 219 and 367.
+// rows (5 %), and slopes and learned biases, which leave a row few keys of weight (128 columns: 22 %, biased 16 %).  dq of the long histories above is 2.4e-3 off (relative,
+// all of it) in one part and 1.7e-3 in two, which is its own rounding, with a bias too; of 2048 histories of up to 200 items, slopes, 1.8e-3 in two.
+// Bound as the forward is: the sizes above take 576 us (844 TFLOP/s), 197 us and 379 us (66 TFLOP/s); with a learned bias 790, 219 and 367.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROUPS, PARTS)) void seq_attn_dq_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
   constexpr int BK = W::BK, TILE = W::TILE, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * GROUPS * PARTS;
-  constexpr bool TWO = DT != DLRM_F32 && (DP <= 64 || (KIND & kSlopes) != 0);  // ds in two parts
+  constexpr bool TWO = DT != DLRM_F32 && (DP <= 64 || (KIND & (kSlopes | kBias)) != 0);  // ds in two parts
   constexpr bool BIAS = (KIND & kBias) != 0;
   typedef Tile<DT, DP> T;
   __shared__ __attribute__((aligned(16))) char lds[W::LDS];
