@@ -605,6 +605,7 @@ size_t dlrm_cache_tree_attn_workspace_bytes(const dlrm_kv_cache* cache, const dl
  * hold and does not get (dlrm_qk_rope_append stores those that are kept).  Scores as for dlrm_seq_batch, with bias or NULL; cached item j stands at place j,
  * a new one at its position.  lens and max_len as for dlrm_cache_attn, but the items of lens[s] all come before the new ones, and max_len may be 0.  An item that
  * sees nothing gets zeros; values that are not finite may show in items of the same sequence they are hidden from.
+ * With 16-bit rows the weights enter their product in two 16-bit parts, as in dlrm_cache_attn: a result is off by its own rounding, however many items are asked at once.
  * max_len plus max_items, and max_items times Hq, <= 2^31 - 1025.  One sequence may take nearly 2^22 workgroups, its chunks (as for dlrm_cache_attn) times its key heads
  * times the blocks of 16 to 256 pairs of an item and a head that these have, and where it has several chunks max_items times Hq may be 2^25; more is DLRM_ERR_BAD_SHAPE.
  * workspace: 256-byte aligned device memory; contents are scratch.

@@ -26,7 +26,7 @@ static int64_t blocks_of(const dlrm_kv_cache* c, int Hq, int max_items) {
 static int64_t groups_of(const dlrm_kv_cache* c, int Hq, int max_items) { return c->B * c->Hk * blocks_of(c, Hq, max_items); }
 static int64_t most_of_chunk(const dlrm_kv_cache* c) { return (int64_t)(kTablePages - 1) * c->page; }  // (it need not start on a page)
 // Keys of a chunk: as many as leave 2048 workgroups, so that sequences of mixed lengths fill the device to the end, but no fewer than `fine` for it; else as many as
-// leave each CU the workgroups that it holds.  Every chunk leaves a row of sums for each column, which are written and read again.  (128 sequences of up to
+// leave each CU the workgroups that it holds.  Every chunk leaves a row of sums for each column, which are written and read again.  (Weights in one part: 128 sequences of up to
 // 8192 items with trees of up to 60, bf16, d 128: one chunk a sequence 735 us, two 694, four 671;  256 sequences of up to 8192 with one item: 431 and, cut in two,
 // 422;  one of 131072 items under 64 with 256 columns, each CU one workgroup 123 us, two 144, four 192, eight 248.)
 constexpr int kMany = 2048;

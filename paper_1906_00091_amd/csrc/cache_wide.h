@@ -5,11 +5,10 @@
 // workgroup holds, two wavefronts share 32 of them, each with half of a tile's keys, and join at the end.  New items are keys behind the cached
 // ones, as in cache_tree.h.
 //
-// Weights are 16-bit numbers in their product, in one part: bound by arithmetic, this would pay a third for two, and a result is off by up to one and a half times its
-// rounding (bf16 2.1e-3, rounding alone 1.7e-3).  128 sequences of up to 8192 items with trees of up to 60, 16 query heads on 4, bf16, d 128, a bias of 64 buckets, capped:
-// 543 us and 36 for the join, 238 TFLOP/s of visible pairs; with 60 items to 8192 each 1116 us in all, 462 TFLOP/s (vector work 60 % of the time, matrix cores 21 %, one
-// after the other for the most part).  The difference is rows of no column in a wavefront's 32 and wavefronts with none in a workgroup.  One sequence of
-// 131072 items under 64: 117 us in all, 590 TFLOP/s.
+// 16-bit weights enter their product in two parts, as for up to 32 columns: an item's result is off by its own rounding whatever is asked with it.  (One part would take
+// 575, 87 and 128 us where two take 683, 103 and 155, the three sizes below, and be 1.2 to 1.4 times as far off.)  128 sequences of up to 8192 items with trees of up to 60, 16 query heads
+// on 4, bf16, d 128, a bias of 64 buckets, capped: 683 us with the join; 500 candidate lists over up to 1000 items, fp16, d 40: 103 us; one sequence of 131072 items
+// under 64: 155 us.
 #pragma once
 
 #include "seq_attn.h"
@@ -20,10 +19,11 @@ namespace dlrm {
 constexpr int kWidePages = 1024;  // pages of a chunk, at most
 
 // Registers leave room for four wavefronts a SIMD up to 64 columns, two workgroups of eight a CU: 25 of them are spilled for it (500 candidate lists over up to 1000
-// items, fp16, d 40: 89 us, 115 with one workgroup).
+// items, fp16, d 40, weights in one part: 89 us, 115 with one workgroup).
 template <int DT, int DP, int WAVES, bool BEND>
 __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) void cache_wide_kernel(TreeArgs a) {
   typedef Tile<DT, DP> T;
+  constexpr bool TWO = DT != DLRM_F32;  // weights in two parts
   constexpr int EB = Tab<DT>::EB, STEPS = DP / 16, NB = DP / 32, THREADS = 64 * WAVES, BK = 64;
   constexpr int CH = DP * EB / 16, N = (BK * CH + THREADS - 1) / THREADS;  // chunks of 16 bytes: of a row; of a tile, per thread
   constexpr int TILE = BK * T::STRIDE, BUFS = 4 * TILE > (DT == DLRM_F32 || WAVES == 8 ? 120 : 70) * 1024 ? 1 : 2;
@@ -246,15 +246,21 @@ __global__ __launch_bounds__(64 * WAVES, DT == DLRM_F32 ? 1 : DP <= 64 ? 4 : 2) 
       const float ms = m == -kInf ? 0.0f : m - kWeightLift<DT>;
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        Op<DT> p;
+        Op<DT> p, low;
+        float e[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(x[8 * g + r], cc, -ms));
-          l += e;
-          p.set(r, e);
+          e[r] = __builtin_amdgcn_exp2f(fmaf(x[8 * g + r], cc, -ms));
+          l += e[r];
+          if constexpr (!TWO) p.set(r, e[r]);
         }
+        if constexpr (TWO) op_two_parts(e, p, low);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) o[b] = Op<DT>::mma(T::by_column(vs, 16 * g, b, lane), p, o[b]);
+        for (int b = 0; b < NB; ++b) {
+          const Op<DT> vt = T::by_column(vs, 16 * g, b, lane);
+          o[b] = Op<DT>::mma(vt, p, o[b]);
+          if constexpr (TWO) o[b] = Op<DT>::mma(vt, low, o[b]);
+        }
       }
     }
     if (BUFS == 1) __syncthreads();

@@ -7,6 +7,7 @@ import paper_1906_00091_amd as hot
 
 import bias_ref as ref
 from history_ref import offsets
+from test_gpu_cache_tree import Paged
 from test_gpu_relative_bias import DEV, DT, gen, rand, run
 
 pytestmark = pytest.mark.gpu
@@ -40,4 +41,38 @@ def test_queries_gradients_of_wide_rows_are_off_by_their_own_rounding(dtype, kin
     more[off[:-1]] = False
     share = wrongly_rounded(got["dq"].cpu()[more], want["dq"][more])
     print("[share]", dtype, kind, d, share, flush=True)
+    assert share < 0.05
+
+
+MANY = [
+    # query heads, key heads, d, cached, new items, bias, cap
+    (4, 2, 64, [300, 17], 3, True, 0.0),          # 6 columns: the kernel for few
+    (8, 2, 128, [400, 40], 10, True, 20.0),       # 40: two wavefronts to 32 columns
+    (8, 2, 64, [400, 0], 30, False, 0.0),         # 120
+    (16, 4, 96, [90, 333], 60, True, 0.0),        # 240: a workgroup of eight wavefronts
+    (16, 4, 128, [9000], 64, False, 0.0),         # several chunks
+    (8, 1, 40, [1200, 700], 70, True, 30.0),      # several blocks
+    (64, 1, 32, [200, 100], 20, False, 0.0),
+]
+
+
+@pytest.mark.parametrize("i", range(len(MANY)))
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_new_items_are_off_by_their_own_rounding_however_many(dtype, i):
+    """Weights enter their product in two parts, 2^-17 (bf16) or 2^-22 (fp16) of each off: as above, about one result of 128 in bf16 is wrongly rounded, and in one part a third."""
+    Hq, Hk, d, lens, m, with_bias, cap = MANY[i]
+    g, dt, B = gen(40 + i), DT[dtype], len(lens)
+    c = Paged(g, lens, -(-max(lens) // 16), 16, Hk, d, dt)
+    x = {n: rand(g, B * m, H, d, dtype=dt) for n, H in (("q", Hq), ("k", Hk), ("v", Hk))}
+    pos, last = torch.cat([torch.arange(y, y + m) for y in lens]).to(torch.int32), torch.full((B * m,), m - 1, dtype=torch.int32)
+    table, bounds = (rand(g, Hq, 32), hot.relative_bounds(32, 300)) if with_bias else (None, None)
+    items = hot.NewItems(offsets([m] * B).to(DEV), B * m, m, positions=pos.to(DEV))
+    out = torch.empty_like(x["q"]).to(DEV)
+    hot.dlrm_cache_tree_attn(c.cache, c.dlens, max(lens), items, *(x[n].to(DEV) for n in "qkv"), out,
+                             hot.alloc_cache_tree_attn_workspace(c.cache, Hq, max(lens), items),
+                             bias=hot.RelBias(table.to(DEV), bounds.to(DEV)) if with_bias else None, cap=cap)
+    want = torch.cat([ref.cached(x["q"][I], c.k[s], c.v[s], x["k"][I], x["v"][I], pos[I], last[I], None, table, bounds, d ** -0.5, cap)[0]
+                      for s, I in ((s, slice(s * m, (s + 1) * m)) for s in range(B))])
+    share = wrongly_rounded(out, want)
+    print("[share]", dtype, i, share, flush=True)
     assert share < 0.05
