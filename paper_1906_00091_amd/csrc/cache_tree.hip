@@ -81,6 +81,7 @@ static int run(const dlrm_kv_cache* c, const int32_t* lens, int max_len, int max
   const int eb = elem_bytes(c->dtype);
   for (const dlrm_heads* x : {q, out})
     if (int st = check_heads(x, T, Hq, c->d, eb)) return st;
+  if (T == 0) return DLRM_OK;  // nothing to answer
   a.q = rows_of(q, T, Hq, c->d, eb);
   a.out = rows_of(out, T, Hq, c->d, eb);
   a.k = static_cast<const char*>(c->k);
@@ -184,12 +185,6 @@ extern "C" int32_t dlrm_cache_tree_attn(const dlrm_kv_cache* c, const int32_t* l
   a.slopes = slopes;
   a.scale = scale;
   a.cap = cap;
-  if (x->T == 0) {  // nothing to answer; the other arguments are checked all the same
-    if (!lens) return DLRM_ERR_NULL;
-    for (const dlrm_heads* y : {q, out})
-      if (int st = check_heads(y, 0, Hq, c->d, eb)) return st;
-    return DLRM_OK;
-  }
   return run(c, lens, max_len, items, x->T, Hq, a, q, out, bias, dlrm_cache_tree_attn_workspace_bytes(c, x, Hq, max_len), workspace,
              workspace_bytes, stream);
 }

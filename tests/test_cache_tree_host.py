@@ -159,3 +159,14 @@ def test_an_item_of_a_tree_sees_its_ancestors_and_itself(seed):
             above.add(at[y])
             y = mixed[y]
         assert above == {j for j in range(60) if j <= i <= last[j]} and depth[i] == len(above) - 1
+
+
+def test_a_call_without_items_is_checked_like_any_other():
+    none = dict(ws=None, n=0, **{n: heads(data=None) for n in ("q", "k", "v", "o")})
+    x = items(T=0, last=None, positions=None)
+    assert tree(cache(), x, **none) == 0
+    for kw, want in SCORE:
+        assert tree(cache(), x, **dict(none, **kw)) == want, kw
+    for n in ("q", "k", "v", "o"):
+        assert tree(cache(), x, **dict(none, **{n: heads(data=P + 8)})) == SHAPE, n
+    assert tree(cache(), x, lens=None, **none) == NULL
