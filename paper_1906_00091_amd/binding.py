@@ -479,6 +479,14 @@ def _vector(fn: str, x: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> O
     return x.data_ptr()
 
 
+def _same_device(fn: str, x, *others):
+    """Refuses arrays and plans on another device than x: a kernel that is given a host address faults."""
+    at = x.device
+    for y in others:
+        if y is not None and y.device != at:
+            raise ValueError("%s: an array is on %s, others are on %s" % (fn, y.device, at))
+
+
 def _workspace(x: Optional[torch.Tensor]):
     return (None, 0) if x is None else (x.data_ptr(), x.numel() * x.element_size())
 
@@ -575,7 +583,7 @@ class KvCache:
         if k.dtype not in _DTYPE_OF:
             raise DlrmError("KvCache", -3)
         self.k, self.v, self.table = k, v, table
-        self.B = int(table.shape[0])
+        self.B, self.device = int(table.shape[0]), table.device
         self.n_pages, self.Hk, self.page, self.d = (int(x) for x in k.shape)
         self.dtype = _DTYPE_OF[k.dtype]
         self.c = _KvCacheC(k.data_ptr(), v.data_ptr(), table.data_ptr(), self.B, int(table.shape[1]), self.n_pages, self.page, self.Hk,
@@ -604,7 +612,7 @@ class SeqBatch:
                  prefix: Optional[torch.Tensor] = None, slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None,
                  cap: float = 0.0):
         self.B = int(q_off.numel()) - 1
-        self.q_off, self.k_off, self.prefix, self.slopes, self.scale = q_off, k_off, prefix, slopes, scale
+        self.q_off, self.k_off, self.prefix, self.slopes, self.scale, self.device = q_off, k_off, prefix, slopes, scale, q_off.device
         if slopes is not None and (slopes.dtype != torch.float32 or not slopes.is_contiguous()):
             raise ValueError("SeqBatch: slopes are contiguous float32, one for each query head")
         self.Tq, self.Tk = int(Tq), int(Tk)
@@ -656,7 +664,7 @@ def alloc_seq_attn_workspace(seq: SeqBatch, Hq: int, Hk: int, d: int, dtype: Opt
 
 class RelBias:
     """A learned bias of scores by buckets of relative places (dlrm_rel_bias).  table: fp32 [Hq, n]; bounds: int32 [n - 1], ascending (see
-    relative_bounds; None for one bucket)."""
+    relative_bounds; None for one bucket), on the table's device."""
 
     def __init__(self, table: torch.Tensor, bounds: Optional[torch.Tensor]):
         if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous():
@@ -664,7 +672,8 @@ class RelBias:
         self.Hq, self.n = (int(x) for x in table.shape)
         if bounds is None and self.n != 1:
             raise ValueError("RelBias: %d buckets have %d bounds" % (self.n, self.n - 1))
-        self.table, self.bounds = table, bounds
+        _same_device("RelBias", table, bounds)
+        self.table, self.bounds, self.device = table, bounds, table.device
         self.c = _RelBiasC(table.data_ptr(), _vector("RelBias", bounds, self.n - 1, torch.int32), self.n)
 
     def ref(self, Hq: int):
@@ -675,7 +684,8 @@ class RelBias:
 
 def relative_bounds(n: int, far: int, both: bool = False, device=None) -> torch.Tensor:
     """Bounds of n buckets for RelBias: half of them for distances 0, 1, 2, ... alone, the others wider by equal factors, the last from `far` on.
-    With `both` half of the n are for keys behind the query: a distance of -x has a bucket of its own where x has."""
+    With `both` half of the n are for keys behind the query: a distance of -x has a bucket of its own where x has.  On the host unless a device
+    is given; RelBias wants them where its table is."""
     def up(m):
         near = (m + 1) // 2
         b = list(range(1, near + 1))
@@ -694,6 +704,7 @@ def dlrm_seq_attn_bias_fwd(seq: SeqBatch, bias: RelBias, q: torch.Tensor, k: tor
     """dlrm_seq_attn_fwd with a learned bias."""
     fn = "dlrm_seq_attn_bias_fwd"
     (_, Hq, d), dt = _first(fn, q)
+    _same_device(fn, q, seq, bias)
     Hk = _first(fn, k)[0][1]
     rq, rk = (seq.Tq, Hq, d), (seq.Tk, Hk, d)
     _check(fn, lib().dlrm_seq_attn_bias_fwd(seq.ref(Hq, d), bias.ref(Hq), Hq, Hk, d, dt, *_heads(fn, dt, ((q, rq), (k, rk), (v, rk), (out, rq))),
@@ -705,6 +716,7 @@ def dlrm_seq_attn_bias_bwd(seq: SeqBatch, bias: RelBias, q: torch.Tensor, k: tor
     """dlrm_seq_attn_bwd with a learned bias; out, lse: dlrm_seq_attn_bias_fwd's; dtable: fp32 [Hq, n], written."""
     fn = "dlrm_seq_attn_bias_bwd"
     (_, Hq, d), dt = _first(fn, q)
+    _same_device(fn, q, seq, bias)
     Hk = _first(fn, k)[0][1]
     rq, rk = (seq.Tq, Hq, d), (seq.Tk, Hk, d)
     h = _heads(fn, dt, ((q, rq), (k, rk), (v, rk), (out, rq), (dout, rq), (dq, rq), (dk, rk), (dv, rk)))
@@ -748,6 +760,7 @@ def dlrm_cache_attn_bias(cache: KvCache, lens: torch.Tensor, max_len: int, bias:
     """dlrm_cache_attn with a learned bias."""
     fn = "dlrm_cache_attn_bias"
     Hq = _first(fn, q)[0][1]
+    _same_device(fn, q, cache, lens, bias)
     rows = (cache.B, Hq, cache.d)
     a, b = _heads(fn, cache.dtype, ((q, rows), (out, rows)))
     ws, ws_bytes = _workspace(workspace)
@@ -770,7 +783,8 @@ class NewItems:
 
     def __init__(self, off: torch.Tensor, T: int, max_items: int, last: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
         self.B, self.T, self.max_items = int(off.numel()) - 1, int(T), int(max_items)
-        self.off, self.last, self.positions = off, last, positions
+        _same_device("NewItems", off, last, positions)
+        self.off, self.last, self.positions, self.device = off, last, positions, off.device
         self.c = _NewItemsC(self.T, self.max_items, _vector("NewItems", off, self.B + 1, torch.int64), _vector("NewItems", last, self.T, torch.int32),
                             _vector("NewItems", positions, self.T, torch.int32))
 
@@ -810,6 +824,7 @@ def dlrm_cache_tree_attn(cache: KvCache, lens: torch.Tensor, max_len: int, items
     """q, out: [T, Hq, d]; k, v: [T, Hk, d], the new items' own; lens: int32 [B], items of every sequence in the cache, which all come before the new ones."""
     fn = "dlrm_cache_tree_attn"
     Hq = _first(fn, q)[0][1]
+    _same_device(fn, q, cache, lens, items, bias)
     rq, rk = (items.T, Hq, cache.d), (items.T, cache.Hk, cache.d)
     ws, ws_bytes = _workspace(workspace)
     _check(fn, lib().dlrm_cache_tree_attn(cache.ref(), _vector(fn, lens, cache.B, torch.int32), max_len, items.ref(cache.B), Hq,

@@ -141,3 +141,30 @@ def test_the_64_bit_form_against_differences(causal, slopes, cap):
                 y[n].view(-1)[at] += step
                 sides.append(float((run(y)["out"] * do).sum()))
             assert abs((sides[0] - sides[1]) / 2e-5 - float(grad.view(-1)[at])) < 1e-8, (n, at)
+
+
+def test_plans_and_calls_refuse_arrays_on_several_devices():
+    """(the other device is torch's own "meta" here: with a GPU it is the host, whose addresses a kernel must not get)"""
+    meta = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device="meta")
+    table, bounds, off, i32 = torch.zeros(4, 8), hot.relative_bounds(8, 20), torch.tensor([0, 4]), torch.zeros(4, dtype=torch.int32)
+    for bad in (lambda: hot.RelBias(table, bounds.to("meta")), lambda: hot.RelBias(meta(4, 8), bounds),
+                lambda: hot.NewItems(off, 4, 4, last=i32.to("meta")), lambda: hot.NewItems(off, 4, 4, positions=i32.to("meta")),
+                lambda: hot.NewItems(off.to("meta"), 4, 4, last=i32)):
+        with pytest.raises(ValueError, match="on meta"):
+            bad()
+    b, there = hot.RelBias(table, bounds), hot.RelBias(meta(4, 8), bounds.to("meta"))
+    s, x, lse, dtable = hot.SeqBatch(off, off, 4, 4, 4, 4), torch.zeros(4, 4, 8), torch.zeros(4, 4), torch.zeros(4, 8)
+    elsewhere = hot.SeqBatch(off.to("meta"), off.to("meta"), 4, 4, 4, 4)
+    pool = torch.zeros(2, 8, 4, 16, 8)
+    c, lens, items = hot.KvCache(pool[0], pool[1], torch.zeros(1, 2, dtype=torch.int32)), torch.zeros(1, dtype=torch.int32), hot.NewItems(off, 4, 4)
+    c2 = hot.KvCache(pool[0].to("meta"), pool[1].to("meta"), torch.zeros(1, 2, dtype=torch.int32, device="meta"))
+    one, far = torch.zeros(1, 4, 8), hot.NewItems(off.to("meta"), 4, 4)
+    for bad in (lambda: hot.dlrm_seq_attn_bias_fwd(s, there, x, x, x, x), lambda: hot.dlrm_seq_attn_bias_fwd(elsewhere, b, x, x, x, x),
+                lambda: hot.dlrm_seq_attn_bias_bwd(s, there, x, x, x, x, lse, x, x, x, x, dtable, None),
+                lambda: hot.dlrm_seq_attn_bias_bwd(elsewhere, b, x, x, x, x, lse, x, x, x, x, dtable, None),
+                lambda: hot.dlrm_cache_attn_bias(c, lens, 32, there, one, one, None), lambda: hot.dlrm_cache_attn_bias(c, lens.to("meta"), 32, b, one, one, None),
+                lambda: hot.dlrm_cache_attn_bias(c2, lens, 32, b, one, one, None), lambda: hot.dlrm_cache_tree_attn(c2, lens, 32, items, x, x, x, x, None),
+                lambda: hot.dlrm_cache_tree_attn(c, lens.to("meta"), 32, items, x, x, x, x, None),
+                lambda: hot.dlrm_cache_tree_attn(c, lens, 32, far, x, x, x, x, None), lambda: hot.dlrm_cache_tree_attn(c, lens, 32, items, x, x, x, x, None, bias=there)):
+        with pytest.raises(ValueError, match="on meta"):
+            bad()
