@@ -23,13 +23,17 @@ static int64_t blocks_of(const dlrm_kv_cache* c, int Hq, int max_items) {
   const int cols = 16 * tiles_of(c, Hq, max_items);
   return ((int64_t)(max_items < 1 ? 1 : max_items) * (Hq / c->Hk) + cols - 1) / cols;
 }
-static int64_t groups_of(const dlrm_kv_cache* c, int Hq, int max_items) { return c->B * c->Hk * blocks_of(c, Hq, max_items); }
+// (2^58 at most; from kMany on none is cut for there being few of them, and this times a length stays far below 2^63)
+constexpr int kMany = 2048;
+static int64_t groups_of(const dlrm_kv_cache* c, int Hq, int max_items) {
+  const int64_t n = (int64_t)c->B * c->Hk * blocks_of(c, Hq, max_items);
+  return n < kMany ? n : kMany;
+}
 static int64_t most_of_chunk(const dlrm_kv_cache* c) { return (int64_t)(kTablePages - 1) * c->page; }  // (it need not start on a page)
-// Keys of a chunk: as many as leave 2048 workgroups, so that sequences of mixed lengths fill the device to the end, but no fewer than `fine` for it; else as many as
+// Keys of a chunk: as many as leave kMany workgroups, so that sequences of mixed lengths fill the device to the end, but no fewer than `fine` for it; else as many as
 // leave each CU the workgroups that it holds.  Every chunk leaves a row of sums for each column, which are written and read again.  (Weights in one part: 128 sequences of up to
 // 8192 items with trees of up to 60, bf16, d 128: one chunk a sequence 735 us, two 694, four 671;  256 sequences of up to 8192 with one item: 431 and, cut in two,
 // 422;  one of 131072 items under 64 with 256 columns, each CU one workgroup 123 us, two 144, four 192, eight 248.)
-constexpr int kMany = 2048;
 static int64_t fill_of(int tiles) { return tiles > kWide ? 256 : tiles == kWide ? 512 : 1024; }
 static int64_t fine_of(int tiles) { return tiles == kWide ? 1024 : 2048; }
 static int chunk_of(const dlrm_kv_cache* c, int tiles, int64_t groups, int64_t total) {

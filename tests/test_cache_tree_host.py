@@ -170,3 +170,18 @@ def test_a_call_without_items_is_checked_like_any_other():
     for n in ("q", "k", "v", "o"):
         assert tree(cache(), x, **dict(none, **{n: heads(data=P + 8)})) == SHAPE, n
     assert tree(cache(), x, lens=None, **none) == NULL
+
+
+@pytest.mark.parametrize("B,Hk", [(1 << 27, 16), ((1 << 28) - 1, 16), (1 << 28, 16), (2 ** 31 - 1, 1), (2 ** 31 - 1, 1024)])
+@pytest.mark.parametrize("page", [1, 16])
+def test_batches_whose_sequences_times_heads_pass_32_bits(B, Hk, page):
+    """2^31 and more groups of a sequence and a key head: none is cut but where a chunk's table of 1024 pages ends."""
+    c, max_len, d = cache(B=B, Hk=Hk, d=8, page=page, table_cols=1 << 16), 1 << 16, 8
+    pieces = -(-max_len // (1023 * page))
+    need = hot.lib().dlrm_cache_attn_bias_workspace_bytes(C.byref(c), Hk, max_len)
+    assert need >= B * Hk * pieces * (d + 2) * 4
+    x = items(T=2 ** 31 - 1, max_items=1)
+    need = hot.lib().dlrm_cache_tree_attn_workspace_bytes(C.byref(c), C.byref(x), Hk, max_len)
+    assert need >= x.T * Hk * -(-(max_len + 1) // (1023 * page)) * (d + 2) * 4
+    x = items(T=2 ** 31 - 1, max_items=1 << 20)   # a loose bound: 2^16 and more blocks of columns for each sequence
+    assert hot.lib().dlrm_cache_tree_attn_workspace_bytes(C.byref(c), C.byref(x), Hk, max_len) >= x.T * Hk * pieces * (d + 2) * 4
