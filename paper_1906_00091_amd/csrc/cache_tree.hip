@@ -1,65 +1,12 @@
 // Attention of new items over a paged cache: entry points and argument checks (the kernels: cache_tree.h).
 #include "tree_args.h"
+#include "tree_cut.h"
 
 #include <math.h>
 
 #include <initializer_list>
 
 using namespace dlrm;
-
-// Columns of a workgroup in tiles of 16: a wavefront's up to 32 (cache_tree.h), all wavefronts' beyond (cache_wide.h: four wavefronts, or eight); one tile where `max_items` is 0,
-// for one item that is in the cache.  (The biases of a block's heads stand in LDS: more than 64 heads to a key head keep to the small blocks.)
-constexpr int kWide = 8;  // tiles from which on a workgroup's wavefronts share them
-static int tiles_of(const dlrm_kv_cache* c, int Hq, int max_items) {
-  const int G = Hq / c->Hk;
-  const int64_t n = (int64_t)max_items * G;
-  if (n <= 16) return 1;
-  if (n <= 32 || G > 64) return 2;
-  return n <= 128 || c->dtype == DLRM_F32 ? kWide : 2 * kWide;
-}
-
-constexpr int kTablePages = 1024, kLeastChunk = 256;
-static int64_t blocks_of(const dlrm_kv_cache* c, int Hq, int max_items) {
-  const int cols = 16 * tiles_of(c, Hq, max_items);
-  return ((int64_t)(max_items < 1 ? 1 : max_items) * (Hq / c->Hk) + cols - 1) / cols;
-}
-// (2^58 at most; from kMany on none is cut for there being few of them, and this times a length stays far below 2^63)
-constexpr int kMany = 2048;
-static int64_t groups_of(const dlrm_kv_cache* c, int Hq, int max_items) {
-  const int64_t n = (int64_t)c->B * c->Hk * blocks_of(c, Hq, max_items);
-  return n < kMany ? n : kMany;
-}
-static int64_t most_of_chunk(const dlrm_kv_cache* c) { return (int64_t)(kTablePages - 1) * c->page; }  // (it need not start on a page)
-// Keys of a chunk: as many as leave kMany workgroups, so that sequences of mixed lengths fill the device to the end, but no fewer than `fine` for it; else as many as
-// leave each CU the workgroups that it holds.  Every chunk leaves a row of sums for each column, which are written and read again.  (Weights in one part: 128 sequences of up to
-// 8192 items with trees of up to 60, bf16, d 128: one chunk a sequence 735 us, two 694, four 671;  256 sequences of up to 8192 with one item: 431 and, cut in two,
-// 422;  one of 131072 items under 64 with 256 columns, each CU one workgroup 123 us, two 144, four 192, eight 248.)
-static int64_t fill_of(int tiles) { return tiles > kWide ? 256 : tiles == kWide ? 512 : 1024; }
-static int64_t fine_of(int tiles) { return tiles == kWide ? 1024 : 2048; }
-static int chunk_of(const dlrm_kv_cache* c, int tiles, int64_t groups, int64_t total) {
-  int64_t n = (groups * total + kMany - 1) / kMany;
-  if (n < fine_of(tiles)) {
-    n = (groups * total + fill_of(tiles) - 1) / fill_of(tiles);
-    if (n > fine_of(tiles) + 128) n = fine_of(tiles) + 128;
-  }
-  if (n < kLeastChunk) n = kLeastChunk;
-  n = (n + 127) / 128 * 128;
-  if (n > most_of_chunk(c)) n = most_of_chunk(c);
-  return (int)(n > total ? total : n);
-}
-static int64_t held_of(const dlrm_kv_cache* c) { return (int64_t)c->table_cols * c->page; }
-
-// The most chunks that bounds of up to max_len cached and `extra` new items give a sequence.  (A smaller bound may give more of them than max_len.)  A chunk has the fewest
-// keys there are, as many as a page table's piece holds, enough for `fine` keys, or enough for the workgroups wanted.
-static int64_t most_splits(const dlrm_kv_cache* c, int tiles, int64_t groups, int max_len, int extra) {
-  const int64_t held = held_of(c), n = (max_len > held ? held : max_len) + extra;
-  if (n < 1) return 1;
-  auto pieces = [&](int64_t keys) { return (n - 1) / keys + 1; };
-  int64_t most = (fill_of(tiles) - 1) / groups + 1;
-  if (pieces(fine_of(tiles)) > most) most = pieces(fine_of(tiles));
-  if (pieces(most_of_chunk(c)) > most) most = pieces(most_of_chunk(c));
-  return pieces(kLeastChunk) < most ? pieces(kLeastChunk) : most;
-}
 
 static int check_common(const dlrm_kv_cache* c, int Hq) {
   if (int st = check_cache(c)) return st;
@@ -103,11 +50,11 @@ static int run(const dlrm_kv_cache* c, const int32_t* lens, int max_len, int max
   a.max_len = max_len > held ? (int)held : max_len;
   a.max_items = max_items < 1 ? 1 : max_items;
   TreeLaunch how = {};
-  how.tiles = tiles_of(c, Hq, max_items);
-  const int64_t groups = groups_of(c, Hq, max_items), blocks = blocks_of(c, Hq, max_items), total = (int64_t)a.max_len + max_items;
-  a.blocks = (int)blocks;
-  a.chunk = total > 0 ? chunk_of(c, how.tiles, groups, total) : 1;
-  a.splits = total > 0 ? (int)((total - 1) / a.chunk) + 1 : 1;
+  const TreeCut cut = tree_cut(c, Hq, max_len, max_items);
+  how.tiles = cut.tiles;
+  a.blocks = (int)cut.blocks;
+  a.chunk = cut.chunk;
+  a.splits = cut.splits;
   if (bias) {
     a.table = bias->table;
     a.bounds = bias->bounds;
@@ -118,8 +65,8 @@ static int run(const dlrm_kv_cache* c, const int32_t* lens, int max_len, int max
     how.lds = (unsigned)(a.bias_rows * (bias->n | 1) * sizeof(float));
   }
   // a launch takes fewer than 2^32 threads, and the joining one 65535 sequences: more than that go in several
-  const int64_t per_seq = (int64_t)a.splits * a.Hk * blocks;
-  how.each = (kLaunchThreads / 512 - 8 * blocks) / per_seq;
+  const int64_t per_seq = (int64_t)a.splits * a.Hk * cut.blocks;
+  how.each = (kLaunchThreads / 512 - 8 * cut.blocks) / per_seq;
   if (how.each < 1) return DLRM_ERR_BAD_SHAPE;
   if (a.splits > 1) {
     if (how.each > 65535) how.each = 65535;
@@ -138,14 +85,9 @@ static int run(const dlrm_kv_cache* c, const int32_t* lens, int max_len, int max
   }
 }
 
-static size_t parts_bytes(const dlrm_kv_cache* c, int64_t rows, int64_t splits) {
-  const size_t n = splits > 1 ? (size_t)rows * splits * (c->d + 2) * sizeof(float) : 0;
-  return n < 256 ? 256 : (n + 255) / 256 * 256;
-}
-
 extern "C" size_t dlrm_cache_attn_bias_workspace_bytes(const dlrm_kv_cache* c, int32_t Hq, int32_t max_len) {
   if (check_common(c, Hq) != DLRM_OK || max_len < 1) return 0;
-  return parts_bytes(c, (int64_t)c->B * Hq, most_splits(c, tiles_of(c, Hq, 0), groups_of(c, Hq, 0), max_len, 0));
+  return tree_workspace(c, Hq, (int64_t)c->B * Hq, max_len, 0);
 }
 
 extern "C" int32_t dlrm_cache_attn_bias(const dlrm_kv_cache* c, const int32_t* lens, int32_t max_len, const dlrm_rel_bias* bias, int32_t Hq,
@@ -164,7 +106,7 @@ extern "C" int32_t dlrm_cache_attn_bias(const dlrm_kv_cache* c, const int32_t* l
 extern "C" size_t dlrm_cache_tree_attn_workspace_bytes(const dlrm_kv_cache* c, const dlrm_new_items* x, int32_t Hq, int32_t max_len) {
   int items;
   if (check_tree(c, x, Hq, max_len, items) != DLRM_OK) return 0;
-  return parts_bytes(c, x->T * Hq, most_splits(c, tiles_of(c, Hq, items), groups_of(c, Hq, items), max_len, items));
+  return tree_workspace(c, Hq, x->T * Hq, max_len, items);
 }
 
 extern "C" int32_t dlrm_cache_tree_attn(const dlrm_kv_cache* c, const int32_t* lens, int32_t max_len, const dlrm_new_items* x, int32_t Hq,
