@@ -6,9 +6,10 @@ import torch
 import paper_1906_00091_amd as hot
 
 import bias_ref as ref
+from bias_table_ref import LIMIT, off, table_gradient
 from history_ref import offsets
 from test_gpu_cache_tree import Paged
-from test_gpu_relative_bias import DEV, DT, gen, rand, run
+from test_gpu_relative_bias import CASES, DEV, DT, gen, rand, run, setup
 
 pytestmark = pytest.mark.gpu
 
@@ -28,17 +29,17 @@ def test_queries_gradients_of_wide_rows_are_off_by_their_own_rounding(dtype, kin
     2^-12 off, a quarter of the spacing at their root mean square: a third of the results.  (The first item of a sequence sees itself alone: its gradient is rounding alone.)"""
     g, dt, Hq, Hk = gen(d), DT[dtype], 4, 2
     lens = [32, 5, 17, 30, 2, 29, 31, 11] * 4
-    off, T = offsets(lens), sum(lens)
+    starts, T = offsets(lens), sum(lens)
     x = {n: rand(g, T, H, d, dtype=dt) for n, H in (("q", Hq), ("k", Hk), ("v", Hk), ("do", Hq))}
     slopes = torch.tensor([0.5, 0.25, 0.7, 0.1]) if kind == "slopes" else None
     bounds = torch.arange(1, 16, dtype=torch.int32)
     table = rand(g, Hq, 16) * (1 if slopes is not None else 2)
     cap = 8.0 if kind == "cap" else 0.0
-    seq = hot.SeqBatch(off.to(DEV), off.to(DEV), T, T, 32, 32, slopes=None if slopes is None else slopes.to(DEV), cap=cap)
+    seq = hot.SeqBatch(starts.to(DEV), starts.to(DEV), T, T, 32, 32, slopes=None if slopes is None else slopes.to(DEV), cap=cap)
     got = run(x, seq, hot.RelBias(table.to(DEV), bounds.to(DEV)), "rows")
-    want = ref.attention(x["q"], x["k"], x["v"], off, off, True, None, slopes, table, bounds, d ** -0.5, cap, x["do"])
+    want = ref.attention(x["q"], x["k"], x["v"], starts, starts, True, None, slopes, table, bounds, d ** -0.5, cap, x["do"])
     more = torch.ones(T, dtype=torch.bool)
-    more[off[:-1]] = False
+    more[starts[:-1]] = False
     share = wrongly_rounded(got["dq"].cpu()[more], want["dq"][more])
     print("[share]", dtype, kind, d, share, flush=True)
     assert share < 0.05
@@ -76,3 +77,12 @@ def test_new_items_are_off_by_their_own_rounding_however_many(dtype, i):
     share = wrongly_rounded(out, want)
     print("[share]", dtype, i, share, flush=True)
     assert share < 0.05
+
+
+@pytest.mark.parametrize("i", range(len(CASES)))
+def test_the_table_s_gradient_has_fp32_s_digits(i):
+    x, how, seq, bias, where = setup(i)
+    got = run(x, seq, bias, where)["dtable"]
+    want, size = table_gradient(x, *how)
+    print("[off]", i, off(got, want, size), flush=True)
+    assert off(got, want, size) < LIMIT
