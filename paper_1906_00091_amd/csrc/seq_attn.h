@@ -273,8 +273,8 @@ struct Score {
   }
 };
 
-// tanh(s zs) of a tile of products, relative error 1.2e-7: polynomials in z^2 for tanh(z) / z up to 0.25 and 0.625 (fitted at Chebyshev points; 9.2e-8, 9.5e-8),
-// 1 - 2 / (exp(2 |z|) + 1) beyond.  Scores mostly lie far below their cap, so a wavefront whose products all do takes the first polynomial alone, which is also
+// tanh(s zs) of a tile of products: polynomials in z^2 for tanh(z) / z up to 0.25 and 0.625 (fitted at Chebyshev points; relative errors up to 9.1e-8 and 1.02e-7),
+// 1 - 2 / (exp(2 |z|) + 1) beyond, whose difference is up to 2.7e-7 off just past 0.625 and 1.4e-7 from 1 on (exponential and reciprocal off by a last digit each).  Scores mostly lie far below their cap, so a wavefront whose products all do takes the first polynomial alone, which is also
 // less work than an exponential and a reciprocal.
 __device__ inline void bend(f32x16& s, float zs) {
   constexpr float END = 0.625f;
@@ -327,7 +327,7 @@ __device__ inline float other_half(float v) { return __shfl_xor(v, 32, DLRM_WAVE
 
 // ---------------------------------------------------------------------------------------------------------------
 // A learned bias by buckets (kBias).  The bias of a pair goes by its distance alone, and a tile of 32 x 32 pairs of one head has 63 of them: a wavefront
-// finds the buckets of all at once, one distance a lane, by a binary search in LDS, puts their biases side by side in LDS (the tile's window), and each lane
+// finds the buckets of all at once, one distance a lane (buckets_from), puts their biases side by side in LDS (the tile's window), and each lane
 // reads its 16 from there, at offsets known at compile time.  So wavefronts with a bias hold 32 items of ONE head (not packed by heads as RowWork's
 // others are).  Beyond the outer bounds there is one bias and no search.  Slopes go into the same values.  Without a cap the window holds bias / scale,
 // and the product of queries and keys starts from it; with one the bias is added to the bent score.  (No branch chooses between one bias and several for

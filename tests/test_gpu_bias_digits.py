@@ -86,3 +86,20 @@ def test_the_table_s_gradient_has_fp32_s_digits(i):
     want, size = table_gradient(x, *how)
     print("[off]", i, off(got, want, size), flush=True)
     assert off(got, want, size) < LIMIT
+
+
+def test_a_cap_beside_a_bias_bends_scores_to_the_last_digits():
+    """One key for each query, so lse is the score, cap tanh(z) with a cap of 1.  tanh is off by 2.7e-7 of itself at most (1.02e-7 up to 0.625, by a polynomial), its
+    factor log2 e, lse's factor ln 2 and the product of 8 columns by half a step each, with the factors' own roundings 5 half steps of 2^-24."""
+    z = torch.cat([torch.logspace(-20, -2, 300, base=2), torch.linspace(0.2, 0.7, 1000), torch.linspace(0.7, 9, 700)])
+    z = torch.cat([z, -z])
+    T, off_ = z.numel(), torch.arange(z.numel() + 1, device=DEV)
+    q, k = torch.zeros(T, 1, 8, device=DEV), torch.zeros(T, 1, 8, device=DEV)
+    q[:, 0, 3], k[:, 0, 3] = z.to(DEV), 1.0
+    out, lse = torch.empty_like(q), torch.empty(1, T, device=DEV)
+    seq = hot.SeqBatch(off_, off_, T, T, 1, 1, scale=1.0, cap=1.0)
+    hot.dlrm_seq_attn_bias_fwd(seq, hot.RelBias(torch.zeros(1, 1, device=DEV), None), q, k, k, out, lse)
+    want = torch.tanh(z.double())
+    off_by = ((lse[0].cpu().double() - want) / want).abs()
+    print("[off]", float(off_by[z.abs() <= 0.625].max()), float(off_by[z.abs() > 0.625].max()), flush=True)
+    assert bool((off_by <= torch.where(z.abs() <= 0.625, 1.02e-7, 2.7e-7) + 5 * 2.0 ** -24).all())
