@@ -689,8 +689,10 @@ def relative_bounds(n: int, far: int, both: bool = False, device=None) -> torch.
     def up(m):
         near = (m + 1) // 2
         b = list(range(1, near + 1))
-        for k in range(1, m - near + 1):
+        for k in range(1, m - near):
             b.append(max(b[-1] + 1, math.ceil(near * (max(far, near + 1) / near) ** (k / (m - near)))))
+        if near < m:  # (a power that should be `far` may be the next number)
+            b.append(max(b[-1] + 1, far))
         return b
     if n < 1:
         raise ValueError("relative_bounds: at least one bucket is needed")

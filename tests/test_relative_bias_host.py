@@ -168,3 +168,16 @@ def test_plans_and_calls_refuse_arrays_on_several_devices():
                 lambda: hot.dlrm_cache_tree_attn(c, lens, 32, far, x, x, x, x, None), lambda: hot.dlrm_cache_tree_attn(c, lens, 32, items, x, x, x, x, None, bias=there)):
         with pytest.raises(ValueError, match="on meta"):
             bad()
+
+
+def test_the_last_bucket_begins_where_it_is_said_to():
+    """At `far`, wherever as many bounds one after the other do not pass it; of either sign, and up to the largest integer."""
+    for m in range(2, 128):
+        for far in [*range(m + m, 700), 2041, 4096, 10 ** 6, 2 ** 31 - 1]:
+            b = hot.relative_bounds(m + 1, far).tolist()
+            assert b[-1] == far and all(x < y for x, y in zip(b, b[1:])), (m, far, b)
+    for n in (9, 32, 33, 128):
+        for far in (200, 233, 2043, 2 ** 31 - 1):
+            b = hot.relative_bounds(n, far, True).tolist()
+            assert b[-1] == far and b[0] == 1 - far, (n, far, b)
+    assert hot.relative_bounds(5, 2).tolist() == [1, 2, 3, 4]
