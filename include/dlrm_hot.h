@@ -543,7 +543,8 @@ int32_t dlrm_seq_attn_bias_fwd(const dlrm_seq_batch* seq, const dlrm_rel_bias* b
                                int32_t dtype, const dlrm_heads* q, const dlrm_heads* k, const dlrm_heads* v,
                                const dlrm_heads* out, float* lse, void* stream);
 
-/* Bytes of workspace dlrm_seq_attn_bias_bwd needs; 0 for an unsupported shape. */
+/* Bytes of workspace dlrm_seq_attn_bias_bwd needs; 0 for an unsupported shape.  The table's gradient takes Hq * n sums of 4 bytes for every 16 to 32 keys, where all sequences
+ * may be laid out as if they had the longest one's. */
 size_t dlrm_seq_attn_bias_bwd_workspace_bytes(const dlrm_seq_batch* seq, const dlrm_rel_bias* bias, int32_t Hq, int32_t Hk,
                                               int32_t d, int32_t dtype);
 

@@ -10,7 +10,7 @@
 // The length is split over workgroups in chunks; their parts (unnormalised sums, maxima, weights) are joined by a second kernel in the order of the chunks.
 //
 // Bound by memory where there is enough of it: 256 sequences of up to 8192 items under one item with a bias of 64 buckets, 16 query heads on 4, bf16, d 128, capped:
-// 387 us and 5 for the join for 2.15 GB, 5.5 TB/s.  64 sequences of up to 200 items: 10 us, a launch and a chain of loads (length, page, key, value); 64 of up to 200 under trees of 8: 12 us.
+// 403 us and 5 for the join for 2.15 GB, 5.3 TB/s.  64 sequences of up to 200 items: 11 us, a launch and a chain of loads (length, page, key, value); 64 of up to 200 under trees of 8: 12 us.
 #pragma once
 
 #include "cache_ops.h"

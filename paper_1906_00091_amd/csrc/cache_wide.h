@@ -6,9 +6,10 @@
 // ones, as in cache_tree.h.
 //
 // 16-bit weights enter their product in two parts, as for up to 32 columns: an item's result is off by its own rounding whatever is asked with it.  (One part would take
-// 575, 87 and 128 us where two take 683, 103 and 155, the three sizes below, and be 1.2 to 1.4 times as far off.)  128 sequences of up to 8192 items with trees of up to 60, 16 query heads
-// on 4, bf16, d 128, a bias of 64 buckets, capped: 683 us with the join; 500 candidate lists over up to 1000 items, fp16, d 40: 103 us; one sequence of 131072 items
-// under 64: 155 us.
+// 575, 87 and 128 us where two take 683, 103 and 155, the sizes below on one card, and be 1.2 to 1.4 times as far off.)  128 sequences of up to 8192 items with trees of up to 60, 16 query heads
+// on 4, bf16, d 128, a bias of 64 buckets, capped: 652 us and 36 for the join, 188 TFLOP/s of visible pairs; with 60 items to 8192 each 1268 and 69, 387 TFLOP/s (vector work 54 % of the
+// time, matrix cores 26 %, one after the other for the most part).  The difference is rows of no column in a wavefront's 32 and wavefronts with none in a workgroup.  500
+// candidate lists over up to 1000 items, fp16, d 40: 105 us.  One sequence of 131072 items under 64: 157 us and 14, 400 TFLOP/s.
 #pragma once
 
 #include "seq_attn.h"

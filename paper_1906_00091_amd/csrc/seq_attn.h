@@ -617,8 +617,8 @@ constexpr int fwd_resident(int dt, int dp, int groups, int parts, int sub) {
 // of bf16 on the same card: 1192), bound by the exponentials and reciprocals beside the products: two wavefronts a SIMD, each of which can
 // multiply while the other does not.  2048 histories of up to 200 items, 4 heads, d 64, slopes: 127 us; a workgroup walks over four tiles and
 // waits for most of its time (four a CU hide part of it).  fp32, 13 histories of up to 1999 items, d 72: 281 us, 59 TFLOP/s of 154, and 72 with
-// the columns that pad 72 to 96.  With a learned bias (of 64, 32 and 33 buckets, the second without slopes): 497 us, 144 and 278; 500 lists of up to 40 candidates over up to
-// 1000 items, fp16, d 40: 60 us, 47 without.
+// the columns that pad 72 to 96.  With a learned bias (of 64, 32 and 33 buckets, the second without slopes): 518 us, 148 and 281; 500 lists of up to 40 candidates over up to
+// 1000 items, fp16, d 40: 59 us, 47 without.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS, int SUB>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, fwd_resident(DT, DP, GROUPS, PARTS, SUB)) void seq_attn_fwd_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, SUB> W;
@@ -811,7 +811,7 @@ constexpr int dq_resident(int dt, int dp, int kind, int groups, int parts) {
 // of the output leaves is made up for by taking ds in two 16-bit parts, with a second product, where that costs little or is most needed: narrow
 // rows (5 %), and slopes and learned biases, which leave a row few keys of weight (128 columns: 22 %, biased 16 %).  dq of the long histories above is 2.4e-3 off (relative,
 // all of it) in one part and 1.7e-3 in two, which is its own rounding, with a bias too; of 2048 histories of up to 200 items, slopes, 1.8e-3 in two.
-// Bound as the forward is: the sizes above take 576 us (844 TFLOP/s), 197 us and 379 us (66 TFLOP/s); with a learned bias 790, 219 and 367.
+// Bound as the forward is: the sizes above take 576 us (844 TFLOP/s), 197 us and 379 us (66 TFLOP/s); with a learned bias 784, 223 and 374.
 template <int DT, int DP, int KIND, int GROUPS, int PARTS>
 __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROUPS, PARTS)) void seq_attn_dq_kernel(SeqArgs a) {
   typedef Walk<DT, DP, GROUPS, PARTS, 1> W;
@@ -1013,7 +1013,7 @@ __global__ __launch_bounds__(64 * GROUPS * PARTS, dq_resident(DT, DP, KIND, GROU
 // Two wavefronts share 32 keys, one for each half of a tile's 64 queries, and add their sums at the end: the keys that all
 // queries of a long sequence see are the longest work of all, and go by in half the steps.
 // The sizes above: 885 us (733 TFLOP/s: one workgroup of eight wavefronts a CU, which meet at a barrier for each tile), 229 us (latency of short
-// walks) and 518 us with 13 for the join (62 TFLOP/s).  With a learned bias and its gradient 1486 us (940 without the buckets and the sums), 279 and 563.
+// walks) and 518 us with 13 for the join (62 TFLOP/s).  With a learned bias and its gradient 1505 us (940 without the buckets and the sums), 289 and 569.
 template <int DT, int DP, bool BIAS, int GROUPS_, int PARTS_>
 struct Dkv {
   static constexpr int GROUPS = GROUPS_, PARTS = PARTS_, KEYS = 32 * GROUPS, THREADS = 64 * GROUPS * PARTS, BQ = 32 * PARTS;
@@ -1022,7 +1022,7 @@ struct Dkv {
   // not fit the registers of two wavefronts per SIMD.
   static constexpr bool V_LDS = DT != DLRM_F32 && DP > 64;
   // With a bias some of the keys' operands too, which else are spilled, and a reload waits for the tile that is on its way (8 histories of up to 4096
-  // items, d 128, cap: 1918 us with 81 registers spilled).
+  // items, d 128, cap: 1918 us with 81 registers spilled;  d 96, forward and backward: three steps in LDS 2265 us, none 2305, without a cap 1918 and 1915).
   static constexpr int K_LDS = BIAS && V_LDS && PARTS == 2 ? (DP > 96 ? 6 : 3) : 0;  // steps
   static constexpr int K_STRIDE = 32 * K_LDS + 16, K_BYTES = K_LDS > 0 ? KEYS * K_STRIDE : 0;
   typedef Tile<DT, DP> T;
