@@ -447,3 +447,21 @@ def test_calls_on_two_streams_at_once_are_what_they_are_alone():
     torch.cuda.synchronize()
     for a, b in zip(alone, both):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m", [3, 20, 70])
+def test_infinite_values_that_are_seen_stay_infinite(dtype, m):
+    """12, 80 and 280 columns: a weight's two parts both meet the value, and zero times an infinity would be NaN.  Other columns are what they are without it."""
+    g, Hq, Hk, d, dt = gen(60 + m), 8, 2, 64, DT[dtype]
+    c = Paged(g, [300, 40], 20, 16, Hk, d, dt)
+    x = {n: rand(g, 2 * m, H, d, dtype=dt) for n, H in (("q", Hq), ("k", Hk), ("v", Hk))}
+    items = hot.NewItems(offsets([m, m]).to(DEV), 2 * m, m)
+    plain = run_tree(c, x, items, None, None, 0.0, "rows")
+    page = c.cache.table[0, 1]
+    c.dev[1][page.long(), :, 5, 7] = math.inf   # item 21 of the first sequence
+    x["v"][0, :, 9] = -math.inf                 # its first new item, which all of them see
+    out = run_tree(c, x, items, None, None, 0.0, "rows")
+    assert (out[:m, :, 7] == math.inf).all() and (out[:m, :, 9] == -math.inf).all()
+    rest = [i for i in range(d) if i not in (7, 9)]
+    assert torch.equal(out[:, :, rest], plain[:, :, rest]) and torch.equal(out[m:], plain[m:])
