@@ -529,7 +529,8 @@ int32_t dlrm_seq_attn_bwd(const dlrm_seq_batch* seq, int32_t Hq, int32_t Hk, int
  * A learned bias of scores by the buckets of relative places (host struct, device arrays).  The distance of a pair is the query's
  * place less the key's, negative for keys behind the query; its bucket is the number of bounds that are at most the distance, and
  * table[h][bucket] is added to the score (after the cap, beside the slopes): x + table[h * n + bucket].  Distances below bounds[0] are in bucket
- * 0, those from bounds[n - 2] on in bucket n - 1; the buckets between bounds that are the same are empty.  A bias of DLRM_BIAS_HIDES or less, -inf among them, hides its bucket: its pairs are not visible.
+ * 0, those from bounds[n - 2] on in bucket n - 1; the buckets between bounds that are the same are empty.
+ * A bias of DLRM_BIAS_HIDES or less, -inf among them, hides its bucket: its pairs are not visible.
  */
 #define DLRM_BIAS_HIDES (-60000.0f)
 typedef struct dlrm_rel_bias {

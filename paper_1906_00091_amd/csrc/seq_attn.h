@@ -274,8 +274,8 @@ struct Score {
 };
 
 // tanh(s zs) of a tile of products: polynomials in z^2 for tanh(z) / z up to 0.25 and 0.625 (fitted at Chebyshev points; relative errors up to 9.1e-8 and 1.02e-7),
-// 1 - 2 / (exp(2 |z|) + 1) beyond, whose difference is up to 2.7e-7 off just past 0.625 and 1.4e-7 from 1 on (exponential and reciprocal off by a last digit each).  Scores mostly lie far below their cap, so a wavefront whose products all do takes the first polynomial alone, which is also
-// less work than an exponential and a reciprocal.
+// 1 - 2 / (exp(2 |z|) + 1) beyond, whose difference is up to 2.7e-7 off just past 0.625 and 1.4e-7 from 1 on (exponential and reciprocal off by a last digit each).  Scores mostly lie
+// far below their cap, so a wavefront whose products all do takes the first polynomial alone, which is also less work than an exponential and a reciprocal.
 __device__ inline void bend(f32x16& s, float zs) {
   constexpr float END = 0.625f;
   auto near_zero = [](float z) {
